@@ -18,12 +18,13 @@
  *     [0, V), a watchdog expiry inside a kernel) set bits of a sticky device error word that
  *     af_check_device_errors reads; affected outputs are NaN; no kernel traps.
  *   - A context serves one stream at a time: calls on one context must not overlap on the GPU
- *     (they share its workspace).  Use one context per concurrent stream.
+ *     (they share its workspace), captured and replayed ones included.  Use one context per concurrent
+ *     stream.
  *   - Workspace grows on demand with cudaMalloc (which may synchronise).  Call af_reserve once
  *     with the largest sizes to keep allocation out of the hot calls.
  *   - Stream capture: once af_reserve has covered the sizes (and the tuning is unchanged), every
- *     call except af_pack_microbatch, af_unpack_microbatch, af_check_device_errors, af_reserve and
- *     af_destroy issues only kernel launches and asynchronous memsets on `stream`, so a sequence
+ *     call except af_pack_microbatch, af_unpack_microbatch, af_check_device_errors, af_reserve (and its
+ *     kin af_reserve_candidates and af_reserve_preference) and af_destroy issues only kernel launches and asynchronous memsets on `stream`, so a sequence
  *     of them may be recorded into a CUDA graph and replayed on new contents of the same buffers.
  *     af_pack_microbatch and af_unpack_microbatch build a table from their host index list (and
  *     for large batches stage it through pinned host memory, waiting on an event of their own);
@@ -57,8 +58,12 @@ typedef enum {
   AF_ERR_DEVICE_FLAGGED = -9      /* af_check_device_errors found the error word non-zero    */
 } af_status;
 
+/* element type of an output that comes in either */
+typedef enum { AF_F32 = 0, AF_BF16 = 1 } af_dtype;
+
 /* bits of the device error word */
-#define AF_DEVERR_TARGET_RANGE 1u /* a target id was outside [0, V): that token's outputs are NaN */
+#define AF_DEVERR_TARGET_RANGE 1u /* a target id was outside [0, V): that token's outputs are NaN;
+                                     a candidate id >= V: that slot's log-prob is NaN              */
 #define AF_DEVERR_WATCHDOG 2u     /* a bounded wait inside a kernel ran out; results invalid      */
 #define AF_DEVERR_CU_SEQLENS 4u   /* cu_seqlens not non-decreasing from 0 to T                     */
 #define AF_DEVERR_SAMPLE_INDEX 8u /* af_controller_put met an index outside [0, N): entry skipped  */
@@ -339,6 +344,167 @@ af_status af_policy_update(af_ctx* ctx, const void* hidden, const void* W, const
                            const af_loss_params* params, af_loss_out* out, float* logp, float* entropy,
                            float* lse, float* dlogp, void* d_hidden, float* d_W, int32_t accumulate_dW,
                            void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * af_candidate_logprob / af_candidate_logprob_backward -- the LM head scored at K listed ids per
+ * token, and the gradient of that (distillation from a teacher's top logits; scoring of
+ * alternatives).  The paper's actor update knows one target per token; these are the textbook
+ * log-softmax and its gradient at K of them.
+ *
+ * Forward, for each token t and slot k (z as in af_token_logprob, lse_t = log sum_v exp z_tv):
+ *   cand_logp[t,k] = z_{t, cand[t,k]} - lse_t;   entropy_t = lse_t - sum_v softmax_tv * z_tv.
+ *   An id below 0 marks an unused slot: its log-prob is -inf.  An id >= V gives NaN in that slot and
+ *   raises AF_DEVERR_TARGET_RANGE.  The same id may be listed more than once.
+ * Backward, from dcand[t,k] = dL / dcand_logp[t,k] (slots without a valid id are not looked at):
+ *   G_t = sum_k dcand[t,k];   dZ_tv = sum_{k: cand[t,k] = v} dcand[t,k] - G_t * exp(z_tv - lse[t])
+ *   d_hidden[t,:] = sum_v dZ_tv * W[v,:]      -> [T,d] bf16
+ *   d_W[v,:]      = sum_t dZ_tv * hidden[t,:] -> [V,d] of type dW_type, or NULL (a frozen head)
+ * accumulate_dW adds to an fp32 d_W; with AF_BF16, which is rounded once from fp32 sums over the
+ * whole batch, it is refused (AF_ERR_INVALID_ARG).  The logits are recomputed, dZ is rounded to bf16
+ * for the two products and exists for one token block only, as in af_policy_loss_backward; a
+ * registered "d_W ready" event (af_set_dw_ready_event) is recorded where d_W is complete, when there
+ * is a d_W.  The forward accumulates logits in parts that are added in fp32 with rounding to nearest
+ * (the tensor core's own accumulation truncates): against 64 bits its log-probs are about ten times
+ * closer than af_token_logprob's.  It always runs on CTA pairs; gemm_variant 1 of af_set_tuning
+ * applies to the backward only, v_splits and bwd_token_block as elsewhere.
+ *
+ * hidden [T,d], W [V,d] bf16 dev, row-major, 16-byte aligned, d % 8 == 0 (backward: V % 8 == 0, d_hidden
+ * and d_W 16-byte aligned too).  cand [T,K] int32, cand_logp, dcand [T,K], entropy (nullable), lse
+ * (nullable in the forward) [T] fp32, dev.  1 <= K <= AF_MAX_CANDIDATES, V <= 2^24 - 256, 0 <= T < 2^31
+ * (AF_ERR_SHAPE otherwise).  Workspace: 4 bytes per slot for the sorted lists (one token block of them in
+ * the backward), the forward's softmax states and the backward's dZ, and 4 V d bytes behind a bf16 d_W
+ * of more than one token block; af_reserve_candidates sizes all of it ahead.
+ * ------------------------------------------------------------------------------------------- */
+#define AF_MAX_CANDIDATES 256
+af_status af_candidate_logprob(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand,
+                               int64_t T, int32_t K, int32_t d, int32_t V, float* cand_logp,
+                               float* entropy, float* lse, void* stream);
+af_status af_candidate_logprob_backward(af_ctx* ctx, const void* hidden, const void* W,
+                                        const int32_t* cand, const float* lse, const float* dcand,
+                                        int64_t T, int32_t K, int32_t d, int32_t V, void* d_hidden,
+                                        void* d_W, int32_t dW_type, int32_t accumulate_dW, void* stream);
+
+/* Pre-size the workspace of the calls of this section and of af_distill_update for batches of up to max_T
+ * tokens, K slots and head shape (d, V): with_backward 0 = scoring only, 1 = the backward too, 2 = and
+ * af_distill_update.  dW_type: the type of d_W that will be asked for (AF_BF16 keeps fp32 sums when a
+ * batch has more than one token block).  Synchronous (allocates).  Smaller T, K, d and V of the same
+ * kind fit in what it leaves; af_set_tuning may not change in between. */
+af_status af_reserve_candidates(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d, int32_t V,
+                                int32_t with_backward, int32_t dW_type);
+
+/* ---------------------------------------------------------------------------------------------
+ * af_distill_loss -- divergence between a teacher's and the student's log-probs of K listed ids per
+ * token, aggregated over a packed micro-batch, with its gradient in the student's log-probs (the
+ * loss of a distillation task; the paper's loss, af_policy_loss, learns from rewards instead).
+ *
+ * lt = teacher_logp[t,k], lq = cand_logp[t,k] (from af_candidate_logprob), both over the whole
+ * vocabulary.  A slot with lt = -inf is absent: its lq is not looked at and its gradient is 0; a token
+ * whose slots are all absent has loss 0.  p = exp(lt), q = exp(lq); sums run over the present slots;
+ * 0 log 0 = 0.
+ *   divergence 0: from teacher to student;  1: from student to teacher.
+ *   support 0 (as listed):   0: sum p (lt - lq);   1: sum q (lq - lt)
+ *   support 1 (renormalised): a = softmax(lt / tau), b = softmax(lq / tau) over the present slots;
+ *                            0: tau^2 sum a log(a / b);   1: tau^2 sum b log(b / a)
+ *   support 2 (with a tail): one more outcome holds the rest of either mass, no less than 2^-16:
+ *                            p_r = max(1 - sum p, 2^-16), q_r = max(1 - sum q, 2^-16);
+ *                            0: sum p (lt - lq) + p_r log(p_r / q_r);   1: sum q (lq - lt) + q_r log(q_r / p_r)
+ *                            (a q_r held at 2^-16 carries no gradient)
+ *   tau = temperature, > 0; it has a meaning for support 1 only and has to be 1 for the others.
+ * token_loss[t] is that sum; agg_mode and loss_scale aggregate it exactly as in af_policy_loss:
+ * agg_mode 0: loss = loss_scale * mean_i( mean_{t in i} ); 1: loss_scale * mean_t.  dcand[t,k] =
+ * dloss / dcand_logp[t,k].  teacher_mass and student_mass are means over tokens of sum p and sum q.
+ *
+ * cand_logp, teacher_logp, dcand (nullable): [T,K] fp32 dev; token_loss (nullable): [T] fp32 dev;
+ * cu_seqlens as in af_policy_loss; `out`: device struct.  1 <= K <= AF_MAX_CANDIDATES.  Sums are taken in
+ * a fixed order: results are bit-reproducible.
+ * Errors: AF_ERR_INVALID_ARG for null pointers, unknown enum values, a temperature that is not finite and
+ * positive or not 1 where it has to be; AF_ERR_SHAPE for K or T out of range.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t divergence;
+  int32_t support;
+  int32_t agg_mode;
+  float temperature;
+  float loss_scale;
+} af_distill_params;
+
+typedef struct {
+  float loss, teacher_mass, student_mass;
+  int32_t reserved;
+  int64_t n_tokens;
+} af_distill_out;
+
+af_status af_distill_loss(af_ctx* ctx, const float* cand_logp, const float* teacher_logp,
+                          const int32_t* cu_seqlens, int32_t B, int64_t T, int32_t K,
+                          const af_distill_params* params, af_distill_out* out, float* token_loss,
+                          float* dcand, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * af_distill_update -- scoring, distillation loss and backward of one packed micro-batch in one call
+ * (what af_policy_update is to the policy loss).
+ *
+ * Computes what af_candidate_logprob, af_distill_loss and af_candidate_logprob_backward compute one
+ * after the other, with the logits evaluated once per token: a token block's fp32 logits stay in
+ * scratch between the log-softmax and dZ.  entropy, token_loss, dcand and d_W may be NULL; every other
+ * pointer is required when T > 0.  Arguments, requirements and errors as for the three calls (d % 8 == 0,
+ * V % 8 == 0).  The same token may not be scored by another teacher in the same call: lists of several
+ * teachers are several calls with an accumulated fp32 d_W.
+ * ------------------------------------------------------------------------------------------- */
+af_status af_distill_update(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand,
+                            const float* teacher_logp, const int32_t* cu_seqlens, int32_t B, int64_t T,
+                            int32_t K, int32_t d, int32_t V, const af_distill_params* params,
+                            af_distill_out* out, float* cand_logp, float* entropy, float* lse,
+                            float* token_loss, float* dcand, void* d_hidden, void* d_W, int32_t dW_type,
+                            int32_t accumulate_dW, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * af_preference_loss -- preference loss over pairs of packed sequences, with the gradient per token
+ * (post-training from comparisons; stands where af_policy_loss stands, and its dlogp goes to
+ * af_policy_loss_backward in the same way).
+ *
+ * The packed batch holds B = 2 P sequences.  Pair p is (chosen, rejected) = (2p, 2p + 1) with
+ * pair_layout 0, (p, P + p) with pair_layout 1; af_pack_microbatch packs them in the order of its index
+ * list, and a response that takes part in several pairs is listed once per pair.
+ *   S_j = sum_{t in j} (logp[t] - ref_logp[t]), or sum logp[t] without ref_logp (NULL);
+ *   n_j = 1 / L_j if length_norm else 1;   seq_score[j] = beta * n_j * S_j
+ *   x_p = seq_score[chosen] - seq_score[rejected] - margin
+ *   kind 0 (logistic): l_p = -(1 - e) log s(x_p) - e log s(-x_p), s the logistic function, e = label_smoothing
+ *   kind 1 (squared):  l_p = ((x_p - 1/2) / beta)^2
+ *   kind 2 (hinge):    l_p = max(0, 1 - x_p)
+ *   nll_p = mean over the chosen's tokens of -logp (0 for an empty sequence)
+ *   pair_loss[p] = l_p + nll_coef * nll_p;   loss = loss_scale * mean_p pair_loss[p]
+ *   dlogp[t] = dloss / dlogp[t], constant over a sequence.
+ * The record: loss, and the means over pairs of l_p, nll_p, "chosen scores above rejected" (strictly), and
+ * the two scores.  An empty sequence has S = 0.  The squared loss compares the log ratio with 1 / (2 beta).
+ *
+ * logp, ref_logp (nullable), dlogp (nullable): [T] fp32 dev; cu_seqlens [B+1] as in af_policy_loss;
+ * pair_loss [P], seq_score [B] fp32 dev (nullable); `out`: device struct.  Sums in fp64 in a fixed order:
+ * results are bit-reproducible.  Workspace: 20 bytes per sequence and 32 per 256 tokens, grown on demand or
+ * by af_reserve_preference.
+ * Errors: AF_ERR_INVALID_ARG for null pointers, unknown enum values, beta not finite and positive,
+ * label_smoothing outside [0, 1); AF_ERR_SHAPE for an odd B or T >= 2^31 - 65536.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t kind;
+  int32_t length_norm;
+  int32_t pair_layout;
+  float beta;
+  float label_smoothing;
+  float margin;
+  float nll_coef;
+  float loss_scale;
+} af_preference_params;
+
+typedef struct {
+  float loss, pair_loss, nll, accuracy, chosen_score, rejected_score;
+  int64_t n_pairs;
+} af_preference_out;
+
+af_status af_preference_loss(af_ctx* ctx, const float* logp, const float* ref_logp,
+                             const int32_t* cu_seqlens, int32_t B, int64_t T,
+                             const af_preference_params* params, af_preference_out* out,
+                             float* pair_loss, float* seq_score, float* dlogp, void* stream);
+af_status af_reserve_preference(af_ctx* ctx, int64_t max_T, int32_t max_B);
 
 /* ---------------------------------------------------------------------------------------------
  * af_controller_put / af_controller_get / af_controller_clear -- the status table of the

@@ -28,8 +28,15 @@ EXPORTS = ["af_create", "af_destroy", "af_status_string", "af_reserve", "af_work
            "af_grpo_advantage", "af_policy_loss", "af_policy_loss_backward", "af_token_logprob_static",
            "af_controller_put", "af_controller_get", "af_controller_clear", "af_balance_partitions",
            "af_token_logprob_shard", "af_merge_logprob_shards", "af_policy_update", "af_unpack_microbatch", "af_policy_loss_backward_shard", "af_set_dw_ready_event", "af_die_split", "af_selftest_bounded_wait",
-           "af_plan_token_logprob", "af_plan_units"]
+           "af_plan_token_logprob", "af_plan_units",
+           "af_candidate_logprob", "af_candidate_logprob_backward", "af_reserve_candidates", "af_distill_loss",
+           "af_distill_update", "af_preference_loss", "af_reserve_preference"]
 MAX_WRITE_COLS = 4
+MAX_CANDIDATES = 256
+F32, BF16 = 0, 1                                                     # af_dtype
+DIVERGENCE_FORWARD, DIVERGENCE_REVERSE = 0, 1                        # teacher to student, student to teacher
+SUPPORT_LISTED, SUPPORT_RENORMALISED, SUPPORT_TAIL = 0, 1, 2
+PREFERENCE_LOGISTIC, PREFERENCE_SQUARED, PREFERENCE_HINGE = 0, 1, 2
 
 
 class AfError(RuntimeError):
@@ -60,6 +67,26 @@ class LossOut(C.Structure):
     _fields_ = [("loss", C.c_float), ("pg_loss", C.c_float), ("kl_mean", C.c_float),
                 ("clip_frac", C.c_float), ("entropy_mean", C.c_float), ("reserved", C.c_int32),
                 ("n_tokens", C.c_int64)]
+
+
+class DistillParams(C.Structure):
+    _fields_ = [("divergence", C.c_int32), ("support", C.c_int32), ("agg_mode", C.c_int32), ("temperature", C.c_float),
+                ("loss_scale", C.c_float)]
+
+
+class DistillOut(C.Structure):
+    _fields_ = [("loss", C.c_float), ("teacher_mass", C.c_float), ("student_mass", C.c_float), ("reserved", C.c_int32),
+                ("n_tokens", C.c_int64)]
+
+
+class PreferenceParams(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("length_norm", C.c_int32), ("pair_layout", C.c_int32), ("beta", C.c_float),
+                ("label_smoothing", C.c_float), ("margin", C.c_float), ("nll_coef", C.c_float), ("loss_scale", C.c_float)]
+
+
+class PreferenceOut(C.Structure):
+    _fields_ = [("loss", C.c_float), ("pair_loss", C.c_float), ("nll", C.c_float), ("accuracy", C.c_float),
+                ("chosen_score", C.c_float), ("rejected_score", C.c_float), ("n_pairs", C.c_int64)]
 
 
 class ControllerView(C.Structure):
@@ -124,6 +151,14 @@ def load_library() -> C.CDLL:
     lib.af_policy_loss_backward_shard.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, i32, vp]
     lib.af_unpack_microbatch.argtypes = [vp, vp, i64, vp, i32, C.POINTER(WriteCols), C.POINTER(ControllerView), u32,
                                          C.POINTER(i64), vp]
+    lib.af_candidate_logprob.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, vp, vp]
+    lib.af_candidate_logprob_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp, i32, i32, vp]
+    lib.af_reserve_candidates.argtypes = [vp, i64, i32, i32, i32, i32, i32]
+    lib.af_distill_loss.argtypes = [vp, vp, vp, vp, i32, i64, i32, C.POINTER(DistillParams), vp, vp, vp, vp]
+    lib.af_distill_update.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i32, i32, i32, C.POINTER(DistillParams), vp,
+                                      vp, vp, vp, vp, vp, vp, vp, i32, i32, vp]
+    lib.af_preference_loss.argtypes = [vp, vp, vp, vp, i32, i64, C.POINTER(PreferenceParams), vp, vp, vp, vp, vp]
+    lib.af_reserve_preference.argtypes = [vp, i64, i32]
     for name in EXPORTS:
         if name not in ("af_status_string", "af_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
@@ -332,6 +367,93 @@ class Context:
                                          _ptr(out), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(dlogp), _ptr(d_hidden),
                                          _ptr(d_W), int(accumulate_dW), _stream(stream)), "af_policy_update")
 
+    # -- listed candidates, distillation, preferences ----------------------------------------------
+    @staticmethod
+    def _dtype(d_W: Optional[torch.Tensor]) -> int:
+        if d_W is None or d_W.dtype == torch.float32:
+            return F32
+        if d_W.dtype == torch.bfloat16:
+            return BF16
+        raise ValueError("d_W is float32 or bfloat16")
+
+    @staticmethod
+    def _list_width(cand: torch.Tensor, T: int, *others: Optional[torch.Tensor]) -> int:
+        """K of [T, K] lists of 4-byte ids or values; every other tensor is float32, equally wide, with enough rows."""
+        if cand.dim() != 2 or cand.shape[0] < T or cand.element_size() != 4:
+            raise ValueError("candidate lists are [T, K] with 4-byte elements")
+        for o in others:
+            if o is not None and (o.dim() != 2 or o.shape[0] < T or o.shape[1] != cand.shape[1] or o.dtype != torch.float32):
+                raise ValueError("tensors over the candidate lists are float32 [T, K] like the lists")
+        return cand.shape[1]
+
+    def candidate_logprob(self, hidden, W, cand, cand_logp, entropy=None, lse=None, T=None, stream=None):
+        """``cand``: int32 [T, K] vocabulary ids (below 0: unused slot); ``cand_logp``: float32 [T, K]."""
+        T = hidden.shape[0] if T is None else T
+        d, V = W.shape[1], W.shape[0]
+        K = self._list_width(cand, T, cand_logp)
+        _check(self.lib.af_candidate_logprob(self.handle, _ptr(hidden), _ptr(W), _ptr(cand), T, K, d, V,
+                                             _ptr(cand_logp), _ptr(entropy), _ptr(lse), _stream(stream)),
+               "af_candidate_logprob")
+
+    def candidate_logprob_backward(self, hidden, W, cand, lse, dcand, d_hidden, d_W=None, accumulate_dW=False, T=None,
+                                   stream=None):
+        """``d_W``: float32 or bfloat16 [V, d], or None (a frozen head)."""
+        T = hidden.shape[0] if T is None else T
+        d, V = W.shape[1], W.shape[0]
+        K = self._list_width(cand, T, dcand)
+        _check(self.lib.af_candidate_logprob_backward(self.handle, _ptr(hidden), _ptr(W), _ptr(cand), _ptr(lse),
+                                                      _ptr(dcand), T, K, d, V, _ptr(d_hidden), _ptr(d_W),
+                                                      self._dtype(d_W), int(accumulate_dW), _stream(stream)),
+               "af_candidate_logprob_backward")
+
+    def reserve_candidates(self, max_T: int, K: int, d: int, V: int, with_backward=0, dW_type: int = F32):
+        """Workspace of the candidate calls; with_backward: 0 scoring, 1 backward, 2 distill_update too."""
+        _check(self.lib.af_reserve_candidates(self.handle, max_T, K, d, V, int(with_backward), dW_type),
+               "af_reserve_candidates")
+
+    def distill_loss(self, cand_logp, teacher_logp, cu_seqlens, out, token_loss=None, dcand=None, divergence=0, support=1,
+                     temperature=1.0, agg_mode=0, loss_scale=1.0, B=None, T=None, stream=None):
+        """``out``: device uint8 tensor of ``ctypes.sizeof(DistillOut)`` bytes (see read_distill_out)."""
+        B = cu_seqlens.shape[0] - 1 if B is None else B
+        T = cand_logp.shape[0] if T is None else T
+        K = self._list_width(cand_logp, T, teacher_logp, dcand)
+        prm = DistillParams(divergence, support, agg_mode, temperature, loss_scale)
+        _check(self.lib.af_distill_loss(self.handle, _ptr(cand_logp), _ptr(teacher_logp), _ptr(cu_seqlens), B, T, K,
+                                        C.byref(prm), _ptr(out), _ptr(token_loss), _ptr(dcand), _stream(stream)),
+               "af_distill_loss")
+
+    def distill_update(self, hidden, W, cand, teacher_logp, cu_seqlens, out, cand_logp, lse, d_hidden, d_W=None,
+                       entropy=None, token_loss=None, dcand=None, accumulate_dW=False, divergence=0, support=1,
+                       temperature=1.0, agg_mode=0, loss_scale=1.0, B=None, T=None, stream=None):
+        """``af_distill_update``: scoring, distillation loss and backward of one packed micro-batch."""
+        B = cu_seqlens.shape[0] - 1 if B is None else B
+        T = hidden.shape[0] if T is None else T
+        d, V = W.shape[1], W.shape[0]
+        K = self._list_width(cand, T, teacher_logp, cand_logp, dcand)
+        prm = DistillParams(divergence, support, agg_mode, temperature, loss_scale)
+        _check(self.lib.af_distill_update(self.handle, _ptr(hidden), _ptr(W), _ptr(cand), _ptr(teacher_logp),
+                                          _ptr(cu_seqlens), B, T, K, d, V, C.byref(prm), _ptr(out), _ptr(cand_logp),
+                                          _ptr(entropy), _ptr(lse), _ptr(token_loss), _ptr(dcand), _ptr(d_hidden),
+                                          _ptr(d_W), self._dtype(d_W), int(accumulate_dW), _stream(stream)),
+               "af_distill_update")
+
+    def preference_loss(self, logp, ref_logp, cu_seqlens, out, pair_loss=None, seq_score=None, dlogp=None, kind=0,
+                        beta=0.1, label_smoothing=0.0, margin=0.0, nll_coef=0.0, length_norm=False, pair_layout=0,
+                        loss_scale=1.0, B=None, T=None, stream=None):
+        """``ref_logp`` None: reference-free.  ``out``: device uint8 tensor of ``ctypes.sizeof(PreferenceOut)``
+        bytes (see read_preference_out)."""
+        B = cu_seqlens.shape[0] - 1 if B is None else B
+        T = logp.shape[0] if T is None else T
+        if logp.dtype != torch.float32 or (ref_logp is not None and ref_logp.dtype != torch.float32):
+            raise ValueError("log-probs are float32")
+        prm = PreferenceParams(kind, int(length_norm), pair_layout, beta, label_smoothing, margin, nll_coef, loss_scale)
+        _check(self.lib.af_preference_loss(self.handle, _ptr(logp), _ptr(ref_logp), _ptr(cu_seqlens), B, T, C.byref(prm),
+                                           _ptr(out), _ptr(pair_loss), _ptr(seq_score), _ptr(dlogp), _stream(stream)),
+               "af_preference_loss")
+
+    def reserve_preference(self, max_T: int, max_B: int):
+        _check(self.lib.af_reserve_preference(self.handle, max_T, max_B), "af_reserve_preference")
+
     # -- controller: status table of the streaming store ----------------------------------------
     @staticmethod
     def _table(table: dict) -> ControllerView:
@@ -416,6 +538,26 @@ def read_loss_out(buf: torch.Tensor) -> dict:
     raw = buf.cpu().numpy().tobytes()
     o = LossOut.from_buffer_copy(raw)
     return {k: getattr(o, k) for k, _ in LossOut._fields_ if k != "reserved"}
+
+
+def new_distill_out(device) -> torch.Tensor:
+    return torch.zeros(C.sizeof(DistillOut), dtype=torch.uint8, device=device)
+
+
+def read_distill_out(buf: torch.Tensor) -> dict:
+    """Copy the device ``af_distill_out`` to the host (synchronises) and return it as a dict."""
+    o = DistillOut.from_buffer_copy(buf.cpu().numpy().tobytes())
+    return {k: getattr(o, k) for k, _ in DistillOut._fields_ if k != "reserved"}
+
+
+def new_preference_out(device) -> torch.Tensor:
+    return torch.zeros(C.sizeof(PreferenceOut), dtype=torch.uint8, device=device)
+
+
+def read_preference_out(buf: torch.Tensor) -> dict:
+    """Copy the device ``af_preference_out`` to the host (synchronises) and return it as a dict."""
+    o = PreferenceOut.from_buffer_copy(buf.cpu().numpy().tobytes())
+    return {k: getattr(o, k) for k, _ in PreferenceOut._fields_}
 
 
 def token_logprob_static(hidden, W, target, logp, entropy=None, lse=None, device_flags=None, T=None,

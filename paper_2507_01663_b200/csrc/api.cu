@@ -108,7 +108,8 @@ af_status af_destroy(af_ctx* c) {
   if (!c) return AF_ERR_INVALID_ARG;
   DeviceGuard guard(c->device);
   cudaDeviceSynchronize();
-  Buf* bufs[] = {&c->partial, &c->loss_ws, &c->pack_meta, &c->dz, &c->ctrl_ws, &c->zlog, &c->adv_ws};
+  Buf* bufs[] = {&c->partial, &c->loss_ws, &c->pack_meta, &c->dz, &c->ctrl_ws, &c->zlog, &c->adv_ws, &c->cand_keys,
+                 &c->dw_sums, &c->distill_ws, &c->pref_ws};
   for (Buf* b : bufs) if (b->p) cudaFree(b->p);
   for (int i = 0; i < kPackRing; ++i) {
     if (c->pack_host[i]) cudaFreeHost(c->pack_host[i]);
@@ -121,7 +122,8 @@ af_status af_destroy(af_ctx* c) {
 
 int64_t af_workspace_bytes(const af_ctx* c) {
   if (!c) return 0;
-  return (int64_t)(c->partial.cap + c->loss_ws.cap + c->pack_meta.cap + c->dz.cap + c->ctrl_ws.cap + c->zlog.cap + c->adv_ws.cap);
+  return (int64_t)(c->partial.cap + c->loss_ws.cap + c->pack_meta.cap + c->dz.cap + c->ctrl_ws.cap + c->zlog.cap + c->adv_ws.cap +
+                   c->cand_keys.cap + c->dw_sums.cap + c->distill_ws.cap + c->pref_ws.cap);
 }
 
 af_status af_selftest_bounded_wait(af_ctx* c, uint32_t* waited_us, void* stream) {
@@ -524,6 +526,140 @@ af_status af_policy_update(af_ctx* c, const void* hidden, const void* W, const i
   return launch_policy_update(c, hidden, W, target, old_logp, ref_logp, adv_seq, cu_seqlens, B, T, d, V, *params, out,
                               logp, entropy, lse, dlogp, d_hidden, d_W, accumulate_dW ? 1 : 0,
                               static_cast<cudaStream_t>(stream));
+}
+
+// What the candidate calls require of their sizes, matrices and head gradient.
+static af_status candidate_sizes(int64_t T, int32_t K, int32_t d, int32_t V) {
+  if (T < 0 || K < 1 || d < 1 || V < 1) return AF_ERR_INVALID_ARG;
+  if (T >= ((int64_t)1 << 31) || K > AF_MAX_CANDIDATES || V > (1 << 24) - 256) return AF_ERR_SHAPE;
+  return AF_OK;
+}
+static af_status candidate_head(const void* hidden, const void* W, const void* d_hidden, const void* d_W, int32_t dW_type,
+                                int32_t accumulate_dW, int32_t d, int32_t V) {
+  if (dW_type != AF_F32 && dW_type != AF_BF16) return AF_ERR_INVALID_ARG;
+  if (d_W && dW_type == AF_BF16 && accumulate_dW) return AF_ERR_INVALID_ARG;    // would round the sum at every call
+  if (d % 8 != 0 || V % 8 != 0) return AF_ERR_ALIGNMENT;
+  if (!aligned16(hidden) || !aligned16(W) || !aligned16(d_hidden) || !aligned16(d_W)) return AF_ERR_ALIGNMENT;
+  return AF_OK;
+}
+static bool positive_finite(float v) { return v > 0.f && v <= 3.402823466e38f; }
+static af_status distill_params_ok(const af_distill_params& p) {
+  if (p.divergence < 0 || p.divergence > 1 || p.support < 0 || p.support > 2 || p.agg_mode < 0 || p.agg_mode > 1)
+    return AF_ERR_INVALID_ARG;
+  if (!positive_finite(p.temperature) || (p.support != 1 && p.temperature != 1.f)) return AF_ERR_INVALID_ARG;
+  return AF_OK;
+}
+
+af_status af_candidate_logprob(af_ctx* c, const void* hidden, const void* W, const int32_t* cand, int64_t T, int32_t K,
+                               int32_t d, int32_t V, float* cand_logp, float* entropy, float* lse, void* stream) {
+  NvtxRange range("af_candidate_logprob");
+  if (!c) return AF_ERR_INVALID_ARG;
+  const af_status st = candidate_sizes(T, K, d, V);
+  if (st != AF_OK || T == 0) return st;
+  if (!hidden || !W || !cand || !cand_logp) return AF_ERR_INVALID_ARG;
+  if (d % 8 != 0 || !aligned16(hidden) || !aligned16(W)) return AF_ERR_ALIGNMENT;
+  DeviceGuard guard(c->device);
+  return launch_candidate_logprob(c, hidden, W, cand, T, K, d, V, cand_logp, entropy, lse,
+                                  static_cast<cudaStream_t>(stream));
+}
+
+af_status af_candidate_logprob_backward(af_ctx* c, const void* hidden, const void* W, const int32_t* cand,
+                                        const float* lse, const float* dcand, int64_t T, int32_t K, int32_t d, int32_t V,
+                                        void* d_hidden, void* d_W, int32_t dW_type, int32_t accumulate_dW, void* stream) {
+  NvtxRange range("af_candidate_logprob_backward");
+  if (!c) return AF_ERR_INVALID_ARG;
+  af_status st = candidate_sizes(T, K, d, V);
+  if (st != AF_OK) return st;
+  if (T > 0 && (!hidden || !W || !cand || !lse || !dcand || !d_hidden)) return AF_ERR_INVALID_ARG;
+  if ((st = candidate_head(hidden, W, d_hidden, d_W, dW_type, accumulate_dW, d, V)) != AF_OK) return st;
+  DeviceGuard guard(c->device);
+  return launch_candidate_backward(c, hidden, W, cand, lse, dcand, T, K, d, V, d_hidden,
+                                   HeadGradient{d_W, dW_type, accumulate_dW != 0}, static_cast<cudaStream_t>(stream));
+}
+
+af_status af_reserve_candidates(af_ctx* c, int64_t max_T, int32_t K, int32_t d, int32_t V, int32_t with_backward,
+                                int32_t dW_type) {
+  NvtxRange range("af_reserve_candidates");
+  if (!c || with_backward < 0 || with_backward > 2 || (dW_type != AF_F32 && dW_type != AF_BF16)) return AF_ERR_INVALID_ARG;
+  af_status st = candidate_sizes(max_T, K, d, V);
+  if (st != AF_OK || max_T == 0) return st;
+  DeviceGuard guard(c->device);
+  st = ws_grow(c->partial, candidate_partial_bytes(c, max_T, d, V));
+  if (st == AF_OK) st = ws_grow(c->cand_keys, (size_t)max_T * K * sizeof(uint32_t));
+  if (st == AF_OK && with_backward >= 1) {
+    const int64_t Tc = backward_token_block(c, max_T);
+    st = ws_grow(c->cand_keys, (size_t)Tc * K * sizeof(uint32_t) + (size_t)Tc * sizeof(float));
+    if (st == AF_OK) st = reserve_head_gradient(c, max_T, d, V, dW_type == AF_BF16);
+  }
+  if (st == AF_OK && with_backward == 2) st = reserve_distill_update(c, max_T, K, V);
+  return st;
+}
+
+af_status af_distill_loss(af_ctx* c, const float* cand_logp, const float* teacher_logp, const int32_t* cu_seqlens,
+                          int32_t B, int64_t T, int32_t K, const af_distill_params* params, af_distill_out* out,
+                          float* token_loss, float* dcand, void* stream) {
+  NvtxRange range("af_distill_loss");
+  if (!c || !params || !out || !cu_seqlens || B < 0 || T < 0 || K < 1) return AF_ERR_INVALID_ARG;
+  if (T > 0 && (!cand_logp || !teacher_logp || B < 1)) return AF_ERR_INVALID_ARG;
+  if (K > AF_MAX_CANDIDATES || T > ((int64_t)1 << 31) - 65536) return AF_ERR_SHAPE;
+  const af_status st = distill_params_ok(*params);
+  if (st != AF_OK) return st;
+  DeviceGuard guard(c->device);
+  return launch_distill_loss(cand_logp, teacher_logp, cu_seqlens, B, T, 0, T, K, *params, out, token_loss, dcand,
+                             c->loss_ws.p, c->d_err, c->sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? AF_OK : AF_ERR_CUDA;
+}
+
+af_status af_distill_update(af_ctx* c, const void* hidden, const void* W, const int32_t* cand, const float* teacher_logp,
+                            const int32_t* cu_seqlens, int32_t B, int64_t T, int32_t K, int32_t d, int32_t V,
+                            const af_distill_params* params, af_distill_out* out, float* cand_logp, float* entropy,
+                            float* lse, float* token_loss, float* dcand, void* d_hidden, void* d_W, int32_t dW_type,
+                            int32_t accumulate_dW, void* stream) {
+  NvtxRange range("af_distill_update");
+  if (!c || !params || !out || !cu_seqlens || B < 0) return AF_ERR_INVALID_ARG;
+  af_status st = candidate_sizes(T, K, d, V);
+  if (st != AF_OK) return st;
+  if (T > 0 && (!hidden || !W || !cand || !teacher_logp || !cand_logp || !lse || !d_hidden || B < 1))
+    return AF_ERR_INVALID_ARG;
+  if (T > ((int64_t)1 << 31) - 65536) return AF_ERR_SHAPE;
+  if ((st = distill_params_ok(*params)) != AF_OK) return st;
+  if ((st = candidate_head(hidden, W, d_hidden, d_W, dW_type, accumulate_dW, d, V)) != AF_OK) return st;
+  DeviceGuard guard(c->device);
+  return launch_distill_update(c, hidden, W, cand, teacher_logp, cu_seqlens, B, T, K, d, V, *params, out, cand_logp,
+                               entropy, lse, token_loss, dcand, d_hidden,
+                               HeadGradient{d_W, dW_type, accumulate_dW != 0}, static_cast<cudaStream_t>(stream));
+}
+
+static af_status preference_sizes(int64_t T, int32_t B) {
+  if (T < 0 || B < 0 || (T > 0 && B < 1)) return AF_ERR_INVALID_ARG;
+  return B % 2 != 0 || T > ((int64_t)1 << 31) - 65536 ? AF_ERR_SHAPE : AF_OK;
+}
+
+af_status af_preference_loss(af_ctx* c, const float* logp, const float* ref_logp, const int32_t* cu_seqlens, int32_t B,
+                             int64_t T, const af_preference_params* params, af_preference_out* out, float* pair_loss,
+                             float* seq_score, float* dlogp, void* stream) {
+  NvtxRange range("af_preference_loss");
+  if (!c || !params || !out || !cu_seqlens || (T > 0 && !logp)) return AF_ERR_INVALID_ARG;
+  af_status st = preference_sizes(T, B);
+  if (st != AF_OK) return st;
+  const af_preference_params& p = *params;
+  if (p.kind < 0 || p.kind > 2 || p.pair_layout < 0 || p.pair_layout > 1 || !positive_finite(p.beta) ||
+      !(p.label_smoothing >= 0.f && p.label_smoothing < 1.f))
+    return AF_ERR_INVALID_ARG;
+  DeviceGuard guard(c->device);
+  if ((st = ws_grow(c->pref_ws, preference_workspace_bytes(B, T))) != AF_OK) return st;
+  return launch_preference_loss(logp, ref_logp, cu_seqlens, B, T, p, out, pair_loss, seq_score, dlogp, c->pref_ws.p,
+                                c->loss_ws.p, c->d_err, c->sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? AF_OK : AF_ERR_CUDA;
+}
+
+af_status af_reserve_preference(af_ctx* c, int64_t max_T, int32_t max_B) {
+  NvtxRange range("af_reserve_preference");
+  if (!c) return AF_ERR_INVALID_ARG;
+  const af_status st = preference_sizes(max_T, max_B);
+  if (st != AF_OK) return st;
+  DeviceGuard guard(c->device);
+  return ws_grow(c->pref_ws, preference_workspace_bytes(max_B, max_T));
 }
 
 af_status af_controller_put(af_ctx* c, const af_controller_view* table, const int32_t* idx, int64_t n,

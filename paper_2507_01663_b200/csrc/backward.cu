@@ -18,6 +18,7 @@
 // vocabulary row write 128 consecutive bytes without any staging.  That orientation also gives the
 // product the forward's memory behaviour: the H_blk panels of the row tiles in flight stay in L2
 // while dZ streams past them (once per round of row tiles).
+#include "candidate.cuh"
 #include "device_util.cuh"
 #include "gemm_launch.cuh"
 
@@ -97,6 +98,68 @@ struct DzEpi {
   static __device__ __forceinline__ void unit_end(State&, const Params&, int, int) {}
 };
 
+// ---- epilogue 1b: logits tile -> dZ of listed candidates --------------------------------------------
+// dZ_tv = sum_{k: cand[t,k] = v} g_tk - G_t exp(z_tv - lse_t),  G_t = sum_k g_tk: the softmax part is dense,
+// the rest lands on the K listed columns, which the sweep meets in the order of the sorted keys.  Both are
+// added in fp32 and rounded to bf16 once.
+struct DzCandidateEpi {
+  struct Params {
+    const uint32_t* keys;   // [rows, K] sorted
+    const float* g;         // [rows, K] in list order
+    const float* gsum;      // [rows]
+    const float* lse;       // [rows]
+    __nv_bfloat16* dz;      // [rows, V]
+    int rows, V, K;
+  };
+  struct State {
+    float gsum, nl;
+    int next;               // -1: the unit's first chunk has not been met
+    uint32_t key;
+  };
+  static constexpr bool kStaged = true;
+  static __device__ __forceinline__ void unit_begin(State& st, const Params& p, int row, int, int) {
+    st.next = -1;
+    st.key = kNoCandidate;
+    if (row < p.rows) {
+      st.gsum = __ldg(p.gsum + row);
+      st.nl = -__ldg(p.lse + row) * kLog2e;
+    } else {
+      st.gsum = 0.f; st.nl = 0.f;
+    }
+  }
+  static __device__ __forceinline__ void chunk(State& st, const Params& p, int row, int col0,
+                                               const uint32_t (&v)[32], uint8_t* stage) {
+    if (col0 >= p.V) return;                       // uniform across the warp
+    const int lane = threadIdx.x & 31;
+    const uint32_t* keys = p.keys + (size_t)row * p.K;      // read for rows < p.rows only
+    if (st.next < 0) {
+      st.next = 0;
+      if (row < p.rows) {
+        st.next = first_candidate(keys, p.K, col0);
+        st.key = candidate_at(keys, p.K, st.next);
+      }
+    }
+    float dzv[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      dzv[j] = -st.gsum * ex2f(fmaf(__uint_as_float(v[j]), kLog2e, st.nl));
+    while ((int)(st.key >> 8) < col0 + 32) {
+      const int j = (int)(st.key >> 8) - col0;
+      const float g = __ldg(p.g + (size_t)row * p.K + (st.key & 255u));
+#pragma unroll
+      for (int i = 0; i < 32; ++i) dzv[i] += i == j ? g : 0.f;
+      ++st.next;
+      st.key = candidate_at(keys, p.K, st.next);
+    }
+    uint32_t w[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(dzv[2 * j], dzv[2 * j + 1]);
+    __syncwarp();
+    store_chunk_bf16(w, stage, lane, p.dz, p.V, row - lane, col0, p.rows, p.V);
+  }
+  static __device__ __forceinline__ void unit_end(State&, const Params&, int, int) {}
+};
+
 // ---- epilogue 2: accumulator tile -> bf16 matrix ------------------------------------------------
 struct StoreBf16Epi {
   struct Params {
@@ -161,6 +224,33 @@ struct StoreF32TransposedEpi {
   static __device__ __forceinline__ void unit_end(State&, const Params&, int, int) {}
 };
 
+// ---- epilogue 3b: the same into a bf16 matrix, on top of fp32 sums of earlier blocks if there are any ----
+struct StoreBf16TransposedEpi {
+  struct Params {
+    __nv_bfloat16* C;     // [N, M] row-major
+    const float* sums;    // [N, M] sums of the earlier token blocks, or null
+    int64_t ldc;
+    int M, N;
+  };
+  struct State {};
+  static constexpr bool kStaged = false;
+  static __device__ __forceinline__ void unit_begin(State&, const Params&, int, int, int) {}
+  static __device__ __forceinline__ void chunk(State&, const Params& p, int row, int col0,
+                                               const uint32_t (&v)[32], uint8_t*) {
+    if (col0 >= p.N || row >= p.M) return;
+    const size_t at = (size_t)col0 * p.ldc + row;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      if (col0 + j < p.N) {
+        float w = __uint_as_float(v[j]);
+        if (p.sums) w += p.sums[at + (size_t)j * p.ldc];
+        p.C[at + (size_t)j * p.ldc] = __float2bfloat16_rn(w);
+      }
+    }
+  }
+  static __device__ __forceinline__ void unit_end(State&, const Params&, int, int) {}
+};
+
 }  // namespace
 
 // The two products that consume a block of dZ [tc, V] (bf16):
@@ -198,6 +288,93 @@ af_status launch_backward_products(af_ctx* ctx, const void* hidden_blk, const vo
   af_status st = dH_product();
   if (st != AF_OK) return st;
   return dW_product();
+}
+
+// The same two products for a head whose gradient is wanted in fp32, in bf16 or not at all.  A bf16 d_W is
+// rounded once: with several token blocks the earlier ones are summed in fp32 in the workspace and the last
+// one's epilogue adds and rounds.
+af_status launch_head_products(af_ctx* ctx, const void* hidden_blk, const void* W, const void* dz_blk, int64_t tc,
+                               int32_t d, int32_t V, void* d_hidden_blk, const HeadGradient& head, bool first_block,
+                               bool last_block, cudaStream_t s) {
+  const GemmEnv env = gemm_env(ctx);
+  const uint64_t dB = (uint64_t)d * 2, vB = (uint64_t)V * 2;
+  const Operand Hblk{hidden_blk, (uint64_t)tc, (uint64_t)d, dB};
+  const Operand Wop{W, (uint64_t)V, (uint64_t)d, dB};
+  const Operand dZop{dz_blk, (uint64_t)tc, (uint64_t)V, vB};
+  auto dH_product = [&]() {
+    StoreBf16Epi::Params p2{static_cast<__nv_bfloat16*>(d_hidden_blk), d, (int)tc, d};
+    return run_gemm<StoreBf16Epi, false, true>(env, dZop, Wop, 0, p2, s);
+  };
+  auto dW_product = [&]() {
+    const int S = logprob_pick_splits((int64_t)d, (int32_t)tc, V, ctx->sm_count, env.pair, 0, 0);
+    if (head.type == AF_BF16 && last_block) {
+      StoreBf16TransposedEpi::Params p3{static_cast<__nv_bfloat16*>(head.d_W),
+                                        first_block ? nullptr : static_cast<const float*>(ctx->dw_sums.p), d, d, V};
+      return run_gemm<StoreBf16TransposedEpi, true, true>(env, Hblk, dZop, S, p3, s);
+    }
+    float* C = head.type == AF_BF16 ? static_cast<float*>(ctx->dw_sums.p) : static_cast<float*>(head.d_W);
+    const bool add = !first_block || (head.type == AF_F32 && head.accumulate);
+    StoreF32TransposedEpi::Params p3{C, d, d, V, add ? 1 : 0};
+    return run_gemm<StoreF32TransposedEpi, true, true>(env, Hblk, dZop, S, p3, s);
+  };
+  if (!head.d_W) return dH_product();
+  if (last_block && ctx->dw_ready) {      // as in launch_backward_products
+    af_status st = dW_product();
+    if (st != AF_OK) return st;
+    if (cudaEventRecord(ctx->dw_ready, s) != cudaSuccess) return AF_ERR_CUDA;
+    return dH_product();
+  }
+  const af_status st = dH_product();
+  return st != AF_OK ? st : dW_product();
+}
+
+// d_W of an empty batch, and the event that says it is complete.
+af_status head_gradient_of_nothing(af_ctx* ctx, const HeadGradient& head, int32_t d, int32_t V, cudaStream_t s) {
+  if (!head.d_W) return AF_OK;
+  const size_t bytes = (size_t)V * d * (head.type == AF_BF16 ? 2 : 4);
+  if (!head.accumulate && cudaMemsetAsync(head.d_W, 0, bytes, s) != cudaSuccess) return AF_ERR_CUDA;
+  if (ctx->dw_ready && cudaEventRecord(ctx->dw_ready, s) != cudaSuccess) return AF_ERR_CUDA;
+  return AF_OK;
+}
+
+// Scratch of the candidate backward: dZ of one token block and, for a bf16 d_W over several blocks, the fp32 sums.
+af_status reserve_head_gradient(af_ctx* ctx, int64_t T, int32_t d, int32_t V, bool bf16_head) {
+  const int64_t Tc = backward_token_block(ctx, T);
+  af_status st = ws_grow(ctx->dz, (size_t)Tc * V * 2);
+  if (st == AF_OK && bf16_head && T > Tc) st = ws_grow(ctx->dw_sums, (size_t)V * d * sizeof(float));
+  return st;
+}
+
+// af_candidate_logprob_backward: per token block the sorted lists and G, then dZ on the tensor cores (the
+// logits recomputed) and the two products.
+af_status launch_candidate_backward(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand,
+                                    const float* lse, const float* g, int64_t T, int32_t K, int32_t d, int32_t V,
+                                    void* d_hidden, const HeadGradient& head, cudaStream_t s) {
+  if (T == 0) return head_gradient_of_nothing(ctx, head, d, V, s);
+  af_status st = reserve_head_gradient(ctx, T, d, V, head.d_W && head.type == AF_BF16);
+  if (st != AF_OK) return st;
+  const int64_t Tc = backward_token_block(ctx, T);
+  const size_t key_bytes = (size_t)Tc * K * sizeof(uint32_t);
+  if ((st = ws_grow(ctx->cand_keys, key_bytes + (size_t)Tc * sizeof(float))) != AF_OK) return st;
+  uint32_t* keys = static_cast<uint32_t*>(ctx->cand_keys.p);
+  float* gsum = reinterpret_cast<float*>(static_cast<char*>(ctx->cand_keys.p) + key_bytes);
+  __nv_bfloat16* dz = static_cast<__nv_bfloat16*>(ctx->dz.p);
+  const __nv_bfloat16* H = static_cast<const __nv_bfloat16*>(hidden);
+  const GemmEnv env = gemm_env(ctx);
+  for (int64_t t0 = 0; t0 < T; t0 += Tc) {
+    const int64_t tc = (T - t0) < Tc ? (T - t0) : Tc;
+    if (launch_sort_candidates(cand + t0 * K, g + t0 * K, tc, K, V, keys, gsum, s) != cudaSuccess) return AF_ERR_CUDA;
+    const Operand Hblk{H + t0 * d, (uint64_t)tc, (uint64_t)d, (uint64_t)d * 2};
+    const Operand Wop{W, (uint64_t)V, (uint64_t)d, (uint64_t)d * 2};
+    DzCandidateEpi::Params p1{keys, g + t0 * K, gsum, lse + t0, dz, (int)tc, V, K};
+    st = run_gemm<DzCandidateEpi, false, false>(
+        env, Hblk, Wop, logprob_pick_splits(tc, d, V, ctx->sm_count, env.pair, ctx->v_splits, env.die0_pairs), p1, s);
+    if (st != AF_OK) return st;
+    st = launch_head_products(ctx, H + t0 * d, W, dz, tc, d, V, static_cast<__nv_bfloat16*>(d_hidden) + t0 * d, head,
+                              t0 == 0, t0 + Tc >= T, s);
+    if (st != AF_OK) return st;
+  }
+  return AF_OK;
 }
 
 // Token block of the backward (and of the fused update): a multiple of 128 rows.

@@ -1,0 +1,299 @@
+// af_candidate_logprob: log-probs of K listed vocabulary ids per token -- the LM-head GEMM with the
+// online log-softmax of af_token_logprob, whose epilogue also hands out the listed logits.
+//
+//   z_tv = h_t . w_v;   lse_t = log sum_v e^{z_tv};   cand_logp[t,k] = z_{t, cand[t,k]} - lse_t
+//
+// Bound: tensor cores for batches (2 T d V), the stream of W for single tokens (2 d V bytes).  The
+// lists cost next to nothing on top: each row's list is sorted into keys once (4 bytes per slot), and
+// a thread of the epilogue, which owns a row and sweeps the vocabulary upwards, compares one key with
+// the end of its columns per 32 of them.  Fetching the K rows of W again for K dot products instead
+// would move 2 K d bytes per token (0.46 MB at K = 64, d = 3584: a tenth of the GEMM's time).
+//
+// The accumulation is promoted to round-to-nearest every kPromoteBlocks K blocks (see umma.cuh).
+#include "candidate.cuh"
+#include "gemm_launch.cuh"
+
+namespace af {
+namespace {
+
+constexpr int kPromoteBlocks = 4;       // K = 256 per part
+
+struct CandidateState {
+  float m, s, u;
+  const uint32_t* keys;                 // this row's sorted list
+  int next;                             // first entry not behind the sweep
+  uint32_t key;                         // that entry
+};
+
+// kStoreZ: write the fp32 logits of the tile (one token block of the fused update, which picks from them
+// later); otherwise the listed logits go to cand_z as the sweep passes them.
+template <bool kStoreZ>
+struct CandidateEpi {
+  struct Params {
+    const uint32_t* keys;   // [T, K] sorted (not kStoreZ)
+    float* cand_z;          // [T, K] (not kStoreZ)
+    float4* partial;        // [T, parts]: m, s, u of every part
+    float* z;               // [T, V] (kStoreZ)
+    int T, V, K, parts;
+  };
+  using State = CandidateState;
+  static __device__ __forceinline__ void unit_begin(State& st, const Params& p, int row, int col0) {
+    st.m = -INFINITY; st.s = 0.f; st.u = 0.f;
+    st.key = kNoCandidate;
+    if constexpr (!kStoreZ) {
+      if (row < p.T) {
+        st.keys = p.keys + (size_t)row * p.K;
+        st.next = first_candidate(st.keys, p.K, col0);
+        st.key = candidate_at(st.keys, p.K, st.next);
+      }
+    }
+  }
+  static __device__ __forceinline__ void tile(State& st, const Params& p, int row, int col0,
+                                              float (&a)[umma::kPromoteCols]) {
+    constexpr int kCols = umma::kPromoteCols;
+    if (col0 >= p.V) return;
+    if constexpr (kStoreZ) {
+      if (row < p.T) {
+        float* dst = p.z + (size_t)row * p.V + col0;           // V % 8 == 0 here: 16-byte aligned
+        if (col0 + kCols <= p.V) {
+#pragma unroll
+          for (int q = 0; q < kCols / 4; ++q)
+            reinterpret_cast<float4*>(dst)[q] = make_float4(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < kCols; ++j) if (col0 + j < p.V) dst[j] = a[j];
+        }
+      }
+    } else {
+      // entries of the other column half that the sweep has passed by
+      while ((int)(st.key >> 8) < col0) { ++st.next; st.key = candidate_at(st.keys, p.K, st.next); }
+#pragma unroll
+      for (int c = 0; c < kCols; c += 32) {
+        while ((int)(st.key >> 8) < col0 + c + 32) {
+          const int j = (int)(st.key >> 8) - (col0 + c);
+          float z = a[c];
+#pragma unroll
+          for (int i = 1; i < 32; ++i) z = i == j ? a[c + i] : z;
+          p.cand_z[(size_t)row * p.K + (st.key & 255u)] = z;
+          ++st.next;
+          st.key = candidate_at(st.keys, p.K, st.next);
+        }
+      }
+    }
+    if (col0 + kCols > p.V) {   // ragged vocabulary tail: columns >= V hold zero-fill, not logits
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) if (col0 + j >= p.V) a[j] = -1.0e30f;
+    }
+    float mx[4] = {a[0], a[1], a[2], a[3]};
+#pragma unroll
+    for (int j = 4; j < kCols; ++j) mx[j & 3] = fmaxf(mx[j & 3], a[j]);
+    const float m_new = fmaxf(st.m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+    const float sc = ex2f((st.m - m_new) * kLog2e);             // 0 on the first tile (m = -inf)
+    const float nm = -m_new * kLog2e;
+    float s[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};   // short sums first: less rounding
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) {
+      const float e = ex2f(fmaf(a[j], kLog2e, nm));
+      s[j & 3] += e;
+      u[j & 3] = fmaf(e, a[j], u[j & 3]);
+    }
+    st.m = m_new;
+    st.s = fmaf(st.s, sc, (s[0] + s[1]) + (s[2] + s[3]));
+    st.u = fmaf(st.u, sc, (u[0] + u[1]) + (u[2] + u[3]));
+  }
+  static __device__ __forceinline__ void unit_end(State& st, const Params& p, int row, int part) {
+    if (row < p.T) p.partial[(size_t)row * p.parts + part] = make_float4(st.m, st.s, st.u, 0.f);
+  }
+};
+
+// ---- the lists -> sorted keys -------------------------------------------------------------------------
+// One warp per token, kE entries per lane (entry i = e * 32 + lane), bitonic network.
+template <int kE>
+__global__ void __launch_bounds__(256) sort_candidates_kernel(
+    const int32_t* __restrict__ cand, const float* __restrict__ g, int64_t rows, int K, int V,
+    uint32_t* __restrict__ keys, float* __restrict__ gsum) {
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 31;
+  uint32_t x[kE];
+  double sum = 0.0;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    const int k = e * 32 + lane;
+    x[e] = kNoCandidate;
+    if (k < K) {
+      const int id = __ldg(cand + row * K + k);
+      if (id >= 0 && id < V) {
+        x[e] = ((uint32_t)id << 8) | (uint32_t)k;
+        if (g) sum += (double)__ldg(g + row * K + k);
+      }
+    }
+  }
+  if (g) {     // 64 bits: the gradients of a renormalised list cancel in this sum
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) gsum[row] = (float)sum;
+  }
+#pragma unroll
+  for (int size = 2; size <= 32 * kE; size <<= 1) {
+#pragma unroll
+    for (int stride = size >> 1; stride > 0; stride >>= 1) {
+      if (stride >= 32) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          const int o = e ^ (stride >> 5);
+          if (o > e) {
+            const bool up = ((e * 32) & size) == 0;          // size > 32 here: the lane does not decide
+            const uint32_t lo = x[e] < x[o] ? x[e] : x[o], hi = x[e] < x[o] ? x[o] : x[e];
+            x[e] = up ? lo : hi;
+            x[o] = up ? hi : lo;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          const uint32_t other = __shfl_xor_sync(0xffffffffu, x[e], stride);
+          const bool up = ((e * 32 + lane) & size) == 0, low = (lane & stride) == 0;
+          x[e] = (up == low) ? (x[e] < other ? x[e] : other) : (x[e] < other ? other : x[e]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    const int k = e * 32 + lane;
+    if (k < K) keys[row * K + k] = x[e];
+  }
+}
+
+// ---- partial softmax states -> lse, entropy; listed logits -> log-probs ----------------------------------
+// One warp per token.  kFromZ: the listed logits are picked from the stored logits z [rows, V] here.
+template <bool kFromZ>
+__global__ void __launch_bounds__(256) finish_candidates_kernel(
+    const float4* __restrict__ partial, int parts, const int32_t* __restrict__ cand, const float* __restrict__ z,
+    int64_t rows, int K, int V, float* __restrict__ cand_logp, float* __restrict__ entropy,
+    float* __restrict__ lse_out, unsigned int* d_err) {
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 31;
+  const float4* q = partial + row * parts;
+  float M = -INFINITY;
+  for (int i = lane; i < parts; i += 32) M = fmaxf(M, __ldg(q + i).x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  float s = 0.f, u = 0.f;
+  for (int i = lane; i < parts; i += 32) {
+    const float4 c = __ldg(q + i);
+    // a part whose columns all lie past the vocabulary's end never began: (-inf, 0, 0)
+    const float w = c.x == -INFINITY ? 0.f : ex2f((c.x - M) * kLog2e);
+    s = fmaf(c.y, w, s);
+    u = fmaf(c.z, w, u);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    s += __shfl_xor_sync(0xffffffffu, s, o);
+    u += __shfl_xor_sync(0xffffffffu, u, o);
+  }
+  const float lse = M + logf(s);
+  if (lane == 0) {
+    if (lse_out) lse_out[row] = lse;
+    if (entropy) entropy[row] = lse - u / s;
+  }
+  for (int k = lane; k < K; k += 32) {
+    const int id = __ldg(cand + row * K + k);
+    float lq;
+    if (id >= 0 && id < V) {
+      lq = (kFromZ ? __ldg(z + (size_t)row * V + id) : cand_logp[row * K + k]) - lse;
+    } else if (id < 0) {
+      lq = -INFINITY;                                          // an unused slot
+    } else {
+      lq = __int_as_float(0x7fc00000);
+      atomicOr(d_err, AF_DEVERR_TARGET_RANGE);
+    }
+    cand_logp[row * K + k] = lq;
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_sort_candidates(const int32_t* cand, const float* g, int64_t rows, int32_t K, int32_t V,
+                                   uint32_t* keys, float* gsum, cudaStream_t s) {
+  const unsigned blocks = (unsigned)((rows + 7) / 8);
+  if (K <= 32) sort_candidates_kernel<1><<<blocks, 256, 0, s>>>(cand, g, rows, K, V, keys, gsum);
+  else if (K <= 64) sort_candidates_kernel<2><<<blocks, 256, 0, s>>>(cand, g, rows, K, V, keys, gsum);
+  else if (K <= 128) sort_candidates_kernel<4><<<blocks, 256, 0, s>>>(cand, g, rows, K, V, keys, gsum);
+  else sort_candidates_kernel<8><<<blocks, 256, 0, s>>>(cand, g, rows, K, V, keys, gsum);
+  return cudaGetLastError();
+}
+
+// Vocabulary ranges per row tile.  Up to a few row tiles the launch is the stream of W, and every CTA pair
+// should carry a share of it; the rule of af_token_logprob stops at 32 ranges.
+int candidate_pick_splits(const af_ctx* ctx, int64_t T, int32_t d, int32_t V) {
+  const int workers = ctx->sm_count / 2 > 0 ? ctx->sm_count / 2 : 1;
+  const int64_t m_tiles = (T + umma::kPairBM - 1) / umma::kPairBM;
+  const int n_tiles = (V + umma::kBN - 1) / umma::kBN;
+  if (ctx->v_splits == 0 && m_tiles * 32 < workers) {
+    const int S = (int)(workers / m_tiles);
+    return S < n_tiles ? S : n_tiles;
+  }
+  const int die0_pairs = ctx->die_aware && ctx->die0_sms > 0 ? ctx->die0_sms / 2 : 0;
+  return logprob_pick_splits(T, d, V, ctx->sm_count, true, ctx->v_splits, die0_pairs);
+}
+
+size_t candidate_partial_bytes(const af_ctx* ctx, int64_t max_T, int32_t d, int32_t V) {
+  const int64_t S = candidate_pick_splits(ctx, max_T, d, V);
+  // smaller batches may pick up to 8 ranges whatever their size, and more only while there are at most 8
+  // units per pair (one unit = 256 rows of two parts)
+  const int64_t need = (S > 8 ? S : 8) * 2 * max_T;
+  const int64_t small = (int64_t)(ctx->sm_count / 2 + 1) * 8 * 2 * umma::kPairBM;
+  return (size_t)(need > small ? need : small) * sizeof(float4);
+}
+
+// Logits of `T` rows (kStoreZ) or their listed ones, and the partial softmax states; *parts: states per row.
+static af_status candidate_gemm(af_ctx* ctx, const void* hidden, const void* W, int64_t T, int32_t d, int32_t V,
+                                int32_t K, const uint32_t* keys, float* cand_z, float* z, int* parts,
+                                cudaStream_t s) {
+  const GemmEnv env = gemm_env(ctx);
+  const int n_tiles = (V + umma::kBN - 1) / umma::kBN;
+  int S = candidate_pick_splits(ctx, T, d, V);
+  if (S > n_tiles) S = n_tiles;
+  *parts = 2 * S;
+  af_status st = ws_grow(ctx->partial, (size_t)*parts * (size_t)T * sizeof(float4));
+  if (st != AF_OK) return st;
+  const Operand Hop{hidden, (uint64_t)T, (uint64_t)d, (uint64_t)d * 2};
+  const Operand Wop{W, (uint64_t)V, (uint64_t)d, (uint64_t)d * 2};
+  float4* partial = static_cast<float4*>(ctx->partial.p);
+  if (z) {
+    CandidateEpi<true>::Params ep{nullptr, nullptr, partial, z, (int)T, V, K, *parts};
+    return run_gemm_promoted<CandidateEpi<true>, kPromoteBlocks>(env, Hop, Wop, S, ep, s);
+  }
+  CandidateEpi<false>::Params ep{keys, cand_z, partial, nullptr, (int)T, V, K, *parts};
+  return run_gemm_promoted<CandidateEpi<false>, kPromoteBlocks>(env, Hop, Wop, S, ep, s);
+}
+
+af_status launch_candidate_logprob(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand, int64_t T,
+                                   int32_t K, int32_t d, int32_t V, float* cand_logp, float* entropy, float* lse,
+                                   cudaStream_t s) {
+  af_status st = ws_grow(ctx->cand_keys, (size_t)T * K * sizeof(uint32_t));
+  if (st != AF_OK) return st;
+  uint32_t* keys = static_cast<uint32_t*>(ctx->cand_keys.p);
+  if (launch_sort_candidates(cand, nullptr, T, K, V, keys, nullptr, s) != cudaSuccess) return AF_ERR_CUDA;
+  int parts = 0;
+  if ((st = candidate_gemm(ctx, hidden, W, T, d, V, K, keys, cand_logp, nullptr, &parts, s)) != AF_OK) return st;
+  finish_candidates_kernel<false><<<(unsigned)((T + 7) / 8), 256, 0, s>>>(
+      static_cast<const float4*>(ctx->partial.p), parts, cand, nullptr, T, K, V, cand_logp, entropy, lse, ctx->d_err);
+  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+}
+
+af_status launch_candidate_logprob_z(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand, int64_t T,
+                                     int32_t K, int32_t d, int32_t V, float* cand_logp, float* entropy, float* lse,
+                                     float* z, cudaStream_t s) {
+  int parts = 0;
+  const af_status st = candidate_gemm(ctx, hidden, W, T, d, V, K, nullptr, nullptr, z, &parts, s);
+  if (st != AF_OK) return st;
+  finish_candidates_kernel<true><<<(unsigned)((T + 7) / 8), 256, 0, s>>>(
+      static_cast<const float4*>(ctx->partial.p), parts, cand, z, T, K, V, cand_logp, entropy, lse, ctx->d_err);
+  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+}
+
+}  // namespace af

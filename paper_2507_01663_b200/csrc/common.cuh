@@ -91,6 +91,10 @@ struct af_ctx {
   af::Buf ctrl_ws;    // per-block aggregates of af_controller_get
   af::Buf zlog;       // fp32 logits [Tc, V] of one token block (fused actor update)
   af::Buf adv_ws;     // per-group accumulators of af_grpo_advantage with group ids
+  af::Buf cand_keys;  // sorted candidate lists [T, K] (and sums of their gradients [Tc] in the backward)
+  af::Buf dw_sums;    // fp32 sums [V, d] behind a bf16 d_W of several token blocks
+  af::Buf distill_ws; // gradients [Tc, K] of one token block of af_distill_update when the caller wants none
+  af::Buf pref_ws;    // partial sums of the sequences of af_preference_loss
 
   // pinned staging ring for pack metadata
   void* pack_host[af::kPackRing] = {};
@@ -193,6 +197,49 @@ af_status launch_policy_update(af_ctx* ctx, const void* hidden, const void* W, c
                                const af_loss_params& params, af_loss_out* out, float* logp, float* entropy,
                                float* lse, float* dlogp, void* d_hidden, float* d_W, int32_t accumulate_dW,
                                cudaStream_t s);
+
+// ---- listed candidates and distillation -------------------------------------------------------
+struct HeadGradient {       // where the gradient of the LM head goes
+  void* d_W;                // [V, d], or null: a frozen head
+  int32_t type;             // AF_F32 or AF_BF16
+  bool accumulate;          // add to d_W (AF_F32 only)
+};
+int candidate_pick_splits(const af_ctx* ctx, int64_t T, int32_t d, int32_t V);
+size_t candidate_partial_bytes(const af_ctx* ctx, int64_t max_T, int32_t d, int32_t V);
+af_status launch_candidate_logprob(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand, int64_t T,
+                                   int32_t K, int32_t d, int32_t V, float* cand_logp, float* entropy, float* lse,
+                                   cudaStream_t s);
+// The same with the fp32 logits [T, V] kept in z.
+af_status launch_candidate_logprob_z(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand, int64_t T,
+                                     int32_t K, int32_t d, int32_t V, float* cand_logp, float* entropy, float* lse,
+                                     float* z, cudaStream_t s);
+af_status reserve_head_gradient(af_ctx* ctx, int64_t T, int32_t d, int32_t V, bool bf16_head);
+af_status launch_head_products(af_ctx* ctx, const void* hidden_blk, const void* W, const void* dz_blk, int64_t tc,
+                               int32_t d, int32_t V, void* d_hidden_blk, const HeadGradient& head, bool first_block,
+                               bool last_block, cudaStream_t s);
+af_status head_gradient_of_nothing(af_ctx* ctx, const HeadGradient& head, int32_t d, int32_t V, cudaStream_t s);
+af_status launch_candidate_backward(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand,
+                                    const float* lse, const float* g, int64_t T, int32_t K, int32_t d, int32_t V,
+                                    void* d_hidden, const HeadGradient& head, cudaStream_t s);
+
+// Rows [t0, t0 + rows) of a batch of T tokens; the per-token pointers start at token t0, cu is the batch's.
+// `out` (nullable) receives the record of these rows: pass it for a call over the whole batch.
+cudaError_t launch_distill_loss(const float* cand_logp, const float* teacher_logp, const int32_t* cu, int32_t B,
+                                int64_t T, int64_t t0, int64_t rows, int32_t K, const af_distill_params& p,
+                                af_distill_out* out, float* token_loss, float* dcand, void* ws, unsigned int* d_err,
+                                int sm_count, cudaStream_t s);
+af_status launch_distill_update(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand,
+                                const float* teacher_logp, const int32_t* cu_seqlens, int32_t B, int64_t T, int32_t K,
+                                int32_t d, int32_t V, const af_distill_params& params, af_distill_out* out,
+                                float* cand_logp, float* entropy, float* lse, float* token_loss, float* dcand,
+                                void* d_hidden, const HeadGradient& head, cudaStream_t s);
+af_status reserve_distill_update(af_ctx* ctx, int64_t T, int32_t K, int32_t V);
+
+size_t preference_workspace_bytes(int32_t B, int64_t T);
+cudaError_t launch_preference_loss(const float* logp, const float* ref_logp, const int32_t* cu, int32_t B, int64_t T,
+                                   const af_preference_params& p, af_preference_out* out, float* pair_loss,
+                                   float* seq_score, float* dlogp, void* ws, void* loss_ws, unsigned int* d_err,
+                                   int sm_count, cudaStream_t s);
 
 af_status launch_backward(af_ctx* ctx, const void* hidden, const void* W, const int32_t* target,
                           const float* lse, const float* dlogp, int64_t T, int32_t d, int32_t V,

@@ -129,6 +129,31 @@ af_status run_gemm(const GemmEnv& env, const Operand& A, const Operand& B, int s
   return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
+// The same product on K-major operands with promoted accumulation (see umma.cuh): always the CTA-pair
+// main loop.  E is a functor of the promoted form.
+template <class E, int kPromote>
+af_status run_gemm_promoted(const GemmEnv& env, const Operand& A, const Operand& B, int splits,
+                            const typename E::Params& ep, cudaStream_t s) {
+  CUtensorMap ta, tb;
+  af_status st = encode_operand(env, &ta, A, umma::kBM);
+  if (st != AF_OK) return st;
+  st = encode_operand(env, &tb, B, umma::kBN / 2);
+  if (st != AF_OK) return st;
+  umma::GemmShape g = gemm_shape(A.rows, B.rows, A.cols, splits, true);
+  const int64_t units = (int64_t)g.m_tiles * g.splits;
+  static SmemAttrOnce once;
+  if (set_smem_once(once, umma::gemm_pair_kernel<E, false, false, kPromote>, umma::kPairSmemBytes) != cudaSuccess)
+    return AF_ERR_CUDA;
+  const int pairs = env.sm_count / 2;
+  const int grid = 2 * (int)(units < pairs ? units : pairs);
+  unsigned int* clock = env.tile_clock;
+  const bool by_die = env.die_of_sm && clock && deal_by_die(g, pairs, env.die0_pairs);
+  if (clock && cudaMemsetAsync(clock, 0, (by_die ? 3 : 1) * sizeof(unsigned int), s) != cudaSuccess) return AF_ERR_CUDA;
+  umma::gemm_pair_kernel<E, false, false, kPromote><<<grid, umma::kPromoteThreads, umma::kPairSmemBytes, s>>>(
+      ta, tb, g, ep, env.d_err, clock, by_die ? clock + 1 : nullptr, env.die_of_sm);
+  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+}
+
 inline GemmEnv gemm_env(af_ctx* ctx) {
   return GemmEnv{ctx->encode, ctx->sm_count, ctx->d_err, ctx->gemm_pair != 0, ctx->d_err + kTileClockWord,
                  &ctx->tmaps, reinterpret_cast<const unsigned char*>(ctx->d_err) + kDieTableByte,

@@ -388,6 +388,19 @@ constexpr int kPairStageBytes = kABytes + kPairBBytes;        // 32 KB
 constexpr int kPairSmemBytes = kPairStages * kPairStageBytes + 1024 /*alignment slack*/ + 256 /*barriers*/;
 constexpr int kPairSmemBytesStaged = kPairSmemBytes + 4 * kEpiStageBytes;
 
+// Promoted accumulation.  The tensor core does not round its fp32 accumulator to nearest: every K = 16
+// step drops the bits below the accumulator's last place, so a logit of 13 after 224 steps (d = 3584)
+// comes out 1e-5 .. 5e-5 too small, always in the same direction.  A softmax over 1.5e5 such logits
+// inherits the bias (measured against 64 bits: lse -3.3e-5, entropy 2.4e-5 relative), which is nothing
+// for a policy loss held to 2e-3 but more than fp32 outputs are expected to be off by.  With kPromote > 0
+// the K loop is cut into parts of kPromote K blocks, each accumulated from zero in one of the two
+// tensor-memory accumulators, and the epilogue threads add the parts up in registers, rounding to
+// nearest: the truncation then acts on values `parts` times smaller.  Eight epilogue warps instead of
+// four share the 256 columns, so a thread holds 128 running sums; adding a part up takes a fraction of
+// the time the MMAs need for the next one and is hidden behind it.
+constexpr int kPromoteCols = kBN / 2;                         // columns per epilogue thread
+constexpr int kPromoteThreads = 64 + 256;                     // producer and MMA warps, eight epilogue warps
+
 __device__ __forceinline__ uint32_t cluster_ctarank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -479,8 +492,15 @@ __device__ __forceinline__ int pair_work_most(const GemmShape& g, int n_pairs) {
 
 // Work decomposition of the pair kernel: a unit is one 256-row tile times a range of B tiles;
 // see PairWork for which units a pair processes.
-template <class E, bool kAMN = false, bool kBMN = false>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+//
+// kPromote = 0: the epilogue functor is the one of gemm_kernel.  kPromote > 0 (promoted accumulation,
+// kPromote K blocks per part) calls for a functor of this form instead, whose threads own half a
+// tile's columns:
+//   static __device__ void unit_begin(State&, const Params&, int row, int col0);   col0: first column of the unit
+//   static __device__ void tile(State&, const Params&, int row, int col0, float (&a)[kPromoteCols]);
+//   static __device__ void unit_end(State&, const Params&, int row, int part);     part = 2 * split + column half
+template <class E, bool kAMN = false, bool kBMN = false, int kPromote = 0>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromote > 0 ? kPromoteThreads : kThreads, 1)
 gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                  const GemmShape g, const typename E::Params ep, unsigned int* d_err, unsigned int* tile_clock,
                  unsigned int* die_counters, const unsigned char* die_of_sm) {
@@ -504,7 +524,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int s = 0; s < kPairStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 8); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), kPromote > 0 ? 16 : 8); }
     fence_mbar_init();
     tma_prefetch_desc(&tmap_a);
     tma_prefetch_desc(&tmap_b);
@@ -638,11 +658,23 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
         const int s = (work.base_unit + q) % g.splits;
         const int nb = split_begin(g, s), ne = split_begin(g, s + 1);
         for (int nt = nb; nt < ne && ok; ++nt, ++tile_count) {
-          const uint32_t acc = tile_count & 1u, acc_phase = (tile_count >> 1) & 1u;
+          uint32_t acc = tile_count & 1u, acc_phase = (tile_count >> 1) & 1u;
           if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, &abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t d_tmem = tmem_base + acc * kBN;
+          uint32_t d_tmem = tmem_base + acc * kBN;
+          int part_kb = 0;                               // K blocks in the current part (kPromote > 0)
           for (int kb = 0; kb < g.k_blocks; ++kb) {
+            if constexpr (kPromote > 0) {
+              if (part_kb == kPromote) {                 // next part: publish this one, take the other accumulator
+                mma_commit_pair(tfull_bar(acc));
+                ++tile_count;                            // counts parts here
+                acc = tile_count & 1u; acc_phase = (tile_count >> 1) & 1u;
+                if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, &abort_flag)) { ok = false; break; }
+                tc_fence_after();
+                d_tmem = tmem_base + acc * kBN;
+                part_kb = 0;
+              }
+            }
             if (!mbar_wait(full_bar(stage), phase, &abort_flag)) { ok = false; break; }
             tc_fence_after();
             const uint32_t a_addr = tiles + stage * kPairStageBytes;
@@ -651,9 +683,10 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
 #pragma unroll
             for (int k = 0; k < kBK / kUmmaK; ++k) {
               mma_bf16_ss_pair(d_tmem, a_desc + (uint64_t)k * a_step, b_desc + (uint64_t)k * b_step, idesc,
-                               (kb | k) != 0 ? 1u : 0u);
+                               ((kPromote > 0 ? part_kb : kb) | k) != 0 ? 1u : 0u);
             }
             mma_commit_pair(empty_bar(stage));   // both CTAs' slots reusable once these MMAs have read them
+            ++part_kb;
             if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
           }
           if (ok) mma_commit_pair(tfull_bar(acc));  // accumulator complete in both CTAs
@@ -661,6 +694,44 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
       }
     }
     __syncwarp();
+  } else if constexpr (kPromote > 0) {
+    // ------------------------------------------- epilogue, promoted accumulation (warps 2..9, both CTAs)
+    const int quarter = warp & 3, half = (warp - 2) >> 2;         // TMEM lanes this warp may touch; its column half
+    const int row_in_tile = (int)rank * kBM + quarter * 32 + lane;
+    const int parts = (g.k_blocks + kPromote - 1) / kPromote;
+    uint32_t part_count = 0; bool ok = true;
+    typename E::State st;
+    for (int q = work.first; q < work.end && ok; q += work.step) {
+      const int u = work.base_unit + q;
+      const int m_tile = u / g.splits, s = u % g.splits;
+      const int nb = split_begin(g, s), ne = split_begin(g, s + 1);
+      const int row = m_tile * kPairBM + row_in_tile;
+      E::unit_begin(st, ep, row, nb * kBN);
+      for (int nt = nb; nt < ne && ok; ++nt) {
+        float a[kPromoteCols];
+#pragma unroll
+        for (int j = 0; j < kPromoteCols; ++j) a[j] = 0.f;
+        for (int p = 0; p < parts; ++p, ++part_count) {
+          const uint32_t acc = part_count & 1u, acc_phase = (part_count >> 1) & 1u;
+          if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, &abort_flag))) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * kBN + half * kPromoteCols;
+#pragma unroll
+          for (int c = 0; c < kPromoteCols / 32; ++c) {
+            uint32_t v[32];
+            tmem_ld32(t_row + c * 32, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) a[c * 32 + j] += __uint_as_float(v[j]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(tempty_bar(acc), 0);   // one arrival per warp, on the leader
+        }
+        if (ok) E::tile(st, ep, row, nt * kBN + half * kPromoteCols, a);
+      }
+      if (ok) E::unit_end(st, ep, row, 2 * s + half);
+    }
   } else {
     // ---------------------------------------------------------------- epilogue (warps 2..5, both CTAs)
     const int quarter = warp & 3;
