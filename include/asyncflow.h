@@ -398,8 +398,8 @@ af_status af_reserve_candidates(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d
  * loss of a distillation task; the paper's loss, af_policy_loss, learns from rewards instead).
  *
  * lt = teacher_logp[t,k], lq = cand_logp[t,k] (from af_candidate_logprob), both over the whole
- * vocabulary.  A slot with lt = -inf is absent: its lq is not looked at and its gradient is 0; a token
- * whose slots are all absent has loss 0.  p = exp(lt), q = exp(lq); sums run over the present slots;
+ * vocabulary.  A slot with lt = -inf is absent: its lq is not looked at and its gradient is 0 (a NaN in a
+ * present slot makes its whole token NaN); a token whose slots are all absent has loss 0.  p = exp(lt), q = exp(lq); sums run over the present slots;
  * 0 log 0 = 0.
  *   divergence 0: from teacher to student;  1: from student to teacher.
  *   support 0 (as listed):   0: sum p (lt - lq);   1: sum q (lq - lt)
@@ -479,8 +479,8 @@ af_status af_distill_update(af_ctx* ctx, const void* hidden, const void* W, cons
  *
  * logp, ref_logp (nullable), dlogp (nullable): [T] fp32 dev; cu_seqlens [B+1] as in af_policy_loss;
  * pair_loss [P], seq_score [B] fp32 dev (nullable); `out`: device struct.  Sums in fp64 in a fixed order:
- * results are bit-reproducible.  Workspace: 20 bytes per sequence and 32 per 256 tokens, grown on demand or
- * by af_reserve_preference.
+ * results are bit-reproducible.  Workspace: 20 bytes per sequence and 0.3 MB, grown on demand or by
+ * af_reserve_preference.
  * Errors: AF_ERR_INVALID_ARG for null pointers, unknown enum values, beta not finite and positive,
  * label_smoothing outside [0, 1); AF_ERR_SHAPE for an odd B or T >= 2^31 - 65536.
  * ------------------------------------------------------------------------------------------- */

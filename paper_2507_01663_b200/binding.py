@@ -179,6 +179,15 @@ def _stream(stream) -> C.c_void_p:
     return C.c_void_p(s.cuda_stream)
 
 
+def _addr(t: Optional[torch.Tensor]):
+    """As _ptr, as the plain integer that ctypes converts by itself (these calls can be a few microseconds long)."""
+    if t is None:
+        return None
+    if t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("device buffers must be contiguous CUDA tensors")
+
+
 def _check(status: int, where: str):
     if status != AF_OK:
         raise AfError(status, where)
@@ -368,6 +377,10 @@ class Context:
                                          _ptr(d_W), int(accumulate_dW), _stream(stream)), "af_policy_update")
 
     # -- listed candidates, distillation, preferences ----------------------------------------------
+    def _stream_of(self, stream) -> int:
+        """The given stream, or the context's device's current one."""
+        return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
+
     @staticmethod
     def _dtype(d_W: Optional[torch.Tensor]) -> int:
         if d_W is None or d_W.dtype == torch.float32:
@@ -379,20 +392,22 @@ class Context:
     @staticmethod
     def _list_width(cand: torch.Tensor, T: int, *others: Optional[torch.Tensor]) -> int:
         """K of [T, K] lists of 4-byte ids or values; every other tensor is float32, equally wide, with enough rows."""
-        if cand.dim() != 2 or cand.shape[0] < T or cand.element_size() != 4:
+        shape = cand.shape
+        if len(shape) != 2 or shape[0] < T or cand.element_size() != 4:
             raise ValueError("candidate lists are [T, K] with 4-byte elements")
         for o in others:
-            if o is not None and (o.dim() != 2 or o.shape[0] < T or o.shape[1] != cand.shape[1] or o.dtype != torch.float32):
+            if o is not None and (o.dtype is not torch.float32 or
+                                  (o.shape != shape and (o.dim() != 2 or o.shape[0] < T or o.shape[1] != shape[1]))):
                 raise ValueError("tensors over the candidate lists are float32 [T, K] like the lists")
-        return cand.shape[1]
+        return shape[1]
 
     def candidate_logprob(self, hidden, W, cand, cand_logp, entropy=None, lse=None, T=None, stream=None):
         """``cand``: int32 [T, K] vocabulary ids (below 0: unused slot); ``cand_logp``: float32 [T, K]."""
         T = hidden.shape[0] if T is None else T
         d, V = W.shape[1], W.shape[0]
         K = self._list_width(cand, T, cand_logp)
-        _check(self.lib.af_candidate_logprob(self.handle, _ptr(hidden), _ptr(W), _ptr(cand), T, K, d, V,
-                                             _ptr(cand_logp), _ptr(entropy), _ptr(lse), _stream(stream)),
+        _check(self.lib.af_candidate_logprob(self.handle, _addr(hidden), _addr(W), _addr(cand), T, K, d, V,
+                                             _addr(cand_logp), _addr(entropy), _addr(lse), self._stream_of(stream)),
                "af_candidate_logprob")
 
     def candidate_logprob_backward(self, hidden, W, cand, lse, dcand, d_hidden, d_W=None, accumulate_dW=False, T=None,
@@ -401,9 +416,9 @@ class Context:
         T = hidden.shape[0] if T is None else T
         d, V = W.shape[1], W.shape[0]
         K = self._list_width(cand, T, dcand)
-        _check(self.lib.af_candidate_logprob_backward(self.handle, _ptr(hidden), _ptr(W), _ptr(cand), _ptr(lse),
-                                                      _ptr(dcand), T, K, d, V, _ptr(d_hidden), _ptr(d_W),
-                                                      self._dtype(d_W), int(accumulate_dW), _stream(stream)),
+        _check(self.lib.af_candidate_logprob_backward(self.handle, _addr(hidden), _addr(W), _addr(cand), _addr(lse),
+                                                      _addr(dcand), T, K, d, V, _addr(d_hidden), _addr(d_W),
+                                                      self._dtype(d_W), int(accumulate_dW), self._stream_of(stream)),
                "af_candidate_logprob_backward")
 
     def reserve_candidates(self, max_T: int, K: int, d: int, V: int, with_backward=0, dW_type: int = F32):
@@ -418,8 +433,8 @@ class Context:
         T = cand_logp.shape[0] if T is None else T
         K = self._list_width(cand_logp, T, teacher_logp, dcand)
         prm = DistillParams(divergence, support, agg_mode, temperature, loss_scale)
-        _check(self.lib.af_distill_loss(self.handle, _ptr(cand_logp), _ptr(teacher_logp), _ptr(cu_seqlens), B, T, K,
-                                        C.byref(prm), _ptr(out), _ptr(token_loss), _ptr(dcand), _stream(stream)),
+        _check(self.lib.af_distill_loss(self.handle, _addr(cand_logp), _addr(teacher_logp), _addr(cu_seqlens), B, T, K,
+                                        C.byref(prm), _addr(out), _addr(token_loss), _addr(dcand), self._stream_of(stream)),
                "af_distill_loss")
 
     def distill_update(self, hidden, W, cand, teacher_logp, cu_seqlens, out, cand_logp, lse, d_hidden, d_W=None,
@@ -431,10 +446,10 @@ class Context:
         d, V = W.shape[1], W.shape[0]
         K = self._list_width(cand, T, teacher_logp, cand_logp, dcand)
         prm = DistillParams(divergence, support, agg_mode, temperature, loss_scale)
-        _check(self.lib.af_distill_update(self.handle, _ptr(hidden), _ptr(W), _ptr(cand), _ptr(teacher_logp),
-                                          _ptr(cu_seqlens), B, T, K, d, V, C.byref(prm), _ptr(out), _ptr(cand_logp),
-                                          _ptr(entropy), _ptr(lse), _ptr(token_loss), _ptr(dcand), _ptr(d_hidden),
-                                          _ptr(d_W), self._dtype(d_W), int(accumulate_dW), _stream(stream)),
+        _check(self.lib.af_distill_update(self.handle, _addr(hidden), _addr(W), _addr(cand), _addr(teacher_logp),
+                                          _addr(cu_seqlens), B, T, K, d, V, C.byref(prm), _addr(out), _addr(cand_logp),
+                                          _addr(entropy), _addr(lse), _addr(token_loss), _addr(dcand), _addr(d_hidden),
+                                          _addr(d_W), self._dtype(d_W), int(accumulate_dW), self._stream_of(stream)),
                "af_distill_update")
 
     def preference_loss(self, logp, ref_logp, cu_seqlens, out, pair_loss=None, seq_score=None, dlogp=None, kind=0,
@@ -447,8 +462,8 @@ class Context:
         if logp.dtype != torch.float32 or (ref_logp is not None and ref_logp.dtype != torch.float32):
             raise ValueError("log-probs are float32")
         prm = PreferenceParams(kind, int(length_norm), pair_layout, beta, label_smoothing, margin, nll_coef, loss_scale)
-        _check(self.lib.af_preference_loss(self.handle, _ptr(logp), _ptr(ref_logp), _ptr(cu_seqlens), B, T, C.byref(prm),
-                                           _ptr(out), _ptr(pair_loss), _ptr(seq_score), _ptr(dlogp), _stream(stream)),
+        _check(self.lib.af_preference_loss(self.handle, _addr(logp), _addr(ref_logp), _addr(cu_seqlens), B, T, C.byref(prm),
+                                           _addr(out), _addr(pair_loss), _addr(seq_score), _addr(dlogp), self._stream_of(stream)),
                "af_preference_loss")
 
     def reserve_preference(self, max_T: int, max_B: int):

@@ -36,8 +36,9 @@ struct DeviceGuard {
   int prev = -1;
   bool ok = true;
   explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; prev = -1; return; }
+    if (prev == dev) { prev = -1; return; }        // nothing to put back
+    if (cudaSetDevice(dev) != cudaSuccess) ok = false;
   }
   ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
 };
@@ -630,6 +631,13 @@ af_status af_distill_update(af_ctx* c, const void* hidden, const void* W, const 
                                HeadGradient{d_W, dW_type, accumulate_dW != 0}, static_cast<cudaStream_t>(stream));
 }
 
+// The workspace of the preference loss starts with a header that a call finds zero and leaves zero.
+static af_status grow_preference_ws(af_ctx* c, int32_t B) {
+  const void* before = c->pref_ws.p;
+  const af_status st = ws_grow(c->pref_ws, preference_workspace_bytes(B));
+  if (st != AF_OK || c->pref_ws.p == before) return st;
+  return cudaMemset(c->pref_ws.p, 0, preference_header_bytes()) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+}
 static af_status preference_sizes(int64_t T, int32_t B) {
   if (T < 0 || B < 0 || (T > 0 && B < 1)) return AF_ERR_INVALID_ARG;
   return B % 2 != 0 || T > ((int64_t)1 << 31) - 65536 ? AF_ERR_SHAPE : AF_OK;
@@ -647,9 +655,9 @@ af_status af_preference_loss(af_ctx* c, const float* logp, const float* ref_logp
       !(p.label_smoothing >= 0.f && p.label_smoothing < 1.f))
     return AF_ERR_INVALID_ARG;
   DeviceGuard guard(c->device);
-  if ((st = ws_grow(c->pref_ws, preference_workspace_bytes(B, T))) != AF_OK) return st;
+  if ((st = grow_preference_ws(c, B)) != AF_OK) return st;
   return launch_preference_loss(logp, ref_logp, cu_seqlens, B, T, p, out, pair_loss, seq_score, dlogp, c->pref_ws.p,
-                                c->loss_ws.p, c->d_err, c->sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess
+                                c->d_err, c->sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess
              ? AF_OK : AF_ERR_CUDA;
 }
 
@@ -659,7 +667,7 @@ af_status af_reserve_preference(af_ctx* c, int64_t max_T, int32_t max_B) {
   const af_status st = preference_sizes(max_T, max_B);
   if (st != AF_OK) return st;
   DeviceGuard guard(c->device);
-  return ws_grow(c->pref_ws, preference_workspace_bytes(max_B, max_T));
+  return grow_preference_ws(c, max_B);
 }
 
 af_status af_controller_put(af_ctx* c, const af_controller_view* table, const int32_t* idx, int64_t n,

@@ -16,7 +16,7 @@
 namespace af {
 namespace {
 
-constexpr int kPromoteBlocks = 4;       // K = 256 per part
+constexpr int kPromoteBlocks = 8;       // K = 512 per part
 
 struct CandidateState {
   float m, s, u;
@@ -253,7 +253,8 @@ size_t candidate_partial_bytes(const af_ctx* ctx, int64_t max_T, int32_t d, int3
 static af_status candidate_gemm(af_ctx* ctx, const void* hidden, const void* W, int64_t T, int32_t d, int32_t V,
                                 int32_t K, const uint32_t* keys, float* cand_z, float* z, int* parts,
                                 cudaStream_t s) {
-  const GemmEnv env = gemm_env(ctx);
+  GemmEnv env = gemm_env(ctx);
+  if (T <= umma::kPairBM) env.tile_clock = nullptr;   // one row tile: every pair reads its own part of W, none shares
   const int n_tiles = (V + umma::kBN - 1) / umma::kBN;
   int S = candidate_pick_splits(ctx, T, d, V);
   if (S > n_tiles) S = n_tiles;

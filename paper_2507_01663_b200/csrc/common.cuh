@@ -235,11 +235,12 @@ af_status launch_distill_update(af_ctx* ctx, const void* hidden, const void* W, 
                                 void* d_hidden, const HeadGradient& head, cudaStream_t s);
 af_status reserve_distill_update(af_ctx* ctx, int64_t T, int32_t K, int32_t V);
 
-size_t preference_workspace_bytes(int32_t B, int64_t T);
+size_t preference_workspace_bytes(int32_t B);
+size_t preference_header_bytes();     // the start of it, zero before the first call
 cudaError_t launch_preference_loss(const float* logp, const float* ref_logp, const int32_t* cu, int32_t B, int64_t T,
                                    const af_preference_params& p, af_preference_out* out, float* pair_loss,
-                                   float* seq_score, float* dlogp, void* ws, void* loss_ws, unsigned int* d_err,
-                                   int sm_count, cudaStream_t s);
+                                   float* seq_score, float* dlogp, void* ws, unsigned int* d_err, int sm_count,
+                                   cudaStream_t s);
 
 af_status launch_backward(af_ctx* ctx, const void* hidden, const void* W, const int32_t* target,
                           const float* lse, const float* dlogp, int64_t T, int32_t d, int32_t V,

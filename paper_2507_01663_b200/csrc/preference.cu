@@ -4,57 +4,86 @@
 //   l_p = f(x_p) + nll_coef * mean(-logp over the chosen);    dlogp is constant over a sequence.
 //
 // 8 (or 4, without reference) bytes read and 4 written per token: HBM-bound, in two passes with the pairs in
-// between, since a token's gradient needs its pair's sums.
-//   1. sums    a warp per slice of 256 tokens: eight tokens per lane in registers, one warp reduction per
-//              sequence that meets the slice.  A sequence inside one slice is done; one that crosses slice
-//              borders leaves a piece per slice (16 bytes per 256 tokens), at most one coming in (head) and one
-//              going out (tail), so pieces need no counters and their order is fixed.
+// between, since a token's gradient needs its pair's sums.  One cooperative launch does all three, with a
+// grid barrier after the first and the second phase:
+//   1. sums    a warp walks a range in steps of 512 tokens, eight per lane at a time, each lane adding up its tokens of the
+//              current sequence and the warp joining them when the sequence or the range ends.  The next steps come
+//              by bulk copies into a ring of the warp's own, so nothing waits on another warp, and the border of the
+//              sequence after the next is fetched ahead, so nothing waits on cu_seqlens either.  A sequence inside one
+//              range is done; one that crosses ranges leaves a piece in each, at most one coming in (head) and one
+//              going out (tail), so pieces need no counters and no atomics.
 //   2. pairs   a few lanes per pair add the pieces, evaluate the loss and write the two sequences' coefficients.
-//   3. fill    a warp per slice again: the coefficient of each token's sequence.
+//   3. fill    the same ranges again: the coefficient of each token's sequence.
 // All sums are fp64 (thousands of near-cancelling terms, and the card has the rate: two additions per token)
 // and taken in a fixed order, so results are bit-reproducible.
 #include "common.cuh"
 #include "device_util.cuh"
+#include "umma.cuh"
 
 namespace af {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kSlice = 256;                 // tokens of a warp's slice: two groups of 4 per lane, 128 apart
+constexpr int kBlocksPerSm = 3;
+constexpr int kSlice = 256;                 // tokens a warp works on at a time: two groups of 4 per lane, 128 apart
+constexpr int kStep = 2 * kSlice;           // tokens of a stage of its ring
+constexpr int kStages = 2;
+constexpr int kStageBytes = 2 * kStep * 4;  // logp | ref
+constexpr int kSmemBytes = kWarps * kStages * kStageBytes + 128 /*alignment*/ + kWarps * kStages * 8 /*barriers*/;
 constexpr int kNumSums = 6;                 // loss, pair loss, nll, accuracy, chosen score, rejected score
+constexpr int kMaxBlocks = 1024;
 
+struct PrefHeader {                         // zero between calls
+  unsigned int arrived;                     // blocks at the grid barriers (counts up through both)
+  unsigned int left;                        // blocks that are done
+  unsigned int failed;                      // a barrier's wait ran out
+  unsigned int pad[13];
+};
 struct PrefWs {                             // device views into the workspace
-  double2* seq;                             // [B] sums of the sequences that lie inside one slice: S, sum of logp
-  double2* head;                            // [slices] piece of the sequence that comes into the slice
-  double2* tail;                            // [slices] piece of the sequence that starts in it and goes on
+  PrefHeader* header;
+  double2* seq;                             // [B] sums of the sequences that lie inside one range: S, sum of logp
+  double2* head;                            // [workers] piece of the sequence that comes into the range
+  double2* tail;                            // [workers] piece of the sequence that starts in it and goes on
+  double* partial;                          // [blocks][kNumSums]
   float* coef;                              // [B] dloss/dlogp of a sequence's tokens
-  double* partial;                          // [pair blocks][kNumSums]
 };
 
-int64_t slices_of(int64_t T) { return (T + kSlice - 1) / kSlice; }
-constexpr int kMaxPairBlocks = 1024;
+int64_t steps_of(int64_t T) { return (T + kStep - 1) / kStep; }
 
-PrefWs carve(void* ws, int32_t B, int64_t T) {
+PrefWs carve(void* ws, int32_t B) {
   PrefWs w;
-  w.seq = static_cast<double2*>(ws);
-  w.head = w.seq + B;
-  w.tail = w.head + slices_of(T);
-  w.partial = reinterpret_cast<double*>(w.tail + slices_of(T));
-  w.coef = reinterpret_cast<float*>(w.partial + (size_t)kMaxPairBlocks * kNumSums);
+  w.header = static_cast<PrefHeader*>(ws);
+  w.partial = reinterpret_cast<double*>(w.header + 1);
+  w.head = reinterpret_cast<double2*>(w.partial + (size_t)kMaxBlocks * kNumSums);
+  w.tail = w.head + kMaxBlocks * kWarps;
+  w.seq = w.tail + kMaxBlocks * kWarps;
+  w.coef = reinterpret_cast<float*>(w.seq + B);
   return w;
 }
 
 // Token of slot i (0..7) of a lane: group i / 4 starts 128 tokens after the first.
 __device__ __forceinline__ int slot_token(int base, int lane, int i) { return base + (i >> 2) * 128 + lane * 4 + (i & 3); }
 
-// The lane's eight values of a column; zeros past the end.
-__device__ __forceinline__ void load_slice(const float* __restrict__ p, int base, int lane, int T, bool vec, float (&v)[8]) {
+__device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               :: "r"(dst_smem), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ float4 lds128(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+
+// The lane's eight values of a column of a slice staged at `stage`; zeros past the end.  A group of four that no bulk
+// copy brought (the last, not full one, or any of a column that does not start on 16 bytes) is read directly.
+__device__ __forceinline__ void load_slice(const float* __restrict__ p, uint32_t stage, int base, int lane, int T,
+                                           bool staged, float (&v)[8]) {
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const int t = slot_token(base, lane, 4 * q);
-    if (vec && t + 4 <= T) {
-      const float4 x = __ldcs(reinterpret_cast<const float4*>(p + t));
+    if (staged && t + 4 <= T) {
+      const float4 x = lds128(stage + (uint32_t)(q * 128 + lane * 4) * 4u);
       v[4 * q] = x.x; v[4 * q + 1] = x.y; v[4 * q + 2] = x.z; v[4 * q + 3] = x.w;
     } else {
 #pragma unroll
@@ -63,69 +92,200 @@ __device__ __forceinline__ void load_slice(const float* __restrict__ p, int base
   }
 }
 
-// Calls f(j, beg, end) for every non-empty sequence that meets tokens [base, last), in order.  Uniform over the
-// warp; ends whatever cu holds.
-template <class F>
-__device__ __forceinline__ void for_sequences(const int32_t* __restrict__ cu, int B, int base, int last, int lane, F f) {
-  int t = base;
-  int j = find_seq_warp(cu, B, t, lane);
-  for (;;) {
-    const int beg = __ldg(cu + j), end = __ldg(cu + j + 1);
-    f(j, beg, end);
-    if (end >= last || end <= t || j + 1 >= B) return;
-    t = end;
+// A warp's place in the list of sequences, with the next border (and coefficient) already on its way.  Uniform over
+// the warp; every loop over it ends whatever cu holds.
+struct Place {
+  const int32_t* __restrict__ cu;
+  const float* coef;                // null in the first phase
+  int B, lane;
+  int j, beg, end, next_end;
+  float c, next_c;
+  __device__ __forceinline__ void ahead() {
+    next_end = j + 2 <= B ? __ldg(cu + j + 2) : end;
+    if (coef) next_c = j + 1 < B ? __ldcg(coef + j + 1) : 0.f;
+  }
+  __device__ __forceinline__ void find(int t) {
+    j = find_seq_warp(cu, B, t, lane);
+    beg = __ldg(cu + j);
+    end = __ldg(cu + j + 1);
+    if (coef) c = __ldcg(coef + j);
+    ahead();
+  }
+  __device__ __forceinline__ void advance(int t) {                   // to the next non-empty sequence, which holds t
+    if (j + 1 >= B) return;
     ++j;
-    if (__ldg(cu + j + 1) <= t) j = find_seq_warp(cu, B, t, lane);      // a pile of empty sequences
+    beg = end;
+    end = next_end;
+    if (coef) c = next_c;
+    if (end <= t) find(t);                                           // a pile of empty sequences
+    else ahead();
+  }
+};
+
+// Calls f(place) for every non-empty sequence that meets tokens [base, last), `at` holding token base; leaves `at`
+// at the sequence of token `last` if there is one.
+template <class F>
+__device__ __forceinline__ void over_sequences(Place& at, int T, int base, int last, F f) {
+  int t = base;
+  for (;;) {
+    f(at);
+    if (at.end >= last || at.end <= t || at.j + 1 >= at.B) break;
+    t = at.end;
+    at.advance(t);
+  }
+  if (at.end <= last && last < T) at.advance(last);
+}
+
+__device__ __forceinline__ void warp_sums(double& s, double& l, bool both) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (both) s += __shfl_xor_sync(0xffffffffu, s, o);
   }
 }
 
-__global__ void __launch_bounds__(kThreads) pref_sums_kernel(
-    const float* __restrict__ logp, const float* __restrict__ ref, const int32_t* __restrict__ cu, int B, int T,
-    PrefWs ws, int vec) {
-  const int lane = threadIdx.x & 31;
-  const int slice = blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int base = slice * kSlice;
-  if (base >= T) return;
-  const int last = T - base < kSlice ? T : base + kSlice;
-  float lp[8], rf[8];
-  load_slice(logp, base, lane, T, vec != 0, lp);
-  if (ref) load_slice(ref, base, lane, T, vec != 0, rf);
-  for_sequences(cu, B, base, last, lane, [&](int j, int beg, int end) {
-    double s = 0.0, l = 0.0;
+// Phase 1 over the steps [s0, s1) of worker `me`.  ring: the warp's stages, bars: their barriers.
+__device__ __forceinline__ void sum_steps(const float* __restrict__ logp, const float* __restrict__ ref,
+                                          const int32_t* __restrict__ cu, int B, int T, const PrefWs& ws, bool bulk,
+                                          int me, int s0, int s1, uint32_t ring, uint32_t bars, int lane,
+                                          volatile int* abort_flag) {
+  if (s0 >= s1) return;
+  const bool both = ref != nullptr;
+  auto issue = [&](int it) {                       // lane 0; a step is copied up to its last whole group of 4 tokens
+    const int base = (s0 + it) * kStep, left = T - base < kStep ? T - base : kStep;
+    const uint32_t bytes = bulk ? (uint32_t)(left & ~3) * 4u : 0u;
+    const uint32_t bar = bars + 8u * (it % kStages), dst = ring + (uint32_t)(it % kStages) * kStageBytes;
+    umma::mbar_arrive_expect_tx(bar, both ? 2 * bytes : bytes);
+    if (bytes > 0) {
+      bulk_load(dst, logp + base, bytes, bar);
+      if (both) bulk_load(dst + kStep * 4, ref + base, bytes, bar);
+    }
+  };
+  if (lane == 0)
+    for (int it = 0; it < kStages && s0 + it < s1; ++it) issue(it);
+  const int range_beg = s0 * kStep;
+  Place at{cu, nullptr, B, lane};
+  at.find(range_beg);
+  double s = 0.0, l = 0.0;                         // the lane's share of the current sequence
+  auto leave = [&](double2* where) {
+    warp_sums(s, l, both);
+    if (lane == 0) *where = make_double2(both ? s : l, l);
+    s = 0.0;
+    l = 0.0;
+  };
+  int last = range_beg;
+  for (int step = s0; step < s1; ++step) {
+    const int it = step - s0;
+    const uint32_t stage = ring + (uint32_t)(it % kStages) * kStageBytes;
+    if (!__all_sync(0xffffffffu, umma::mbar_wait(bars + 8u * (it % kStages), (uint32_t)(it / kStages) & 1u, abort_flag)))
+      return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int t = slot_token(base, lane, i);
-      if (t >= beg && t < end) {
-        l += (double)lp[i];
-        if (ref) s += (double)lp[i] - (double)rf[i];
+    for (int half = 0; half < 2; ++half) {
+      const int base = step * kStep + half * kSlice;
+      if (half > 0 && base >= T) break;
+      float lp[8], rf[8];
+      if (bulk && base + kSlice <= T) {            // as the others, without a question per lane
+        const uint32_t from = stage + (uint32_t)(half * kSlice + lane * 4) * 4u;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const float4 x = lds128(from + q * 512);
+          lp[4 * q] = x.x; lp[4 * q + 1] = x.y; lp[4 * q + 2] = x.z; lp[4 * q + 3] = x.w;
+          if (both) {
+            const float4 y = lds128(from + kStep * 4 + q * 512);
+            rf[4 * q] = y.x; rf[4 * q + 1] = y.y; rf[4 * q + 2] = y.z; rf[4 * q + 3] = y.w;
+          }
+        }
+        last = base + kSlice;
+      } else {
+        const uint32_t from = stage + (uint32_t)(half * kSlice) * 4u;
+        load_slice(logp, from, base, lane, T, bulk, lp);
+        if (both) load_slice(ref, from + kStep * 4, base, lane, T, bulk, rf);
+        last = T - base < kSlice ? T : base + kSlice;
+      }
+      if (half == 1 || last == T) {
+        __syncwarp();                              // every lane has its values: the stage may be filled again
+        if (lane == 0 && step + kStages < s1) issue(it + kStages);
+      }
+      auto add_all = [&]() {                       // the whole slice (past the end the values are zero)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          l += (double)lp[i];
+          if (both) s += (double)lp[i] - (double)rf[i];
+        }
+      };
+      if (at.beg <= base && at.end > last) {       // most often: one sequence from before this slice to behind it
+        add_all();
+        continue;
+      }
+      over_sequences(at, T, base, last, [&](const Place& q) {
+        if (q.beg <= base && q.end >= last) {
+          add_all();
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int t = slot_token(base, lane, i);
+            if (t >= q.beg && t < q.end) {
+              l += (double)lp[i];
+              if (both) s += (double)lp[i] - (double)rf[i];
+            }
+          }
+        }
+        if (q.end <= last) leave(q.beg >= range_beg ? ws.seq + q.j : ws.head + me);
+      });
+    }
+  }
+  if (at.beg < last && at.end > last) leave(at.beg >= range_beg ? ws.tail + me : ws.head + me);
+}
+
+// Phase 3 over the steps [s0, s1).
+__device__ __forceinline__ void fill_steps(const int32_t* __restrict__ cu, int B, int T, const PrefWs& ws, float* dlogp,
+                                           bool vec, int s0, int s1, int lane) {
+  if (s0 >= s1) return;
+  Place at{cu, ws.coef, B, lane};
+  at.find(s0 * kStep);
+  const int end = s1 * (int64_t)kStep < T ? s1 * kStep : T;
+  for (int base = s0 * kStep; base < end; base += kSlice) {
+    const int last = T - base < kSlice ? T : base + kSlice;
+    float* const out = dlogp + slot_token(base, lane, 0);
+    if (vec && at.beg <= base && at.end > last && base + kSlice <= T) {
+      const float4 v = make_float4(at.c, at.c, at.c, at.c);
+      __stcs(reinterpret_cast<float4*>(out), v);
+      __stcs(reinterpret_cast<float4*>(out + 128), v);
+      continue;
+    }
+    float g[8] = {};
+    over_sequences(at, T, base, last, [&](const Place& q) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int t = slot_token(base, lane, i);
+        if (t >= q.beg && t < q.end) g[i] = q.c;
+      }
+    });
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int t = slot_token(base, lane, 4 * q);
+      if (vec && t + 4 <= T) {
+        __stcs(reinterpret_cast<float4*>(out + q * 128), make_float4(g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (t + i < T) dlogp[t + i] = g[4 * q + i];
       }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      l += __shfl_xor_sync(0xffffffffu, l, o);
-      if (ref) s += __shfl_xor_sync(0xffffffffu, s, o);
-    }
-    if (lane == 0) {
-      const double2 v = make_double2(ref ? s : l, l);
-      if (beg < base) ws.head[slice] = v;
-      else if (end > last) ws.tail[slice] = v;
-      else ws.seq[j] = v;
-    }
-  });
+  }
 }
 
 // Sums of one sequence, by kLanes lanes together (all get the result; every lane of the warp takes part).
-// beg and end lie in [0, T].
+// beg and end lie in [0, T]; a range is `per` steps.
 template <int kLanes>
-__device__ __forceinline__ double2 sequence_sum(const PrefWs& ws, int j, int beg, int end, int lane) {
+__device__ __forceinline__ double2 sequence_sum(const PrefWs& ws, int j, int beg, int end, int per, int lane) {
   double s = 0.0, l = 0.0;
   if (end > beg) {
-    const int first = beg / kSlice, final = (end - 1) / kSlice;
+    const int first = beg / kStep / per, final = (end - 1) / kStep / per;
     if (first == final) {
-      if (lane == 0) { const double2 v = ws.seq[j]; s = v.x; l = v.y; }
+      if (lane == 0) { const double2 v = __ldcg(ws.seq + j); s = v.x; l = v.y; }
     } else {
       for (int i = first + lane; i <= final; i += kLanes) {
-        const double2 v = i == first ? ws.tail[i] : ws.head[i];
+        const double2 v = __ldcg((i == first ? ws.tail : ws.head) + i);
         s += v.x; l += v.y;
       }
     }
@@ -138,18 +298,15 @@ __device__ __forceinline__ double2 sequence_sum(const PrefWs& ws, int j, int beg
   return make_double2(s, l);
 }
 
+// Phase 2: pairs p0, p0 + step, ... of this block; `sum` gains the block's share of the record.
 template <int kLanes>
-__global__ void __launch_bounds__(kThreads) pref_pairs_kernel(
-    const int32_t* __restrict__ cu, int B, int T, af_preference_params prm, PrefWs ws,
-    af_preference_out* __restrict__ out, float* __restrict__ pair_loss, float* __restrict__ seq_score,
-    unsigned int* ticket, unsigned int* d_err) {
+__device__ __forceinline__ void pair_terms(const int32_t* __restrict__ cu, int B, int T, const af_preference_params& prm,
+                                           const PrefWs& ws, int per, float* __restrict__ pair_loss,
+                                           float* __restrict__ seq_score, double (&sum)[kNumSums]) {
   constexpr int kPairs = kThreads / kLanes;
   const int P = B / 2;
   const int lane = threadIdx.x % kLanes;
-  for (int q = blockIdx.x * kThreads + threadIdx.x; q < B; q += gridDim.x * kThreads)
-    if (__ldg(cu + q) > __ldg(cu + q + 1)) atomicOr(d_err, AF_DEVERR_CU_SEQLENS);
   const double beta = (double)prm.beta, w = P > 0 ? (double)prm.loss_scale / (double)P : 0.0;
-  double sum[kNumSums] = {};
   for (int p0 = blockIdx.x * kPairs; p0 < P; p0 += gridDim.x * kPairs) {
     const int p = p0 + threadIdx.x / kLanes;
     const bool live = p < P;
@@ -157,8 +314,8 @@ __global__ void __launch_bounds__(kThreads) pref_pairs_kernel(
     // clamped: a cu_seqlens out of order is flagged, but must not index anything
     const int cb = min(max(__ldg(cu + c), 0), T), ce = min(max(__ldg(cu + c + 1), 0), T);
     const int rb = min(max(__ldg(cu + r), 0), T), re = min(max(__ldg(cu + r + 1), 0), T);
-    const double2 sc = sequence_sum<kLanes>(ws, c, cb, live ? ce : cb, lane);
-    const double2 sr = sequence_sum<kLanes>(ws, r, rb, live ? re : rb, lane);
+    const double2 sc = sequence_sum<kLanes>(ws, c, cb, live ? ce : cb, per, lane);
+    const double2 sr = sequence_sum<kLanes>(ws, r, rb, live ? re : rb, per, lane);
     if (!live || lane != 0) continue;
     const double per_c = 1.0 / (double)(ce > cb ? ce - cb : 1), per_r = 1.0 / (double)(re > rb ? re - rb : 1);
     const double n_c = prm.length_norm ? per_c : 1.0, n_r = prm.length_norm ? per_r : 1.0;
@@ -187,116 +344,138 @@ __global__ void __launch_bounds__(kThreads) pref_pairs_kernel(
     sum[3] += score_c > score_r ? 1.0 : 0.0;
     sum[4] += score_c; sum[5] += score_r;
   }
+}
 
+// All blocks of the launch meet (a cooperative launch: they are all resident).  `target`: blocks times barriers so
+// far.  False if the wait ran out of time here or elsewhere: the caller goes on to its end, touching nothing more.
+__device__ __forceinline__ bool grid_barrier(PrefHeader* h, unsigned int target) {
+  __shared__ int s_ok;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    atomicAdd(&h->arrived, 1u);
+    const unsigned long long t0 = umma::globaltimer_ns();
+    int ok = 1;
+    for (unsigned int spins = 0;; ++spins) {
+      unsigned int seen;
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(&h->arrived) : "memory");
+      if (seen >= target) break;
+      if ((spins & 63u) == 63u) {
+        unsigned int failed;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(failed) : "l"(&h->failed) : "memory");
+        if (failed || umma::globaltimer_ns() - t0 > umma::kWaitLimitNs) { atomicExch(&h->failed, 1u); ok = 0; break; }
+      }
+    }
+    __threadfence();
+    s_ok = ok;
+  }
+  __syncthreads();
+  return s_ok != 0;
+}
+
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) preference_kernel(
+    const float* __restrict__ logp, const float* __restrict__ ref, const int32_t* __restrict__ cu, int B, int T,
+    const af_preference_params prm, const PrefWs ws, af_preference_out* __restrict__ out, float* __restrict__ pair_loss,
+    float* __restrict__ seq_score, float* __restrict__ dlogp, int vec, int wide_pairs, unsigned int* d_err) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ int abort_flag;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int P = B / 2;
+  const uint32_t smem = (umma::smem_u32(smem_raw) + 127u) & ~127u;
+  const uint32_t ring = smem + (uint32_t)(warp * kStages) * kStageBytes;
+  const uint32_t bars = smem + kWarps * kStages * kStageBytes + (uint32_t)(warp * kStages) * 8u;
+  if (threadIdx.x == 0) abort_flag = 0;
+  if (lane == 0) {
+    for (int q = 0; q < kStages; ++q) umma::mbar_init(bars + 8u * q, 1);
+    umma::fence_mbar_init();
+  }
+  __syncthreads();
+  const int steps = (int)(((int64_t)T + kStep - 1) / kStep);
+  const int workers = gridDim.x * kWarps, me = blockIdx.x * kWarps + warp;
+  const int per = steps > workers ? (steps + workers - 1) / workers : 1;       // steps of a range
+  const int s0 = (int64_t)me * per < steps ? me * per : steps, s1 = steps - s0 < per ? steps : s0 + per;
+
+  sum_steps(logp, ref, cu, B, T, ws, vec & 1, me, s0, s1, ring, bars, lane, &abort_flag);
+  for (int q = blockIdx.x * kThreads + threadIdx.x; q < B; q += gridDim.x * kThreads)
+    if (__ldg(cu + q) > __ldg(cu + q + 1)) atomicOr(d_err, AF_DEVERR_CU_SEQLENS);
+  bool ok = grid_barrier(ws.header, gridDim.x);
+  double sum[kNumSums] = {};
+  if (ok) {
+    if (wide_pairs) pair_terms<32>(cu, B, T, prm, ws, per, pair_loss, seq_score, sum);
+    else pair_terms<4>(cu, B, T, prm, ws, per, pair_loss, seq_score, sum);
+  }
   __shared__ double s_part[kWarps][kNumSums];
-  __shared__ int s_last;
-  const int wlane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __syncwarp();
 #pragma unroll
   for (int q = 0; q < kNumSums; ++q)
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], o);
-  if (wlane == 0)
+  if (lane == 0)
     for (int q = 0; q < kNumSums; ++q) s_part[warp][q] = sum[q];
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int q = 0; q < kNumSums; ++q) {
-      double t = 0.0;
-      for (int i = 0; i < kWarps; ++i) t += s_part[i][q];
-      ws.partial[(size_t)blockIdx.x * kNumSums + q] = t;
+  if (threadIdx.x < kNumSums) {
+    double t = 0.0;
+    for (int i = 0; i < kWarps; ++i) t += s_part[i][threadIdx.x];
+    ws.partial[(size_t)blockIdx.x * kNumSums + threadIdx.x] = t;
+  }
+  ok = grid_barrier(ws.header, 2 * gridDim.x) && ok;
+  if (ok && dlogp) fill_steps(cu, B, T, ws, dlogp, (vec & 2) != 0, s0, s1, lane);
+  if (ok && blockIdx.x == 0 && warp < kNumSums) {      // the record: a warp per sum, the blocks in a fixed order
+    double t = 0.0;
+    for (int b = lane; b < (int)gridDim.x; b += 32) t += __ldcg(ws.partial + (size_t)b * kNumSums + warp);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    if (lane == 0) {
+      const double inv = P > 0 ? 1.0 / (double)P : 0.0;
+      reinterpret_cast<float*>(out)[warp] = (float)(warp == 0 ? inv * (double)prm.loss_scale * t : inv * t);
+      if (warp == 0) {
+        out->n_pairs = P;
+        if (__ldg(cu) != 0 || __ldg(cu + B) != T) atomicOr(d_err, AF_DEVERR_CU_SEQLENS);
+      }
     }
-    __threadfence();
-    s_last = atomicAdd(ticket, 1u) == gridDim.x - 1;
   }
   __syncthreads();
-  if (!s_last) return;
-  __threadfence();
-  if (warp == 0) {
-    double tot[kNumSums] = {};
-    for (int b = wlane; b < (int)gridDim.x; b += 32)
-      for (int q = 0; q < kNumSums; ++q) tot[q] += __ldcg(ws.partial + (size_t)b * kNumSums + q);
-#pragma unroll
-    for (int q = 0; q < kNumSums; ++q)
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) tot[q] += __shfl_xor_sync(0xffffffffu, tot[q], o);
-    if (wlane == 0) {
-      const double inv = P > 0 ? 1.0 / (double)P : 0.0;
-      af_preference_out r;
-      r.loss = (float)(w * tot[0]);
-      r.pair_loss = (float)(inv * tot[1]);
-      r.nll = (float)(inv * tot[2]);
-      r.accuracy = (float)(inv * tot[3]);
-      r.chosen_score = (float)(inv * tot[4]);
-      r.rejected_score = (float)(inv * tot[5]);
-      r.n_pairs = P;
-      *out = r;
-      if (__ldg(cu) != 0 || __ldg(cu + B) != T) atomicOr(d_err, AF_DEVERR_CU_SEQLENS);
-      *ticket = 0;           // ready for the next call on this stream
-    }
+  if (abort_flag) {          // a bulk copy did not arrive in time: let copies in flight land
+    if (threadIdx.x == 0) atomicExch(&ws.header->failed, 1u);
+    __nanosleep(1000000);
   }
-}
-
-__global__ void __launch_bounds__(kThreads) pref_fill_kernel(const int32_t* __restrict__ cu, int B, int T, PrefWs ws,
-                                                             float* __restrict__ dlogp, int vec) {
-  const int lane = threadIdx.x & 31;
-  const int base = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * kSlice;
-  if (base >= T) return;
-  const int last = T - base < kSlice ? T : base + kSlice;
-  float g[8] = {};
-  for_sequences(cu, B, base, last, lane, [&](int j, int beg, int end) {
-    const float c = __ldg(ws.coef + j);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int t = slot_token(base, lane, i);
-      if (t >= beg && t < end) g[i] = c;
-    }
-  });
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int t = slot_token(base, lane, 4 * q);
-    if (vec && t + 4 <= T) {
-      __stcs(reinterpret_cast<float4*>(dlogp + t), make_float4(g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) if (t + i < T) dlogp[t + i] = g[4 * q + i];
-    }
+  if (threadIdx.x == 0 && atomicAdd(&ws.header->left, 1u) == gridDim.x - 1) {   // every block is past both barriers
+    if (ws.header->failed) atomicOr(d_err, umma::kWatchdogBit);
+    ws.header->arrived = 0; ws.header->failed = 0; ws.header->left = 0;
+    __threadfence();
   }
 }
 
 }  // namespace
 
-size_t preference_workspace_bytes(int32_t B, int64_t T) {
-  return (size_t)B * (sizeof(double2) + sizeof(float)) + (size_t)slices_of(T) * 2 * sizeof(double2) +
-         (size_t)kMaxPairBlocks * kNumSums * sizeof(double);
+size_t preference_workspace_bytes(int32_t B) {
+  return sizeof(PrefHeader) + (size_t)kMaxBlocks * (kNumSums * sizeof(double) + 2 * kWarps * sizeof(double2)) +
+         (size_t)B * (sizeof(double2) + sizeof(float));
 }
+size_t preference_header_bytes() { return sizeof(PrefHeader); }
 
 cudaError_t launch_preference_loss(const float* logp, const float* ref_logp, const int32_t* cu, int32_t B, int64_t T,
                                    const af_preference_params& p, af_preference_out* out, float* pair_loss,
-                                   float* seq_score, float* dlogp, void* ws_mem, void* loss_ws, unsigned int* d_err,
-                                   int sm_count, cudaStream_t s) {
+                                   float* seq_score, float* dlogp, void* ws_mem, unsigned int* d_err, int sm_count,
+                                   cudaStream_t s) {
   auto al = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
-  const PrefWs ws = carve(ws_mem, B, T);
-  const unsigned slice_blocks = (unsigned)((slices_of(T) + kWarps - 1) / kWarps);
-  if (T > 0) {
-    pref_sums_kernel<<<slice_blocks, kThreads, 0, s>>>(logp, ref_logp, cu, B, (int)T, ws, al(logp) && al(ref_logp));
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-  }
-  // eight lanes per pair while sequences have few pieces, a warp beyond 4096 tokens on average
-  const int P = B / 2;
-  const int lanes = B > 0 && T / B > 4096 ? 32 : 8;
-  const int wanted = (P + kThreads / lanes - 1) / (kThreads / lanes);
-  int most = sm_count * 4 < kMaxPairBlocks ? sm_count * 4 : kMaxPairBlocks;
-  const int blocks = wanted < 1 ? 1 : wanted < most ? wanted : most;
-  unsigned int* ticket = static_cast<unsigned int*>(loss_ws);      // the reductions' ticket of this context
-  if (lanes == 8)
-    pref_pairs_kernel<8><<<blocks, kThreads, 0, s>>>(cu, B, (int)T, p, ws, out, pair_loss, seq_score, ticket, d_err);
-  else
-    pref_pairs_kernel<32><<<blocks, kThreads, 0, s>>>(cu, B, (int)T, p, ws, out, pair_loss, seq_score, ticket, d_err);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || T == 0 || !dlogp) return e;
-  pref_fill_kernel<<<slice_blocks, kThreads, 0, s>>>(cu, B, (int)T, ws, dlogp, al(dlogp));
-  return cudaGetLastError();
+  PrefWs ws = carve(ws_mem, B);
+  static SmemAttrOnce once;
+  const cudaError_t e = set_smem_once(once, preference_kernel, kSmemBytes);
+  if (e != cudaSuccess) return e;
+  // four lanes per pair while sequences have few pieces, a warp for long ones (a range is 512 tokens at least)
+  int wide = B > 0 && T / B > 2048 ? 1 : 0;
+  const int64_t by_steps = (steps_of(T) + kWarps - 1) / kWarps;
+  const int64_t by_pairs = ((int64_t)B / 2 * (wide ? 32 : 4) + kThreads - 1) / kThreads;
+  const int64_t want = by_steps > by_pairs ? by_steps : by_pairs;
+  const int64_t most = (int64_t)sm_count * kBlocksPerSm < kMaxBlocks ? (int64_t)sm_count * kBlocksPerSm : kMaxBlocks;
+  const int blocks = (int)(want < 1 ? 1 : want < most ? want : most);
+  int vec = (al(logp) && al(ref_logp) ? 1 : 0) | (al(dlogp) ? 2 : 0);
+  int Bi = B, Ti = (int)T;
+  af_preference_params prm = p;
+  void* args[] = {&logp, &ref_logp, &cu, &Bi, &Ti, &prm, &ws, &out, &pair_loss, &seq_score, &dlogp, &vec, &wide, &d_err};
+  return cudaLaunchCooperativeKernel(reinterpret_cast<const void*>(preference_kernel), dim3(blocks), dim3(kThreads), args,
+                                     kSmemBytes, s);
 }
 
 }  // namespace af

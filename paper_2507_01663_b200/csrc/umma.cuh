@@ -140,6 +140,15 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
         "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr) : "memory");
 }
+// 16 of them.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void tmem_ld_wait() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
@@ -716,13 +725,15 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
           if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, &abort_flag))) { ok = false; break; }
           tc_fence_after();
           const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * kBN + half * kPromoteCols;
+          // 16 columns at a time, the next 16 on their way while these are added
+          uint32_t v[2][16];
+          tmem_ld16(t_row, v[0]);
 #pragma unroll
-          for (int c = 0; c < kPromoteCols / 32; ++c) {
-            uint32_t v[32];
-            tmem_ld32(t_row + c * 32, v);
+          for (int c = 0; c < kPromoteCols / 16; ++c) {
             tmem_ld_wait();
+            if (c + 1 < kPromoteCols / 16) tmem_ld16(t_row + (c + 1) * 16, v[(c + 1) & 1]);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) a[c * 32 + j] += __uint_as_float(v[j]);
+            for (int j = 0; j < 16; ++j) a[c * 16 + j] += __uint_as_float(v[c & 1][j]);
           }
           tc_fence_before();
           __syncwarp();

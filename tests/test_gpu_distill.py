@@ -74,8 +74,9 @@ def row_scales(lq, lt, how):
             if how[1] == 2:
                 pr, qr = max(1 - a.sum(), D.TAIL_FLOOR), max(1 - b.sum(), D.TAIL_FLOOR)
                 ratio = abs(math.log(pr / qr)) + 1
-                # the masses are off by c, what they leave by c / pr and c / qr relative
-                sl[t] += 8 * c * (ratio + pr / qr + 1)
+                # the masses are off by c absolutely.  d(pr log(pr / qr)) = (log(pr / qr) + 1) dpr - (pr / qr) dqr, and
+                # for the other direction the same with pr and qr exchanged: either ratio can be the large one
+                sl[t] += 8 * c * (ratio + pr / qr + qr / pr + 1)
                 sg[t, on] += 8 * c * b * (ratio + 1 / qr + 1 / pr + pr / qr * (1 + 1 / qr))
     return sl, sg
 
