@@ -585,8 +585,7 @@ af_status af_reserve_candidates(af_ctx* c, int64_t max_T, int32_t K, int32_t d, 
   af_status st = candidate_sizes(max_T, K, d, V);
   if (st != AF_OK || max_T == 0) return st;
   DeviceGuard guard(c->device);
-  st = ws_grow(c->partial, candidate_partial_bytes(c, max_T, d, V));
-  if (st == AF_OK) st = ws_grow(c->cand_keys, (size_t)max_T * K * sizeof(uint32_t));
+  st = reserve_candidate_logprob(c, max_T, K, d, V);
   if (st == AF_OK && with_backward >= 1) {
     const int64_t Tc = backward_token_block(c, max_T);
     st = ws_grow(c->cand_keys, (size_t)Tc * K * sizeof(uint32_t) + (size_t)Tc * sizeof(float));

@@ -240,7 +240,7 @@ int candidate_pick_splits(const af_ctx* ctx, int64_t T, int32_t d, int32_t V) {
   return logprob_pick_splits(T, d, V, ctx->sm_count, true, ctx->v_splits, die0_pairs);
 }
 
-size_t candidate_partial_bytes(const af_ctx* ctx, int64_t max_T, int32_t d, int32_t V) {
+static size_t candidate_partial_bytes(const af_ctx* ctx, int64_t max_T, int32_t d, int32_t V) {
   const int64_t S = candidate_pick_splits(ctx, max_T, d, V);
   // smaller batches may pick up to 8 ranges whatever their size, and more only while there are at most 8
   // units per pair (one unit = 256 rows of two parts)
@@ -272,9 +272,29 @@ static af_status candidate_gemm(af_ctx* ctx, const void* hidden, const void* W, 
   return run_gemm_promoted<CandidateEpi<false>, kPromoteBlocks>(env, Hop, Wop, S, ep, s);
 }
 
+// Workspace of the one-pass kernel: softmax states in `partial`, logits in `cand_keys`.
+static af_status reserve_stream(af_ctx* ctx, int64_t T, int32_t V) {
+  const af_status st = ws_grow(ctx->partial, (size_t)T * ctx->sm_count * sizeof(float4));
+  return st != AF_OK ? st : ws_grow(ctx->cand_keys, (size_t)T * V * sizeof(float));
+}
+af_status reserve_candidate_logprob(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d, int32_t V) {
+  af_status st = ws_grow(ctx->partial, candidate_partial_bytes(ctx, max_T, d, V));
+  if (st == AF_OK) st = ws_grow(ctx->cand_keys, (size_t)max_T * K * sizeof(uint32_t));
+  if (st == AF_OK) st = reserve_stream(ctx, max_T < kStreamTokens ? max_T : kStreamTokens, V);
+  return st;
+}
+
 af_status launch_candidate_logprob(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand, int64_t T,
                                    int32_t K, int32_t d, int32_t V, float* cand_logp, float* entropy, float* lse,
                                    cudaStream_t s) {
+  if (ctx->v_splits == 0 && stream_fits(T, d)) {
+    const af_status fits = reserve_stream(ctx, T, V);
+    if (fits != AF_OK) return fits;
+    const StreamCall c{hidden, W, cand, (int)T, K, d, V, static_cast<float*>(ctx->cand_keys.p),
+                       static_cast<float4*>(ctx->partial.p), cand_logp, entropy, lse,
+                       static_cast<unsigned int*>(ctx->loss_ws.p), ctx->d_err};      // the reductions' ticket of this context
+    return launch_candidate_stream(c, ctx->sm_count, s);
+  }
   af_status st = ws_grow(ctx->cand_keys, (size_t)T * K * sizeof(uint32_t));
   if (st != AF_OK) return st;
   uint32_t* keys = static_cast<uint32_t*>(ctx->cand_keys.p);

@@ -32,4 +32,22 @@ __device__ __forceinline__ uint32_t candidate_at(const uint32_t* __restrict__ ke
 cudaError_t launch_sort_candidates(const int32_t* cand, const float* g, int64_t rows, int32_t K, int32_t V,
                                    uint32_t* keys, float* gsum, cudaStream_t s);
 
+// The one-pass kernel for a few tokens (candidate_stream.cu).
+constexpr int kStreamTokens = 16;
+struct StreamCall {
+  const void* hidden;
+  const void* W;
+  const int32_t* cand;
+  int T, K, d, V;
+  float* z;               // [T, V] workspace
+  float4* partial;        // [T, CTAs] workspace
+  float* cand_logp;
+  float* entropy;
+  float* lse;
+  unsigned int* ticket;   // zero between calls
+  unsigned int* d_err;
+};
+bool stream_fits(int64_t T, int32_t d);
+af_status launch_candidate_stream(const StreamCall& c, int sm_count, cudaStream_t s);
+
 }  // namespace af
