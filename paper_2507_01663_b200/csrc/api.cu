@@ -110,7 +110,7 @@ af_status af_destroy(af_ctx* c) {
   DeviceGuard guard(c->device);
   cudaDeviceSynchronize();
   Buf* bufs[] = {&c->partial, &c->loss_ws, &c->pack_meta, &c->dz, &c->ctrl_ws, &c->zlog, &c->adv_ws, &c->cand_keys,
-                 &c->dw_sums, &c->distill_ws, &c->pref_ws};
+                 &c->dw_sums, &c->split_k, &c->distill_ws, &c->pref_ws};
   for (Buf* b : bufs) if (b->p) cudaFree(b->p);
   for (int i = 0; i < kPackRing; ++i) {
     if (c->pack_host[i]) cudaFreeHost(c->pack_host[i]);
@@ -124,7 +124,7 @@ af_status af_destroy(af_ctx* c) {
 int64_t af_workspace_bytes(const af_ctx* c) {
   if (!c) return 0;
   return (int64_t)(c->partial.cap + c->loss_ws.cap + c->pack_meta.cap + c->dz.cap + c->ctrl_ws.cap + c->zlog.cap + c->adv_ws.cap +
-                   c->cand_keys.cap + c->dw_sums.cap + c->distill_ws.cap + c->pref_ws.cap);
+                   c->cand_keys.cap + c->dw_sums.cap + c->split_k.cap + c->distill_ws.cap + c->pref_ws.cap);
 }
 
 af_status af_selftest_bounded_wait(af_ctx* c, uint32_t* waited_us, void* stream) {

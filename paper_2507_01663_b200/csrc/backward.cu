@@ -290,6 +290,105 @@ af_status launch_backward_products(af_ctx* ctx, const void* hidden_blk, const vo
   return dW_product();
 }
 
+namespace {
+
+// ---- epilogue 2b: accumulator tile of one range of the reduction -> fp32 partial sums [part][M, N] ----------
+struct StorePartialEpi {
+  struct Params {
+    float* P;
+    int M, N;
+  };
+  struct State {
+    float* row;
+  };
+  static constexpr bool kStaged = false;
+  static __device__ __forceinline__ void unit_begin(State& st, const Params& p, int row, int, int part) {
+    st.row = p.P + ((size_t)part * p.M + row) * p.N;
+  }
+  static __device__ __forceinline__ void chunk(State& st, const Params& p, int row, int col0, const uint32_t (&v)[32],
+                                               uint8_t*) {
+    if (row >= p.M) return;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)        // N % 8 == 0
+      if (col0 + 4 * q < p.N)
+        *reinterpret_cast<uint4*>(st.row + col0 + 4 * q) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+  }
+  static __device__ __forceinline__ void unit_end(State&, const Params&, int, int) {}
+};
+
+// Adds the parts in order and rounds once: 8 values per thread.
+__global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ P, int parts, size_t n,
+                                                        __nv_bfloat16* __restrict__ out) {
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= n) return;
+  float a[8] = {};
+  for (int k = 0; k < parts; ++k) {
+    const float4 x = __ldcs(reinterpret_cast<const float4*>(P + k * n + i));
+    const float4 y = __ldcs(reinterpret_cast<const float4*>(P + k * n + i) + 1);
+    a[0] += x.x; a[1] += x.y; a[2] += x.z; a[3] += x.w;
+    a[4] += y.x; a[5] += y.y; a[6] += y.z; a[7] += y.w;
+  }
+  *reinterpret_cast<uint4*>(out + i) =
+      make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(a[4], a[5]), pack_bf16x2(a[6], a[7]));
+}
+
+// How dH = dZ W is cut: its reduction is the vocabulary, its tiles are few (16 x 14 for 4001 tokens of the 7B-shaped
+// head), and a last round of tiles that is not full costs as much as a full one (224 tiles on 74 pairs: 4 rounds for
+// 3.03).  The last `rows` row tiles are cut into `parts` ranges of K instead, as many as spread them evenly.
+struct TailPlan {
+  int rows, parts;
+};
+constexpr int kMaxTailRounds = 4;      // tiles x parts of the tail, per pair: bounds its workspace
+TailPlan plan_tail(int m_tiles, int n_tiles, int k_blocks, int pairs) {
+  TailPlan best{0, 1};
+  const double tile_us = 0.25 * k_blocks;      // a 256 x 256 x 64 block takes a pair about 0.25 us
+  double best_us = tile_us * ((m_tiles * (int64_t)n_tiles + pairs - 1) / pairs);
+  for (int r = 1; r <= m_tiles && r <= pairs; ++r) {
+    const int64_t rounds = ((m_tiles - r) * (int64_t)n_tiles + pairs - 1) / pairs;
+    for (int k = 2; k <= 32 && k * 4 <= k_blocks; ++k) {
+      const int64_t units = (int64_t)r * n_tiles * k;
+      if (units > (int64_t)kMaxTailRounds * pairs) break;
+      // the split launch and the sum of its parts (written and read once each), and a second GEMM launch
+      const double us = tile_us * (rounds + (double)((units + pairs - 1) / pairs) / k) + 0.13 * units + (r < m_tiles ? 7.0 : 4.0);
+      if (us < best_us) { best_us = us; best = TailPlan{r, k}; }
+    }
+  }
+  return best;
+}
+
+// dH_blk = dZ W with the tail cut that way.
+af_status hidden_gradient(af_ctx* ctx, const GemmEnv& env, const Operand& dZ, const Operand& W, int64_t tc, int32_t d,
+                          __nv_bfloat16* d_hidden, cudaStream_t s) {
+  const int pairs = env.sm_count / 2;
+  const int m_tiles = (int)((tc + umma::kPairBM - 1) / umma::kPairBM), n_tiles = (d + umma::kBN - 1) / umma::kBN;
+  const TailPlan tail = env.pair ? plan_tail(m_tiles, n_tiles, (int)((dZ.cols + umma::kBK - 1) / umma::kBK), pairs)
+                                 : TailPlan{0, 1};
+  const int64_t first = tail.rows > 0 ? (int64_t)(m_tiles - tail.rows) * umma::kPairBM : tc;   // rows before the tail
+  af_status st = AF_OK;
+  if (first > 0) {
+    const Operand A{dZ.base, (uint64_t)first, dZ.cols, dZ.pitch_bytes};
+    StoreBf16Epi::Params p{d_hidden, d, (int)first, d};
+    st = run_gemm<StoreBf16Epi, false, true>(unpaced_if_cached(env, A, W), A, W, 0, p, s);
+    if (st != AF_OK) return st;
+  }
+  if (first == tc) return AF_OK;
+  const int64_t rows = tc - first;
+  const size_t n = (size_t)rows * d;
+  float* P = static_cast<float*>(ctx->split_k.p);
+  const Operand A{static_cast<const char*>(dZ.base) + (size_t)first * dZ.pitch_bytes, (uint64_t)rows, dZ.cols, dZ.pitch_bytes};
+  StorePartialEpi::Params p{P, (int)rows, d};
+  if ((st = run_gemm_split_k<StorePartialEpi, false, true>(env, A, W, tail.parts, p, s)) != AF_OK) return st;
+  sum_parts_kernel<<<(unsigned)((n / 8 + 255) / 256), 256, 0, s>>>(P, tail.parts, n, d_hidden + (size_t)first * d);
+  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+}
+
+// Most that plan_tail may ask for, whatever the batch: a tile of partial sums per unit.
+size_t split_k_bytes(int sm_count) {
+  return (size_t)kMaxTailRounds * (sm_count / 2) * umma::kPairBM * umma::kBN * sizeof(float);
+}
+
+}  // namespace
+
 // The same two products for a head whose gradient is wanted in fp32, in bf16 or not at all.  A bf16 d_W is
 // rounded once: with several token blocks the earlier ones are summed in fp32 in the workspace and the last
 // one's epilogue adds and rounds.
@@ -302,20 +401,19 @@ af_status launch_head_products(af_ctx* ctx, const void* hidden_blk, const void* 
   const Operand Wop{W, (uint64_t)V, (uint64_t)d, dB};
   const Operand dZop{dz_blk, (uint64_t)tc, (uint64_t)V, vB};
   auto dH_product = [&]() {
-    StoreBf16Epi::Params p2{static_cast<__nv_bfloat16*>(d_hidden_blk), d, (int)tc, d};
-    return run_gemm<StoreBf16Epi, false, true>(env, dZop, Wop, 0, p2, s);
+    return hidden_gradient(ctx, env, dZop, Wop, tc, d, static_cast<__nv_bfloat16*>(d_hidden_blk), s);
   };
   auto dW_product = [&]() {
     const int S = logprob_pick_splits((int64_t)d, (int32_t)tc, V, ctx->sm_count, env.pair, 0, 0);
     if (head.type == AF_BF16 && last_block) {
       StoreBf16TransposedEpi::Params p3{static_cast<__nv_bfloat16*>(head.d_W),
                                         first_block ? nullptr : static_cast<const float*>(ctx->dw_sums.p), d, d, V};
-      return run_gemm<StoreBf16TransposedEpi, true, true>(env, Hblk, dZop, S, p3, s);
+      return run_gemm<StoreBf16TransposedEpi, true, true>(unpaced_if_cached(env, Hblk, dZop), Hblk, dZop, S, p3, s);
     }
     float* C = head.type == AF_BF16 ? static_cast<float*>(ctx->dw_sums.p) : static_cast<float*>(head.d_W);
     const bool add = !first_block || (head.type == AF_F32 && head.accumulate);
     StoreF32TransposedEpi::Params p3{C, d, d, V, add ? 1 : 0};
-    return run_gemm<StoreF32TransposedEpi, true, true>(env, Hblk, dZop, S, p3, s);
+    return run_gemm<StoreF32TransposedEpi, true, true>(unpaced_if_cached(env, Hblk, dZop), Hblk, dZop, S, p3, s);
   };
   if (!head.d_W) return dH_product();
   if (last_block && ctx->dw_ready) {      // as in launch_backward_products
@@ -341,6 +439,7 @@ af_status head_gradient_of_nothing(af_ctx* ctx, const HeadGradient& head, int32_
 af_status reserve_head_gradient(af_ctx* ctx, int64_t T, int32_t d, int32_t V, bool bf16_head) {
   const int64_t Tc = backward_token_block(ctx, T);
   af_status st = ws_grow(ctx->dz, (size_t)Tc * V * 2);
+  if (st == AF_OK) st = ws_grow(ctx->split_k, split_k_bytes(ctx->sm_count));
   if (st == AF_OK && bf16_head && T > Tc) st = ws_grow(ctx->dw_sums, (size_t)V * d * sizeof(float));
   return st;
 }
@@ -368,7 +467,7 @@ af_status launch_candidate_backward(af_ctx* ctx, const void* hidden, const void*
     const Operand Wop{W, (uint64_t)V, (uint64_t)d, (uint64_t)d * 2};
     DzCandidateEpi::Params p1{keys, g + t0 * K, gsum, lse + t0, dz, (int)tc, V, K};
     st = run_gemm<DzCandidateEpi, false, false>(
-        env, Hblk, Wop, logprob_pick_splits(tc, d, V, ctx->sm_count, env.pair, ctx->v_splits, env.die0_pairs), p1, s);
+        unpaced_if_cached(env, Hblk, Wop), Hblk, Wop, logprob_pick_splits(tc, d, V, ctx->sm_count, env.pair, ctx->v_splits, env.die0_pairs), p1, s);
     if (st != AF_OK) return st;
     st = launch_head_products(ctx, H + t0 * d, W, dz, tc, d, V, static_cast<__nv_bfloat16*>(d_hidden) + t0 * d, head,
                               t0 == 0, t0 + Tc >= T, s);

@@ -253,7 +253,9 @@ static size_t candidate_partial_bytes(const af_ctx* ctx, int64_t max_T, int32_t 
 static af_status candidate_gemm(af_ctx* ctx, const void* hidden, const void* W, int64_t T, int32_t d, int32_t V,
                                 int32_t K, const uint32_t* keys, float* cand_z, float* z, int* parts,
                                 cudaStream_t s) {
-  GemmEnv env = gemm_env(ctx);
+  const Operand Hop{hidden, (uint64_t)T, (uint64_t)d, (uint64_t)d * 2};
+  const Operand Wop{W, (uint64_t)V, (uint64_t)d, (uint64_t)d * 2};
+  GemmEnv env = unpaced_if_cached(gemm_env(ctx), Hop, Wop);
   if (T <= umma::kPairBM) env.tile_clock = nullptr;   // one row tile: every pair reads its own part of W, none shares
   const int n_tiles = (V + umma::kBN - 1) / umma::kBN;
   int S = candidate_pick_splits(ctx, T, d, V);
@@ -261,8 +263,6 @@ static af_status candidate_gemm(af_ctx* ctx, const void* hidden, const void* W, 
   *parts = 2 * S;
   af_status st = ws_grow(ctx->partial, (size_t)*parts * (size_t)T * sizeof(float4));
   if (st != AF_OK) return st;
-  const Operand Hop{hidden, (uint64_t)T, (uint64_t)d, (uint64_t)d * 2};
-  const Operand Wop{W, (uint64_t)V, (uint64_t)d, (uint64_t)d * 2};
   float4* partial = static_cast<float4*>(ctx->partial.p);
   if (z) {
     CandidateEpi<true>::Params ep{nullptr, nullptr, partial, z, (int)T, V, K, *parts};

@@ -93,6 +93,7 @@ struct af_ctx {
   af::Buf adv_ws;     // per-group accumulators of af_grpo_advantage with group ids
   af::Buf cand_keys;  // sorted candidate lists [T, K] (and sums of their gradients [Tc] in the backward)
   af::Buf dw_sums;    // fp32 sums [V, d] behind a bf16 d_W of several token blocks
+  af::Buf split_k;    // partial sums of the tail of the candidate backward's d_hidden product
   af::Buf distill_ws; // gradients [Tc, K] of one token block of af_distill_update when the caller wants none
   af::Buf pref_ws;    // partial sums of the sequences of af_preference_loss
 

@@ -56,6 +56,7 @@ inline umma::GemmShape gemm_shape(uint64_t M, uint64_t N, uint64_t K, int splits
   g.k_blocks = (int)((K + umma::kBK - 1) / umma::kBK);
   g.die0_pairs = 0;
   g.die0_rows = 0;
+  g.k_parts = 1;
   return g;
 }
 // Die-aware dealing of a pair launch: only when every SM pair gets a CTA pair and it costs no extra
@@ -129,6 +130,14 @@ af_status run_gemm(const GemmEnv& env, const Operand& A, const Operand& B, int s
   return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
+// The environment without the pacing clock where there is nothing to pace: the clock keeps the pairs from losing one
+// another's tiles in L2, and operands that fit there as a whole are not lost.  (1195 tokens of a 256 x 4096 head:
+// the three products of a backward take 15 us less, a memset and a wait per tile each.)
+inline GemmEnv unpaced_if_cached(GemmEnv env, const Operand& A, const Operand& B) {
+  if (A.rows * A.pitch_bytes + B.rows * B.pitch_bytes <= (48ull << 20)) env.tile_clock = nullptr;
+  return env;
+}
+
 // The same product on K-major operands with promoted accumulation (see umma.cuh): always the CTA-pair
 // main loop.  E is a functor of the promoted form.
 template <class E, int kPromote>
@@ -151,6 +160,30 @@ af_status run_gemm_promoted(const GemmEnv& env, const Operand& A, const Operand&
   if (clock && cudaMemsetAsync(clock, 0, (by_die ? 3 : 1) * sizeof(unsigned int), s) != cudaSuccess) return AF_ERR_CUDA;
   umma::gemm_pair_kernel<E, false, false, kPromote><<<grid, umma::kPromoteThreads, umma::kPairSmemBytes, s>>>(
       ta, tb, g, ep, env.d_err, clock, by_die ? clock + 1 : nullptr, env.die_of_sm);
+  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+}
+
+// The product with its reduction cut into k_parts ranges: a unit is one tile times one range, and E stores fp32
+// partial sums (see umma.cuh).  Always the CTA-pair main loop, without pacing.
+template <class E, bool kAMN, bool kBMN>
+af_status run_gemm_split_k(const GemmEnv& env, const Operand& A, const Operand& B, int k_parts,
+                           const typename E::Params& ep, cudaStream_t s) {
+  CUtensorMap ta, tb;
+  af_status st = encode_operand(env, &ta, A, kAMN ? 64 : umma::kBM);
+  if (st != AF_OK) return st;
+  st = encode_operand(env, &tb, B, kBMN ? 64 : umma::kBN / 2);
+  if (st != AF_OK) return st;
+  umma::GemmShape g = gemm_shape(kAMN ? A.cols : A.rows, kBMN ? B.cols : B.rows, kAMN ? A.rows : A.cols, 0, true);
+  g.k_parts = k_parts;
+  g.splits = g.n_tiles * k_parts;
+  const int64_t units = (int64_t)g.m_tiles * g.splits;
+  constexpr int smem = E::kStaged ? umma::kPairSmemBytesStaged : umma::kPairSmemBytes;
+  static SmemAttrOnce once;
+  if (set_smem_once(once, umma::gemm_pair_kernel<E, kAMN, kBMN, 0, true>, smem) != cudaSuccess) return AF_ERR_CUDA;
+  const int pairs = env.sm_count / 2;
+  const int grid = 2 * (int)(units < pairs ? units : pairs);
+  umma::gemm_pair_kernel<E, kAMN, kBMN, 0, true><<<grid, umma::kThreads, smem, s>>>(ta, tb, g, ep, env.d_err, nullptr,
+                                                                                  nullptr, nullptr);
   return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 

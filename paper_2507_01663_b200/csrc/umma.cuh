@@ -202,6 +202,7 @@ struct GemmShape {
   int k_blocks;         // ceil(K/64)
   int die0_pairs;       // pair kernel only: > 0 = deal the row tiles by die; the number of CTA pairs the first die hosts
   int die0_rows;        // ... and the number of row tiles (the first ones) those pairs share among themselves
+  int k_parts;          // pair kernel with kSplitK only: parts the reduction is cut into; `splits` is then n_tiles * k_parts
 };
 __device__ __forceinline__ int split_begin(const GemmShape& g, int s) {
   return (int)(((long long)g.n_tiles * s) / g.splits);
@@ -508,7 +509,11 @@ __device__ __forceinline__ int pair_work_most(const GemmShape& g, int n_pairs) {
 //   static __device__ void unit_begin(State&, const Params&, int row, int col0);   col0: first column of the unit
 //   static __device__ void tile(State&, const Params&, int row, int col0, float (&a)[kPromoteCols]);
 //   static __device__ void unit_end(State&, const Params&, int row, int part);     part = 2 * split + column half
-template <class E, bool kAMN = false, bool kBMN = false, int kPromote = 0>
+//
+// kSplitK: a unit is one tile times one of k_parts ranges of K blocks, for products with few tiles and a long
+// reduction; the functor's unit_begin receives the range's number in place of the split and leaves fp32 partial
+// sums that a second kernel adds up.
+template <class E, bool kAMN = false, bool kBMN = false, int kPromote = 0, bool kSplitK = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPromote > 0 ? kPromoteThreads : kThreads, 1)
 gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                  const GemmShape g, const typename E::Params ep, unsigned int* d_err, unsigned int* tile_clock,
@@ -569,6 +574,18 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
   // both CTAs work from the leader's rank
   const int pair = (int)ld_shared_cluster_u32(map_to_cta(smem_u32(&s_pair_rank), 0));
   const PairWork work = pair_work(g, pair, n_pairs);  // m_tiles counts 256-row tiles here
+  // B tiles and K blocks of split s
+  auto tiles_of = [&](int s, int& nb, int& ne, int& kb0, int& kb1) {
+    if constexpr (kSplitK) {
+      const int part = s % g.k_parts;
+      nb = s / g.k_parts; ne = nb + 1;
+      kb0 = (int)((long long)g.k_blocks * part / g.k_parts);
+      kb1 = (int)((long long)g.k_blocks * (part + 1) / g.k_parts);
+    } else {
+      nb = split_begin(g, s); ne = split_begin(g, s + 1);
+      kb0 = 0; kb1 = g.k_blocks;
+    }
+  };
 
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA producer (both CTAs)
@@ -602,11 +619,12 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
       for (int q = work.first; q < work.end && ok; q += work.step) {
         const int u = work.base_unit + q;
         const int m_tile = u / g.splits, s = u % g.splits;
-        const int nb = split_begin(g, s), ne = split_begin(g, s + 1);
+        int nb, ne, kb0, kb1;
+        tiles_of(s, nb, ne, kb0, kb1);
         const int m0 = m_tile * kPairBM + (int)rank * kBM;          // this CTA's 128 rows of A
         for (int nt = nb; nt < ne && ok; ++nt) {
           const int n0 = nt * kBN + (int)rank * (kBN / 2);          // this CTA's 128 rows of B
-          for (int kb = 0; kb < g.k_blocks; ++kb) {
+          for (int kb = kb0; kb < kb1; ++kb) {
             if (clock_on && to_next_tick-- == 0) {
               to_next_tick = tick_len - 1;
               if (my_ticks >= kClockWindow && my_ticks >= skip_until) {
@@ -665,14 +683,15 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
       int stage = 0; uint32_t phase = 0; uint32_t tile_count = 0; bool ok = true;
       for (int q = work.first; q < work.end && ok; q += work.step) {
         const int s = (work.base_unit + q) % g.splits;
-        const int nb = split_begin(g, s), ne = split_begin(g, s + 1);
+        int nb, ne, kb0, kb1;
+        tiles_of(s, nb, ne, kb0, kb1);
         for (int nt = nb; nt < ne && ok; ++nt, ++tile_count) {
           uint32_t acc = tile_count & 1u, acc_phase = (tile_count >> 1) & 1u;
           if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, &abort_flag)) { ok = false; break; }
           tc_fence_after();
           uint32_t d_tmem = tmem_base + acc * kBN;
           int part_kb = 0;                               // K blocks in the current part (kPromote > 0)
-          for (int kb = 0; kb < g.k_blocks; ++kb) {
+          for (int kb = kb0; kb < kb1; ++kb) {
             if constexpr (kPromote > 0) {
               if (part_kb == kPromote) {                 // next part: publish this one, take the other accumulator
                 mma_commit_pair(tfull_bar(acc));
@@ -692,7 +711,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
 #pragma unroll
             for (int k = 0; k < kBK / kUmmaK; ++k) {
               mma_bf16_ss_pair(d_tmem, a_desc + (uint64_t)k * a_step, b_desc + (uint64_t)k * b_step, idesc,
-                               ((kPromote > 0 ? part_kb : kb) | k) != 0 ? 1u : 0u);
+                               ((kPromote > 0 ? part_kb : kb - kb0) | k) != 0 ? 1u : 0u);
             }
             mma_commit_pair(empty_bar(stage));   // both CTAs' slots reusable once these MMAs have read them
             ++part_kb;
@@ -753,9 +772,10 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
     for (int q = work.first; q < work.end && ok; q += work.step) {
       const int u = work.base_unit + q;
       const int m_tile = u / g.splits, s = u % g.splits;
-      const int nb = split_begin(g, s), ne = split_begin(g, s + 1);
+      int nb, ne, kb0, kb1;
+      tiles_of(s, nb, ne, kb0, kb1);
       const int row = m_tile * kPairBM + row_in_tile;
-      E::unit_begin(st, ep, row, m_tile, s);
+      E::unit_begin(st, ep, row, m_tile, kSplitK ? s % g.k_parts : s);
       for (int nt = nb; nt < ne && ok; ++nt, ++tile_count) {
         const uint32_t acc = tile_count & 1u, acc_phase = (tile_count >> 1) & 1u;
         if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, &abort_flag))) { ok = false; break; }
