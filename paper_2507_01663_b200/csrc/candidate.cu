@@ -37,6 +37,7 @@ struct CandidateEpi {
     int T, V, K, parts;
   };
   using State = CandidateState;
+  static constexpr bool kStaged = kStoreZ;
   static __device__ __forceinline__ void unit_begin(State& st, const Params& p, int row, int col0) {
     st.m = -INFINITY; st.s = 0.f; st.u = 0.f;
     st.key = kNoCandidate;
@@ -49,20 +50,29 @@ struct CandidateEpi {
     }
   }
   static __device__ __forceinline__ void tile(State& st, const Params& p, int row, int col0,
-                                              float (&a)[umma::kPromoteCols]) {
+                                              float (&a)[umma::kPromoteCols], uint8_t* stage) {
     constexpr int kCols = umma::kPromoteCols;
     if (col0 >= p.V) return;
     if constexpr (kStoreZ) {
-      if (row < p.T) {
-        float* dst = p.z + (size_t)row * p.V + col0;           // V % 8 == 0 here: 16-byte aligned
-        if (col0 + kCols <= p.V) {
+      // a lane has a row's 128 values; stored that way, an instruction would write 16 bytes to each of 32 rows.  By
+      // way of shared memory it writes four whole 128-byte lines (32 x 32 values at a time; slot q of row r sits at
+      // q ^ (r & 7), so that neither side meets bank conflicts)
+      const int lane = threadIdx.x & 31;
+      float4* const st4 = reinterpret_cast<float4*>(stage);
 #pragma unroll
-          for (int q = 0; q < kCols / 4; ++q)
-            reinterpret_cast<float4*>(dst)[q] = make_float4(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]);
-        } else {
+      for (int c = 0; c < kCols; c += 32) {
 #pragma unroll
-          for (int j = 0; j < kCols; ++j) if (col0 + j < p.V) dst[j] = a[j];
+        for (int q = 0; q < 8; ++q)
+          st4[lane * 8 + (q ^ (lane & 7))] = make_float4(a[c + 4 * q], a[c + 4 * q + 1], a[c + 4 * q + 2], a[c + 4 * q + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = i * 4 + (lane >> 3), q = lane & 7;
+          const int zr = row - lane + r, zc = col0 + c + 4 * q;
+          if (zr < p.T && zc < p.V)           // V % 8 == 0 here: whole float4s, 16-byte aligned
+            __stcs(reinterpret_cast<float4*>(p.z + (size_t)zr * p.V + zc), st4[r * 8 + (q ^ (r & 7))]);
         }
+        __syncwarp();
       }
     } else {
       // entries of the other column half that the sweep has passed by

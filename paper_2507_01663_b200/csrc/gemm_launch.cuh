@@ -151,14 +151,14 @@ af_status run_gemm_promoted(const GemmEnv& env, const Operand& A, const Operand&
   umma::GemmShape g = gemm_shape(A.rows, B.rows, A.cols, splits, true);
   const int64_t units = (int64_t)g.m_tiles * g.splits;
   static SmemAttrOnce once;
-  if (set_smem_once(once, umma::gemm_pair_kernel<E, false, false, kPromote>, umma::kPairSmemBytes) != cudaSuccess)
-    return AF_ERR_CUDA;
+  constexpr int smem = E::kStaged ? umma::kPromoteSmemBytesStaged : umma::kPairSmemBytes;
+  if (set_smem_once(once, umma::gemm_pair_kernel<E, false, false, kPromote>, smem) != cudaSuccess) return AF_ERR_CUDA;
   const int pairs = env.sm_count / 2;
   const int grid = 2 * (int)(units < pairs ? units : pairs);
   unsigned int* clock = env.tile_clock;
   const bool by_die = env.die_of_sm && clock && deal_by_die(g, pairs, env.die0_pairs);
   if (clock && cudaMemsetAsync(clock, 0, (by_die ? 3 : 1) * sizeof(unsigned int), s) != cudaSuccess) return AF_ERR_CUDA;
-  umma::gemm_pair_kernel<E, false, false, kPromote><<<grid, umma::kPromoteThreads, umma::kPairSmemBytes, s>>>(
+  umma::gemm_pair_kernel<E, false, false, kPromote><<<grid, umma::kPromoteThreads, smem, s>>>(
       ta, tb, g, ep, env.d_err, clock, by_die ? clock + 1 : nullptr, env.die_of_sm);
   return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }

@@ -410,6 +410,7 @@ constexpr int kPairSmemBytesStaged = kPairSmemBytes + 4 * kEpiStageBytes;
 // the time the MMAs need for the next one and is hidden behind it.
 constexpr int kPromoteCols = kBN / 2;                         // columns per epilogue thread
 constexpr int kPromoteThreads = 64 + 256;                     // producer and MMA warps, eight epilogue warps
+constexpr int kPromoteSmemBytesStaged = kPairSmemBytes + 8 * kEpiStageBytes;
 
 __device__ __forceinline__ uint32_t cluster_ctarank() {
   uint32_t r;
@@ -507,7 +508,9 @@ __device__ __forceinline__ int pair_work_most(const GemmShape& g, int n_pairs) {
 // kPromote K blocks per part) calls for a functor of this form instead, whose threads own half a
 // tile's columns:
 //   static __device__ void unit_begin(State&, const Params&, int row, int col0);   col0: first column of the unit
-//   static __device__ void tile(State&, const Params&, int row, int col0, float (&a)[kPromoteCols]);
+//   static constexpr bool kStaged;
+//   static __device__ void tile(State&, const Params&, int row, int col0, float (&a)[kPromoteCols], uint8_t* stage);
+//        -- called by all 32 lanes of a warp together; stage: the warp's private kEpiStageBytes (kStaged only)
 //   static __device__ void unit_end(State&, const Params&, int row, int part);     part = 2 * split + column half
 //
 // kSplitK: a unit is one tile times one of k_parts ranges of K blocks, for products with few tiles and a long
@@ -729,6 +732,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
     const int parts = (g.k_blocks + kPromote - 1) / kPromote;
     uint32_t part_count = 0; bool ok = true;
     typename E::State st;
+    uint8_t* const stage = E::kStaged ? epi_stage_base + (warp - 2) * kEpiStageBytes : nullptr;
     for (int q = work.first; q < work.end && ok; q += work.step) {
       const int u = work.base_unit + q;
       const int m_tile = u / g.splits, s = u % g.splits;
@@ -758,7 +762,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(tempty_bar(acc), 0);   // one arrival per warp, on the leader
         }
-        if (ok) E::tile(st, ep, row, nt * kBN + half * kPromoteCols, a);
+        if (ok) E::tile(st, ep, row, nt * kBN + half * kPromoteCols, a, stage);
       }
       if (ok) E::unit_end(st, ep, row, 2 * s + half);
     }
