@@ -319,6 +319,8 @@ struct StorePartialEpi {
 // Adds the parts in order and rounds once: 8 values per thread.
 __global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ P, int parts, size_t n,
                                                         __nv_bfloat16* __restrict__ out) {
+  wait_for_predecessor();
+  let_successor_start();
   const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (i >= n) return;
   float a[8] = {};
@@ -378,8 +380,8 @@ af_status hidden_gradient(af_ctx* ctx, const GemmEnv& env, const Operand& dZ, co
   const Operand A{static_cast<const char*>(dZ.base) + (size_t)first * dZ.pitch_bytes, (uint64_t)rows, dZ.cols, dZ.pitch_bytes};
   StorePartialEpi::Params p{P, (int)rows, d};
   if ((st = run_gemm_split_k<StorePartialEpi, false, true>(env, A, W, tail.parts, p, s)) != AF_OK) return st;
-  sum_parts_kernel<<<(unsigned)((n / 8 + 255) / 256), 256, 0, s>>>(P, tail.parts, n, d_hidden + (size_t)first * d);
-  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  return launch_overlapped(sum_parts_kernel, (unsigned)((n / 8 + 255) / 256), 256, 0, s, P, tail.parts, n,
+                           d_hidden + (size_t)first * d) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
 // Most that plan_tail may ask for, whatever the batch: a tile of partial sums per unit.
@@ -395,7 +397,8 @@ size_t split_k_bytes(int sm_count) {
 af_status launch_head_products(af_ctx* ctx, const void* hidden_blk, const void* W, const void* dz_blk, int64_t tc,
                                int32_t d, int32_t V, void* d_hidden_blk, const HeadGradient& head, bool first_block,
                                bool last_block, cudaStream_t s) {
-  const GemmEnv env = gemm_env(ctx);
+  GemmEnv env = gemm_env(ctx);
+  env.overlapped = true;
   const uint64_t dB = (uint64_t)d * 2, vB = (uint64_t)V * 2;
   const Operand Hblk{hidden_blk, (uint64_t)tc, (uint64_t)d, dB};
   const Operand Wop{W, (uint64_t)V, (uint64_t)d, dB};
@@ -459,7 +462,8 @@ af_status launch_candidate_backward(af_ctx* ctx, const void* hidden, const void*
   float* gsum = reinterpret_cast<float*>(static_cast<char*>(ctx->cand_keys.p) + key_bytes);
   __nv_bfloat16* dz = static_cast<__nv_bfloat16*>(ctx->dz.p);
   const __nv_bfloat16* H = static_cast<const __nv_bfloat16*>(hidden);
-  const GemmEnv env = gemm_env(ctx);
+  GemmEnv env = gemm_env(ctx);
+  env.overlapped = true;
   for (int64_t t0 = 0; t0 < T; t0 += Tc) {
     const int64_t tc = (T - t0) < Tc ? (T - t0) : Tc;
     if (launch_sort_candidates(cand + t0 * K, g + t0 * K, tc, K, V, keys, gsum, s) != cudaSuccess) return AF_ERR_CUDA;

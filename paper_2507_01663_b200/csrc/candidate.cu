@@ -122,6 +122,8 @@ template <int kE>
 __global__ void __launch_bounds__(256) sort_candidates_kernel(
     const int32_t* __restrict__ cand, const float* __restrict__ g, int64_t rows, int K, int V,
     uint32_t* __restrict__ keys, float* __restrict__ gsum) {
+  wait_for_predecessor();
+  let_successor_start();
   const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= rows) return;
   const int lane = threadIdx.x & 31;
@@ -183,6 +185,8 @@ __global__ void __launch_bounds__(256) finish_candidates_kernel(
     const float4* __restrict__ partial, int parts, const int32_t* __restrict__ cand, const float* __restrict__ z,
     int64_t rows, int K, int V, float* __restrict__ cand_logp, float* __restrict__ entropy,
     float* __restrict__ lse_out, unsigned int* d_err) {
+  wait_for_predecessor();
+  let_successor_start();
   const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= rows) return;
   const int lane = threadIdx.x & 31;
@@ -229,11 +233,9 @@ __global__ void __launch_bounds__(256) finish_candidates_kernel(
 cudaError_t launch_sort_candidates(const int32_t* cand, const float* g, int64_t rows, int32_t K, int32_t V,
                                    uint32_t* keys, float* gsum, cudaStream_t s) {
   const unsigned blocks = (unsigned)((rows + 7) / 8);
-  if (K <= 32) sort_candidates_kernel<1><<<blocks, 256, 0, s>>>(cand, g, rows, K, V, keys, gsum);
-  else if (K <= 64) sort_candidates_kernel<2><<<blocks, 256, 0, s>>>(cand, g, rows, K, V, keys, gsum);
-  else if (K <= 128) sort_candidates_kernel<4><<<blocks, 256, 0, s>>>(cand, g, rows, K, V, keys, gsum);
-  else sort_candidates_kernel<8><<<blocks, 256, 0, s>>>(cand, g, rows, K, V, keys, gsum);
-  return cudaGetLastError();
+  auto kernel = K <= 32 ? sort_candidates_kernel<1> : K <= 64 ? sort_candidates_kernel<2>
+              : K <= 128 ? sort_candidates_kernel<4> : sort_candidates_kernel<8>;
+  return launch_overlapped(kernel, blocks, 256, 0, s, cand, g, rows, K, V, keys, gsum);
 }
 
 // Vocabulary ranges per row tile.  Up to a few row tiles the launch is the stream of W, and every CTA pair
@@ -311,9 +313,9 @@ af_status launch_candidate_logprob(af_ctx* ctx, const void* hidden, const void* 
   if (launch_sort_candidates(cand, nullptr, T, K, V, keys, nullptr, s) != cudaSuccess) return AF_ERR_CUDA;
   int parts = 0;
   if ((st = candidate_gemm(ctx, hidden, W, T, d, V, K, keys, cand_logp, nullptr, &parts, s)) != AF_OK) return st;
-  finish_candidates_kernel<false><<<(unsigned)((T + 7) / 8), 256, 0, s>>>(
-      static_cast<const float4*>(ctx->partial.p), parts, cand, nullptr, T, K, V, cand_logp, entropy, lse, ctx->d_err);
-  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  return launch_overlapped(finish_candidates_kernel<false>, (unsigned)((T + 7) / 8), 256, 0, s,
+                           static_cast<const float4*>(ctx->partial.p), parts, cand, nullptr, T, K, V, cand_logp, entropy, lse,
+                           ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
 af_status launch_candidate_logprob_z(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand, int64_t T,
@@ -322,9 +324,9 @@ af_status launch_candidate_logprob_z(af_ctx* ctx, const void* hidden, const void
   int parts = 0;
   const af_status st = candidate_gemm(ctx, hidden, W, T, d, V, K, nullptr, nullptr, z, &parts, s);
   if (st != AF_OK) return st;
-  finish_candidates_kernel<true><<<(unsigned)((T + 7) / 8), 256, 0, s>>>(
-      static_cast<const float4*>(ctx->partial.p), parts, cand, z, T, K, V, cand_logp, entropy, lse, ctx->d_err);
-  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  return launch_overlapped(finish_candidates_kernel<true>, (unsigned)((T + 7) / 8), 256, 0, s,
+                           static_cast<const float4*>(ctx->partial.p), parts, cand, z, T, K, V, cand_logp, entropy, lse,
+                           ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
 }  // namespace af

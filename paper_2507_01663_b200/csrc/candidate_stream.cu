@@ -81,6 +81,8 @@ __global__ void __launch_bounds__(kThreads, 1) candidate_stream_kernel(
   __shared__ int s_last, abort_flag;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
+  wait_for_predecessor();
+  let_successor_start();
   const uint32_t ring = umma::smem_u32(smem), bars = umma::smem_u32(s_bars);
   const uint32_t row_bytes = (uint32_t)d * 2, stage_bytes = kRows * row_bytes;
   auto full_bar = [&](int s) { return bars + 8u * s; };
@@ -262,10 +264,9 @@ af_status launch_stream(const StreamCall& c, int blocks, cudaStream_t s) {
   static SmemAttrOnce once;
   if (set_smem_once(once, candidate_stream_kernel<kTokens, kLines>, kRingBytes) != cudaSuccess) return AF_ERR_CUDA;
   const int stages = stream_stages(c.d);
-  candidate_stream_kernel<kTokens, kLines><<<blocks, kThreads, stages * kRows * c.d * 2 + 128, s>>>(
-      static_cast<const uint4*>(c.hidden), static_cast<const char*>(c.W), c.cand, c.T, c.K, c.d, c.V, stages, c.z, c.partial,
-      c.cand_logp, c.entropy, c.lse, c.ticket, c.d_err);
-  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  return launch_overlapped(candidate_stream_kernel<kTokens, kLines>, blocks, kThreads, (size_t)stages * kRows * c.d * 2 + 128, s,
+                           static_cast<const uint4*>(c.hidden), static_cast<const char*>(c.W), c.cand, c.T, c.K, c.d, c.V, stages,
+                           c.z, c.partial, c.cand_logp, c.entropy, c.lse, c.ticket, c.d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
 }  // namespace

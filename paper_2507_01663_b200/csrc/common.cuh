@@ -63,6 +63,25 @@ inline cudaError_t set_smem_once(SmemAttrOnce& once, Kernel kernel, int bytes) {
   return e;
 }
 
+// Launch whose blocks may become resident while the stream's previous kernel drains; the kernel calls
+// wait_for_predecessor before it touches memory.  A chain of short kernels (the calls on listed candidates at small
+// sizes) saves one or two microseconds per link; recorded into a graph it keeps that property.
+template <class... Params, class... Args>
+inline cudaError_t launch_overlapped(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
+                                     Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
 }  // namespace af
 
 struct af_ctx {

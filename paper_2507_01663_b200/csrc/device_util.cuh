@@ -16,6 +16,13 @@ __device__ __forceinline__ float ex2f(float x) {
   return y;
 }
 
+// For a kernel launched with launch_overlapped (common.cuh): it may start while its predecessor in the stream still
+// runs, and touches no memory before this has returned (by then everything earlier is complete and visible).  Every
+// thread that reads or writes global memory calls it.  Without that kind of launch it does nothing.
+__device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Lets such a successor start once every block has called this or ended.
+__device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Two floats rounded to nearest-even bf16, packed low | high.
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);

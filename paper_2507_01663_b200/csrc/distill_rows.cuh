@@ -215,6 +215,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_loss_kernel(
     float* __restrict__ token_loss, float* __restrict__ dcand, DistillWs* ws, unsigned int* d_err) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ int abort_flag;
+  wait_for_predecessor();
+  let_successor_start();
   constexpr int kRows = kThreads / kG;              // rows the CTA works on at a time
   const int step_rows = kRows * batches;            // rows of a step, one ring stage
   constexpr int kWarpRows = 32 / kG;                // rows a warp works on at a time
@@ -440,8 +442,8 @@ cudaError_t launch_rows(const DistillCall& c, cudaStream_t s) {
   if (batches < 1) batches = 1;
   const int64_t steps = ((int64_t)c.rows + kRows * batches - 1) / (kRows * batches);
   const int blocks = (int)(steps < 1 ? 1 : steps < most ? steps : most);
-  distill_loss_kernel<kSupport, kForward, kG, kE, kVec><<<blocks, kThreads, kSmemBytes, s>>>(
-      c.cand_logp, c.teacher_logp, c.cu, c.B, c.T, c.t0, c.rows, c.K, batches, c.bulk & (32 / kG * c.K % 4 == 0 ? 3 : 1), c.prm, c.out, c.token_loss,
+  return launch_overlapped(
+      distill_loss_kernel<kSupport, kForward, kG, kE, kVec>, blocks, kThreads, kSmemBytes, s, c.cand_logp, c.teacher_logp, c.cu, c.B, c.T, c.t0, c.rows, c.K, batches, c.bulk & (32 / kG * c.K % 4 == 0 ? 3 : 1), c.prm, c.out, c.token_loss,
       c.dcand, c.ws, c.d_err);
   return cudaGetLastError();
 }

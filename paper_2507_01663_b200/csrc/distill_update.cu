@@ -24,6 +24,8 @@ __global__ void __launch_bounds__(kThreads) dz_candidates_kernel(
   __shared__ int s_id[AF_MAX_CANDIDATES];
   __shared__ float s_g[AF_MAX_CANDIDATES];
   __shared__ double s_sum[kThreads / 32];
+  wait_for_predecessor();
+  let_successor_start();
   const size_t row = blockIdx.x;
   const int k = threadIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int id = -1;
@@ -100,8 +102,9 @@ af_status launch_distill_update(af_ctx* ctx, const void* hidden, const void* W, 
                             one_block ? token_loss : nullptr, g, ctx->loss_ws.p, ctx->d_err, ctx->sm_count,
                             s) != cudaSuccess)
       return AF_ERR_CUDA;
-    dz_candidates_kernel<<<(unsigned)tc, kThreads, 0, s>>>(zlog, dz, V, cand + t0 * K, g, lq, lse + t0, K);
-    if (cudaGetLastError() != cudaSuccess) return AF_ERR_CUDA;
+    if (launch_overlapped(dz_candidates_kernel, (unsigned)tc, kThreads, 0, s, zlog, dz, V, cand + t0 * K, g, lq, lse + t0, K) !=
+        cudaSuccess)
+      return AF_ERR_CUDA;
     st = launch_head_products(ctx, H + t0 * d, W, dz, tc, d, V, static_cast<__nv_bfloat16*>(d_hidden) + t0 * d, head,
                               t0 == 0, t0 + Tc >= T, s);
     if (st != AF_OK) return st;

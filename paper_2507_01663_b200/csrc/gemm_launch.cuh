@@ -24,6 +24,7 @@ struct GemmEnv {
   TmapCache* cache;          // tensor maps encoded earlier (a context's), or null
   const unsigned char* die_of_sm;  // measured die of every SM id, or null
   int die0_pairs;            // > 0: deal row tiles to pairs by die; CTA pairs the first die hosts
+  bool overlapped = false;   // start while the previous kernel of the stream drains (pair variant)
 };
 
 // Die-aware dealing of a pair GEMM's units (see umma::PairWork): can the first rows0 row tiles go to
@@ -118,6 +119,9 @@ af_status run_gemm(const GemmEnv& env, const Operand& A, const Operand& B, int s
     unsigned int* clock = env.tile_clock;
     const bool by_die = env.die_of_sm && clock && deal_by_die(g, pairs, env.die0_pairs);
     if (clock && cudaMemsetAsync(clock, 0, (by_die ? 3 : 1) * sizeof(unsigned int), s) != cudaSuccess) return AF_ERR_CUDA;
+    if (env.overlapped)
+      return launch_overlapped(umma::gemm_pair_kernel<E, kAMN, kBMN>, grid, umma::kThreads, smem, s, ta, tb, g, ep, env.d_err,
+                               clock, by_die ? clock + 1 : nullptr, env.die_of_sm) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
     umma::gemm_pair_kernel<E, kAMN, kBMN><<<grid, umma::kThreads, smem, s>>>(ta, tb, g, ep, env.d_err, clock,
                                                                              by_die ? clock + 1 : nullptr, env.die_of_sm);
   } else {
@@ -158,9 +162,9 @@ af_status run_gemm_promoted(const GemmEnv& env, const Operand& A, const Operand&
   unsigned int* clock = env.tile_clock;
   const bool by_die = env.die_of_sm && clock && deal_by_die(g, pairs, env.die0_pairs);
   if (clock && cudaMemsetAsync(clock, 0, (by_die ? 3 : 1) * sizeof(unsigned int), s) != cudaSuccess) return AF_ERR_CUDA;
-  umma::gemm_pair_kernel<E, false, false, kPromote><<<grid, umma::kPromoteThreads, smem, s>>>(
-      ta, tb, g, ep, env.d_err, clock, by_die ? clock + 1 : nullptr, env.die_of_sm);
-  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  return launch_overlapped(umma::gemm_pair_kernel<E, false, false, kPromote>, grid, umma::kPromoteThreads, smem, s, ta, tb, g,
+                           ep, env.d_err, clock, by_die ? clock + 1 : nullptr, env.die_of_sm) == cudaSuccess
+             ? AF_OK : AF_ERR_CUDA;
 }
 
 // The product with its reduction cut into k_parts ranges: a unit is one tile times one range, and E stores fp32
@@ -182,9 +186,8 @@ af_status run_gemm_split_k(const GemmEnv& env, const Operand& A, const Operand& 
   if (set_smem_once(once, umma::gemm_pair_kernel<E, kAMN, kBMN, 0, true>, smem) != cudaSuccess) return AF_ERR_CUDA;
   const int pairs = env.sm_count / 2;
   const int grid = 2 * (int)(units < pairs ? units : pairs);
-  umma::gemm_pair_kernel<E, kAMN, kBMN, 0, true><<<grid, umma::kThreads, smem, s>>>(ta, tb, g, ep, env.d_err, nullptr,
-                                                                                  nullptr, nullptr);
-  return cudaGetLastError() == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  return launch_overlapped(umma::gemm_pair_kernel<E, kAMN, kBMN, 0, true>, grid, umma::kThreads, smem, s, ta, tb, g, ep, env.d_err,
+                           nullptr, nullptr, nullptr) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
 inline GemmEnv gemm_env(af_ctx* ctx) {

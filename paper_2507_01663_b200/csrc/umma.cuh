@@ -22,6 +22,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "device_util.cuh"
+
 namespace af {
 namespace umma {
 
@@ -538,6 +540,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();          // 0 = leader
   const int n_pairs = gridDim.x >> 1;
+  if (g.die0_pairs > 0) wait_for_predecessor();     // the rank counters below are memory too
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int s = 0; s < kPairStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -569,6 +572,8 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
     tmem_alloc_pair(tmem_slot, kTmemCols);
     tmem_relinquish_pair();
   }
+  wait_for_predecessor();   // from here on operands and the epilogue's inputs are read
+  let_successor_start();
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();       // the peer's barriers exist before anything is signalled across CTAs
