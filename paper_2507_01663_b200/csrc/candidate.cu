@@ -49,7 +49,7 @@ struct CandidateEpi {
       }
     }
   }
-  static __device__ __forceinline__ void tile(State& st, const Params& p, int row, int col0,
+  static __device__ __forceinline__ void tile(State& st, const Params& p, int row, int col0, int cols,
                                               float (&a)[umma::kPromoteCols], uint8_t* stage) {
     constexpr int kCols = umma::kPromoteCols;
     if (col0 >= p.V) return;
@@ -79,7 +79,8 @@ struct CandidateEpi {
       while ((int)(st.key >> 8) < col0) { ++st.next; st.key = candidate_at(st.keys, p.K, st.next); }
 #pragma unroll
       for (int c = 0; c < kCols; c += 32) {
-        while ((int)(st.key >> 8) < col0 + c + 32) {
+        const int end = col0 + (c + 32 < cols ? c + 32 : cols);
+        while ((int)(st.key >> 8) < end) {
           const int j = (int)(st.key >> 8) - (col0 + c);
           float z = a[c];
 #pragma unroll
@@ -90,9 +91,10 @@ struct CandidateEpi {
         }
       }
     }
-    if (col0 + kCols > p.V) {   // ragged vocabulary tail: columns >= V hold zero-fill, not logits
+    if (col0 + kCols > p.V || cols < kCols) {   // columns >= V hold zero-fill, columns past the tile's width nothing
+      const int n = p.V - col0 < cols ? p.V - col0 : cols;
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) if (col0 + j >= p.V) a[j] = -1.0e30f;
+      for (int j = 0; j < kCols; ++j) if (j >= n) a[j] = -1.0e30f;
     }
     float mx[4] = {a[0], a[1], a[2], a[3]};
 #pragma unroll
@@ -238,24 +240,45 @@ cudaError_t launch_sort_candidates(const int32_t* cand, const float* g, int64_t 
   return launch_overlapped(kernel, blocks, 256, 0, s, cand, g, rows, K, V, keys, gsum);
 }
 
-// Vocabulary ranges per row tile.  Up to a few row tiles the launch is the stream of W, and every CTA pair
-// should carry a share of it; the rule of af_token_logprob stops at 32 ranges.
-int candidate_pick_splits(const af_ctx* ctx, int64_t T, int32_t d, int32_t V) {
-  const int workers = ctx->sm_count / 2 > 0 ? ctx->sm_count / 2 : 1;
+// How the scoring GEMM is cut: vocabulary ranges per row tile, columns of a tile, CTA pairs or single CTAs.
+// Up to 128 tokens it is the stream of W, and the MMAs should not stand in its way: a pair multiplies 256 rows of
+// hidden states whatever their number, a single CTA 128, and the tile's width is free to share the columns out evenly
+// (152064 columns on 148 SMs: 5 tiles of 208 for 4.94; on 74 pairs 9 tiles of 256 for 8.03).  64 tokens of 3584 over
+// 152064 words: 183 us against 228 on pairs (191 with tiles of 256); 17 tokens 209 against 242; 64 tokens of 5120, 255
+// against 326.  From there on the rule of af_token_logprob holds, except that it stops at 32 ranges, too few for one or
+// two row tiles.
+struct CandidateTiling {
+  int splits, bn;
+  bool single;
+};
+static CandidateTiling candidate_tiling(const af_ctx* ctx, int64_t T, int32_t d, int32_t V, bool store_z) {
   const int64_t m_tiles = (T + umma::kPairBM - 1) / umma::kPairBM;
   const int n_tiles = (V + umma::kBN - 1) / umma::kBN;
-  if (ctx->v_splits == 0 && m_tiles * 32 < workers) {
-    const int S = (int)(workers / m_tiles);
-    return S < n_tiles ? S : n_tiles;
+  if (ctx->v_splits == 0 && T <= umma::kBM && !store_z) {
+    int bn = umma::kBN;
+    int64_t least = INT64_MAX;
+    for (int b = umma::kBN; b >= 128; b -= 16) {
+      const int64_t tiles = (V + b - 1) / b, columns = (tiles + ctx->sm_count - 1) / ctx->sm_count * b;   // of the busiest SM
+      if (columns < least) { least = columns; bn = b; }
+    }
+    const int tiles = (V + bn - 1) / bn;
+    return CandidateTiling{ctx->sm_count < tiles ? ctx->sm_count : tiles, bn, true};
   }
-  const int die0_pairs = ctx->die_aware && ctx->die0_sms > 0 ? ctx->die0_sms / 2 : 0;
-  return logprob_pick_splits(T, d, V, ctx->sm_count, true, ctx->v_splits, die0_pairs);
+  const int workers = ctx->sm_count / 2 > 0 ? ctx->sm_count / 2 : 1;
+  int S;
+  if (ctx->v_splits == 0 && m_tiles * 32 < workers) {
+    S = (int)(workers / m_tiles);
+  } else {
+    const int die0_pairs = ctx->die_aware && ctx->die0_sms > 0 ? ctx->die0_sms / 2 : 0;
+    S = logprob_pick_splits(T, d, V, ctx->sm_count, true, ctx->v_splits, die0_pairs);
+  }
+  return CandidateTiling{S < n_tiles ? S : n_tiles, umma::kBN, false};
 }
 
 static size_t candidate_partial_bytes(const af_ctx* ctx, int64_t max_T, int32_t d, int32_t V) {
-  const int64_t S = candidate_pick_splits(ctx, max_T, d, V);
+  const int64_t S = candidate_tiling(ctx, max_T, d, V, true).splits;
   // smaller batches may pick up to 8 ranges whatever their size, and more only while there are at most 8
-  // units per pair (one unit = 256 rows of two parts)
+  // units per pair (one unit = 256 rows of two parts) or one per SM (128 rows)
   const int64_t need = (S > 8 ? S : 8) * 2 * max_T;
   const int64_t small = (int64_t)(ctx->sm_count / 2 + 1) * 8 * 2 * umma::kPairBM;
   return (size_t)(need > small ? need : small) * sizeof(float4);
@@ -269,9 +292,8 @@ static af_status candidate_gemm(af_ctx* ctx, const void* hidden, const void* W, 
   const Operand Wop{W, (uint64_t)V, (uint64_t)d, (uint64_t)d * 2};
   GemmEnv env = unpaced_if_cached(gemm_env(ctx), Hop, Wop);
   if (T <= umma::kPairBM) env.tile_clock = nullptr;   // one row tile: every pair reads its own part of W, none shares
-  const int n_tiles = (V + umma::kBN - 1) / umma::kBN;
-  int S = candidate_pick_splits(ctx, T, d, V);
-  if (S > n_tiles) S = n_tiles;
+  const CandidateTiling tiling = candidate_tiling(ctx, T, d, V, z != nullptr);
+  const int S = tiling.splits;
   *parts = 2 * S;
   af_status st = ws_grow(ctx->partial, (size_t)*parts * (size_t)T * sizeof(float4));
   if (st != AF_OK) return st;
@@ -281,6 +303,7 @@ static af_status candidate_gemm(af_ctx* ctx, const void* hidden, const void* W, 
     return run_gemm_promoted<CandidateEpi<true>, kPromoteBlocks>(env, Hop, Wop, S, ep, s);
   }
   CandidateEpi<false>::Params ep{keys, cand_z, partial, nullptr, (int)T, V, K, *parts};
+  if (tiling.single) return run_gemm_promoted_single<CandidateEpi<false>, kPromoteBlocks>(env, Hop, Wop, S, tiling.bn, ep, s);
   return run_gemm_promoted<CandidateEpi<false>, kPromoteBlocks>(env, Hop, Wop, S, ep, s);
 }
 

@@ -224,7 +224,6 @@ struct HeadGradient {       // where the gradient of the LM head goes
   int32_t type;             // AF_F32 or AF_BF16
   bool accumulate;          // add to d_W (AF_F32 only)
 };
-int candidate_pick_splits(const af_ctx* ctx, int64_t T, int32_t d, int32_t V);
 af_status reserve_candidate_logprob(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d, int32_t V);
 af_status launch_candidate_logprob(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand, int64_t T,
                                    int32_t K, int32_t d, int32_t V, float* cand_logp, float* entropy, float* lse,

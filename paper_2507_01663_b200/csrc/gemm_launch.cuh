@@ -58,6 +58,7 @@ inline umma::GemmShape gemm_shape(uint64_t M, uint64_t N, uint64_t K, int splits
   g.die0_pairs = 0;
   g.die0_rows = 0;
   g.k_parts = 1;
+  g.bn = umma::kBN;
   return g;
 }
 // Die-aware dealing of a pair launch: only when every SM pair gets a CTA pair and it costs no extra
@@ -165,6 +166,27 @@ af_status run_gemm_promoted(const GemmEnv& env, const Operand& A, const Operand&
   return launch_overlapped(umma::gemm_pair_kernel<E, false, false, kPromote>, grid, umma::kPromoteThreads, smem, s, ta, tb, g,
                            ep, env.d_err, clock, by_die ? clock + 1 : nullptr, env.die_of_sm) == cudaSuccess
              ? AF_OK : AF_ERR_CUDA;
+}
+
+// The same on single CTAs with tiles of 128 rows and `bn` columns (a multiple of 16, up to 256), one unit per tile range.
+template <class E, int kPromote>
+af_status run_gemm_promoted_single(const GemmEnv& env, const Operand& A, const Operand& B, int splits, int bn,
+                                   const typename E::Params& ep, cudaStream_t s) {
+  CUtensorMap ta, tb;
+  af_status st = encode_operand(env, &ta, A, umma::kBM);
+  if (st != AF_OK) return st;
+  st = encode_operand(env, &tb, B, (uint32_t)bn);
+  if (st != AF_OK) return st;
+  umma::GemmShape g = gemm_shape(A.rows, B.rows, A.cols, splits, false);
+  g.bn = bn;
+  g.n_tiles = (int)((B.rows + bn - 1) / bn);
+  g.splits = splits > 0 && splits < g.n_tiles ? splits : g.n_tiles;
+  const int64_t units = (int64_t)g.m_tiles * g.splits;
+  static SmemAttrOnce once;
+  if (set_smem_once(once, umma::gemm_kernel<E, false, false, kPromote>, umma::kSmemBytes) != cudaSuccess) return AF_ERR_CUDA;
+  const int grid = (int)(units < env.sm_count ? units : env.sm_count);
+  return launch_overlapped(umma::gemm_kernel<E, false, false, kPromote>, grid, umma::kPromoteThreads, umma::kSmemBytes, s, ta, tb,
+                           g, ep, env.d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
 // The product with its reduction cut into k_parts ranges: a unit is one tile times one range, and E stores fp32

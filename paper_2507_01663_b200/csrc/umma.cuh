@@ -205,9 +205,52 @@ struct GemmShape {
   int die0_pairs;       // pair kernel only: > 0 = deal the row tiles by die; the number of CTA pairs the first die hosts
   int die0_rows;        // ... and the number of row tiles (the first ones) those pairs share among themselves
   int k_parts;          // pair kernel with kSplitK only: parts the reduction is cut into; `splits` is then n_tiles * k_parts
+  int bn;               // gemm_kernel with kPromote only: columns of a tile, a multiple of 16 up to kBN
 };
 __device__ __forceinline__ int split_begin(const GemmShape& g, int s) {
   return (int)(((long long)g.n_tiles * s) / g.splits);
+}
+
+// Promoted accumulation.  The tensor core does not round its fp32 accumulator to nearest: every K = 16
+// step drops the bits below the accumulator's last place, so a logit of 13 after 224 steps (d = 3584)
+// comes out 1e-5 .. 5e-5 too small, always in the same direction.  A softmax over 1.5e5 such logits
+// inherits the bias (measured against 64 bits: lse -3.3e-5, entropy 2.4e-5 relative), which is nothing
+// for a policy loss held to 2e-3 but more than fp32 outputs are expected to be off by.  With kPromote > 0
+// the K loop is cut into parts of kPromote K blocks, each accumulated from zero in one of the two
+// tensor-memory accumulators, and the epilogue threads add the parts up in registers, rounding to
+// nearest: the truncation then acts on values `parts` times smaller.  Eight epilogue warps instead of
+// four share the 256 columns, so a thread holds 128 running sums; adding a part up takes a fraction of
+// the time the MMAs need for the next one and is hidden behind it.
+constexpr int kPromoteCols = kBN / 2;                         // columns per epilogue thread
+constexpr int kPromoteThreads = 64 + 256;                     // producer and MMA warps, eight epilogue warps
+
+// The epilogue's side of one tile: adds its parts up in `a` as the MMA warp publishes them.  t_row: this warp's lanes and
+// first column in accumulator 0; tfull0: barrier of accumulator 0; release(acc): one arrival per warp on the
+// accumulator's "empty" barrier.  False if a wait ran out of time.
+template <class Release>
+__device__ __forceinline__ bool promote_parts(float (&a)[kPromoteCols], int parts, uint32_t& part_count, uint32_t t_row,
+                                              uint32_t tfull0, volatile int* abort_flag, Release release) {
+#pragma unroll
+  for (int j = 0; j < kPromoteCols; ++j) a[j] = 0.f;
+  for (int p = 0; p < parts; ++p, ++part_count) {
+    const uint32_t acc = part_count & 1u, acc_phase = (part_count >> 1) & 1u;
+    if (!__all_sync(0xffffffffu, mbar_wait(tfull0 + 8u * acc, acc_phase, abort_flag))) return false;
+    tc_fence_after();
+    // 16 columns at a time, the next 16 on their way while these are added
+    uint32_t v[2][16];
+    tmem_ld16(t_row + acc * kBN, v[0]);
+#pragma unroll
+    for (int c = 0; c < kPromoteCols / 16; ++c) {
+      tmem_ld_wait();
+      if (c + 1 < kPromoteCols / 16) tmem_ld16(t_row + acc * kBN + (c + 1) * 16, v[(c + 1) & 1]);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) a[c * 16 + j] += __uint_as_float(v[c & 1][j]);
+    }
+    tc_fence_before();
+    __syncwarp();
+    release(acc);
+  }
+  return true;
 }
 
 // The epilogue functor E provides:
@@ -220,8 +263,11 @@ __device__ __forceinline__ int split_begin(const GemmShape& g, int s) {
 //           the warp's private kEpiStageBytes of shared memory (kStaged only, else null), used to
 //           turn row-per-lane data into coalesced global stores.
 //   static __device__ void unit_end(State&, const Params&, int row, int split);
-template <class E, bool kAMN = false, bool kBMN = false>
-__global__ void __launch_bounds__(kThreads, 1)
+//
+// kPromote > 0: promoted accumulation, see the CTA-pair variant below for what it is and for the form of the functor.
+// The tile may then be narrower than 256 columns (g.bn, a multiple of 16).
+template <class E, bool kAMN = false, bool kBMN = false, int kPromote = 0>
+__global__ void __launch_bounds__(kPromote > 0 ? kPromoteThreads : kThreads, 1)
 gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
             const GemmShape g, const typename E::Params ep, unsigned int* d_err) {
   extern __shared__ uint8_t smem_raw[];
@@ -240,10 +286,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
   __shared__ int abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int bn = kPromote > 0 ? g.bn : kBN;
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), kEpiThreads); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), kPromote > 0 ? 8 : kEpiThreads); }
     fence_mbar_init();
     tma_prefetch_desc(&tmap_a);
     tma_prefetch_desc(&tmap_b);
@@ -252,6 +299,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
     tmem_alloc(tmem_slot, kTmemCols);
     tmem_relinquish();
   }
+  wait_for_predecessor();   // from here on operands and the epilogue's inputs are read
+  let_successor_start();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -270,7 +319,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
           for (int kb = 0; kb < g.k_blocks; ++kb) {
             if (!mbar_wait(empty_bar(stage), phase ^ 1u, &abort_flag)) { ok = false; break; }
             const uint32_t a_dst = tiles + stage * kStageBytes;
-            mbar_arrive_expect_tx(full_bar(stage), kStageBytes);
+            mbar_arrive_expect_tx(full_bar(stage), kPromote > 0 ? kABytes + bn * kBK * 2 : kStageBytes);
             if constexpr (kAMN) {
 #pragma unroll
               for (int b = 0; b < kBM / 64; ++b)
@@ -283,7 +332,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
               for (int b = 0; b < kBN / 64; ++b)
                 tma_load_2d(a_dst + kABytes + b * kMnBoxBytes, &tmap_b, full_bar(stage), nt * kBN + b * 64, kb * kBK);
             } else {
-              tma_load_2d(a_dst + kABytes, &tmap_b, full_bar(stage), kb * kBK, nt * kBN);
+              tma_load_2d(a_dst + kABytes, &tmap_b, full_bar(stage), kb * kBK, nt * bn);
             }
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
@@ -294,7 +343,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (lane == 0) {
-      constexpr uint32_t idesc = instr_desc_bf16_f32(kBM, kBN, kAMN, kBMN);
+      const uint32_t idesc = instr_desc_bf16_f32(kBM, bn, kAMN, kBMN);
       // descriptor advance per K = 16 step, in 16-byte units: 32 bytes inside a swizzled K-major
       // row, two 8-row groups (2048 bytes) for an MN-major tile
       constexpr uint64_t a_step = kAMN ? (2048 >> 4) : 2, b_step = kBMN ? (2048 >> 4) : 2;
@@ -303,11 +352,23 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         const int s = u % g.splits;
         const int nb = split_begin(g, s), ne = split_begin(g, s + 1);
         for (int nt = nb; nt < ne && ok; ++nt, ++tile_count) {
-          const uint32_t acc = tile_count & 1u, acc_phase = (tile_count >> 1) & 1u;
+          uint32_t acc = tile_count & 1u, acc_phase = (tile_count >> 1) & 1u;
           if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, &abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t d_tmem = tmem_base + acc * kBN;
+          uint32_t d_tmem = tmem_base + acc * kBN;
+          int part_kb = 0;                               // K blocks in the current part (kPromote > 0)
           for (int kb = 0; kb < g.k_blocks; ++kb) {
+            if constexpr (kPromote > 0) {
+              if (part_kb == kPromote) {                 // next part: publish this one, take the other accumulator
+                mma_commit(tfull_bar(acc));
+                ++tile_count;                            // counts parts here
+                acc = tile_count & 1u; acc_phase = (tile_count >> 1) & 1u;
+                if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, &abort_flag)) { ok = false; break; }
+                tc_fence_after();
+                d_tmem = tmem_base + acc * kBN;
+                part_kb = 0;
+              }
+            }
             if (!mbar_wait(full_bar(stage), phase, &abort_flag)) { ok = false; break; }
             tc_fence_after();
             const uint32_t a_addr = tiles + stage * kStageBytes;
@@ -316,9 +377,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
 #pragma unroll
             for (int k = 0; k < kBK / kUmmaK; ++k) {
               mma_bf16_ss(d_tmem, a_desc + (uint64_t)k * a_step, b_desc + (uint64_t)k * b_step, idesc,
-                          (kb | k) != 0 ? 1u : 0u);
+                          ((kPromote > 0 ? part_kb : kb) | k) != 0 ? 1u : 0u);
             }
             mma_commit(empty_bar(stage));  // smem slot reusable once these MMAs have read it
+            ++part_kb;
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
           }
           if (ok) mma_commit(tfull_bar(acc));  // accumulator complete
@@ -326,6 +388,27 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       }
     }
     __syncwarp();
+  } else if constexpr (kPromote > 0) {
+    // ------------------------------------------------------- epilogue, promoted accumulation (warps 2..9)
+    const int quarter = warp & 3, half = (warp - 2) >> 2;         // TMEM lanes this warp may touch; its column half
+    const int parts = (g.k_blocks + kPromote - 1) / kPromote;
+    const int left = (bn / 2 + 15) / 16 * 16;                     // columns of the first half: loads start at multiples of 16
+    const int first = half * left, cols = half ? bn - left : left;
+    uint32_t part_count = 0; bool ok = true;
+    typename E::State st;
+    for (int u = blockIdx.x; u < total_units && ok; u += gridDim.x) {
+      const int m_tile = u / g.splits, s = u % g.splits;
+      const int nb = split_begin(g, s), ne = split_begin(g, s + 1);
+      const int row = m_tile * kBM + quarter * 32 + lane;
+      E::unit_begin(st, ep, row, nb * bn);
+      for (int nt = nb; nt < ne && ok; ++nt) {
+        float a[kPromoteCols];
+        ok = promote_parts(a, parts, part_count, tmem_base + ((uint32_t)(quarter * 32) << 16) + first, tfull_bar(0),
+                           &abort_flag, [&](uint32_t acc) { if (lane == 0) mbar_arrive(tempty_bar(acc)); });
+        if (ok) E::tile(st, ep, row, nt * bn + first, cols, a, nullptr);
+      }
+      if (ok) E::unit_end(st, ep, row, 2 * s + half);
+    }
   } else {
     // ---------------------------------------------------------------- epilogue (warps 2..5)
     const int quarter = warp & 3;                       // TMEM lanes this warp may touch
@@ -399,19 +482,6 @@ constexpr int kPairBBytes = (kBN / 2) * kBK * 2;              // this CTA's half
 constexpr int kPairStageBytes = kABytes + kPairBBytes;        // 32 KB
 constexpr int kPairSmemBytes = kPairStages * kPairStageBytes + 1024 /*alignment slack*/ + 256 /*barriers*/;
 constexpr int kPairSmemBytesStaged = kPairSmemBytes + 4 * kEpiStageBytes;
-
-// Promoted accumulation.  The tensor core does not round its fp32 accumulator to nearest: every K = 16
-// step drops the bits below the accumulator's last place, so a logit of 13 after 224 steps (d = 3584)
-// comes out 1e-5 .. 5e-5 too small, always in the same direction.  A softmax over 1.5e5 such logits
-// inherits the bias (measured against 64 bits: lse -3.3e-5, entropy 2.4e-5 relative), which is nothing
-// for a policy loss held to 2e-3 but more than fp32 outputs are expected to be off by.  With kPromote > 0
-// the K loop is cut into parts of kPromote K blocks, each accumulated from zero in one of the two
-// tensor-memory accumulators, and the epilogue threads add the parts up in registers, rounding to
-// nearest: the truncation then acts on values `parts` times smaller.  Eight epilogue warps instead of
-// four share the 256 columns, so a thread holds 128 running sums; adding a part up takes a fraction of
-// the time the MMAs need for the next one and is hidden behind it.
-constexpr int kPromoteCols = kBN / 2;                         // columns per epilogue thread
-constexpr int kPromoteThreads = 64 + 256;                     // producer and MMA warps, eight epilogue warps
 constexpr int kPromoteSmemBytesStaged = kPairSmemBytes + 8 * kEpiStageBytes;
 
 __device__ __forceinline__ uint32_t cluster_ctarank() {
@@ -511,8 +581,9 @@ __device__ __forceinline__ int pair_work_most(const GemmShape& g, int n_pairs) {
 // tile's columns:
 //   static __device__ void unit_begin(State&, const Params&, int row, int col0);   col0: first column of the unit
 //   static constexpr bool kStaged;
-//   static __device__ void tile(State&, const Params&, int row, int col0, float (&a)[kPromoteCols], uint8_t* stage);
-//        -- called by all 32 lanes of a warp together; stage: the warp's private kEpiStageBytes (kStaged only)
+//   static __device__ void tile(State&, const Params&, int row, int col0, int cols, float (&a)[kPromoteCols], uint8_t* stage);
+//        -- the first `cols` values are the thread's; called by all 32 lanes of a warp together; stage: the warp's
+//           private kEpiStageBytes (kStaged only)
 //   static __device__ void unit_end(State&, const Params&, int row, int part);     part = 2 * split + column half
 //
 // kSplitK: a unit is one tile times one of k_parts ranges of K blocks, for products with few tiles and a long
@@ -746,28 +817,10 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
       E::unit_begin(st, ep, row, nb * kBN);
       for (int nt = nb; nt < ne && ok; ++nt) {
         float a[kPromoteCols];
-#pragma unroll
-        for (int j = 0; j < kPromoteCols; ++j) a[j] = 0.f;
-        for (int p = 0; p < parts; ++p, ++part_count) {
-          const uint32_t acc = part_count & 1u, acc_phase = (part_count >> 1) & 1u;
-          if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, &abort_flag))) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * kBN + half * kPromoteCols;
-          // 16 columns at a time, the next 16 on their way while these are added
-          uint32_t v[2][16];
-          tmem_ld16(t_row, v[0]);
-#pragma unroll
-          for (int c = 0; c < kPromoteCols / 16; ++c) {
-            tmem_ld_wait();
-            if (c + 1 < kPromoteCols / 16) tmem_ld16(t_row + (c + 1) * 16, v[(c + 1) & 1]);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) a[c * 16 + j] += __uint_as_float(v[c & 1][j]);
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(tempty_bar(acc), 0);   // one arrival per warp, on the leader
-        }
-        if (ok) E::tile(st, ep, row, nt * kBN + half * kPromoteCols, a, stage);
+        ok = promote_parts(a, parts, part_count, tmem_base + ((uint32_t)(quarter * 32) << 16) + half * kPromoteCols,
+                           tfull_bar(0), &abort_flag,
+                           [&](uint32_t acc) { if (lane == 0) mbar_arrive_cluster(tempty_bar(acc), 0); });   // on the leader
+        if (ok) E::tile(st, ep, row, nt * kBN + half * kPromoteCols, kPromoteCols, a, stage);
       }
       if (ok) E::unit_end(st, ep, row, 2 * s + half);
     }

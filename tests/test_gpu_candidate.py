@@ -44,7 +44,8 @@ def check_scores(H, W, cand, got):
 
 SHAPES = [(1, 8, 1, 1), (1, 256, 4096, 20), (2, 24, 129, 2), (5, 64, 127, 3), (37, 128, 300, 31), (64, 264, 1000, 32),
           (255, 256, 4104, 33), (256, 640, 520, 64), (257, 320, 8200, 65), (300, 192, 2051, 128), (70, 512, 4099, 129),
-          (513, 1000, 777, 256)]
+          (513, 1000, 777, 256), (100, 64, 30000, 40), (33, 72, 45001, 7), (128, 136, 20011, 12), (129, 64, 20011, 12),
+          (9, 200, 5003, 30), (16, 4096, 300, 9), (8, 6144, 200, 5), (17, 8, 700, 3)]
 
 
 @pytest.mark.parametrize("T,d,V,K", SHAPES)
