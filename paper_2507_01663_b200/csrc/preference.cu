@@ -8,10 +8,11 @@
 // grid barrier after the first and the second phase:
 //   1. sums    a warp walks a range in steps of 512 tokens, eight per lane at a time, each lane adding up its tokens of the
 //              current sequence and the warp joining them when the sequence or the range ends.  The next steps come
-//              by bulk copies into a ring of the warp's own, so nothing waits on another warp, and the border of the
-//              sequence after the next is fetched ahead, so nothing waits on cu_seqlens either.  A sequence inside one
+//              by bulk copies into a ring of the warp's own, so nothing waits on another warp.  A sequence inside one
 //              range is done; one that crosses ranges leaves a piece in each, at most one coming in (head) and one
-//              going out (tail), so pieces need no counters and no atomics.
+//              going out (tail), so pieces need no counters and no atomics.  Where
+//              sequences end inside a slice, running sums that start anew at every border are taken over it, and a
+//              lane per sequence reads the one at its end: the cost is that of a few reductions however many end.
 //   2. pairs   a few lanes per pair add the pieces, evaluate the loss and write the two sequences' coefficients.
 //   3. fill    the same ranges again: the coefficient of each token's sequence.
 // All sums are fp64 (thousands of near-cancelling terms, and the card has the rate: two additions per token)
@@ -19,6 +20,8 @@
 #include "common.cuh"
 #include "device_util.cuh"
 #include "umma.cuh"
+
+#include <climits>
 
 namespace af {
 namespace {
@@ -92,48 +95,74 @@ __device__ __forceinline__ void load_slice(const float* __restrict__ p, uint32_t
   }
 }
 
-// A warp's place in the list of sequences, with the next border (and coefficient) already on its way.  Uniform over
-// the warp; every loop over it ends whatever cu holds.
+// A warp's place in the list of sequences.  Uniform over the warp.
 struct Place {
   const int32_t* __restrict__ cu;
   const float* coef;                // null in the first phase
-  int B, lane;
-  int j, beg, end, next_end;
-  float c, next_c;
-  __device__ __forceinline__ void ahead() {
-    next_end = j + 2 <= B ? __ldg(cu + j + 2) : end;
-    if (coef) next_c = j + 1 < B ? __ldcg(coef + j + 1) : 0.f;
-  }
-  __device__ __forceinline__ void find(int t) {
-    j = find_seq_warp(cu, B, t, lane);
+  int j, beg, end;
+  float c;
+  __device__ __forceinline__ void set(int i) {                       // i in [0, B)
+    j = i;
     beg = __ldg(cu + j);
     end = __ldg(cu + j + 1);
     if (coef) c = __ldcg(coef + j);
-    ahead();
-  }
-  __device__ __forceinline__ void advance(int t) {                   // to the next non-empty sequence, which holds t
-    if (j + 1 >= B) return;
-    ++j;
-    beg = end;
-    end = next_end;
-    if (coef) c = next_c;
-    if (end <= t) find(t);                                           // a pile of empty sequences
-    else ahead();
   }
 };
 
-// Calls f(place) for every non-empty sequence that meets tokens [base, last), `at` holding token base; leaves `at`
-// at the sequence of token `last` if there is one.
-template <class F>
-__device__ __forceinline__ void over_sequences(Place& at, int T, int base, int last, F f) {
-  int t = base;
+// Marks in bits (8 words of the warp's) where sequences start in (base, last), from the one after j on; start(i, p) is
+// called by one lane for each such sequence that is not empty, p its place in the slice.  Returns how many sequences
+// from j on end at or before last.
+template <class Start>
+__device__ __forceinline__ int mark_starts(const int32_t* __restrict__ cu, int B, int j, int base, int last,
+                                           uint32_t* bits, int lane, Start start) {
+  if (lane < kSlice / 32) bits[lane] = 0u;
+  __syncwarp();
+  int ended = 0;
   for (;;) {
-    f(at);
-    if (at.end >= last || at.end <= t || at.j + 1 >= at.B) break;
-    t = at.end;
-    at.advance(t);
+    const int i = j + ended + lane + 1;
+    const int beg = i <= B ? __ldg(cu + i) : INT_MAX;
+    if (beg > base && beg < last) {
+      const int end = i < B ? __ldg(cu + i + 1) : beg;
+      atomicOr(bits + ((beg - base) >> 5), 1u << ((beg - base) & 31));
+      if (end > beg) start(i, beg - base);
+    }
+    const unsigned on = __ballot_sync(0xffffffffu, beg > last);
+    ended += on ? __ffs(on) - 1 : 32;
+    if (on) break;                                 // at the latest behind cu[B]
   }
-  if (at.end <= last && last < T) at.advance(last);
+  __syncwarp();
+  return ended;
+}
+// The lane's four marks of group q.
+__device__ __forceinline__ unsigned marks_of(const uint32_t* bits, int q, int lane) {
+  return (bits[q * 4 + (lane >> 3)] >> ((lane & 7) * 4)) & 15u;
+}
+
+// Running sums of a slice's values in token order, each from the last mark on; `sum` is what came in and what goes on.
+// A sum takes its own sequence's values only, so that an infinity or a NaN stays with its sequence.
+__device__ __forceinline__ void running_sums(const double (&v)[8], const unsigned (&marks)[2], int lane, double& sum,
+                                             double (&at)[8]) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    double own = lane == 0 ? sum : 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      own = marks[q] >> i & 1u ? v[4 * q + i] : own + v[4 * q + i];
+      at[4 * q + i] = own;
+    }
+    const unsigned before = __ballot_sync(0xffffffffu, marks[q] != 0u) & (0xffffffffu >> (31 - lane));
+    const int back = before ? lane - (31 - __clz(before)) : lane;       // lanes since the last one with a mark
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double x = __shfl_up_sync(0xffffffffu, own, o);
+      if (o <= back) own += x;
+    }
+    const double in = __shfl_up_sync(0xffffffffu, own, 1);
+    const int stop = marks[q] ? __ffs(marks[q]) - 1 : 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (lane > 0 && i < stop) at[4 * q + i] += in;
+    sum = __shfl_sync(0xffffffffu, own, 31);
+  }
 }
 
 __device__ __forceinline__ void warp_sums(double& s, double& l, bool both) {
@@ -147,8 +176,8 @@ __device__ __forceinline__ void warp_sums(double& s, double& l, bool both) {
 // Phase 1 over the steps [s0, s1) of worker `me`.  ring: the warp's stages, bars: their barriers.
 __device__ __forceinline__ void sum_steps(const float* __restrict__ logp, const float* __restrict__ ref,
                                           const int32_t* __restrict__ cu, int B, int T, const PrefWs& ws, bool bulk,
-                                          int me, int s0, int s1, uint32_t ring, uint32_t bars, int lane,
-                                          volatile int* abort_flag) {
+                                          int me, int s0, int s1, uint32_t ring, uint32_t bars, uint32_t* bits,
+                                          int lane, volatile int* abort_flag) {
   if (s0 >= s1) return;
   const bool both = ref != nullptr;
   auto issue = [&](int it) {                       // lane 0; a step is copied up to its last whole group of 4 tokens
@@ -164,15 +193,9 @@ __device__ __forceinline__ void sum_steps(const float* __restrict__ logp, const 
   if (lane == 0)
     for (int it = 0; it < kStages && s0 + it < s1; ++it) issue(it);
   const int range_beg = s0 * kStep;
-  Place at{cu, nullptr, B, lane};
-  at.find(range_beg);
+  Place at{cu, nullptr};
+  at.set(find_seq_warp(cu, B, range_beg, lane));
   double s = 0.0, l = 0.0;                         // the lane's share of the current sequence
-  auto leave = [&](double2* where) {
-    warp_sums(s, l, both);
-    if (lane == 0) *where = make_double2(both ? s : l, l);
-    s = 0.0;
-    l = 0.0;
-  };
   int last = range_beg;
   for (int step = s0; step < s1; ++step) {
     const int it = step - s0;
@@ -217,32 +240,52 @@ __device__ __forceinline__ void sum_steps(const float* __restrict__ logp, const 
         add_all();
         continue;
       }
-      over_sequences(at, T, base, last, [&](const Place& q) {
-        if (q.beg <= base && q.end >= last) {
-          add_all();
-        } else {
+      // sequences end in here: running sums over the slice, and a lane per sequence reads the one at its end
+      const int ended = mark_starts(cu, B, at.j, base, last, bits, lane, [](int, int) {});
+      const unsigned marks[2] = {marks_of(bits, 0, lane), marks_of(bits, 1, lane)};
+      warp_sums(s, l, both);                       // of the first one, from earlier slices
+#pragma unroll 1
+      for (int column = both ? 0 : 1; column < 2; ++column) {
+        double v[8], run[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int t = slot_token(base, lane, i);
-            if (t >= q.beg && t < q.end) {
-              l += (double)lp[i];
-              if (both) s += (double)lp[i] - (double)rf[i];
-            }
+        for (int i = 0; i < 8; ++i) v[i] = column == 0 ? (double)lp[i] - (double)rf[i] : (double)lp[i];
+        double sum = column == 0 ? s : l;
+        running_sums(v, marks, lane, sum, run);
+        for (int done = 0; done < ended; done += 32) {
+          const int i = at.j + done + lane;        // below B where it counts
+          const bool mine = done + lane < ended;
+          const int beg = mine ? __ldg(cu + i) : 0, end = mine ? __ldg(cu + i + 1) : 0;
+          const int x = (end - 1 - base) & (kSlice - 1), slot = (x >> 7) * 4 + (x & 3);
+          double r = 0.0;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const double y = __shfl_sync(0xffffffffu, run[k], (x & 127) >> 2);
+            if (slot == k) r = y;
+          }
+          if (mine && end > beg) {
+            double2* const to = beg < range_beg ? ws.head + me : ws.seq + i;
+            if (column == 0) to->x = r; else to->y = r;
+            if (!both) to->x = r;
           }
         }
-        if (q.end <= last) leave(q.beg >= range_beg ? ws.seq + q.j : ws.head + me);
-      });
+        if (column == 0) s = sum; else l = sum;
+      }
+      at.set(at.j + ended < B ? at.j + ended : B - 1);
+      if (lane > 0 || at.beg >= last) { s = 0.0; l = 0.0; }             // else the sum so far of what goes on
     }
   }
-  if (at.beg < last && at.end > last) leave(at.beg >= range_beg ? ws.tail + me : ws.head + me);
+  if (at.beg < last && at.end > last) {
+    warp_sums(s, l, both);
+    if (lane == 0) (at.beg >= range_beg ? ws.tail : ws.head)[me] = make_double2(both ? s : l, l);
+  }
 }
 
 // Phase 3 over the steps [s0, s1).
 __device__ __forceinline__ void fill_steps(const int32_t* __restrict__ cu, int B, int T, const PrefWs& ws, float* dlogp,
-                                           bool vec, int s0, int s1, int lane) {
+                                           bool vec, int s0, int s1, uint32_t* bits, float* coefs, int lane) {
   if (s0 >= s1) return;
-  Place at{cu, ws.coef, B, lane};
-  at.find(s0 * kStep);
+  Place at{cu, ws.coef};
+  at.set(find_seq_warp(cu, B, s0 * kStep, lane));
   const int end = s1 * (int64_t)kStep < T ? s1 * kStep : T;
   for (int base = s0 * kStep; base < end; base += kSlice) {
     const int last = T - base < kSlice ? T : base + kSlice;
@@ -253,24 +296,35 @@ __device__ __forceinline__ void fill_steps(const int32_t* __restrict__ cu, int B
       __stcs(reinterpret_cast<float4*>(out + 128), v);
       continue;
     }
-    float g[8] = {};
-    over_sequences(at, T, base, last, [&](const Place& q) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int t = slot_token(base, lane, i);
-        if (t >= q.beg && t < q.end) g[i] = q.c;
-      }
-    });
+    // coefficients at the places where sequences start; a token's is the one at the last start before it
+    const int ended = mark_starts(cu, B, at.j, base, last, bits, lane,
+                                  [&](int i, int p) { coefs[p] = __ldcg(ws.coef + i); });
+    int came_in = -1;                              // the last start in earlier groups
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const int t = slot_token(base, lane, 4 * q);
+      const unsigned marks = marks_of(bits, q, lane);
+      const unsigned with = __ballot_sync(0xffffffffu, marks != 0u), before = with & ((1u << lane) - 1u);
+      const int newest = t - base + 31 - __clz(marks | 1u);             // counts where marks is not 0
+      const int left = __shfl_sync(0xffffffffu, newest, before ? 31 - __clz(before) : lane);
+      const int from = before ? left : came_in;
+      const int final = __shfl_sync(0xffffffffu, newest, with ? 31 - __clz(with) : 0);
+      float c = from >= 0 ? coefs[from] : at.c, g[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (marks >> i & 1u) c = coefs[t - base + i];
+        g[i] = c;
+      }
+      if (with) came_in = final;
       if (vec && t + 4 <= T) {
-        __stcs(reinterpret_cast<float4*>(out + q * 128), make_float4(g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]));
+        __stcs(reinterpret_cast<float4*>(out + q * 128), make_float4(g[0], g[1], g[2], g[3]));
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) if (t + i < T) dlogp[t + i] = g[4 * q + i];
+        for (int i = 0; i < 4; ++i) if (t + i < T) dlogp[t + i] = g[i];
       }
     }
+    __syncwarp();                                  // coefs and bits are read
+    at.set(at.j + ended < B ? at.j + ended : B - 1);
   }
 }
 
@@ -379,6 +433,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) preference_kernel(
     float* __restrict__ seq_score, float* __restrict__ dlogp, int vec, int wide_pairs, unsigned int* d_err) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ int abort_flag;
+  __shared__ uint32_t bits[kWarps][kSlice / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int P = B / 2;
   const uint32_t smem = (umma::smem_u32(smem_raw) + 127u) & ~127u;
@@ -395,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) preference_kernel(
   const int per = steps > workers ? (steps + workers - 1) / workers : 1;       // steps of a range
   const int s0 = (int64_t)me * per < steps ? me * per : steps, s1 = steps - s0 < per ? steps : s0 + per;
 
-  sum_steps(logp, ref, cu, B, T, ws, vec & 1, me, s0, s1, ring, bars, lane, &abort_flag);
+  sum_steps(logp, ref, cu, B, T, ws, vec & 1, me, s0, s1, ring, bars, bits[warp], lane, &abort_flag);
   for (int q = blockIdx.x * kThreads + threadIdx.x; q < B; q += gridDim.x * kThreads)
     if (__ldg(cu + q) > __ldg(cu + q + 1)) atomicOr(d_err, AF_DEVERR_CU_SEQLENS);
   bool ok = grid_barrier(ws.header, gridDim.x);
@@ -419,7 +474,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) preference_kernel(
     ws.partial[(size_t)blockIdx.x * kNumSums + threadIdx.x] = t;
   }
   ok = grid_barrier(ws.header, 2 * gridDim.x) && ok;
-  if (ok && dlogp) fill_steps(cu, B, T, ws, dlogp, (vec & 2) != 0, s0, s1, lane);
+  if (ok && dlogp) fill_steps(cu, B, T, ws, dlogp, (vec & 2) != 0, s0, s1, bits[warp],
+                               reinterpret_cast<float*>(smem_raw + (ring - umma::smem_u32(smem_raw))), lane);
   if (ok && blockIdx.x == 0 && warp < kNumSums) {      // the record: a warp per sum, the blocks in a fixed order
     double t = 0.0;
     for (int b = lane; b < (int)gridDim.x; b += 32) t += __ldcg(ws.partial + (size_t)b * kNumSums + warp);

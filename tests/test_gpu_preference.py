@@ -140,6 +140,27 @@ def test_extremes(ctx):
     assert np.isfinite(g[2:]).all() and pair[2] == pytest.approx(math.log(2.0))
 
 
+def test_infinities_stay_in_their_own_short_sequence(ctx):
+    """Sequences of 0 to 9 tokens, some with an infinity, a NaN or 1e30: the others are as if those were not there."""
+    rng = np.random.default_rng(12)
+    lengths = rng.integers(0, 10, 4000)
+    cu = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    T = int(cu[-1])
+    logp = (-2.0 * rng.random(T)).astype(np.float32)
+    ref = (logp + 0.2 * rng.standard_normal(T)).astype(np.float32)
+    spoilt = logp.copy()
+    at = rng.choice(T, 300, replace=False)
+    spoilt[at] = rng.choice(np.array([np.nan, -np.inf, -1e30], np.float32), 300)
+    hit = np.zeros(2000, bool)
+    hit[(np.searchsorted(cu, at, side="right") - 1) // 2] = True
+    a, b = call(ctx, logp, ref, cu), call(ctx, spoilt, ref, cu)
+    check(logp, ref, cu, a)
+    assert 100 < hit.sum() < 500 and np.array_equal(a[1][~hit], b[1][~hit])
+    assert np.array_equal(a[2].reshape(-1, 2)[~hit], b[2].reshape(-1, 2)[~hit])
+    token = np.repeat(~hit, lengths.reshape(-1, 2).sum(1))
+    assert np.array_equal(a[3][token], b[3][token])
+
+
 def test_long_batch_against_float64_sums(ctx):
     """2^26 tokens in sequences of very uneven length."""
     from paper_2507_01663_b200 import binding as B
