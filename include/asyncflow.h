@@ -24,8 +24,9 @@
  *     with the largest sizes to keep allocation out of the hot calls.
  *   - Stream capture: once af_reserve has covered the sizes (and the tuning is unchanged), every
  *     call except af_pack_microbatch, af_unpack_microbatch, af_check_device_errors, af_reserve (and its
- *     kin af_reserve_candidates and af_reserve_preference) and af_destroy issues only kernel launches and asynchronous memsets on `stream`, so a sequence
- *     of them may be recorded into a CUDA graph and replayed on new contents of the same buffers.
+ *     kin af_reserve_candidates and af_reserve_preference) and af_destroy issues only kernel launches and
+ *     asynchronous memsets on `stream`, so a sequence of them may be recorded into a CUDA graph and
+ *     replayed on new contents of the same buffers.
  *     af_pack_microbatch and af_unpack_microbatch build a table from their host index list (and
  *     for large batches stage it through pinned host memory, waiting on an event of their own);
  *     they are not meant to be recorded.  Nothing is claimed for
@@ -364,15 +365,18 @@ af_status af_policy_update(af_ctx* ctx, const void* hidden, const void* W, const
  * for the two products and exists for one token block only, as in af_policy_loss_backward; a
  * registered "d_W ready" event (af_set_dw_ready_event) is recorded where d_W is complete, when there
  * is a d_W.  The forward accumulates logits in parts that are added in fp32 with rounding to nearest
- * (the tensor core's own accumulation truncates): against 64 bits its log-probs are about ten times
- * closer than af_token_logprob's.  It always runs on CTA pairs; gemm_variant 1 of af_set_tuning
- * applies to the backward only, v_splits and bwd_token_block as elsewhere.
+ * (the tensor core's own accumulation truncates): at d = 3584 its log-probs are within 5e-7 of the 64-bit
+ * ones, relative, where af_token_logprob's are 3e-6 off.  How it is launched follows from T alone: one pass over W by
+ * itself for up to 16 tokens, single CTAs up to 128, CTA pairs from there on; gemm_variant 1 of
+ * af_set_tuning applies to the backward only, v_splits > 0 asks for CTA pairs with that many ranges,
+ * bwd_token_block works as elsewhere.
  *
  * hidden [T,d], W [V,d] bf16 dev, row-major, 16-byte aligned, d % 8 == 0 (backward: V % 8 == 0, d_hidden
  * and d_W 16-byte aligned too).  cand [T,K] int32, cand_logp, dcand [T,K], entropy (nullable), lse
  * (nullable in the forward) [T] fp32, dev.  1 <= K <= AF_MAX_CANDIDATES, V <= 2^24 - 256, 0 <= T < 2^31
  * (AF_ERR_SHAPE otherwise).  Workspace: 4 bytes per slot for the sorted lists (one token block of them in
- * the backward), the forward's softmax states and the backward's dZ, and 4 V d bytes behind a bf16 d_W
+ * the backward) or 4 V per token for up to 16 tokens, the forward's softmax states (16 bytes per token and
+ * range), the backward's dZ, up to 78 MB of partial sums of d_hidden, and 4 V d bytes behind a bf16 d_W
  * of more than one token block; af_reserve_candidates sizes all of it ahead.
  * ------------------------------------------------------------------------------------------- */
 #define AF_MAX_CANDIDATES 256
@@ -399,8 +403,8 @@ af_status af_reserve_candidates(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d
  *
  * lt = teacher_logp[t,k], lq = cand_logp[t,k] (from af_candidate_logprob), both over the whole
  * vocabulary.  A slot with lt = -inf is absent: its lq is not looked at and its gradient is 0 (a NaN in a
- * present slot makes its whole token NaN); a token whose slots are all absent has loss 0.  p = exp(lt), q = exp(lq); sums run over the present slots;
- * 0 log 0 = 0.
+ * present slot makes its whole token NaN); a token whose slots are all absent has loss 0.  p = exp(lt),
+ * q = exp(lq); sums run over the present slots; 0 log 0 = 0.
  *   divergence 0: from teacher to student;  1: from student to teacher.
  *   support 0 (as listed):   0: sum p (lt - lq);   1: sum q (lq - lt)
  *   support 1 (renormalised): a = softmax(lt / tau), b = softmax(lq / tau) over the present slots;
@@ -447,8 +451,7 @@ af_status af_distill_loss(af_ctx* ctx, const float* cand_logp, const float* teac
  * after the other, with the logits evaluated once per token: a token block's fp32 logits stay in
  * scratch between the log-softmax and dZ.  entropy, token_loss, dcand and d_W may be NULL; every other
  * pointer is required when T > 0.  Arguments, requirements and errors as for the three calls (d % 8 == 0,
- * V % 8 == 0).  The same token may not be scored by another teacher in the same call: lists of several
- * teachers are several calls with an accumulated fp32 d_W.
+ * V % 8 == 0).  Workspace: as for the three, and 4 V bytes per token of a block for its logits.
  * ------------------------------------------------------------------------------------------- */
 af_status af_distill_update(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand,
                             const float* teacher_logp, const int32_t* cu_seqlens, int32_t B, int64_t T,

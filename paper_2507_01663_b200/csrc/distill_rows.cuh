@@ -198,7 +198,7 @@ __device__ __forceinline__ float row_divergence(const float (&lt)[kE], const flo
       const float p_left = group_rest<kG>(ps), q_left = group_rest<kG>(qs);
       const float pr = p_left < kTailFloor ? kTailFloor : p_left, qr = q_left < kTailFloor ? kTailFloor : q_left;
       // approximate: off by 2^-22 of a ratio near 1, and weighted with the tail's mass
-      const float quot = __fdividef(pr, qr), ratio = __logf(quot);
+      const float quot = pr / qr, ratio = logf(quot);
       const float slope = q_left <= kTailFloor ? 0.f : kForward ? quot : ratio - 1.f;
 #pragma unroll
       for (int i = 0; i < kE; ++i) g[i] = fmaf(q[i], slope, g[i]);
