@@ -102,10 +102,18 @@ __device__ __forceinline__ void store_slots(float* p, const float* v) {
   else *p = v[0];
 }
 
-// Sum over the group in 64 bits of what each lane has in 32: the tail is the small difference of 1 and this.
-template <int kG>
-__device__ __forceinline__ float group_rest(float v) {
-  double x = (double)v;
+// What a distribution's listed probabilities leave of 1: a small difference, so they are added up in 64 bits, from
+// sums of four (one conversion for every slot would cost as much as the rest of the row).
+template <int kG, int kE>
+__device__ __forceinline__ float group_rest(const float (&v)[kE]) {
+  double x = 0.0;
+#pragma unroll
+  for (int i = 0; i < kE; i += 4) {
+    float four = v[i];
+#pragma unroll
+    for (int j = i + 1; j < kE && j < i + 4; ++j) four += v[j];
+    x += (double)four;
+  }
 #pragma unroll
   for (int o = kG / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return (float)(1.0 - x);
@@ -174,10 +182,11 @@ __device__ __forceinline__ float row_divergence(const float (&lt)[kE], const flo
     return tau * tau * loss;
   } else {
     float loss = 0.f, ps = 0.f, qs = 0.f;
-    float q[kE];
+    float q[kE], listed[kE];
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
       const float p = ex2f(lt[i] * kLog2e);
+      listed[i] = p;
       q[i] = ex2f(lq[i] * kLog2e);
       float gap = lt[i] - lq[i];
       ps += p;
@@ -195,7 +204,7 @@ __device__ __forceinline__ float row_divergence(const float (&lt)[kE], const flo
     sm += qs;
     if constexpr (kSupport == 2) {
       // one more outcome holds what the listed ones leave of either distribution
-      const float p_left = group_rest<kG>(ps), q_left = group_rest<kG>(qs);
+      const float p_left = group_rest<kG>(listed), q_left = group_rest<kG>(q);
       const float pr = p_left < kTailFloor ? kTailFloor : p_left, qr = q_left < kTailFloor ? kTailFloor : q_left;
       // approximate: off by 2^-22 of a ratio near 1, and weighted with the tail's mass
       const float quot = pr / qr, ratio = logf(quot);

@@ -11,7 +11,7 @@
 //              by bulk copies into a ring of the warp's own, so nothing waits on another warp.  A sequence inside one
 //              range is done; one that crosses ranges leaves a piece in each, at most one coming in (head) and one
 //              going out (tail), so pieces need no counters and no atomics.  Where
-//              sequences end inside a slice, running sums that start anew at every border are taken over it, and a
+//              several sequences end inside a slice, running sums that start anew at every border are taken over it, and a
 //              lane per sequence reads the one at its end: the cost is that of a few reductions however many end.
 //   2. pairs   a few lanes per pair add the pieces, evaluate the loss and write the two sequences' coefficients.
 //   3. fill    the same ranges again: the coefficient of each token's sequence.
@@ -95,17 +95,34 @@ __device__ __forceinline__ void load_slice(const float* __restrict__ p, uint32_t
   }
 }
 
-// A warp's place in the list of sequences.  Uniform over the warp.
+// A warp's place in the list of sequences, with the border (and coefficient) of the one after already on its way.
+// Uniform over the warp.
 struct Place {
   const int32_t* __restrict__ cu;
   const float* coef;                // null in the first phase
-  int j, beg, end;
-  float c;
+  int B;
+  int j, beg, end, next_end;
+  float c, next_c;
+  __device__ __forceinline__ void ahead() {
+    next_end = j + 2 <= B ? __ldg(cu + j + 2) : INT_MAX;
+    if (coef) next_c = j + 1 < B ? __ldcg(coef + j + 1) : 0.f;
+  }
   __device__ __forceinline__ void set(int i) {                       // i in [0, B)
     j = i;
     beg = __ldg(cu + j);
     end = __ldg(cu + j + 1);
     if (coef) c = __ldcg(coef + j);
+    ahead();
+  }
+  // Whether one sequence ends in (base, last], this one.
+  __device__ __forceinline__ bool one_border(int base, int last) const { return end > base && end <= last && next_end > last; }
+  __device__ __forceinline__ void advance() {
+    if (j + 1 >= B) return;
+    ++j;
+    beg = end;
+    end = next_end;
+    if (coef) c = next_c;
+    ahead();
   }
 };
 
@@ -193,7 +210,7 @@ __device__ __forceinline__ void sum_steps(const float* __restrict__ logp, const 
   if (lane == 0)
     for (int it = 0; it < kStages && s0 + it < s1; ++it) issue(it);
   const int range_beg = s0 * kStep;
-  Place at{cu, nullptr};
+  Place at{cu, nullptr, B};
   at.set(find_seq_warp(cu, B, range_beg, lane));
   double s = 0.0, l = 0.0;                         // the lane's share of the current sequence
   int last = range_beg;
@@ -240,7 +257,25 @@ __device__ __forceinline__ void sum_steps(const float* __restrict__ logp, const 
         add_all();
         continue;
       }
-      // sequences end in here: running sums over the slice, and a lane per sequence reads the one at its end
+      if (at.one_border(base, last)) {             // long sequences: one ends in here
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (slot_token(base, lane, i) < at.end) {
+            l += (double)lp[i];
+            if (both) s += (double)lp[i] - (double)rf[i];
+            lp[i] = 0.f;
+            if (both) rf[i] = 0.f;
+          }
+        }
+        warp_sums(s, l, both);
+        if (lane == 0) *(at.beg >= range_beg ? ws.seq + at.j : ws.head + me) = make_double2(both ? s : l, l);
+        s = 0.0;
+        l = 0.0;
+        at.advance();
+        add_all();                                 // the rest belongs to the next one
+        continue;
+      }
+      // several: running sums over the slice, and a lane per sequence reads the one at its end
       const int ended = mark_starts(cu, B, at.j, base, last, bits, lane, [](int, int) {});
       const unsigned marks[2] = {marks_of(bits, 0, lane), marks_of(bits, 1, lane)};
       warp_sums(s, l, both);                       // of the first one, from earlier slices
@@ -284,7 +319,7 @@ __device__ __forceinline__ void sum_steps(const float* __restrict__ logp, const 
 __device__ __forceinline__ void fill_steps(const int32_t* __restrict__ cu, int B, int T, const PrefWs& ws, float* dlogp,
                                            bool vec, int s0, int s1, uint32_t* bits, float* coefs, int lane) {
   if (s0 >= s1) return;
-  Place at{cu, ws.coef};
+  Place at{cu, ws.coef, B};
   at.set(find_seq_warp(cu, B, s0 * kStep, lane));
   const int end = s1 * (int64_t)kStep < T ? s1 * kStep : T;
   for (int base = s0 * kStep; base < end; base += kSlice) {
@@ -294,6 +329,23 @@ __device__ __forceinline__ void fill_steps(const int32_t* __restrict__ cu, int B
       const float4 v = make_float4(at.c, at.c, at.c, at.c);
       __stcs(reinterpret_cast<float4*>(out), v);
       __stcs(reinterpret_cast<float4*>(out + 128), v);
+      continue;
+    }
+    if (at.one_border(base, last)) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int t = slot_token(base, lane, 4 * q);
+        float g[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] = t + i < at.end ? at.c : at.next_c;
+        if (vec && t + 4 <= T) {
+          __stcs(reinterpret_cast<float4*>(out + q * 128), make_float4(g[0], g[1], g[2], g[3]));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) if (t + i < T) dlogp[t + i] = g[i];
+        }
+      }
+      at.advance();
       continue;
     }
     // coefficients at the places where sequences start; a token's is the one at the last start before it
