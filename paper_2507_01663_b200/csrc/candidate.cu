@@ -16,7 +16,9 @@
 namespace af {
 namespace {
 
-constexpr int kPromoteBlocks = 8;       // K = 512 per part
+// K = 512 per part.  8192 x 3584 x 152064: 7529 us at 256, 6902 at 512, 6692 at 896, 6495 without parts; the error of lse
+// is 3.2e-7 at 512 and 5.8e-7 at 896.
+constexpr int kPromoteBlocks = 8;
 
 struct CandidateState {
   float m, s, u;

@@ -221,6 +221,11 @@ __device__ __forceinline__ int split_begin(const GemmShape& g, int s) {
 // nearest: the truncation then acts on values `parts` times smaller.  Eight epilogue warps instead of
 // four share the 256 columns, so a thread holds 128 running sums; adding a part up takes a fraction of
 // the time the MMAs need for the next one and is hidden behind it.
+// K blocks of a part: kPromote, or half of a short K.
+template <int kPromote>
+__device__ __forceinline__ int part_blocks(int k_blocks) {
+  return k_blocks >= 2 * kPromote ? kPromote : (k_blocks + 1) / 2;
+}
 constexpr int kPromoteCols = kBN / 2;                         // columns per epilogue thread
 constexpr int kPromoteThreads = 64 + 256;                     // producer and MMA warps, eight epilogue warps
 
@@ -359,7 +364,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
           int part_kb = 0;                               // K blocks in the current part (kPromote > 0)
           for (int kb = 0; kb < g.k_blocks; ++kb) {
             if constexpr (kPromote > 0) {
-              if (part_kb == kPromote) {                 // next part: publish this one, take the other accumulator
+              if (part_kb == part_blocks<kPromote>(g.k_blocks)) {   // next part: publish this one, take the other accumulator
                 mma_commit(tfull_bar(acc));
                 ++tile_count;                            // counts parts here
                 acc = tile_count & 1u; acc_phase = (tile_count >> 1) & 1u;
@@ -391,7 +396,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
   } else if constexpr (kPromote > 0) {
     // ------------------------------------------------------- epilogue, promoted accumulation (warps 2..9)
     const int quarter = warp & 3, half = (warp - 2) >> 2;         // TMEM lanes this warp may touch; its column half
-    const int parts = (g.k_blocks + kPromote - 1) / kPromote;
+    const int per_part = part_blocks<kPromote>(g.k_blocks), parts = (g.k_blocks + per_part - 1) / per_part;
     const int left = (bn / 2 + 15) / 16 * 16;                     // columns of the first half: loads start at multiples of 16
     const int first = half * left, cols = half ? bn - left : left;
     uint32_t part_count = 0; bool ok = true;
@@ -772,7 +777,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
           int part_kb = 0;                               // K blocks in the current part (kPromote > 0)
           for (int kb = kb0; kb < kb1; ++kb) {
             if constexpr (kPromote > 0) {
-              if (part_kb == kPromote) {                 // next part: publish this one, take the other accumulator
+              if (part_kb == part_blocks<kPromote>(g.k_blocks)) {   // next part: publish this one, take the other accumulator
                 mma_commit_pair(tfull_bar(acc));
                 ++tile_count;                            // counts parts here
                 acc = tile_count & 1u; acc_phase = (tile_count >> 1) & 1u;
@@ -805,7 +810,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
     // ------------------------------------------- epilogue, promoted accumulation (warps 2..9, both CTAs)
     const int quarter = warp & 3, half = (warp - 2) >> 2;         // TMEM lanes this warp may touch; its column half
     const int row_in_tile = (int)rank * kBM + quarter * 32 + lane;
-    const int parts = (g.k_blocks + kPromote - 1) / kPromote;
+    const int per_part = part_blocks<kPromote>(g.k_blocks), parts = (g.k_blocks + per_part - 1) / per_part;
     uint32_t part_count = 0; bool ok = true;
     typename E::State st;
     uint8_t* const stage = E::kStaged ? epi_stage_base + (warp - 2) * kEpiStageBytes : nullptr;
