@@ -117,6 +117,7 @@ struct DzCandidateEpi {
     uint32_t key;
   };
   static constexpr bool kStaged = true;
+  static constexpr bool kHalves = true;
   static __device__ __forceinline__ void unit_begin(State& st, const Params& p, int row, int, int) {
     st.next = -1;
     st.key = kNoCandidate;
@@ -143,6 +144,7 @@ struct DzCandidateEpi {
 #pragma unroll
     for (int j = 0; j < 32; ++j)
       dzv[j] = -st.gsum * ex2f(fmaf(__uint_as_float(v[j]), kLog2e, st.nl));
+    while ((int)(st.key >> 8) < col0) { ++st.next; st.key = candidate_at(keys, p.K, st.next); }   // another warp's columns
     while ((int)(st.key >> 8) < col0 + 32) {
       const int j = (int)(st.key >> 8) - col0;
       const float g = __ldg(p.g + (size_t)row * p.K + (st.key & 255u));
@@ -234,6 +236,7 @@ struct StoreBf16TransposedEpi {
   };
   struct State {};
   static constexpr bool kStaged = false;
+  static constexpr bool kHalves = true;
   static __device__ __forceinline__ void unit_begin(State&, const Params&, int, int, int) {}
   static __device__ __forceinline__ void chunk(State&, const Params& p, int row, int col0,
                                                const uint32_t (&v)[32], uint8_t*) {
@@ -302,6 +305,7 @@ struct StorePartialEpi {
     float* row;
   };
   static constexpr bool kStaged = false;
+  static constexpr bool kHalves = true;
   static __device__ __forceinline__ void unit_begin(State& st, const Params& p, int row, int, int part) {
     st.row = p.P + ((size_t)part * p.M + row) * p.N;
   }

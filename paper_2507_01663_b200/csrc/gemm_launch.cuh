@@ -112,7 +112,7 @@ af_status run_gemm(const GemmEnv& env, const Operand& A, const Operand& B, int s
   umma::GemmShape g = gemm_shape(M, N, K, splits, env.pair);
   const int64_t units = (int64_t)g.m_tiles * g.splits;
   if (env.pair) {
-    constexpr int smem = E::kStaged ? umma::kPairSmemBytesStaged : umma::kPairSmemBytes;
+    constexpr int smem = umma::kPairSmem<E, false>, threads = umma::kPairThreads<E, false>;
     static SmemAttrOnce once;
     if (set_smem_once(once, umma::gemm_pair_kernel<E, kAMN, kBMN>, smem) != cudaSuccess) return AF_ERR_CUDA;
     const int pairs = env.sm_count / 2;
@@ -121,9 +121,9 @@ af_status run_gemm(const GemmEnv& env, const Operand& A, const Operand& B, int s
     const bool by_die = env.die_of_sm && clock && deal_by_die(g, pairs, env.die0_pairs);
     if (clock && cudaMemsetAsync(clock, 0, (by_die ? 3 : 1) * sizeof(unsigned int), s) != cudaSuccess) return AF_ERR_CUDA;
     if (env.overlapped)
-      return launch_overlapped(umma::gemm_pair_kernel<E, kAMN, kBMN>, grid, umma::kThreads, smem, s, ta, tb, g, ep, env.d_err,
+      return launch_overlapped(umma::gemm_pair_kernel<E, kAMN, kBMN>, grid, threads, smem, s, ta, tb, g, ep, env.d_err,
                                clock, by_die ? clock + 1 : nullptr, env.die_of_sm) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
-    umma::gemm_pair_kernel<E, kAMN, kBMN><<<grid, umma::kThreads, smem, s>>>(ta, tb, g, ep, env.d_err, clock,
+    umma::gemm_pair_kernel<E, kAMN, kBMN><<<grid, threads, smem, s>>>(ta, tb, g, ep, env.d_err, clock,
                                                                              by_die ? clock + 1 : nullptr, env.die_of_sm);
   } else {
     constexpr int smem = E::kStaged ? umma::kSmemBytesStaged : umma::kSmemBytes;
@@ -156,7 +156,7 @@ af_status run_gemm_promoted(const GemmEnv& env, const Operand& A, const Operand&
   umma::GemmShape g = gemm_shape(A.rows, B.rows, A.cols, splits, true);
   const int64_t units = (int64_t)g.m_tiles * g.splits;
   static SmemAttrOnce once;
-  constexpr int smem = E::kStaged ? umma::kPromoteSmemBytesStaged : umma::kPairSmemBytes;
+  constexpr int smem = umma::kPairSmem<E, true>;
   if (set_smem_once(once, umma::gemm_pair_kernel<E, false, false, kPromote>, smem) != cudaSuccess) return AF_ERR_CUDA;
   const int pairs = env.sm_count / 2;
   const int grid = 2 * (int)(units < pairs ? units : pairs);
@@ -203,12 +203,12 @@ af_status run_gemm_split_k(const GemmEnv& env, const Operand& A, const Operand& 
   g.k_parts = k_parts;
   g.splits = g.n_tiles * k_parts;
   const int64_t units = (int64_t)g.m_tiles * g.splits;
-  constexpr int smem = E::kStaged ? umma::kPairSmemBytesStaged : umma::kPairSmemBytes;
+  constexpr int smem = umma::kPairSmem<E, false>, threads = umma::kPairThreads<E, false>;
   static SmemAttrOnce once;
   if (set_smem_once(once, umma::gemm_pair_kernel<E, kAMN, kBMN, 0, true>, smem) != cudaSuccess) return AF_ERR_CUDA;
   const int pairs = env.sm_count / 2;
   const int grid = 2 * (int)(units < pairs ? units : pairs);
-  return launch_overlapped(umma::gemm_pair_kernel<E, kAMN, kBMN, 0, true>, grid, umma::kThreads, smem, s, ta, tb, g, ep, env.d_err,
+  return launch_overlapped(umma::gemm_pair_kernel<E, kAMN, kBMN, 0, true>, grid, threads, smem, s, ta, tb, g, ep, env.d_err,
                            nullptr, nullptr, nullptr) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
