@@ -96,6 +96,23 @@ inline af_status encode_operand(const GemmEnv& env, CUtensorMap* map, const Oper
   return AF_OK;
 }
 
+// Columns of a CTA pair's tile.  A launch of few tiles leaves pairs idle, or some of them with one tile more than the
+// others: tiles of 128 columns, one unit each, where that shortens the longest pair's work.  (Gradient of 1195 tokens at
+// a 256 x 4096 head, d_W in 32 tiles for 16: 47.9 -> 45.5 us; of 64 tokens, dZ in 32 tiles for 16 too: 32 -> 27; of 128
+// tokens at 3584 x 19008, dZ in 149 tiles for 75: 207 -> 200.)  Beyond two rounds of tiles the wider ones are worth
+// more: an operand's row is fetched once per tile.
+inline int pair_tile_columns(int64_t m_tiles, uint64_t N, int64_t pairs) {
+  const int64_t wide = m_tiles * (int64_t)((N + 255) / 256), narrow = m_tiles * (int64_t)((N + 127) / 128);
+  return wide <= 2 * pairs && (narrow + pairs - 1) / pairs < 2 * ((wide + pairs - 1) / pairs) ? 128 : 256;
+}
+// Sets the tile's width to bn columns, and one unit per tile where that is less than 256.
+inline void set_tile_columns(umma::GemmShape& g, uint64_t N, int bn) {
+  g.bn = bn;
+  if (bn == umma::kBN) return;
+  g.n_tiles = (int)((N + bn - 1) / bn);
+  g.splits = g.n_tiles;
+}
+
 // C[M,N] = sum_k A(m,k) B(n,k).  A K-major operand is stored [M or N, K]; an MN-major operand is
 // stored [K, M or N].  TMA box: 64 contiguous elements wide; K-major A 128 rows, K-major B 256
 // rows (128 per CTA of a pair), MN-major 64 K-rows.  `splits` <= 0 means one unit per B tile.
@@ -105,11 +122,12 @@ af_status run_gemm(const GemmEnv& env, const Operand& A, const Operand& B, int s
   CUtensorMap ta, tb;
   af_status st = encode_operand(env, &ta, A, kAMN ? 64 : umma::kBM);
   if (st != AF_OK) return st;
-  st = encode_operand(env, &tb, B, kBMN ? 64 : (env.pair ? umma::kBN / 2 : umma::kBN));
-  if (st != AF_OK) return st;
   const uint64_t M = kAMN ? A.cols : A.rows, K = kAMN ? A.rows : A.cols;
   const uint64_t N = kBMN ? B.cols : B.rows;
   umma::GemmShape g = gemm_shape(M, N, K, splits, env.pair);
+  if (umma::HalvesOf<E>::value && env.pair) set_tile_columns(g, N, pair_tile_columns(g.m_tiles, N, env.sm_count / 2));
+  st = encode_operand(env, &tb, B, kBMN ? 64 : (env.pair ? g.bn / 2 : umma::kBN));
+  if (st != AF_OK) return st;
   const int64_t units = (int64_t)g.m_tiles * g.splits;
   if (env.pair) {
     constexpr int smem = umma::kPairSmem<E, false>, threads = umma::kPairThreads<E, false>;
@@ -117,7 +135,7 @@ af_status run_gemm(const GemmEnv& env, const Operand& A, const Operand& B, int s
     if (set_smem_once(once, umma::gemm_pair_kernel<E, kAMN, kBMN>, smem) != cudaSuccess) return AF_ERR_CUDA;
     const int pairs = env.sm_count / 2;
     const int grid = 2 * (int)(units < pairs ? units : pairs);
-    unsigned int* clock = env.tile_clock;
+    unsigned int* clock = g.bn < umma::kBN ? nullptr : env.tile_clock;     // few tiles: nothing to pace
     const bool by_die = env.die_of_sm && clock && deal_by_die(g, pairs, env.die0_pairs);
     if (clock && cudaMemsetAsync(clock, 0, (by_die ? 3 : 1) * sizeof(unsigned int), s) != cudaSuccess) return AF_ERR_CUDA;
     if (env.overlapped)
@@ -151,9 +169,9 @@ af_status run_gemm_promoted(const GemmEnv& env, const Operand& A, const Operand&
   CUtensorMap ta, tb;
   af_status st = encode_operand(env, &ta, A, umma::kBM);
   if (st != AF_OK) return st;
+  umma::GemmShape g = gemm_shape(A.rows, B.rows, A.cols, splits, true);
   st = encode_operand(env, &tb, B, umma::kBN / 2);
   if (st != AF_OK) return st;
-  umma::GemmShape g = gemm_shape(A.rows, B.rows, A.cols, splits, true);
   const int64_t units = (int64_t)g.m_tiles * g.splits;
   static SmemAttrOnce once;
   constexpr int smem = umma::kPairSmem<E, true>;

@@ -207,7 +207,8 @@ struct GemmShape {
   int die0_pairs;       // pair kernel only: > 0 = deal the row tiles by die; the number of CTA pairs the first die hosts
   int die0_rows;        // ... and the number of row tiles (the first ones) those pairs share among themselves
   int k_parts;          // pair kernel with kSplitK only: parts the reduction is cut into; `splits` is then n_tiles * k_parts
-  int bn;               // gemm_kernel with kPromote only: columns of a tile, a multiple of 16 up to kBN
+  int bn;               // columns of a tile: gemm_kernel with kPromote, a multiple of 16 up to kBN; gemm_pair_kernel with
+                        // E::kHalves, 256 or 128; kBN elsewhere
 };
 __device__ __forceinline__ int split_begin(const GemmShape& g, int s) {
   return (int)(((long long)g.n_tiles * s) / g.splits);
@@ -630,6 +631,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();          // 0 = leader
   const int n_pairs = gridDim.x >> 1;
+  const int bn = HalvesOf<E>::value ? g.bn : kBN;
   if (g.die0_pairs > 0) wait_for_predecessor();     // the rank counters below are memory too
   if (threadIdx.x == 0) {
     abort_flag = 0;
@@ -721,7 +723,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
         tiles_of(s, nb, ne, kb0, kb1);
         const int m0 = m_tile * kPairBM + (int)rank * kBM;          // this CTA's 128 rows of A
         for (int nt = nb; nt < ne && ok; ++nt) {
-          const int n0 = nt * kBN + (int)rank * (kBN / 2);          // this CTA's 128 rows of B
+          const int n0 = nt * bn + (int)rank * (bn / 2);            // this CTA's half of B's rows
           for (int kb = kb0; kb < kb1; ++kb) {
             if (clock_on && to_next_tick-- == 0) {
               to_next_tick = tick_len - 1;
@@ -750,7 +752,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
             if (!mbar_wait(empty_bar(stage), phase ^ 1u, &abort_flag)) { ok = false; break; }
             const uint32_t a_dst = tiles + stage * kPairStageBytes;
             const uint32_t lbar = leader_full0 + 8u * stage;
-            if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), 2 * kPairStageBytes);
+            if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), 2 * (kABytes + bn * kBK));
             if constexpr (kAMN) {
 #pragma unroll
               for (int b = 0; b < kBM / 64; ++b)
@@ -761,7 +763,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
             if constexpr (kBMN) {
 #pragma unroll
               for (int b = 0; b < kBN / 128; ++b)
-                tma_load_2d_pair(a_dst + kABytes + b * kMnBoxBytes, &tmap_b, lbar, n0 + b * 64, kb * kBK);
+                if (b < bn / 128) tma_load_2d_pair(a_dst + kABytes + b * kMnBoxBytes, &tmap_b, lbar, n0 + b * 64, kb * kBK);
             } else {
               tma_load_2d_pair(a_dst + kABytes, &tmap_b, lbar, kb * kBK, n0);
             }
@@ -776,7 +778,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer (leader only)
     if (lane == 0 && rank == 0) {
-      constexpr uint32_t idesc = instr_desc_bf16_f32(kPairBM, kBN, kAMN, kBMN);
+      const uint32_t idesc = instr_desc_bf16_f32(kPairBM, bn, kAMN, kBMN);
       constexpr uint64_t a_step = kAMN ? (2048 >> 4) : 2, b_step = kBMN ? (2048 >> 4) : 2;
       int stage = 0; uint32_t phase = 0; uint32_t tile_count = 0; bool ok = true;
       for (int q = work.first; q < work.end && ok; q += work.step) {
@@ -845,8 +847,8 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
     }
   } else {
     // ---------------------------------------------------------------- epilogue (warps 2..5 or 2..9, both CTAs)
-    constexpr int kChunks = kBN / 32 / (HalvesOf<E>::value ? 2 : 1);
-    const int quarter = warp & 3, c0 = HalvesOf<E>::value ? ((warp - 2) >> 2) * kChunks : 0;
+    const int chunks = bn / 32 / (HalvesOf<E>::value ? 2 : 1);
+    const int quarter = warp & 3, c0 = HalvesOf<E>::value ? ((warp - 2) >> 2) * chunks : 0;
     const int row_in_tile = (int)rank * kBM + quarter * 32 + lane;
     uint32_t tile_count = 0; bool ok = true;
     typename E::State st;
@@ -864,11 +866,11 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
         tc_fence_after();
         const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * kBN;
 #pragma unroll 1
-        for (int c = c0; c < c0 + kChunks; ++c) {
+        for (int c = c0; c < c0 + chunks; ++c) {
           uint32_t v[32];
           tmem_ld32(t_row + c * 32, v);
           tmem_ld_wait();
-          E::chunk(st, ep, row, nt * kBN + c * 32, v, stage);
+          E::chunk(st, ep, row, nt * bn + c * 32, v, stage);
         }
         tc_fence_before();
         __syncwarp();
