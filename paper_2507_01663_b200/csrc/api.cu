@@ -635,7 +635,9 @@ static af_status grow_preference_ws(af_ctx* c, int32_t B) {
   const void* before = c->pref_ws.p;
   const af_status st = ws_grow(c->pref_ws, preference_workspace_bytes(B));
   if (st != AF_OK || c->pref_ws.p == before) return st;
-  return cudaMemset(c->pref_ws.p, 0, preference_header_bytes()) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  // waited for: the caller's stream may be one that does not wait for the default stream
+  return cudaMemset(c->pref_ws.p, 0, preference_header_bytes()) == cudaSuccess &&
+         cudaStreamSynchronize(nullptr) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 static af_status preference_sizes(int64_t T, int32_t B) {
   if (T < 0 || B < 0 || (T > 0 && B < 1)) return AF_ERR_INVALID_ARG;
