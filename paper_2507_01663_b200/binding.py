@@ -390,6 +390,12 @@ class Context:
         raise ValueError("d_W is float32 or bfloat16")
 
     @staticmethod
+    def _sequences(cu_seqlens: torch.Tensor, B: Optional[int]) -> int:
+        if cu_seqlens.dtype is not torch.int32 or (B is not None and cu_seqlens.shape[0] <= B):
+            raise ValueError("cu_seqlens is int32 with B + 1 entries")
+        return cu_seqlens.shape[0] - 1 if B is None else B
+
+    @staticmethod
     def _list_width(cand: torch.Tensor, T: int, *others: Optional[torch.Tensor]) -> int:
         """K of [T, K] lists of 4-byte ids or values; every other tensor is float32, equally wide, with enough rows."""
         shape = cand.shape
@@ -429,7 +435,7 @@ class Context:
     def distill_loss(self, cand_logp, teacher_logp, cu_seqlens, out, token_loss=None, dcand=None, divergence=0, support=1,
                      temperature=1.0, agg_mode=0, loss_scale=1.0, B=None, T=None, stream=None):
         """``out``: device uint8 tensor of ``ctypes.sizeof(DistillOut)`` bytes (see read_distill_out)."""
-        B = cu_seqlens.shape[0] - 1 if B is None else B
+        B = self._sequences(cu_seqlens, B)
         T = cand_logp.shape[0] if T is None else T
         K = self._list_width(cand_logp, T, teacher_logp, dcand)
         prm = DistillParams(divergence, support, agg_mode, temperature, loss_scale)
@@ -441,7 +447,7 @@ class Context:
                        entropy=None, token_loss=None, dcand=None, accumulate_dW=False, divergence=0, support=1,
                        temperature=1.0, agg_mode=0, loss_scale=1.0, B=None, T=None, stream=None):
         """``af_distill_update``: scoring, distillation loss and backward of one packed micro-batch."""
-        B = cu_seqlens.shape[0] - 1 if B is None else B
+        B = self._sequences(cu_seqlens, B)
         T = hidden.shape[0] if T is None else T
         d, V = W.shape[1], W.shape[0]
         K = self._list_width(cand, T, teacher_logp, cand_logp, dcand)
@@ -457,7 +463,7 @@ class Context:
                         loss_scale=1.0, B=None, T=None, stream=None):
         """``ref_logp`` None: reference-free.  ``out``: device uint8 tensor of ``ctypes.sizeof(PreferenceOut)``
         bytes (see read_preference_out)."""
-        B = cu_seqlens.shape[0] - 1 if B is None else B
+        B = self._sequences(cu_seqlens, B)
         T = logp.shape[0] if T is None else T
         if logp.dtype != torch.float32 or (ref_logp is not None and ref_logp.dtype != torch.float32):
             raise ValueError("log-probs are float32")

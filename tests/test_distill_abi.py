@@ -31,3 +31,13 @@ def test_no_context_is_refused(lib):
                                  None, None, None, None, 0, 0, None) == -1
     assert lib.af_preference_loss(None, None, None, None, 0, 0, ctypes.byref(pp), None, None, None, None, None) == -1
     assert lib.af_reserve_preference(None, 1, 2) == -1
+
+
+def test_sequence_borders_are_int32():
+    import torch
+    from paper_2507_01663_b200 import binding as B
+    cu = torch.zeros(4, dtype=torch.int32)
+    assert B.Context._sequences(cu, None) == 3 and B.Context._sequences(cu, 2) == 2
+    for bad, n in ((cu.long(), None), (cu.float(), None), (cu, 4)):
+        with pytest.raises(ValueError):
+            B.Context._sequences(bad, n)
