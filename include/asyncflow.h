@@ -402,8 +402,9 @@ af_status af_reserve_candidates(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d
  * loss of a distillation task; the paper's loss, af_policy_loss, learns from rewards instead).
  *
  * lt = teacher_logp[t,k], lq = cand_logp[t,k] (from af_candidate_logprob), both over the whole
- * vocabulary.  A slot with lt = -inf is absent: its lq is not looked at and its gradient is 0 (a NaN in a
- * present slot makes its whole token NaN); a token whose slots are all absent has loss 0.  p = exp(lt),
+ * vocabulary.  A slot with lt = -inf, or any value down from -1e30 (a mask of the type's lowest value), is
+ * absent: its lq is not looked at and its gradient is 0 (a NaN in a present slot makes its whole token NaN); a
+ * token whose slots are all absent has loss 0.  p = exp(lt),
  * q = exp(lq); sums run over the present slots; 0 log 0 = 0.
  *   divergence 0: from teacher to student;  1: from student to teacher.
  *   support 0 (as listed):   0: sum p (lt - lq);   1: sum q (lq - lt)

@@ -14,6 +14,7 @@ import numpy as np
 from .grpo_oracle import bf16_bits_to_f64
 
 TAIL_FLOOR = 2.0 ** -16
+ABSENT = float(np.float32(-1e30))      # teacher values down from here mark an absent slot
 
 
 def _logits(H_bits, W_bits):
@@ -54,10 +55,10 @@ def candidate_backward_ref(H_bits, W_bits, cand, lse, dcand):
 
 
 def divergence_ref(lt, lq, divergence, support, temperature=1.0):
-    """One token: (loss, gradient in lq) over the slots with lt > -inf."""
+    """One token: (loss, gradient in lq) over the slots with lt > -1e30."""
     lt, lq = np.asarray(lt, dtype=np.float64), np.asarray(lq, dtype=np.float64)
     grad = np.zeros(lt.shape)
-    on = np.flatnonzero(lt != -math.inf)
+    on = np.flatnonzero(~(lt <= ABSENT))
     if support == 1:
         if on.size == 0:
             return 0.0, grad
@@ -116,7 +117,7 @@ def distill_loss_ref(cand_logp, teacher_logp, cu, divergence=0, support=1, tempe
     for t in range(T):
         token[t], g = divergence_ref(lt[t], lq[t], divergence, support, temperature)
         grad[t] = w[t] * g
-        on = lt[t] != -math.inf
+        on = ~(lt[t] <= ABSENT)
         mt += np.exp(lt[t][on]).sum()
         ms += np.exp(lq[t][on]).sum()
     return {"loss": float((w * token).sum()), "teacher_mass": mt / T if T else 0.0, "student_mass": ms / T if T else 0.0,

@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_loss_kernel(
       }
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
-        const bool present = e / kVec < valid && lt[e] != -INFINITY;
+        const bool present = e / kVec < valid && !(lt[e] <= kAbsentLogp);      // a NaN is present
         lt[e] = present ? lt[e] : kAbsentLogp;
         lq[e] = present ? lq[e] : kAbsentLogp;
       }
@@ -455,9 +455,9 @@ cudaError_t launch_rows(const DistillCall& c, cudaStream_t s) {
   const int64_t steps = ((int64_t)c.rows + kRows * batches - 1) / (kRows * batches);
   const int blocks = (int)(steps < 1 ? 1 : steps < most ? steps : most);
   return launch_overlapped(
-      distill_loss_kernel<kSupport, kForward, kG, kE, kVec>, blocks, kThreads, kSmemBytes, s, c.cand_logp, c.teacher_logp, c.cu, c.B, c.T, c.t0, c.rows, c.K, batches, c.bulk & (32 / kG * c.K % 4 == 0 ? 3 : 1), c.prm, c.out, c.token_loss,
-      c.dcand, c.ws, c.d_err);
-  return cudaGetLastError();
+      distill_loss_kernel<kSupport, kForward, kG, kE, kVec>, blocks, kThreads, kSmemBytes, s, c.cand_logp, c.teacher_logp, c.cu,
+      c.B, c.T, c.t0, c.rows, c.K, batches, c.bulk & (32 / kG * c.K % 4 == 0 ? 3 : 1), c.prm, c.out, c.token_loss, c.dcand, c.ws,
+      c.d_err);
 }
 // Rows that start on 16 bytes (K a multiple of 4) are read four slots at a time, even ones two.
 // The fewest slots per lane that hold the row: what a lane has beyond that is computed for nothing.

@@ -40,7 +40,7 @@ def loss_call(ctx, lq, lt, cu, how, agg=0, scale=1.0, offset=0, **kw):
     _, b = place(lt)
     gbuf, g = place(None)
     out, token = B.new_distill_out(dev), torch.full((T,), 3.0, device=dev)
-    ctx.distill_loss(a, b, dev_of(cu), out, token_loss=token, dcand=g, divergence=how[0], support=how[1], temperature=how[2],
+    ctx.distill_loss(a, b, dev_of(np.asarray(cu, np.int32)), out, token_loss=token, dcand=g, divergence=how[0], support=how[1], temperature=how[2],
                      agg_mode=agg, loss_scale=scale, **kw)
     res = B.read_distill_out(out)
     assert bool((gbuf[:offset] == 3.0).all()) and bool((gbuf[offset + T * K:] == 3.0).all())
@@ -153,6 +153,19 @@ def test_loss_edges(ctx):
     _, token, g = loss_call(ctx, lq, lt, [0, 6], (0, 1, 1.0), 1)
     assert np.isnan(token[3]) and np.isfinite(np.delete(token, 3)).all() and np.isfinite(np.delete(g, 3, 0)).all()
     ctx.check_device_errors()
+
+
+def test_masks_of_the_lowest_value(ctx):
+    """Absent slots marked by the lowest float32 or bf16 value instead of -inf, whole rows of them too: the same bits."""
+    lt, lq = teacher_lists(np.random.default_rng(8), 60, 20)
+    lq = np.where(np.isfinite(lq), lq, np.float32(-4.0))
+    for how in HOWS:
+        want = loss_call(ctx, lq, lt, [0, 25, 60], how)
+        for low in (np.finfo(np.float32).min, torch.finfo(torch.bfloat16).min, -1e30):
+            for under in (lq, np.where(np.isneginf(lt), np.float32(low), lq)):
+                got = loss_call(ctx, under.astype(np.float32), np.where(np.isneginf(lt), np.float32(low), lt), [0, 25, 60], how)
+                assert got[0] == want[0] and np.array_equal(got[1], want[1]) and np.array_equal(got[2], want[2])
+    assert ctx.check_device_errors() == 0
 
 
 def test_loss_leaves_rows_behind_the_batch(ctx):

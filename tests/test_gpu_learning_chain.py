@@ -243,6 +243,37 @@ def test_calls_of_different_kinds_in_turn(ctx):
     assert ctx.check_device_errors() == 0
 
 
+def test_what_is_reserved_holds_every_smaller_batch(ctx):
+    """No call within the reserved sizes allocates, whatever way of launching its shape leads to."""
+    from paper_2507_01663_b200 import binding as B
+    dev = device()
+    rng = np.random.default_rng(77)
+    T, K, d, V = 1500, 40, 512, 6000
+    ctx.set_tuning(0, 256)
+    ctx.reserve_candidates(T, K, d, V, with_backward=2, dW_type=B.BF16)
+    ctx.reserve_preference(T, 100)
+    reserved = ctx.workspace_bytes()
+    H, W = torch.randn(T * d, device=dev).to(torch.bfloat16), (0.05 * torch.randn(V * d, device=dev)).to(torch.bfloat16)
+    shapes = [(T, K, d, V), (1, 1, 8, 8), (16, K, d, V), (17, K, d, V), (128, K, d, V), (129, K, d, V), (257, 3, 64, 5992)]
+    shapes += [(int(rng.integers(1, T + 1)), int(rng.integers(1, K + 1)), 8 * int(rng.integers(1, d // 8 + 1)),
+                8 * int(rng.integers(1, V // 8 + 1))) for _ in range(25)]
+    for t, k, e, v in shapes:
+        h, w = H[:t * e].view(t, e), W[:v * e].view(v, e)
+        cand = torch.randint(0, v, (t, k), dtype=torch.int32, device=dev)
+        lt, lq, g = -5 * torch.rand(t, k, device=dev), torch.empty(t, k, device=dev), torch.empty(t, k, device=dev)
+        lse, dH, dW = torch.empty(t, device=dev), torch.empty_like(h), torch.empty_like(w)
+        cu = dev_of(cuts(rng, 4, t))
+        ctx.candidate_logprob(h, w, cand, lq, lse=lse)
+        first = lq.clone()
+        ctx.distill_update(h, w, cand, lt, cu, B.new_distill_out(dev), lq, lse, dH, dW, dcand=g)
+        ctx.candidate_logprob_backward(h, w, cand, lse, g, dH, dW)
+        ctx.preference_loss(lse, None, cu, B.new_preference_out(dev), T=t)
+        assert ctx.workspace_bytes() == reserved, (t, k, e, v)
+        assert float((first - lq).abs().max()) <= 1e-4, (t, k, e, v)
+    ctx.set_tuning(0, 0)
+    assert ctx.check_device_errors() == 0
+
+
 @pytest.mark.parametrize("fused", [False, True])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_dw_ready_event(ctx, dtype, fused):

@@ -161,3 +161,15 @@ def test_preference_closed_forms():
     a = D.preference_loss_ref([-1.0, -2.0, -3.0, -5.0], None, [0, 1, 2, 3, 4], beta=1.0, pair_layout=0)
     b = D.preference_loss_ref([-1.0, -3.0, -2.0, -5.0], None, [0, 1, 2, 3, 4], beta=1.0, pair_layout=1)
     assert a["loss"] == pytest.approx(b["loss"]) and a["pair_loss"] == pytest.approx(b["pair_loss"])
+
+
+def test_a_mask_of_the_lowest_value_is_absent():
+    lt = np.array([-1.0, -np.inf, -2.0], np.float64)
+    lq = np.array([-1.5, -0.5, -0.7], np.float64)
+    for div in (0, 1):
+        for support in (0, 1, 2):
+            want = D.divergence_ref(lt, lq, div, support)
+            for low in (np.finfo(np.float32).min, -1e30, -3.0e38):
+                got = D.divergence_ref(np.where(np.isneginf(lt), np.float32(low), lt), lq, div, support)
+                assert got[0] == want[0] and np.array_equal(got[1], want[1])
+    assert D.divergence_ref(np.full(3, -3.4e38), lq, 0, 1)[0] == 0.0
