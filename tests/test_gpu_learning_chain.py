@@ -243,6 +243,27 @@ def test_calls_of_different_kinds_in_turn(ctx):
     assert ctx.check_device_errors() == 0
 
 
+@pytest.mark.parametrize("T,d,V,K,block", [(300, 128, 4104, 12, 0), (300, 128, 1000, 12, 128), (40, 64, 2048, 20, 0), (9, 256, 520, 3, 0)])
+def test_two_batches_in_turn_through_the_same_buffers(ctx, T, d, V, K, block):
+    """Call after call without a pause, two sets of inputs and one of outputs and workspace: every call reads what the
+    kernel before it in the same call wrote, not what the other batch had left there."""
+    a, b = Work(95, T, d, V, K, torch.bfloat16), Work(96, T, d, V, K, torch.bfloat16)
+    b.o = a.o
+    ctx.set_tuning(0, block)
+    want = []
+    for w in (a, b):
+        w.calls(ctx)
+        want.append(w.results())
+    assert not torch.equal(want[0]["g"], want[1]["g"])
+    for n in range(1, 41):
+        for i in range(n % 7 + 1):
+            last = (n + i) & 1
+            (a, b)[last].calls(ctx, (0, 1, 2, 3) if n % 2 else (1, 3, 0, 2))
+        same(want[last], a.results())
+    ctx.set_tuning(0, 0)
+    assert ctx.check_device_errors() == 0
+
+
 def test_what_is_reserved_holds_every_smaller_batch(ctx):
     """No call within the reserved sizes allocates, whatever way of launching its shape leads to."""
     from paper_2507_01663_b200 import binding as B
