@@ -330,6 +330,55 @@ struct StorePartialEpi {
   static __device__ __forceinline__ void unit_end(State&, const Params&, int, int) {}
 };
 
+// ---- epilogue 3c: accumulator tile [v, d] -> d_W [V, d] in either type, by way of shared memory as whole pieces of rows ----
+template <bool kF32>
+struct StoreHeadEpi {
+  struct Params {
+    void* C;
+    int M, N;
+    int accumulate;       // kF32 only
+  };
+  struct State {};
+  static constexpr bool kStaged = true;
+  static constexpr bool kHalves = true;
+  static __device__ __forceinline__ void unit_begin(State&, const Params&, int, int, int) {}
+  static __device__ __forceinline__ void chunk(State&, const Params& p, int row, int col0, const uint32_t (&v)[32],
+                                               uint8_t* stage) {
+    if (col0 >= p.N) return;                       // uniform across the warp
+    const int lane = threadIdx.x & 31;
+    if constexpr (kF32) {
+      // slot q (16 bytes) of row r sits at q ^ (r & 7): no bank conflicts on either side
+      float4* const st = reinterpret_cast<float4*>(stage);
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        st[lane * 8 + (q ^ (lane & 7))] = make_float4(__uint_as_float(v[4 * q]), __uint_as_float(v[4 * q + 1]),
+                                                      __uint_as_float(v[4 * q + 2]), __uint_as_float(v[4 * q + 3]));
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = i * 4 + (lane >> 3), q = lane & 7;
+        const int grow = row - lane + r, gcol = col0 + 4 * q;
+        if (grow < p.M && gcol < p.N) {            // N % 8 == 0
+          float4* const to = reinterpret_cast<float4*>(static_cast<float*>(p.C) + (size_t)grow * p.N + gcol);
+          float4 w = st[r * 8 + (q ^ (r & 7))];
+          if (p.accumulate) {
+            const float4 o = *to;
+            w = make_float4(o.x + w.x, o.y + w.y, o.z + w.z, o.w + w.w);
+          }
+          *to = w;
+        }
+      }
+      __syncwarp();
+    } else {
+      uint32_t w[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+      store_chunk_bf16(w, stage, lane, static_cast<__nv_bfloat16*>(p.C), p.N, row - lane, col0, p.M, p.N);
+    }
+  }
+  static __device__ __forceinline__ void unit_end(State&, const Params&, int, int) {}
+};
+
 // Adds the parts in order and rounds once: 8 values per thread.
 __global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ P, int parts, size_t n,
                                                         __nv_bfloat16* __restrict__ out) {
@@ -421,6 +470,18 @@ af_status launch_head_products(af_ctx* ctx, const void* hidden_blk, const void* 
     return hidden_gradient(ctx, env, dZop, Wop, tc, d, static_cast<__nv_bfloat16*>(d_hidden_blk), s);
   };
   auto dW_product = [&]() {
+    // With dZ^T as the first operand a thread holds a piece of a row of d_W in place of a column, and a warp stores 16
+    // bytes per lane, which is what counts for few tokens, when the product is a stream of d_W; dZ streams past once, and
+    // the hidden states stay in L2 as long as they take 32 MB or less.  3584 x 152064, the whole call: 29 tokens 691 us
+    // against 1100, 400 tokens 1.28 ms against 1.57, 700 tokens 1.86 against 2.13, 4001 tokens 10.3 against 10.4.
+    // Beyond that the order whose panels of hidden states take turns in L2.
+    if (env.pair && first_block && last_block && tc * (int64_t)d <= (16 << 20)) {
+      GemmEnv stream = env;
+      stream.tile_clock = nullptr;
+      if (head.type == AF_BF16)
+        return run_gemm<StoreHeadEpi<false>, true, true>(stream, dZop, Hblk, 0, {head.d_W, V, d, 0}, s);
+      return run_gemm<StoreHeadEpi<true>, true, true>(stream, dZop, Hblk, 0, {head.d_W, V, d, head.accumulate ? 1 : 0}, s);
+    }
     const int S = logprob_pick_splits((int64_t)d, (int32_t)tc, V, ctx->sm_count, env.pair, 0, 0);
     if (head.type == AF_BF16 && last_block) {
       StoreBf16TransposedEpi::Params p3{static_cast<__nv_bfloat16*>(head.d_W),
@@ -484,8 +545,15 @@ af_status launch_candidate_backward(af_ctx* ctx, const void* hidden, const void*
     const Operand Hblk{H + t0 * d, (uint64_t)tc, (uint64_t)d, (uint64_t)d * 2};
     const Operand Wop{W, (uint64_t)V, (uint64_t)d, (uint64_t)d * 2};
     DzCandidateEpi::Params p1{keys, g + t0 * K, gsum, lse + t0, dz, (int)tc, V, K};
-    st = run_gemm<DzCandidateEpi, false, false>(
-        unpaced_if_cached(env, Hblk, Wop), Hblk, Wop, logprob_pick_splits(tc, d, V, ctx->sm_count, env.pair, ctx->v_splits, env.die0_pairs), p1, s);
+    // one or two row tiles: a range of W per pair, as in the scoring call (32 ranges, the most of the other rule, leave
+    // pairs idle: 29 tokens at 3584 x 152064, 338 us); and one row tile shares nothing that needs pacing
+    const int64_t m_tiles = (tc + umma::kPairBM - 1) / umma::kPairBM, workers = ctx->sm_count / 2;
+    const int S = env.pair && ctx->v_splits == 0 && m_tiles * 32 < workers
+                      ? (int)(workers / m_tiles)
+                      : logprob_pick_splits(tc, d, V, ctx->sm_count, env.pair, ctx->v_splits, env.die0_pairs);
+    GemmEnv dz_env = unpaced_if_cached(env, Hblk, Wop);
+    if (tc <= umma::kPairBM) dz_env.tile_clock = nullptr;
+    st = run_gemm<DzCandidateEpi, false, false>(dz_env, Hblk, Wop, S, p1, s);
     if (st != AF_OK) return st;
     st = launch_head_products(ctx, H + t0 * d, W, dz, tc, d, V, static_cast<__nv_bfloat16*>(d_hidden) + t0 * d, head,
                               t0 == 0, t0 + Tc >= T, s);

@@ -349,6 +349,13 @@ af_status launch_candidate_logprob(af_ctx* ctx, const void* hidden, const void* 
 af_status launch_candidate_logprob_z(af_ctx* ctx, const void* hidden, const void* W, const int32_t* cand, int64_t T,
                                      int32_t K, int32_t d, int32_t V, float* cand_logp, float* entropy, float* lse,
                                      float* z, cudaStream_t s) {
+  if (ctx->v_splits == 0 && stream_fits(T, d)) {
+    const af_status fits = ws_grow(ctx->partial, (size_t)T * ctx->sm_count * sizeof(float4));
+    if (fits != AF_OK) return fits;
+    const StreamCall c{hidden, W, cand, (int)T, K, d, V, z, static_cast<float4*>(ctx->partial.p), cand_logp, entropy, lse,
+                       static_cast<unsigned int*>(ctx->loss_ws.p), ctx->d_err};
+    return launch_candidate_stream(c, ctx->sm_count, s);
+  }
   int parts = 0;
   const af_status st = candidate_gemm(ctx, hidden, W, T, d, V, K, nullptr, nullptr, z, &parts, s);
   if (st != AF_OK) return st;

@@ -13,16 +13,18 @@
 // logits moves its 6 bytes per logit at 6.3 TB/s (4100 rows of 152064: 0.59 ms).
 #include "candidate.cuh"
 
+#include <algorithm>
+
 namespace af {
 namespace {
 
 constexpr int kThreads = 256;
 
-// One CTA per token row of the block.  The dense part -G q_v goes out first; the listed columns are then
-// written over it, rounded once from fp32: sum of the gradients that name the column, minus G q.
+// One CTA per token row of the block and range of columns (one range, unless the rows are too few to fill the device: 29
+// rows of 152064 take 45 us that way, 9 in ranges).  The dense part -G q_v goes out first; the listed columns are then written over it, rounded once from fp32: sum of the gradients that name the column, minus G q.
 __global__ void __launch_bounds__(kThreads) dz_candidates_kernel(
     const float* __restrict__ z, __nv_bfloat16* __restrict__ dz, int V, const int32_t* __restrict__ cand,
-    const float* __restrict__ g, const float* __restrict__ cand_logp, const float* __restrict__ lse, int K) {
+    const float* __restrict__ g, const float* __restrict__ cand_logp, const float* __restrict__ lse, int K, int range) {
   __shared__ int s_id[AF_MAX_CANDIDATES];
   __shared__ float s_g[AF_MAX_CANDIDATES];
   __shared__ double s_sum[kThreads / 32];
@@ -51,7 +53,8 @@ __global__ void __launch_bounds__(kThreads) dz_candidates_kernel(
   const float nl = -__ldg(lse + row) * kLog2e;
   const float4* zr = reinterpret_cast<const float4*>(z + row * V);
   uint4* out = reinterpret_cast<uint4*>(dz + row * V);
-  for (int c8 = threadIdx.x; c8 * 8 < V; c8 += kThreads) {      // 8 columns per thread per step
+  const int begin = blockIdx.y * range, end = V - begin < range ? V : begin + range;     // range % 8 == 0
+  for (int c8 = begin / 8 + threadIdx.x; c8 * 8 < end; c8 += kThreads) {      // 8 columns per thread per step
     const float4 a = __ldcs(zr + 2 * c8), b = __ldcs(zr + 2 * c8 + 1);
     float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -60,6 +63,7 @@ __global__ void __launch_bounds__(kThreads) dz_candidates_kernel(
                          pack_bf16x2(v[6], v[7]));
   }
   float total = 0.f, q = 0.f;
+  if (id < begin || id >= end) id = -1;                         // another CTA's
   if (id >= 0) {
     for (int i = 0; i < K; ++i) total += s_id[i] == id ? s_g[i] : 0.f;   // the same order for every slot naming id
     q = ex2f(__ldg(cand_logp + row * K + k) * kLog2e);
@@ -104,8 +108,11 @@ af_status launch_distill_update(af_ctx* ctx, const void* hidden, const void* W, 
                             one_block ? token_loss : nullptr, g, ctx->loss_ws.p, ctx->d_err, ctx->sm_count,
                             s) != cudaSuccess)
       return AF_ERR_CUDA;
-    if (launch_overlapped(dz_candidates_kernel, (unsigned)tc, kThreads, 0, s, zlog, dz, V, cand + t0 * K, g, lq, lse + t0, K) !=
-        cudaSuccess)
+    // ranges of at least 2048 columns, as many as it takes for four CTAs per SM
+    const int64_t ranges = std::min<int64_t>((4 * (int64_t)ctx->sm_count + tc - 1) / tc, (V + 2047) / 2048);
+    const int range = (int)(((V + ranges - 1) / ranges + 7) / 8 * 8);
+    if (launch_overlapped(dz_candidates_kernel, dim3((unsigned)tc, (unsigned)((V + range - 1) / range)), kThreads, 0, s, zlog, dz, V,
+                          cand + t0 * K, g, lq, lse + t0, K, range) != cudaSuccess)
       return AF_ERR_CUDA;
     st = launch_head_products(ctx, H + t0 * d, W, dz, tc, d, V, static_cast<__nv_bfloat16*>(d_hidden) + t0 * d, head,
                               t0 == 0, t0 + Tc >= T, s);

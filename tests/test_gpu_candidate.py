@@ -218,6 +218,20 @@ def test_gradient_over_several_token_blocks(ctx, dtype):
     check_gradient(H, W, cand, lse, np.nan_to_num(g), dH, dW, blocks=6)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,d,V", [(1, 264, 20008), (2, 3584, 264), (29, 136, 19000), (129, 520, 4104), (300, 1032, 1160), (520, 8, 40)])
+def test_gradient_of_few_tokens(ctx, T, d, V, dtype):
+    """Products whose work is to write d_W, ragged in both directions; and fp32 sums on top of what was there."""
+    H, W, cand, lse, g = backward_inputs(T + d, T, d, V, 9)
+    dH, dW = gradient(ctx, H, W, cand, lse, g, dtype)
+    check_gradient(H, W, cand, lse, np.nan_to_num(g), dH, dW)
+    if dtype == torch.float32:
+        base = torch.randn(V, d, device=device())
+        _, more = gradient(ctx, H, W, cand, lse, g, accumulate=True, start=base)
+        assert float((more - (base + dW)).abs().max()) <= 2 * U * float(base.abs().max() + dW.abs().max())
+    assert ctx.check_device_errors() == 0
+
+
 def test_gradient_accumulates_in_fp32_only(ctx):
     from paper_2507_01663_b200 import binding as B
     dev = device()

@@ -294,6 +294,21 @@ def test_update_matches_the_oracle_stage_by_stage(ctx, T, d, V, K, block, how, a
     check_gradient(H, W, cand, np_of(o["lse"]), np_of(o["g"]), o["dH"], o["dW"], blocks=4)
 
 
+@pytest.mark.parametrize("T,d,V,K", [(1, 64, 20008, 30), (5, 256, 9000, 256), (16, 136, 12000, 7), (17, 64, 2056, 3), (90, 128, 6152, 64)])
+def test_update_of_few_tokens(ctx, T, d, V, K):
+    """Rows cut into ranges of columns for dZ; scoring in one pass over W up to 16 tokens."""
+    H, W, cand, lt, cu = update_inputs(T + V, T, d, V, K, 2)
+    o = update_call(ctx, H, W, cand, lt, cu, (1, 2, 1.0), 1, 1.0, torch.bfloat16)
+    assert ctx.check_device_errors() == 0
+    want, went, wlse = D.candidate_logprob_ref(bits(H), bits(W), cand)
+    ok = np.isfinite(want)
+    z_max = float(np.abs(wlse).max()) + float(np.abs(want[ok]).max(initial=0.0))
+    tz, tl = logit_tol(H, W, True), lse_tol(H, W, z_max)
+    assert np.abs(np_of(o["lse"]) - wlse).max() <= tl
+    assert np.array_equal(np.isfinite(np_of(o["lq"])), ok) and np.abs(np_of(o["lq"])[ok] - want[ok]).max(initial=0.0) <= tz + tl + 2 * U * z_max
+    check_gradient(H, W, cand, np_of(o["lse"]), np_of(o["g"]), o["dH"], o["dW"])
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_update_equals_the_three_calls(ctx, dtype):
     from paper_2507_01663_b200 import binding as B
