@@ -474,6 +474,7 @@ af_status launch_head_products(af_ctx* ctx, const void* hidden_blk, const void* 
     // bytes per lane, which is what counts for few tokens, when the product is a stream of d_W; dZ streams past once, and
     // the hidden states stay in L2 as long as they take 32 MB or less.  3584 x 152064, the whole call: 29 tokens 691 us
     // against 1100, 400 tokens 1.28 ms against 1.57, 700 tokens 1.86 against 2.13, 4001 tokens 10.3 against 10.4.
+    // d_W of 29 tokens alone: 1.09 GB in 314 us, 3.5 TB/s of writes (728 us the other way round).
     // Beyond that the order whose panels of hidden states take turns in L2.
     if (env.pair && first_block && last_block && tc * (int64_t)d <= (16 << 20)) {
       GemmEnv stream = env;
