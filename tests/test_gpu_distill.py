@@ -309,6 +309,26 @@ def test_update_of_few_tokens(ctx, T, d, V, K):
     check_gradient(H, W, cand, np_of(o["lse"]), np_of(o["g"]), o["dH"], o["dW"])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, None], ids=["f32", "bf16", "frozen"])
+def test_update_whose_last_block_is_a_few_tokens(ctx, dtype):
+    H, W, cand, lt, cu = update_inputs(264, 264, 136, 4104, 21, 5)
+    ctx.set_tuning(0, 128)
+    try:
+        o = update_call(ctx, H, W, cand, lt, cu, (0, 1, 1.0), 0, 1.0, dtype)
+    finally:
+        ctx.set_tuning(0, 0)
+    assert ctx.check_device_errors() == 0
+    want, _, wlse = D.candidate_logprob_ref(bits(H), bits(W), cand)
+    ok = np.isfinite(want)
+    z_max = float(np.abs(wlse).max()) + float(np.abs(want[ok]).max())
+    tl = lse_tol(H, W, z_max)
+    assert np.abs(np_of(o["lse"]) - wlse).max() <= tl
+    assert np.abs(np_of(o["lq"])[ok] - want[ok]).max() <= logit_tol(H, W, True) + tl + 2 * U * z_max
+    check_loss(np_of(o["lq"]), lt, cu, (0, 1, 1.0), 0, 1.0,
+               (o["res"], np_of(o["token"]).astype(np.float64), np_of(o["g"]).astype(np.float64)))
+    check_gradient(H, W, cand, np_of(o["lse"]), np_of(o["g"]), o["dH"], o["dW"], blocks=3)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_update_equals_the_three_calls(ctx, dtype):
     from paper_2507_01663_b200 import binding as B
