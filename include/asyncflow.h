@@ -366,10 +366,10 @@ af_status af_policy_update(af_ctx* ctx, const void* hidden, const void* W, const
  * registered "d_W ready" event (af_set_dw_ready_event) is recorded where d_W is complete, when there
  * is a d_W.  The forward accumulates logits in parts that are added in fp32 with rounding to nearest
  * (the tensor core's own accumulation truncates): at d = 3584 its log-probs are within 5e-7 of the 64-bit
- * ones, relative, where af_token_logprob's are 3e-6 off.  How it is launched follows from T alone: one pass over W by
- * itself for up to 16 tokens, single CTAs up to 128, CTA pairs from there on; gemm_variant 1 of
- * af_set_tuning applies to the backward only, v_splits > 0 asks for CTA pairs with that many ranges,
- * bwd_token_block works as elsewhere.
+ * ones, relative, where af_token_logprob's are 3e-6 off.  How it is launched follows from T and d: one pass
+ * over W by itself for up to 16 tokens (8 where d > 4096, none where d > 5880), single CTAs up to 128
+ * tokens, CTA pairs from there on; gemm_variant 1 of af_set_tuning applies to the backward only,
+ * v_splits > 0 asks for CTA pairs with that many ranges, bwd_token_block works as elsewhere.
  *
  * hidden [T,d], W [V,d] bf16 dev, row-major, 16-byte aligned, d % 8 == 0 (backward: V % 8 == 0, d_hidden
  * and d_W 16-byte aligned too).  cand [T,K] int32, cand_logp, dcand [T,K], entropy (nullable), lse
