@@ -403,9 +403,9 @@ af_status af_reserve_candidates(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d
  *
  * lt = teacher_logp[t,k], lq = cand_logp[t,k] (from af_candidate_logprob), both over the whole
  * vocabulary.  A slot with lt = -inf, or any value down from -1e30 (a mask of the type's lowest value), is
- * absent: its lq is not looked at and its gradient is 0 (a NaN in a present slot makes its whole token NaN); a
- * token whose slots are all absent has loss 0.  p = exp(lt),
- * q = exp(lq); sums run over the present slots; 0 log 0 = 0.
+ * absent: its lq is not looked at and its gradient is 0; a token whose slots are all absent has loss 0.  A NaN
+ * in a present slot makes its whole token NaN: its loss, which the record inherits, and the gradients of all its
+ * slots.  p = exp(lt), q = exp(lq); sums run over the present slots; 0 log 0 = 0.
  *   divergence 0: from teacher to student;  1: from student to teacher.
  *   support 0 (as listed):   0: sum p (lt - lq);   1: sum q (lq - lt)
  *   support 1 (renormalised): a = softmax(lt / tau), b = softmax(lq / tau) over the present slots;

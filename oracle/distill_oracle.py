@@ -55,7 +55,7 @@ def candidate_backward_ref(H_bits, W_bits, cand, lse, dcand):
 
 
 def divergence_ref(lt, lq, divergence, support, temperature=1.0):
-    """One token: (loss, gradient in lq) over the slots with lt > -1e30."""
+    """One token: (loss, gradient in lq) over the slots with lt > -1e30; with a NaN among them all of it is NaN."""
     lt, lq = np.asarray(lt, dtype=np.float64), np.asarray(lq, dtype=np.float64)
     grad = np.zeros(lt.shape)
     on = np.flatnonzero(~(lt <= ABSENT))
@@ -72,27 +72,33 @@ def divergence_ref(lt, lq, divergence, support, temperature=1.0):
         a, b = np.exp(la), np.exp(lb)
         if divergence == 0:
             grad[on] = tau * (b - a)
-            return tau * tau * sum(x * (u - v) for x, u, v in zip(a, la, lb) if x > 0), grad
-        r = sum(y * (v - u) for y, u, v in zip(b, la, lb) if y > 0)
-        grad[on] = [tau * y * ((v - u) - r) if y > 0 else 0.0 for y, u, v in zip(b, la, lb)]
-        return tau * tau * r, grad
+            loss = tau * tau * sum(x * (u - v) for x, u, v in zip(a, la, lb) if not (x == 0 and not math.isnan(v)))
+        else:
+            r = sum(y * (v - u) for y, u, v in zip(b, la, lb) if not (y == 0 and not math.isnan(u)))
+            grad[on] = [0.0 if y == 0 else tau * y * ((v - u) - r) for y, u, v in zip(b, la, lb)]
+            loss = tau * tau * r
+        if math.isnan(loss):
+            grad[on] = math.nan
+        return loss, grad
     loss = ps = qs = 0.0
     for i in on:
         p, q = math.exp(lt[i]), math.exp(lq[i])
         ps, qs = ps + p, qs + q
         if divergence == 0:
-            loss += p * (lt[i] - lq[i]) if p > 0 else 0.0
+            loss += 0.0 if p == 0 and not math.isnan(lq[i]) else p * (lt[i] - lq[i])
             grad[i] = -p
-        elif q > 0:
+        elif not (q == 0 and not math.isnan(lt[i])):
             loss += q * (lq[i] - lt[i])
             grad[i] = q * (lq[i] - lt[i] + 1.0)
     if support == 2:
-        pr, qr = max(1.0 - ps, TAIL_FLOOR), max(1.0 - qs, TAIL_FLOOR)
+        pr, qr = (TAIL_FLOOR if 1.0 - s < TAIL_FLOOR else 1.0 - s for s in (ps, qs))      # a NaN stays one
         # qr = 1 - sum q, so d qr / d lq_i = -q_i unless it is held at the floor
         slope = 0.0 if 1.0 - qs <= TAIL_FLOOR else (-pr / qr if divergence == 0 else math.log(qr / pr) + 1.0)
         loss += pr * math.log(pr / qr) if divergence == 0 else qr * math.log(qr / pr)
         for i in on:
             grad[i] += slope * -math.exp(lq[i])
+    if math.isnan(loss):                   # a NaN of one slot is the whole token's
+        grad[on] = math.nan
     return loss, grad
 
 

@@ -52,6 +52,13 @@ __device__ __forceinline__ void bulk_store(void* dst, uint32_t src_smem, uint32_
   asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" :: "l"(dst), "r"(src_smem), "r"(bytes) : "memory");
 }
 
+// min(v, 1e30), so that times 0 is 0; a NaN stays one (fminf would drop it).
+__device__ __forceinline__ float finite_above(float v) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(1.0e30f));
+  return r;
+}
+
 // a log(a / b) + b - a with d = log(a / b): the terms of a divergence between two distributions, each of them
 // non-negative.  The b - a sum to nothing, but with them an error of the sums that normalise a and b, which
 // shifts every d alike, no longer moves the result to first order.
@@ -63,7 +70,7 @@ __device__ __forceinline__ float divergence_term(float a, float b, float d) {
   f = fmaf(d, -f, 1.f / 6.f);
   f = fmaf(d, -f, 0.5f);
   const float series = (a * d) * (d * f);
-  const float direct = a > 0.f ? fmaf(a, d, b - a) : b;       // d is infinite where b is 0
+  const float direct = a == 0.f ? b : fmaf(a, d, b - a);      // d is infinite where b is 0; a NaN stays one
   return fabsf(d) < 0.5f ? series : direct;
 }
 
@@ -173,7 +180,7 @@ __device__ __forceinline__ float row_divergence(const float (&lt)[kE], const flo
         g[i] = tau * (b - p);
       } else {
         loss += divergence_term(b, p, -d);
-        a[i] = fminf(d, 1.0e30f);               // kept for the gradient; finite, so that b = 0 gives 0
+        a[i] = finite_above(d);                 // kept for the gradient: b = 0 gives 0
         g[i] = tau * b;
       }
     }
@@ -195,10 +202,10 @@ __device__ __forceinline__ float row_divergence(const float (&lt)[kE], const flo
       ps += p;
       qs += q[i];
       if constexpr (kForward) {
-        loss += p > 0.f ? p * gap : 0.f;        // an infinite gap counts where p > 0 (a NaN in p is in ps too)
+        loss = fmaf(p, p == 0.f ? finite_above(gap) : gap, loss);      // an infinite gap counts where p > 0
         g[i] = -p;
       } else {
-        gap = fminf(gap, 1.0e30f);              // finite: a q of 0 gives 0
+        gap = finite_above(gap);                // a q of 0 gives 0
         loss -= q[i] * gap;
         g[i] = fmaf(-q[i], gap, q[i]);
       }
@@ -346,8 +353,9 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_loss_kernel(
         if (token_loss) token_loss[row] = loss;
       }
       if (dst) {
+        const float scale = loss == loss ? w : loss;     // a NaN of one slot is in all of the token's gradients
 #pragma unroll
-        for (int e = 0; e < kE; ++e) g[e] *= w;
+        for (int e = 0; e < kE; ++e) g[e] *= scale;
         if (staged && bulk_out) {                   // over the row's own slots, to go out in one piece
 #pragma unroll
           for (int e = 0; e < kE / kVec; ++e)
