@@ -410,6 +410,7 @@ af_status af_reserve_candidates(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d
  *   support 0 (as listed):   0: sum p (lt - lq);   1: sum q (lq - lt)
  *   support 1 (renormalised): a = softmax(lt / tau), b = softmax(lq / tau) over the present slots;
  *                            0: tau^2 sum a log(a / b);   1: tau^2 sum b log(b / a)
+ *                            (NaN for a token where the student gives nothing to any present slot: it has no b)
  *   support 2 (with a tail): one more outcome holds the rest of either mass, no less than 2^-16:
  *                            p_r = max(1 - sum p, 2^-16), q_r = max(1 - sum q, 2^-16);
  *                            0: sum p (lt - lq) + p_r log(p_r / q_r);   1: sum q (lq - lt) + q_r log(q_r / p_r)

@@ -129,10 +129,11 @@ __device__ __forceinline__ float group_rest(const float (&v)[kE]) {
   return (float)(1.0 - x);
 }
 
-constexpr float kAbsentLogp = -1.0e30f;      // its exponential is 0, and so is the difference of two of these
+constexpr float kAbsentLogp = -1.0e30f;      // its exponential is 0; finite, so that a row's maximum of these is a number
 
 // The divergence of one row and its gradient: lane `lane` of the group holds the slots lt / lq, absent ones
-// (and those past K) with kAbsentLogp in both, which makes every term of theirs 0.  Returns the row's loss
+// (and those past K) with kAbsentLogp and -inf, which makes every term of theirs 0 (the student's is -inf so that a
+// student with nothing on the present slots does not find its maximum among the absent ones).  Returns the row's loss
 // (all lanes); g receives dloss/dlq; tm and sm gain the lane's share of the teacher's and the student's mass.
 template <int kSupport, bool kForward, int kG, int kE>
 __device__ __forceinline__ float row_divergence(const float (&lt)[kE], const float (&lq)[kE], float tau, float inv_tau,
@@ -164,7 +165,8 @@ __device__ __forceinline__ float row_divergence(const float (&lt)[kE], const flo
       for (int i = 0; i < kE; ++i) { tm += ex2f(lt[i] * kLog2e); sm += ex2f(lq[i] * kLog2e); }
     } else {
       tm = fmaf(ex2f(ma * kLog2e), za, tm);
-      sm = fmaf(ex2f(mb * kLog2e), zb, sm);
+      // a student with nothing on the present slots has no distribution over them (zb is NaN, as the loss is), but a mass
+      if (mb != -INFINITY) sm = fmaf(ex2f(mb * kLog2e), zb, sm);
     }
     za = group_sum<kG>(za);
     zb = group_sum<kG>(zb);
@@ -341,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) distill_loss_kernel(
       for (int e = 0; e < kE; ++e) {
         const bool present = e / kVec < valid && !(lt[e] <= kAbsentLogp);      // a NaN is present
         lt[e] = present ? lt[e] : kAbsentLogp;
-        lq[e] = present ? lq[e] : kAbsentLogp;
+        lq[e] = present ? lq[e] : -INFINITY;
       }
       if (staged && !bulk_out && b == batches - 1) {    // the values are in registers: this warp is done with the stage
         __syncwarp();
