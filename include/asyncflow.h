@@ -415,7 +415,7 @@ af_status af_reserve_candidates(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d
  *                            p_r = max(1 - sum p, 2^-16), q_r = max(1 - sum q, 2^-16);
  *                            0: sum p (lt - lq) + p_r log(p_r / q_r);   1: sum q (lq - lt) + q_r log(q_r / p_r)
  *                            (a q_r held at 2^-16 carries no gradient)
- *   tau = temperature, > 0; it has a meaning for support 1 only and has to be 1 for the others.
+ *   tau = temperature, from 1e-4 to 1e4; it has a meaning for support 1 only and has to be 1 for the others.
  * token_loss[t] is that sum; agg_mode and loss_scale aggregate it exactly as in af_policy_loss:
  * agg_mode 0: loss = loss_scale * mean_i( mean_{t in i} ); 1: loss_scale * mean_t.  dcand[t,k] =
  * dloss / dcand_logp[t,k].  teacher_mass and student_mass are means over tokens of sum p and sum q.
@@ -423,8 +423,8 @@ af_status af_reserve_candidates(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d
  * cand_logp, teacher_logp, dcand (nullable): [T,K] fp32 dev; token_loss (nullable): [T] fp32 dev;
  * cu_seqlens as in af_policy_loss; `out`: device struct.  1 <= K <= AF_MAX_CANDIDATES.  Sums are taken in
  * a fixed order: results are bit-reproducible.
- * Errors: AF_ERR_INVALID_ARG for null pointers, unknown enum values, a temperature that is not finite and
- * positive or not 1 where it has to be; AF_ERR_SHAPE for K or T out of range.
+ * Errors: AF_ERR_INVALID_ARG for null pointers, unknown enum values, a temperature outside 1e-4 to
+ * 1e4 or not 1 where it has to be; AF_ERR_SHAPE for K or T out of range.
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
   int32_t divergence;

@@ -547,7 +547,10 @@ static bool positive_finite(float v) { return v > 0.f && v <= 3.402823466e38f; }
 static af_status distill_params_ok(const af_distill_params& p) {
   if (p.divergence < 0 || p.divergence > 1 || p.support < 0 || p.support > 2 || p.agg_mode < 0 || p.agg_mode > 1)
     return AF_ERR_INVALID_ARG;
-  if (!positive_finite(p.temperature) || (p.support != 1 && p.temperature != 1.f)) return AF_ERR_INVALID_ARG;
+  // within these ends an absent slot's stand-in of -1e30 stays without weight, and 1 / tau and tau^2 are ordinary numbers;
+  // at the upper one a log ratio of 1e-4 is held to three digits, and beyond it to less and less
+  if (!(p.temperature >= 1e-4f && p.temperature <= 1e4f) || (p.support != 1 && p.temperature != 1.f))
+    return AF_ERR_INVALID_ARG;
   return AF_OK;
 }
 
