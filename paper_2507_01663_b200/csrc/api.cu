@@ -100,6 +100,8 @@ af_status af_create(af_ctx** out, int device) {
   af_status st = ws_grow(c->loss_ws, loss_workspace_bytes(c->sm_count));
   if (st == AF_OK && cudaMemset(c->loss_ws.p, 0, c->loss_ws.cap) != cudaSuccess) st = AF_ERR_CUDA;
   if (st == AF_OK) st = ws_grow(c->ctrl_ws, controller_workspace_bytes(c->sm_count));
+  // the caller's stream may be one that does not wait for the default stream, on which the above was zeroed
+  if (st == AF_OK && cudaStreamSynchronize(nullptr) != cudaSuccess) st = AF_ERR_CUDA;
   if (st != AF_OK) { af_destroy(c); return st; }
   *out = c;
   return AF_OK;
@@ -633,15 +635,6 @@ af_status af_distill_update(af_ctx* c, const void* hidden, const void* W, const 
                                HeadGradient{d_W, dW_type, accumulate_dW != 0}, static_cast<cudaStream_t>(stream));
 }
 
-// The workspace of the preference loss starts with a header that a call finds zero and leaves zero.
-static af_status grow_preference_ws(af_ctx* c, int32_t B) {
-  const void* before = c->pref_ws.p;
-  const af_status st = ws_grow(c->pref_ws, preference_workspace_bytes(B));
-  if (st != AF_OK || c->pref_ws.p == before) return st;
-  // waited for: the caller's stream may be one that does not wait for the default stream
-  return cudaMemset(c->pref_ws.p, 0, preference_header_bytes()) == cudaSuccess &&
-         cudaStreamSynchronize(nullptr) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
-}
 static af_status preference_sizes(int64_t T, int32_t B) {
   if (T < 0 || B < 0 || (T > 0 && B < 1)) return AF_ERR_INVALID_ARG;
   return B % 2 != 0 || T > ((int64_t)1 << 31) - 65536 ? AF_ERR_SHAPE : AF_OK;
@@ -659,9 +652,10 @@ af_status af_preference_loss(af_ctx* c, const float* logp, const float* ref_logp
       !(p.label_smoothing >= 0.f && p.label_smoothing < 1.f))
     return AF_ERR_INVALID_ARG;
   DeviceGuard guard(c->device);
-  if ((st = grow_preference_ws(c, B)) != AF_OK) return st;
+  if ((st = ws_grow(c->pref_ws, preference_workspace_bytes(B))) != AF_OK) return st;
   return launch_preference_loss(logp, ref_logp, cu_seqlens, B, T, p, out, pair_loss, seq_score, dlogp, c->pref_ws.p,
-                                c->d_err, c->sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess
+                                reinterpret_cast<char*>(c->d_err) + kPrefHeaderByte, c->d_err, c->sm_count,
+                                static_cast<cudaStream_t>(stream)) == cudaSuccess
              ? AF_OK : AF_ERR_CUDA;
 }
 
@@ -671,7 +665,7 @@ af_status af_reserve_preference(af_ctx* c, int64_t max_T, int32_t max_B) {
   const af_status st = preference_sizes(max_T, max_B);
   if (st != AF_OK) return st;
   DeviceGuard guard(c->device);
-  return grow_preference_ws(c, max_B);
+  return ws_grow(c->pref_ws, preference_workspace_bytes(max_B));
 }
 
 af_status af_controller_put(af_ctx* c, const af_controller_view* table, const int32_t* idx, int64_t n,

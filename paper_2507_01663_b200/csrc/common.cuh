@@ -15,7 +15,8 @@
 namespace af {
 
 constexpr int kPackRing = 8;  // pinned staging slots for af_pack_microbatch metadata
-constexpr int kDeviceBlockBytes = 1024;  // the context's small device block: error word, tile clock, rank slots
+constexpr int kDeviceBlockBytes = 1024;  // the context's small device block, zeroed at af_create: error word, tile clock, rank slots, barriers
+constexpr int kPrefHeaderByte = 256;  // 64 bytes of that block: grid barriers of af_preference_loss, zero between calls
 constexpr int kTileClockWord = 16;  // word of that block used as the GEMM tile clock
 constexpr int kDieCounterWord = 17;  // two words behind the clock: the per-die rank counters of a GEMM launch
 constexpr int kDieTableByte = 512;   // 256 bytes of that block: die (0 / 1) of every SM id, measured at af_create
@@ -255,11 +256,10 @@ af_status launch_distill_update(af_ctx* ctx, const void* hidden, const void* W, 
 af_status reserve_distill_update(af_ctx* ctx, int64_t T, int32_t K, int32_t V);
 
 size_t preference_workspace_bytes(int32_t B);
-size_t preference_header_bytes();     // the start of it, zero before the first call
 cudaError_t launch_preference_loss(const float* logp, const float* ref_logp, const int32_t* cu, int32_t B, int64_t T,
                                    const af_preference_params& p, af_preference_out* out, float* pair_loss,
-                                   float* seq_score, float* dlogp, void* ws, unsigned int* d_err, int sm_count,
-                                   cudaStream_t s);
+                                   float* seq_score, float* dlogp, void* ws, void* header, unsigned int* d_err,
+                                   int sm_count, cudaStream_t s);
 
 af_status launch_backward(af_ctx* ctx, const void* hidden, const void* W, const int32_t* target,
                           const float* lse, const float* dlogp, int64_t T, int32_t d, int32_t V,

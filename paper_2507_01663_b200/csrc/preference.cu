@@ -40,13 +40,13 @@ constexpr int kSmemBytes = kWarps * kStages * kStageBytes + 128 /*alignment*/ + 
 constexpr int kNumSums = 6;                 // loss, pair loss, nll, accuracy, chosen score, rejected score
 constexpr int kMaxBlocks = 1024;
 
-struct PrefHeader {                         // zero between calls
+struct PrefHeader {                         // in the context's device block; zero between calls
   unsigned int arrived;                     // blocks at the grid barriers (counts up through both)
   unsigned int left;                        // blocks that are done
   unsigned int failed;                      // a barrier's wait ran out
   unsigned int pad[13];
 };
-struct PrefWs {                             // device views into the workspace
+struct PrefWs {                             // device views into the workspace, and the header
   PrefHeader* header;
   double2* seq;                             // [B] sums of the sequences that lie inside one range: S, sum of logp
   double2* head;                            // [workers] piece of the sequence that comes into the range
@@ -57,14 +57,14 @@ struct PrefWs {                             // device views into the workspace
 
 int64_t steps_of(int64_t T) { return (T + kStep - 1) / kStep; }
 
-PrefWs carve(void* ws, int32_t B) {
+PrefWs carve(void* ws, void* header, int32_t B) {
   PrefWs w;
-  w.header = static_cast<PrefHeader*>(ws);
-  w.partial = reinterpret_cast<double*>(w.header + 1);
-  w.head = reinterpret_cast<double2*>(w.partial + (size_t)kMaxBlocks * kNumSums);
+  w.header = static_cast<PrefHeader*>(header);
+  w.head = static_cast<double2*>(ws);
   w.tail = w.head + kMaxBlocks * kWarps;
   w.seq = w.tail + kMaxBlocks * kWarps;
-  w.coef = reinterpret_cast<float*>(w.seq + B);
+  w.partial = reinterpret_cast<double*>(w.seq + B);
+  w.coef = reinterpret_cast<float*>(w.partial + (size_t)kMaxBlocks * kNumSums);
   return w;
 }
 
@@ -560,17 +560,18 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) preference_kernel(
 }  // namespace
 
 size_t preference_workspace_bytes(int32_t B) {
-  return sizeof(PrefHeader) + (size_t)kMaxBlocks * (kNumSums * sizeof(double) + 2 * kWarps * sizeof(double2)) +
+  return (size_t)kMaxBlocks * (kNumSums * sizeof(double) + 2 * kWarps * sizeof(double2)) +
          (size_t)B * (sizeof(double2) + sizeof(float));
 }
-size_t preference_header_bytes() { return sizeof(PrefHeader); }
+static_assert(sizeof(PrefHeader) == 64 && kPrefHeaderByte % 128 == 0 && kPrefHeaderByte + 128 <= kDieTableByte,
+              "the header has a line of the device block to itself");
 
 cudaError_t launch_preference_loss(const float* logp, const float* ref_logp, const int32_t* cu, int32_t B, int64_t T,
                                    const af_preference_params& p, af_preference_out* out, float* pair_loss,
-                                   float* seq_score, float* dlogp, void* ws_mem, unsigned int* d_err, int sm_count,
-                                   cudaStream_t s) {
+                                   float* seq_score, float* dlogp, void* ws_mem, void* header, unsigned int* d_err,
+                                   int sm_count, cudaStream_t s) {
   auto al = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
-  PrefWs ws = carve(ws_mem, B);
+  PrefWs ws = carve(ws_mem, header, B);
   static SmemAttrOnce once;
   const cudaError_t e = set_smem_once(once, preference_kernel, kSmemBytes);
   if (e != cudaSuccess) return e;
