@@ -157,7 +157,7 @@ def preference_loss_ref(logp, ref_logp, cu, kind=0, beta=0.1, label_smoothing=0.
         elif kind == 1:
             value, slope = ((x - 0.5) / beta) ** 2, 2.0 * (x - 0.5) / beta ** 2
         else:
-            value, slope = max(0.0, 1.0 - x), -1.0 if x < 1.0 else 0.0
+            value, slope = (1.0 - x, -1.0) if x < 1.0 else (0.0, 0.0) if x >= 1.0 else (x, x)      # a NaN stays one
         nll = -math.fsum(logp[rows[c]]) / n[c] if n[c] else 0.0
         pair[p] = value + nll_coef * nll
         dlogp[rows[c]] += loss_scale / P * (slope * beta * share[c] - nll_coef / max(n[c], 1))

@@ -440,8 +440,8 @@ __device__ __forceinline__ void pair_terms(const int32_t* __restrict__ cu, int B
       l = y * y;
       slope = 2.0 * y / beta;
     } else {
-      l = x < 1.0 ? 1.0 - x : x >= 1.0 ? 0.0 : x;        // a NaN stays one
-      slope = x < 1.0 ? -1.0 : 0.0;
+      l = x < 1.0 ? 1.0 - x : x >= 1.0 ? 0.0 : x;        // a NaN stays one, here and in the gradient
+      slope = x < 1.0 ? -1.0 : x >= 1.0 ? 0.0 : x;
     }
     const double nll = -sc.y * per_c, nll_coef = (double)prm.nll_coef;
     const double whole = nll_coef != 0.0 ? l + nll_coef * nll : l;
