@@ -152,14 +152,14 @@ def preference_loss_ref(logp, ref_logp, cu, kind=0, beta=0.1, label_smoothing=0.
                 return -math.log1p(math.exp(-v)) if v > 0 else v - math.log1p(math.exp(v))
 
             s = math.exp(log_sigmoid(x))
-            value = -(1 - label_smoothing) * log_sigmoid(x) - label_smoothing * log_sigmoid(-x)
+            value = -(1 - label_smoothing) * log_sigmoid(x) - (label_smoothing * log_sigmoid(-x) if label_smoothing else 0.0)
             slope = -(1 - label_smoothing) * (1 - s) + label_smoothing * s
         elif kind == 1:
             value, slope = ((x - 0.5) / beta) ** 2, 2.0 * (x - 0.5) / beta ** 2
         else:
             value, slope = (1.0 - x, -1.0) if x < 1.0 else (0.0, 0.0) if x >= 1.0 else (x, x)      # a NaN stays one
         nll = -math.fsum(logp[rows[c]]) / n[c] if n[c] else 0.0
-        pair[p] = value + nll_coef * nll
+        pair[p] = value + (nll_coef * nll if nll_coef else 0.0)
         dlogp[rows[c]] += loss_scale / P * (slope * beta * share[c] - nll_coef / max(n[c], 1))
         dlogp[rows[r]] -= loss_scale / P * slope * beta * share[r]
         ls.append(value), nlls.append(nll), wins.append(score[c] > score[r])

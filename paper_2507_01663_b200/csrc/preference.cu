@@ -433,7 +433,7 @@ __device__ __forceinline__ void pair_terms(const int32_t* __restrict__ cu, int B
     double l, slope;
     if (prm.kind == 0) {
       const double eps = (double)prm.label_smoothing;
-      l = log1p(exp(-fabs(x))) + (x < 0.0 ? -x : 0.0) + (eps > 0.0 ? eps * x : 0.0);
+      l = log1p(exp(-fabs(x))) + (x < 0.0 ? (eps - 1.0) * x : eps > 0.0 ? eps * x : 0.0);     // no two infinities meet
       slope = eps - 1.0 / (1.0 + exp(x));
     } else if (prm.kind == 1) {
       const double y = (x - 0.5) / beta;
