@@ -47,21 +47,25 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// m = max z, s = sum 2^x, u = sum 2^x x with x = (z - m) log2 e.  u is taken about the maximum, so that the entropy,
+// log s - log 2 u / s, does not come out as a small difference of two numbers of the size of the logits.
 struct SoftmaxState {
   float m, s, u;
   __device__ __forceinline__ void add(float z) {
     const float m_new = fmaxf(m, z);
-    const float sc = ex2f((m - m_new) * kLog2e), e = ex2f((z - m_new) * kLog2e);
+    const float dm = (m - m_new) * kLog2e, x = (z - m_new) * kLog2e;
+    const float sc = ex2f(dm), e = ex2f(x);
+    u = fmaf(fmaf(s, dm, u), sc, e * x);
     s = fmaf(s, sc, e);
-    u = fmaf(u, sc, e * z);
     m = m_new;
   }
   // states of nothing have m = kNone (finite, so that differences stay numbers)
   __device__ __forceinline__ void join(float m2, float s2, float u2) {
     const float m_new = fmaxf(m, m2);
-    const float a = ex2f((m - m_new) * kLog2e), b = ex2f((m2 - m_new) * kLog2e);
+    const float da = (m - m_new) * kLog2e, db = (m2 - m_new) * kLog2e;
+    const float a = ex2f(da), b = ex2f(db);
+    u = fmaf(fmaf(s, da, u), a, fmaf(s2, db, u2) * b);
     s = fmaf(s, a, s2 * b);
-    u = fmaf(u, a, u2 * b);
     m = m_new;
   }
 };
@@ -231,10 +235,10 @@ __global__ void __launch_bounds__(kThreads, 1) candidate_stream_kernel(
     for (int o = 16; o > 0; o >>= 1)
       a.join(__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.s, o),
              __shfl_xor_sync(0xffffffffu, a.u, o));
-    const float lse = a.m + logf(a.s);
+    const float log_s = logf(a.s), lse = a.m + log_s;
     if (lane == 0) {
       if (lse_out) lse_out[tok] = lse;
-      if (entropy) entropy[tok] = lse - a.u / a.s;
+      if (entropy) entropy[tok] = log_s - a.u / (a.s * kLog2e);
     }
     for (int k = lane; k < K; k += 32) {
       const int id = __ldg(cand + (size_t)tok * K + k);
