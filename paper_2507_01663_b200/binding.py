@@ -179,15 +179,6 @@ def _stream(stream) -> C.c_void_p:
     return C.c_void_p(s.cuda_stream)
 
 
-def _addr(t: Optional[torch.Tensor]):
-    """As _ptr, as the plain integer that ctypes converts by itself (these calls can be a few microseconds long)."""
-    if t is None:
-        return None
-    if t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError("device buffers must be contiguous CUDA tensors")
-
-
 def _check(status: int, where: str):
     if status != AF_OK:
         raise AfError(status, where)
@@ -377,6 +368,39 @@ class Context:
                                          _ptr(d_W), int(accumulate_dW), _stream(stream)), "af_policy_update")
 
     # -- listed candidates, distillation, preferences ----------------------------------------------
+    # Every tensor of these calls is checked against the batch: its type, that it holds what the call reads or writes, and
+    # that it lies in one piece on the context's device.
+    def _addr(self, t: Optional[torch.Tensor]):
+        """As _ptr, as the plain integer that ctypes converts by itself (these calls can be a few microseconds long)."""
+        if t is None:
+            return None
+        if t.get_device() == self.device and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError("device buffers must be contiguous CUDA tensors on the context's device")
+
+    def _floats(self, t: Optional[torch.Tensor], n: int):
+        """Address of at least n float32 values."""
+        if t is not None and (t.dtype is not torch.float32 or t.numel() < n):
+            raise ValueError("per-token, per-pair and per-sequence values are float32, one for each")
+        return self._addr(t)
+
+    def _record(self, out: torch.Tensor, struct):
+        """Address of a result record; its last field is a 64-bit count."""
+        if out.numel() * out.element_size() < C.sizeof(struct) or out.data_ptr() % 8 != 0:
+            raise ValueError(f"out holds at least {C.sizeof(struct)} bytes and starts on a multiple of 8")
+        return self._addr(out)
+
+    @staticmethod
+    def _head(hidden, W, T: int, d_hidden=None, d_W=None):
+        """(d, V) of bfloat16 hidden rows [T, d] and W [V, d], and of their gradients' buffers."""
+        V, d = W.shape
+        for t in (hidden, d_hidden):
+            if t is not None and (t.dtype is not torch.bfloat16 or t.dim() != 2 or t.shape[0] < T or t.shape[1] != d):
+                raise ValueError("hidden and d_hidden are bfloat16 [T, d]")
+        if W.dtype is not torch.bfloat16 or (d_W is not None and d_W.shape != W.shape):
+            raise ValueError("W is bfloat16 [V, d], and d_W has its shape")
+        return d, V
+
     def _stream_of(self, stream) -> int:
         """The given stream, or the context's device's current one."""
         return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
@@ -396,11 +420,11 @@ class Context:
         return cu_seqlens.shape[0] - 1 if B is None else B
 
     @staticmethod
-    def _list_width(cand: torch.Tensor, T: int, *others: Optional[torch.Tensor]) -> int:
-        """K of [T, K] lists of 4-byte ids or values; every other tensor is float32, equally wide, with enough rows."""
-        shape = cand.shape
-        if len(shape) != 2 or shape[0] < T or cand.element_size() != 4:
-            raise ValueError("candidate lists are [T, K] with 4-byte elements")
+    def _list_width(lists: torch.Tensor, dtype: torch.dtype, T: int, *others: Optional[torch.Tensor]) -> int:
+        """K of [T, K] lists of int32 ids or float32 values; every other tensor is float32, equally wide, with enough rows."""
+        shape = lists.shape
+        if len(shape) != 2 or shape[0] < T or lists.dtype is not dtype:
+            raise ValueError(f"the lists are {dtype} [T, K]")
         for o in others:
             if o is not None and (o.dtype is not torch.float32 or
                                   (o.shape != shape and (o.dim() != 2 or o.shape[0] < T or o.shape[1] != shape[1]))):
@@ -410,20 +434,22 @@ class Context:
     def candidate_logprob(self, hidden, W, cand, cand_logp, entropy=None, lse=None, T=None, stream=None):
         """``cand``: int32 [T, K] vocabulary ids (below 0: unused slot); ``cand_logp``: float32 [T, K]."""
         T = hidden.shape[0] if T is None else T
-        d, V = W.shape[1], W.shape[0]
-        K = self._list_width(cand, T, cand_logp)
-        _check(self.lib.af_candidate_logprob(self.handle, _addr(hidden), _addr(W), _addr(cand), T, K, d, V,
-                                             _addr(cand_logp), _addr(entropy), _addr(lse), self._stream_of(stream)),
+        d, V = self._head(hidden, W, T)
+        K = self._list_width(cand, torch.int32, T, cand_logp)
+        at = self._addr
+        _check(self.lib.af_candidate_logprob(self.handle, at(hidden), at(W), at(cand), T, K, d, V, at(cand_logp),
+                                             self._floats(entropy, T), self._floats(lse, T), self._stream_of(stream)),
                "af_candidate_logprob")
 
     def candidate_logprob_backward(self, hidden, W, cand, lse, dcand, d_hidden, d_W=None, accumulate_dW=False, T=None,
                                    stream=None):
         """``d_W``: float32 or bfloat16 [V, d], or None (a frozen head)."""
         T = hidden.shape[0] if T is None else T
-        d, V = W.shape[1], W.shape[0]
-        K = self._list_width(cand, T, dcand)
-        _check(self.lib.af_candidate_logprob_backward(self.handle, _addr(hidden), _addr(W), _addr(cand), _addr(lse),
-                                                      _addr(dcand), T, K, d, V, _addr(d_hidden), _addr(d_W),
+        d, V = self._head(hidden, W, T, d_hidden, d_W)
+        K = self._list_width(cand, torch.int32, T, dcand)
+        at = self._addr
+        _check(self.lib.af_candidate_logprob_backward(self.handle, at(hidden), at(W), at(cand), self._floats(lse, T),
+                                                      at(dcand), T, K, d, V, at(d_hidden), at(d_W),
                                                       self._dtype(d_W), int(accumulate_dW), self._stream_of(stream)),
                "af_candidate_logprob_backward")
 
@@ -437,10 +463,12 @@ class Context:
         """``out``: device uint8 tensor of ``ctypes.sizeof(DistillOut)`` bytes (see read_distill_out)."""
         B = self._sequences(cu_seqlens, B)
         T = cand_logp.shape[0] if T is None else T
-        K = self._list_width(cand_logp, T, teacher_logp, dcand)
+        K = self._list_width(cand_logp, torch.float32, T, teacher_logp, dcand)
         prm = DistillParams(divergence, support, agg_mode, temperature, loss_scale)
-        _check(self.lib.af_distill_loss(self.handle, _addr(cand_logp), _addr(teacher_logp), _addr(cu_seqlens), B, T, K,
-                                        C.byref(prm), _addr(out), _addr(token_loss), _addr(dcand), self._stream_of(stream)),
+        at = self._addr
+        _check(self.lib.af_distill_loss(self.handle, at(cand_logp), at(teacher_logp), at(cu_seqlens), B, T, K, C.byref(prm),
+                                        self._record(out, DistillOut), self._floats(token_loss, T), at(dcand),
+                                        self._stream_of(stream)),
                "af_distill_loss")
 
     def distill_update(self, hidden, W, cand, teacher_logp, cu_seqlens, out, cand_logp, lse, d_hidden, d_W=None,
@@ -449,13 +477,14 @@ class Context:
         """``af_distill_update``: scoring, distillation loss and backward of one packed micro-batch."""
         B = self._sequences(cu_seqlens, B)
         T = hidden.shape[0] if T is None else T
-        d, V = W.shape[1], W.shape[0]
-        K = self._list_width(cand, T, teacher_logp, cand_logp, dcand)
+        d, V = self._head(hidden, W, T, d_hidden, d_W)
+        K = self._list_width(cand, torch.int32, T, teacher_logp, cand_logp, dcand)
         prm = DistillParams(divergence, support, agg_mode, temperature, loss_scale)
-        _check(self.lib.af_distill_update(self.handle, _addr(hidden), _addr(W), _addr(cand), _addr(teacher_logp),
-                                          _addr(cu_seqlens), B, T, K, d, V, C.byref(prm), _addr(out), _addr(cand_logp),
-                                          _addr(entropy), _addr(lse), _addr(token_loss), _addr(dcand), _addr(d_hidden),
-                                          _addr(d_W), self._dtype(d_W), int(accumulate_dW), self._stream_of(stream)),
+        at, floats = self._addr, self._floats
+        _check(self.lib.af_distill_update(self.handle, at(hidden), at(W), at(cand), at(teacher_logp), at(cu_seqlens), B, T, K,
+                                          d, V, C.byref(prm), self._record(out, DistillOut), at(cand_logp),
+                                          floats(entropy, T), floats(lse, T), floats(token_loss, T), at(dcand), at(d_hidden),
+                                          at(d_W), self._dtype(d_W), int(accumulate_dW), self._stream_of(stream)),
                "af_distill_update")
 
     def preference_loss(self, logp, ref_logp, cu_seqlens, out, pair_loss=None, seq_score=None, dlogp=None, kind=0,
@@ -465,11 +494,11 @@ class Context:
         bytes (see read_preference_out)."""
         B = self._sequences(cu_seqlens, B)
         T = logp.shape[0] if T is None else T
-        if logp.dtype != torch.float32 or (ref_logp is not None and ref_logp.dtype != torch.float32):
-            raise ValueError("log-probs are float32")
         prm = PreferenceParams(kind, int(length_norm), pair_layout, beta, label_smoothing, margin, nll_coef, loss_scale)
-        _check(self.lib.af_preference_loss(self.handle, _addr(logp), _addr(ref_logp), _addr(cu_seqlens), B, T, C.byref(prm),
-                                           _addr(out), _addr(pair_loss), _addr(seq_score), _addr(dlogp), self._stream_of(stream)),
+        floats = self._floats
+        _check(self.lib.af_preference_loss(self.handle, floats(logp, T), floats(ref_logp, T), self._addr(cu_seqlens), B, T,
+                                           C.byref(prm), self._record(out, PreferenceOut), floats(pair_loss, B // 2),
+                                           floats(seq_score, B), floats(dlogp, T), self._stream_of(stream)),
                "af_preference_loss")
 
     def reserve_preference(self, max_T: int, max_B: int):
