@@ -89,6 +89,9 @@ class PreferenceOut(C.Structure):
                 ("chosen_score", C.c_float), ("rejected_score", C.c_float), ("n_pairs", C.c_int64)]
 
 
+_DISTILL_OUT_BYTES, _PREFERENCE_OUT_BYTES = C.sizeof(DistillOut), C.sizeof(PreferenceOut)
+
+
 class ControllerView(C.Structure):
     _fields_ = [("n_samples", C.c_int64), ("ready", C.c_void_p), ("consumed", C.c_void_p), ("length", C.c_void_p)]
 
@@ -368,38 +371,35 @@ class Context:
                                          _ptr(d_W), int(accumulate_dW), _stream(stream)), "af_policy_update")
 
     # -- listed candidates, distillation, preferences ----------------------------------------------
-    # Every tensor of these calls is checked against the batch: its type, that it holds what the call reads or writes, and
-    # that it lies in one piece on the context's device.
-    def _addr(self, t: Optional[torch.Tensor]):
-        """As _ptr, as the plain integer that ctypes converts by itself (these calls can be a few microseconds long)."""
+    # Every tensor of these calls is checked against the batch on the way to its address: its type, that it holds what the call
+    # reads or writes, and that it lies in one piece on the context's device.  Addresses are plain integers, which ctypes
+    # converts by itself, and each check asks a tensor for as little as it can: a call can be a few microseconds long.
+    def _array(self, t: Optional[torch.Tensor], dtype: torch.dtype, nbytes: int):
+        """Address of at least nbytes of values of a type; None for None."""
         if t is None:
             return None
-        if t.get_device() == self.device and t.is_contiguous():
+        if t.dtype is dtype and t.nbytes >= nbytes and t.get_device() == self.device and t.is_contiguous():
             return t.data_ptr()
-        raise ValueError("device buffers must be contiguous CUDA tensors on the context's device")
+        raise ValueError(f"expected contiguous {dtype} of at least {nbytes} bytes on device {self.device}, "
+                         f"not {t.dtype} {list(t.shape)} on {t.device}")
 
-    def _floats(self, t: Optional[torch.Tensor], n: int):
-        """Address of at least n float32 values."""
-        if t is not None and (t.dtype is not torch.float32 or t.numel() < n):
-            raise ValueError("per-token, per-pair and per-sequence values are float32, one for each")
-        return self._addr(t)
+    def _matrix(self, t: Optional[torch.Tensor], dtype: torch.dtype, rows: int, cols: int):
+        """Address of a matrix of exactly `cols` columns and at least `rows` rows; None for None."""
+        if t is None:
+            return None
+        shape = t.shape
+        if (t.dtype is dtype and len(shape) == 2 and shape[1] == cols and shape[0] >= rows and
+                t.get_device() == self.device and t.is_contiguous()):
+            return t.data_ptr()
+        raise ValueError(f"expected contiguous {dtype} [{rows}, {cols}] on device {self.device}, "
+                         f"not {t.dtype} {list(shape)} on {t.device}")
 
-    def _record(self, out: torch.Tensor, struct):
+    def _record(self, out: torch.Tensor, nbytes: int):
         """Address of a result record; its last field is a 64-bit count."""
-        if out.numel() * out.element_size() < C.sizeof(struct) or out.data_ptr() % 8 != 0:
-            raise ValueError(f"out holds at least {C.sizeof(struct)} bytes and starts on a multiple of 8")
-        return self._addr(out)
-
-    @staticmethod
-    def _head(hidden, W, T: int, d_hidden=None, d_W=None):
-        """(d, V) of bfloat16 hidden rows [T, d] and W [V, d], and of their gradients' buffers."""
-        V, d = W.shape
-        for t in (hidden, d_hidden):
-            if t is not None and (t.dtype is not torch.bfloat16 or t.dim() != 2 or t.shape[0] < T or t.shape[1] != d):
-                raise ValueError("hidden and d_hidden are bfloat16 [T, d]")
-        if W.dtype is not torch.bfloat16 or (d_W is not None and d_W.shape != W.shape):
-            raise ValueError("W is bfloat16 [V, d], and d_W has its shape")
-        return d, V
+        at = self._array(out, out.dtype, nbytes)
+        if at & 7:
+            raise ValueError("a result record starts on a multiple of 8 bytes")
+        return at
 
     def _stream_of(self, stream) -> int:
         """The given stream, or the context's device's current one."""
@@ -419,38 +419,27 @@ class Context:
             raise ValueError("cu_seqlens is int32 with B + 1 entries")
         return cu_seqlens.shape[0] - 1 if B is None else B
 
-    @staticmethod
-    def _list_width(lists: torch.Tensor, dtype: torch.dtype, T: int, *others: Optional[torch.Tensor]) -> int:
-        """K of [T, K] lists of int32 ids or float32 values; every other tensor is float32, equally wide, with enough rows."""
-        shape = lists.shape
-        if len(shape) != 2 or shape[0] < T or lists.dtype is not dtype:
-            raise ValueError(f"the lists are {dtype} [T, K]")
-        for o in others:
-            if o is not None and (o.dtype is not torch.float32 or
-                                  (o.shape != shape and (o.dim() != 2 or o.shape[0] < T or o.shape[1] != shape[1]))):
-                raise ValueError("tensors over the candidate lists are float32 [T, K] like the lists")
-        return shape[1]
-
     def candidate_logprob(self, hidden, W, cand, cand_logp, entropy=None, lse=None, T=None, stream=None):
         """``cand``: int32 [T, K] vocabulary ids (below 0: unused slot); ``cand_logp``: float32 [T, K]."""
         T = hidden.shape[0] if T is None else T
-        d, V = self._head(hidden, W, T)
-        K = self._list_width(cand, torch.int32, T, cand_logp)
-        at = self._addr
-        _check(self.lib.af_candidate_logprob(self.handle, at(hidden), at(W), at(cand), T, K, d, V, at(cand_logp),
-                                             self._floats(entropy, T), self._floats(lse, T), self._stream_of(stream)),
+        (V, d), K = W.shape, cand.shape[-1]
+        array, matrix, bf16, f32 = self._array, self._matrix, torch.bfloat16, torch.float32
+        _check(self.lib.af_candidate_logprob(self.handle, matrix(hidden, bf16, T, d), matrix(W, bf16, V, d),
+                                             matrix(cand, torch.int32, T, K), T, K, d, V, matrix(cand_logp, f32, T, K),
+                                             array(entropy, f32, 4 * T), array(lse, f32, 4 * T), self._stream_of(stream)),
                "af_candidate_logprob")
 
     def candidate_logprob_backward(self, hidden, W, cand, lse, dcand, d_hidden, d_W=None, accumulate_dW=False, T=None,
                                    stream=None):
         """``d_W``: float32 or bfloat16 [V, d], or None (a frozen head)."""
         T = hidden.shape[0] if T is None else T
-        d, V = self._head(hidden, W, T, d_hidden, d_W)
-        K = self._list_width(cand, torch.int32, T, dcand)
-        at = self._addr
-        _check(self.lib.af_candidate_logprob_backward(self.handle, at(hidden), at(W), at(cand), self._floats(lse, T),
-                                                      at(dcand), T, K, d, V, at(d_hidden), at(d_W),
-                                                      self._dtype(d_W), int(accumulate_dW), self._stream_of(stream)),
+        (V, d), K = W.shape, cand.shape[-1]
+        matrix, bf16, f32 = self._matrix, torch.bfloat16, torch.float32
+        dW_type = self._dtype(d_W)
+        _check(self.lib.af_candidate_logprob_backward(
+            self.handle, matrix(hidden, bf16, T, d), matrix(W, bf16, V, d), matrix(cand, torch.int32, T, K),
+            self._array(lse, f32, 4 * T), matrix(dcand, f32, T, K), T, K, d, V, matrix(d_hidden, bf16, T, d),
+            matrix(d_W, bf16 if dW_type else f32, V, d), dW_type, int(accumulate_dW), self._stream_of(stream)),
                "af_candidate_logprob_backward")
 
     def reserve_candidates(self, max_T: int, K: int, d: int, V: int, with_backward=0, dW_type: int = F32):
@@ -462,13 +451,13 @@ class Context:
                      temperature=1.0, agg_mode=0, loss_scale=1.0, B=None, T=None, stream=None):
         """``out``: device uint8 tensor of ``ctypes.sizeof(DistillOut)`` bytes (see read_distill_out)."""
         B = self._sequences(cu_seqlens, B)
-        T = cand_logp.shape[0] if T is None else T
-        K = self._list_width(cand_logp, torch.float32, T, teacher_logp, dcand)
+        T, K = cand_logp.shape[0] if T is None else T, cand_logp.shape[-1]
+        array, matrix, f32 = self._array, self._matrix, torch.float32
         prm = DistillParams(divergence, support, agg_mode, temperature, loss_scale)
-        at = self._addr
-        _check(self.lib.af_distill_loss(self.handle, at(cand_logp), at(teacher_logp), at(cu_seqlens), B, T, K, C.byref(prm),
-                                        self._record(out, DistillOut), self._floats(token_loss, T), at(dcand),
-                                        self._stream_of(stream)),
+        _check(self.lib.af_distill_loss(self.handle, matrix(cand_logp, f32, T, K), matrix(teacher_logp, f32, T, K),
+                                        array(cu_seqlens, torch.int32, 0), B, T, K, C.byref(prm),
+                                        self._record(out, _DISTILL_OUT_BYTES), array(token_loss, f32, 4 * T),
+                                        matrix(dcand, f32, T, K), self._stream_of(stream)),
                "af_distill_loss")
 
     def distill_update(self, hidden, W, cand, teacher_logp, cu_seqlens, out, cand_logp, lse, d_hidden, d_W=None,
@@ -477,14 +466,16 @@ class Context:
         """``af_distill_update``: scoring, distillation loss and backward of one packed micro-batch."""
         B = self._sequences(cu_seqlens, B)
         T = hidden.shape[0] if T is None else T
-        d, V = self._head(hidden, W, T, d_hidden, d_W)
-        K = self._list_width(cand, torch.int32, T, teacher_logp, cand_logp, dcand)
+        (V, d), K = W.shape, cand.shape[-1]
+        array, matrix, bf16, f32 = self._array, self._matrix, torch.bfloat16, torch.float32
+        dW_type = self._dtype(d_W)
         prm = DistillParams(divergence, support, agg_mode, temperature, loss_scale)
-        at, floats = self._addr, self._floats
-        _check(self.lib.af_distill_update(self.handle, at(hidden), at(W), at(cand), at(teacher_logp), at(cu_seqlens), B, T, K,
-                                          d, V, C.byref(prm), self._record(out, DistillOut), at(cand_logp),
-                                          floats(entropy, T), floats(lse, T), floats(token_loss, T), at(dcand), at(d_hidden),
-                                          at(d_W), self._dtype(d_W), int(accumulate_dW), self._stream_of(stream)),
+        _check(self.lib.af_distill_update(
+            self.handle, matrix(hidden, bf16, T, d), matrix(W, bf16, V, d), matrix(cand, torch.int32, T, K),
+            matrix(teacher_logp, f32, T, K), array(cu_seqlens, torch.int32, 0), B, T, K, d, V, C.byref(prm),
+            self._record(out, _DISTILL_OUT_BYTES), matrix(cand_logp, f32, T, K), array(entropy, f32, 4 * T),
+            array(lse, f32, 4 * T), array(token_loss, f32, 4 * T), matrix(dcand, f32, T, K), matrix(d_hidden, bf16, T, d),
+            matrix(d_W, bf16 if dW_type else f32, V, d), dW_type, int(accumulate_dW), self._stream_of(stream)),
                "af_distill_update")
 
     def preference_loss(self, logp, ref_logp, cu_seqlens, out, pair_loss=None, seq_score=None, dlogp=None, kind=0,
@@ -494,11 +485,12 @@ class Context:
         bytes (see read_preference_out)."""
         B = self._sequences(cu_seqlens, B)
         T = logp.shape[0] if T is None else T
+        array, f32 = self._array, torch.float32
         prm = PreferenceParams(kind, int(length_norm), pair_layout, beta, label_smoothing, margin, nll_coef, loss_scale)
-        floats = self._floats
-        _check(self.lib.af_preference_loss(self.handle, floats(logp, T), floats(ref_logp, T), self._addr(cu_seqlens), B, T,
-                                           C.byref(prm), self._record(out, PreferenceOut), floats(pair_loss, B // 2),
-                                           floats(seq_score, B), floats(dlogp, T), self._stream_of(stream)),
+        _check(self.lib.af_preference_loss(self.handle, array(logp, f32, 4 * T), array(ref_logp, f32, 4 * T),
+                                           array(cu_seqlens, torch.int32, 0), B, T, C.byref(prm),
+                                           self._record(out, _PREFERENCE_OUT_BYTES), array(pair_loss, f32, 4 * (B // 2)),
+                                           array(seq_score, f32, 4 * B), array(dlogp, f32, 4 * T), self._stream_of(stream)),
                "af_preference_loss")
 
     def reserve_preference(self, max_T: int, max_B: int):
