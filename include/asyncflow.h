@@ -424,7 +424,7 @@ af_status af_reserve_candidates(af_ctx* ctx, int64_t max_T, int32_t K, int32_t d
  * cu_seqlens as in af_policy_loss; `out`: device struct.  1 <= K <= AF_MAX_CANDIDATES.  Sums are taken in
  * a fixed order: results are bit-reproducible.
  * Errors: AF_ERR_INVALID_ARG for null pointers, unknown enum values, a temperature outside 1e-4 to
- * 1e4 or not 1 where it has to be; AF_ERR_SHAPE for K or T out of range.
+ * 1e4 or not 1 where it has to be; AF_ERR_SHAPE for K out of range, B > 2^30 or T > 2^31 - 65536.
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
   int32_t divergence;
@@ -487,7 +487,7 @@ af_status af_distill_update(af_ctx* ctx, const void* hidden, const void* W, cons
  * results are bit-reproducible.  Workspace: 20 bytes per sequence and 0.3 MB, grown on demand or by
  * af_reserve_preference.
  * Errors: AF_ERR_INVALID_ARG for null pointers, unknown enum values, beta not finite and positive,
- * label_smoothing outside [0, 1); AF_ERR_SHAPE for an odd B or T >= 2^31 - 65536.
+ * label_smoothing outside [0, 1); AF_ERR_SHAPE for B odd or above 2^30 or T > 2^31 - 65536.
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
   int32_t kind;

@@ -545,6 +545,8 @@ static af_status candidate_head(const void* hidden, const void* W, const void* d
   if (!aligned16(hidden) || !aligned16(W) || !aligned16(d_hidden) || !aligned16(d_W)) return AF_ERR_ALIGNMENT;
   return AF_OK;
 }
+// Searches in cu_seqlens and loops over it add 32-bit numbers of up to B and a grid's threads.
+constexpr int32_t kMaxSequences = 1 << 30;
 static bool positive_finite(float v) { return v > 0.f && v <= 3.402823466e38f; }
 static af_status distill_params_ok(const af_distill_params& p) {
   if (p.divergence < 0 || p.divergence > 1 || p.support < 0 || p.support > 2 || p.agg_mode < 0 || p.agg_mode > 1)
@@ -606,7 +608,7 @@ af_status af_distill_loss(af_ctx* c, const float* cand_logp, const float* teache
   NvtxRange range("af_distill_loss");
   if (!c || !params || !out || !cu_seqlens || B < 0 || T < 0 || K < 1) return AF_ERR_INVALID_ARG;
   if (T > 0 && (!cand_logp || !teacher_logp || B < 1)) return AF_ERR_INVALID_ARG;
-  if (K > AF_MAX_CANDIDATES || T > ((int64_t)1 << 31) - 65536) return AF_ERR_SHAPE;
+  if (K > AF_MAX_CANDIDATES || B > kMaxSequences || T > ((int64_t)1 << 31) - 65536) return AF_ERR_SHAPE;
   const af_status st = distill_params_ok(*params);
   if (st != AF_OK) return st;
   DeviceGuard guard(c->device);
@@ -626,7 +628,7 @@ af_status af_distill_update(af_ctx* c, const void* hidden, const void* W, const 
   if (st != AF_OK) return st;
   if (T > 0 && (!hidden || !W || !cand || !teacher_logp || !cand_logp || !lse || !d_hidden || B < 1))
     return AF_ERR_INVALID_ARG;
-  if (T > ((int64_t)1 << 31) - 65536) return AF_ERR_SHAPE;
+  if (B > kMaxSequences || T > ((int64_t)1 << 31) - 65536) return AF_ERR_SHAPE;
   if ((st = distill_params_ok(*params)) != AF_OK) return st;
   if ((st = candidate_head(hidden, W, d_hidden, d_W, dW_type, accumulate_dW, d, V)) != AF_OK) return st;
   DeviceGuard guard(c->device);
@@ -637,7 +639,7 @@ af_status af_distill_update(af_ctx* c, const void* hidden, const void* W, const 
 
 static af_status preference_sizes(int64_t T, int32_t B) {
   if (T < 0 || B < 0 || (T > 0 && B < 1)) return AF_ERR_INVALID_ARG;
-  return B % 2 != 0 || T > ((int64_t)1 << 31) - 65536 ? AF_ERR_SHAPE : AF_OK;
+  return B % 2 != 0 || B > kMaxSequences || T > ((int64_t)1 << 31) - 65536 ? AF_ERR_SHAPE : AF_OK;
 }
 
 af_status af_preference_loss(af_ctx* c, const float* logp, const float* ref_logp, const int32_t* cu_seqlens, int32_t B,
