@@ -96,14 +96,14 @@ inline af_status encode_operand(const GemmEnv& env, CUtensorMap* map, const Oper
   return AF_OK;
 }
 
-// Columns of a CTA pair's tile.  A launch of few tiles leaves pairs idle, or some of them with one tile more than the
-// others: tiles of 128 columns, one unit each, where that shortens the longest pair's work.  (Gradient of 1195 tokens at
-// a 256 x 4096 head, d_W in 32 tiles for 16: 47.9 -> 45.5 us; of 64 tokens, dZ in 32 tiles for 16 too: 32 -> 27; of 128
-// tokens at 3584 x 19008, dZ in 149 tiles for 75: 207 -> 200.)  Beyond two rounds of tiles the wider ones are worth
-// more: an operand's row is fetched once per tile.
+// Columns of a CTA pair's tile.  A launch of few tiles leaves pairs idle: tiles of 128 columns, one unit each, while there
+// is a pair for every one of them.  (Whole gradients with tiles of 256 -> by this rule: 64 tokens at a 256 x 4096 head
+// 30.0 -> 27.4 us; 300 tokens 34.4 -> 31.7; 500 tokens at 384 x 4104 40.2 -> 38.0.)  With more tiles than pairs the wide
+// ones are worth more, since an operand's row is fetched once per tile, even where narrow ones would share the work out
+// more evenly: dZ of 128 tokens at 3584 x 19008 in 75 wide tiles for 149 narrow ones, 135.9 us against 146.5; 1195
+// tokens at 640 x 8200, 68.8 against 72.5.
 inline int pair_tile_columns(int64_t m_tiles, uint64_t N, int64_t pairs) {
-  const int64_t wide = m_tiles * (int64_t)((N + 255) / 256), narrow = m_tiles * (int64_t)((N + 127) / 128);
-  return wide <= 2 * pairs && (narrow + pairs - 1) / pairs < 2 * ((wide + pairs - 1) / pairs) ? 128 : 256;
+  return m_tiles * (int64_t)((N + 127) / 128) <= pairs ? 128 : 256;
 }
 // Sets the tile's width to bn columns, and one unit per tile where that is less than 256.
 inline void set_tile_columns(umma::GemmShape& g, uint64_t N, int bn) {
