@@ -365,11 +365,14 @@ af_status af_policy_update(af_ctx* ctx, const void* hidden, const void* W, const
  * for the two products and exists for one token block only, as in af_policy_loss_backward; a
  * registered "d_W ready" event (af_set_dw_ready_event) is recorded where d_W is complete, when there
  * is a d_W.  The forward accumulates logits in parts that are added in fp32 with rounding to nearest
- * (the tensor core's own accumulation truncates): at d = 3584 its log-probs are within 5e-7 of the 64-bit
- * ones, relative, where af_token_logprob's are 3e-6 off.  How it is launched follows from T and d: one pass
- * over W by itself for up to 16 tokens (8 where d > 4096, none where d > 5880), single CTAs up to 128
- * tokens, CTA pairs from there on; gemm_variant 1 of af_set_tuning applies to the backward only,
- * v_splits > 0 asks for CTA pairs with that many ranges, bwd_token_block works as elsewhere.
+ * (the tensor core's own accumulation truncates): at d = 3584 log-probs and lse are within 5e-7 of the 64-bit
+ * ones, relative and in root mean square, where af_token_logprob's are 3e-6 off, and the entropy, a difference
+ * of two numbers of lse's size, within 3e-6 (up to 16 tokens 1.1e-6: there it does not inherit the size of
+ * the logits).  The gradients are within 2.5e-3, of which the rounding of a bf16 result alone is 1.7e-3 and that
+ * of dZ as much again.  How the forward is launched follows from T and d: one pass over W by itself for up to 16
+ * tokens (8 where d > 4096, none where d > 5880), single CTAs up to 128 tokens, CTA pairs from there on;
+ * gemm_variant 1 of af_set_tuning applies to the backward only, v_splits > 0 asks for CTA pairs with that many
+ * ranges, bwd_token_block works as elsewhere.
  *
  * hidden [T,d], W [V,d] bf16 dev, row-major, 16-byte aligned, d % 8 == 0 (backward: V % 8 == 0, d_hidden
  * and d_W 16-byte aligned too).  cand [T,K] int32, cand_logp, dcand [T,K], entropy (nullable), lse

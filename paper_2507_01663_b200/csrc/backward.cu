@@ -472,9 +472,10 @@ af_status launch_head_products(af_ctx* ctx, const void* hidden_blk, const void* 
   auto dW_product = [&]() {
     // With dZ^T as the first operand a thread holds a piece of a row of d_W in place of a column, and a warp stores 16
     // bytes per lane, which is what counts for few tokens, when the product is a stream of d_W; dZ streams past once, and
-    // the hidden states stay in L2 as long as they take 32 MB or less.  3584 x 152064, the whole call: 29 tokens 691 us
-    // against 1100, 400 tokens 1.28 ms against 1.57, 700 tokens 1.86 against 2.13, 4001 tokens 10.3 against 10.4.
-    // d_W of 29 tokens alone: 1.09 GB in 314 us, 3.5 TB/s of writes (728 us the other way round).
+    // the hidden states stay in L2 as long as they take 32 MB or less.  3584 x 152064, the whole call: 29 tokens 697 us
+    // against 1106, 400 tokens 1.30 ms against 1.59, 700 tokens 1.94 against 2.38, 4001 tokens 10.1 against 10.2.
+    // d_W of 29 tokens alone: 1.09 GB in 314 us, 3.5 TB/s of writes (728 us the other way round; a plain fill of the same
+    // bytes takes 279 us, 3.9 TB/s).
     // Beyond that the order whose panels of hidden states take turns in L2.
     if (env.pair && first_block && last_block && tc * (int64_t)d <= (16 << 20)) {
       GemmEnv stream = env;

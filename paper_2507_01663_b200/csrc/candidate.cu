@@ -9,8 +9,8 @@
 // the end of its columns per 32 of them.  Fetching the K rows of W again for K dot products instead
 // would move 2 K d bytes per token (0.46 MB at K = 64, d = 3584: a tenth of the GEMM's time).
 //
-// Measured at d = 3584, V = 152064: 8192 tokens, K = 64, 7.1 ms (1.26 PFLOP/s in a stream of calls under the power cap);
-// 64 tokens 187 us (5.8 TB/s of W).
+// Measured at d = 3584, V = 152064: 8192 tokens, K = 64, 7.1-7.2 ms (1.25 PFLOP/s in a stream of calls under the power cap);
+// 64 tokens, K = 20, 187-198 us on several boxes (5.8-5.5 TB/s of W).
 //
 // The accumulation is promoted to round-to-nearest every kPromoteBlocks K blocks (see umma.cuh).
 #include "candidate.cuh"

@@ -7,12 +7,14 @@
 // launch as fragments of mma.m16n8k16 (the tokens as M, the rows as N); the order of k inside a dot product is free, so
 // a lane takes 32 consecutive bytes of its row (16 values of k) as the fragments of four MMAs.  The CTAs' tiles are
 // neighbours: what is being read at one time is one stretch of W.
-// Measured: 159 us for one token, 6.8 TB/s.  What else was measured for one token at the 7B-shaped head: the tcgen05 kernel 280 us (it fetches a 128-row tile of
-// hidden states per stage, 127 rows of which are absent, and balances 256 rows of W per pair); a warp per row tile with
-// loads to registers 182-197 us (DRAM serves 28 000 streams of a few hundred bytes at 5.5 TB/s); loads to registers
-// with k split over the warps 185-600 us (a warp cannot tell more than a few loads in flight apart).
+// Measured: 159 us for one token, 6.9 TB/s.  What else was measured for one token at the 7B-shaped head: the tcgen05 kernel
+// 280 us (it fetches a 128-row tile of hidden states per stage, 127 rows of which are absent, and balances 256 rows of W
+// per pair); a warp per row tile with loads to registers 182-197 us (DRAM serves 28 000 streams of a few hundred bytes at
+// 5.5 TB/s); loads to registers with k split over the warps 185-600 us (a warp cannot tell more than a few loads in flight
+// apart).
 // Each warp's accumulators cover an eighth of k; the parts are added in fp32, rounding to nearest (see umma.cuh on
-// truncation), in the order of the warps, once per kRound tiles.
+// truncation), in the order of the warps, once per kRound tiles.  What the eighths still lose to truncation is one place
+// of lse (1.2e-7 of it).
 // Every logit is also written to the workspace (4 V bytes per token, 0.06 % of W's each): the last CTA to finish
 // joins the softmax states and picks the listed logits from there, so the lists need no sorting and the call is one
 // launch.

@@ -7,15 +7,15 @@
 // to five row reductions and the row's bookkeeping at a few instructions per slot (with eight, the
 // renormalised divergences took 1.15 times as long), and the slots that take no part are turned into
 // values whose every term is 0 once, at the load.  The rows of a step are contiguous in memory: one
-// thread feeds a ring of shared-memory stages with bulk copies of both columns, up to four steps ahead, so
-// the bytes in flight do not depend on registers, and a warp's gradients leave the same way, as one bulk store
-// of its rows from the stage they came in.
-// Measured: 1106674 rows of 50 slots, student to teacher with a tail, 116 us (5.8 TB/s); of 64 slots 152 us (5.6 TB/s);
-// 2000000 rows of 16, 70 us (5.5 TB/s); 32768 rows of 64, renormalised, 13 us, half of it launch, first loads and the
-// last block's sum.
-// Row sums are taken in fp32 over at most 256 terms in a fixed tree, a lane's over up to 128 rows in fp32,
-// the batch's in fp64, all in a fixed order:
-// results are bit-reproducible.
+// thread feeds a ring of two shared-memory stages with bulk copies of both columns, one step while the other is
+// worked on, so the bytes in flight do not depend on registers, and a warp's gradients leave the same way, as
+// one bulk store of its rows from the stage they came in.
+// Measured: 1106674 rows of 50 slots, student to teacher with a tail, 113-122 us (5.9-5.5 TB/s, several boxes); of 64 slots
+// 148 us (5.8 TB/s); 2000000 rows of 16, 67 us (5.9 TB/s); 32768 rows of 64, renormalised, 12 us in a graph (13-14 called one
+// by one), half of it launch, first loads and the last block's sum.
+// Row sums are taken in fp32 over at most 256 terms in a fixed tree, a lane's over up to 256 rows (K = 1; 128 or fewer
+// from there on) in fp32, the batch's in fp64, all in a fixed order: results are bit-reproducible.  The exponentials are
+// ex2.approx (2^-22): a token's loss is within 2e-7 of 64 bits renormalised and 6e-7 with a tail, in root mean square.
 #pragma once
 
 #include "common.cuh"
@@ -32,7 +32,7 @@ constexpr float kTailFloor = 1.f / 65536.f;
 constexpr int kStageSlots = kThreads * 16; // slots of one column in a ring stage, at most
 constexpr int kStageBytes = 2 * kStageSlots * 4;
 constexpr int kStages = 2;                // three kept more in flight and were slower (K = 50: 127 us against 111)
-constexpr int kFlush = 16;                 // steps whose sums a lane keeps in fp32 (at most 128 rows) before fp64
+constexpr int kFlush = 16;                 // steps whose sums a lane keeps in fp32 (at most 256 rows) before fp64
 constexpr int kSmemBytes = kStages * kStageBytes + 128 /*alignment*/ + 64 /*barriers*/ + 1024 /*reads past a row*/;
 
 struct DistillWs {                         // the header and blocks of the policy loss's reduction workspace

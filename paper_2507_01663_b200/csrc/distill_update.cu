@@ -9,8 +9,8 @@
 //               4. one CTA per token: dZ in bf16 (reads 4 V, writes 2 V bytes per token);
 //               5. dH_blk = dZ W and, unless the head is frozen, dW += dZ^T H_blk.
 //   at the end  the record over all tokens, by the loss kernel (in step 3 when one block holds the batch).
-// Measured: 8192 tokens, 3584 x 152064, K = 64, bf16 d_W 22.5 ms; 1195 tokens, 256 x 4096 60 us, seven launches; dZ from the
-// logits moves its 6 bytes per logit at 6.3 TB/s (4100 rows of 152064: 0.59 ms).
+// Measured: 8192 tokens, 3584 x 152064, K = 64, bf16 d_W 22.4-23.1 ms; 32768 tokens (four blocks) 94-97 ms; 1195 tokens,
+// 256 x 4096 59 us, seven launches; dZ from the logits moves its 6 bytes per logit at 6.3 TB/s (4100 rows of 152064: 0.59 ms).
 #include "candidate.cuh"
 
 #include <algorithm>
@@ -21,7 +21,8 @@ namespace {
 constexpr int kThreads = 256;
 
 // One CTA per token row of the block and range of columns (one range, unless the rows are too few to fill the device: 29
-// rows of 152064 take 45 us that way, 9 in ranges).  The dense part -G q_v goes out first; the listed columns are then written over it, rounded once from fp32: sum of the gradients that name the column, minus G q.
+// rows of 152064 take 45 us that way, 9 in ranges).  The dense part -G q_v goes out first; the listed columns are then
+// written over it, rounded once from fp32: sum of the gradients that name the column, minus G q.
 __global__ void __launch_bounds__(kThreads) dz_candidates_kernel(
     const float* __restrict__ z, __nv_bfloat16* __restrict__ dz, int V, const int32_t* __restrict__ cand,
     const float* __restrict__ g, const float* __restrict__ cand_logp, const float* __restrict__ lse, int K, int range) {

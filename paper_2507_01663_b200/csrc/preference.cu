@@ -15,9 +15,10 @@
 //              lane per sequence reads the one at its end: the cost is that of a few reductions however many end.
 //   2. pairs   a few lanes per pair add the pieces, evaluate the loss and write the two sequences' coefficients.
 //   3. fill    the same ranges again: the coefficient of each token's sequence.
-// Measured: 24576 pairs of 1024 tokens without a reference 94 us (403 MB: 4.3 TB/s, of which the read pass 4.5, held by the
-// conversions to fp64, the fill 6, and about 3 us for each barrier); 64 pairs of 2161 tokens 16 us; 49152 sequences of 64
-// tokens 37 us (106 with one warp reduction per sequence).  Three launches in place of one took 173 and 24 us.
+// Measured: 24576 pairs of 1024 tokens on average without a reference 94-96 us (403 MB: 4.3 TB/s, of which the read pass 4.5,
+// held by the conversions to fp64, the fill 6, half of which L2 takes, and about 3 us for each barrier); 64 pairs of 2161 tokens
+// 14 us in a graph, 16 called one by one; 49152 sequences of 64 tokens 33-37 us (106 with one warp reduction per sequence).
+// Three launches in place of one took 173 and 24 us.
 // All sums are fp64 (thousands of near-cancelling terms, and the card has the rate: two additions per token)
 // and taken in a fixed order, so results are bit-reproducible.
 #include "common.cuh"
