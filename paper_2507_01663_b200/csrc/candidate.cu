@@ -10,7 +10,7 @@
 // would move 2 K d bytes per token (0.46 MB at K = 64, d = 3584: a tenth of the GEMM's time).
 //
 // Measured at d = 3584, V = 152064: 8192 tokens, K = 64, 7.1-7.2 ms (1.25 PFLOP/s in a stream of calls under the power cap);
-// 64 tokens, K = 20, 187-198 us on several boxes (5.8-5.5 TB/s of W).
+// 64 tokens, K = 20, 187-198 us on several B200s (5.8-5.5 TB/s of W).
 //
 // The accumulation is promoted to round-to-nearest every kPromoteBlocks K blocks (see umma.cuh).
 #include "candidate.cuh"

@@ -10,7 +10,7 @@
 // thread feeds a ring of two shared-memory stages with bulk copies of both columns, one step while the other is
 // worked on, so the bytes in flight do not depend on registers, and a warp's gradients leave the same way, as
 // one bulk store of its rows from the stage they came in.
-// Measured: 1106674 rows of 50 slots, student to teacher with a tail, 113-122 us (5.9-5.5 TB/s, several boxes); of 64 slots
+// Measured: 1106674 rows of 50 slots, student to teacher with a tail, 113-122 us (5.9-5.5 TB/s, several B200s); of 64 slots
 // 148 us (5.8 TB/s); 2000000 rows of 16, 67 us (5.9 TB/s); 32768 rows of 64, renormalised, 12 us in a graph (13-14 called one
 // by one), half of it launch, first loads and the last block's sum.
 // Row sums are taken in fp32 over at most 256 terms in a fixed tree, a lane's over up to 256 rows (K = 1; 128 or fewer
