@@ -382,7 +382,7 @@ def _own(s):
         return {"token": s["token"], "logp": s["logp"], "n_emitted": s["n_emitted"]}
     ctx.block_slots(s["length"], s["grow"], s["held"], s["table"], s["free"], s["free_count"], s["held_out"], s["free_count_out"],
                     s["cu"], s["slot"], block_size=case["block"], position=s["position"], granted=s["granted"])
-    return {"table": s["table"], "free": s["free"], "free_count": s["free_count_out"][0], "held": s["held_out"], "granted": s["granted"],
+    return {"table": s["table"], "free": s["free"], "free_count": s["free_count_out"], "held": s["held_out"], "granted": s["granted"],
             "cu": s["cu"], "slot": s["slot"], "position": s["position"]}
 
 
