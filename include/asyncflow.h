@@ -24,7 +24,7 @@
  *     with the largest sizes to keep allocation out of the hot calls.
  *   - Stream capture: once af_reserve has covered the sizes (and the tuning is unchanged), every
  *     call except af_pack_microbatch, af_unpack_microbatch, af_check_device_errors, af_reserve (and its
- *     kin af_reserve_candidates and af_reserve_preference) and af_destroy issues only kernel launches and
+ *     kin af_reserve_candidates, af_reserve_preference and af_reserve_rollout) and af_destroy issues only kernel launches and
  *     asynchronous memsets on `stream`, so a sequence of them may be recorded into a CUDA graph and
  *     replayed on new contents of the same buffers.
  *     af_pack_microbatch and af_unpack_microbatch build a table from their host index list (and
@@ -69,6 +69,10 @@ typedef enum { AF_F32 = 0, AF_BF16 = 1 } af_dtype;
 #define AF_DEVERR_CU_SEQLENS 4u   /* cu_seqlens not non-decreasing from 0 to T                     */
 #define AF_DEVERR_SAMPLE_INDEX 8u /* af_controller_put met an index outside [0, N): entry skipped  */
 #define AF_DEVERR_GROUP_ID 16u    /* af_grpo_advantage met a group id outside [0, n_groups): NaN    */
+#define AF_DEVERR_DISTRIBUTION 32u /* af_draft_verify met a row of logits that is no distribution   */
+#define AF_DEVERR_BLOCKS 64u      /* af_block_slots ran out of blocks: a request was refused       */
+#define AF_DEVERR_REQUEST 128u    /* af_block_slots met impossible numbers of a request or of the free list, or more
+                                     tokens than fit its outputs                                      */
 
 /* Create / destroy a context on CUDA device `device`.  af_create fails with
  * AF_ERR_UNSUPPORTED_DEVICE unless the device is compute capability 10.0.  af_destroy
@@ -513,6 +517,110 @@ af_status af_preference_loss(af_ctx* ctx, const float* logp, const float* ref_lo
                              const af_preference_params* params, af_preference_out* out,
                              float* pair_loss, float* seq_score, float* dlogp, void* stream);
 af_status af_reserve_preference(af_ctx* ctx, int64_t max_T, int32_t max_B);
+
+/* ---------------------------------------------------------------------------------------------
+ * af_quantize_head / af_quant_logits -- an LM head in 4 bits, made at a weight refresh, and the logits of a few tokens
+ * from it (rollouts decode with it, or draft with it; the paper names the rollout task and says nothing of its
+ * arithmetic; these are textbook round-to-nearest with a scale per group).
+ *
+ * Row v of W [V,d] is cut into groups of `group` weights (32, 64 or 128; the last one may be short).  Per group:
+ *   s = max|w| / 7 rounded to five significant bits (halves to even);  q = w / s rounded to the nearest whole number,
+ *   halves away from zero (|q| <= 7);  value = s q, which is a bf16 exactly.
+ *   A group whose largest weight is below 2^-100 gets s = 0 and q = 0; one with a NaN, an infinity or a magnitude above
+ *   2^120 gets s = NaN and q = 0, and its values and products are NaN.
+ * Results are those formulas', bit for bit.
+ *   codes [V, d / 8] 32-bit words: weight 8 j + 2 i is digit i (bits 4 i .. 4 i + 3) of word j, weight 8 j + 2 i + 1 digit
+ *   i + 4; a digit holds q + 8.  scale [V, ceil(d / group)] bf16.  values [V,d] bf16, or NULL: the policy that tokens are really
+ *   sampled from -- af_token_logprob on them gives its log-probs.
+ *
+ * af_quant_logits:  logits[t,v] = sum_k hidden[t,k] * scale[v, k / group] * (digit[v,k] - 8), sums in fp32, of type
+ * logits_type (AF_F32 or AF_BF16), row t at logits + t * logits_pitch elements (logits_pitch >= V).  Any digits 0..15 and any
+ * bf16 scales are taken, so heads quantised elsewhere in this layout are too.  A NaN in a scale or in a hidden row stays in
+ * its vocabulary row or token.  0 <= T <= AF_MAX_QUANT_TOKENS; meant for few: it costs one pass over the codes per 64 tokens.
+ *
+ * W, hidden, values bf16 dev; d % 32 == 0; matrices contiguous (but for the logits' pitch) and 16-byte aligned, logits aligned
+ * to their type.  No workspace.
+ * Errors: AF_ERR_INVALID_ARG for null pointers, sizes below 1, another group size or type; AF_ERR_ALIGNMENT; AF_ERR_SHAPE for
+ * T out of range or a pitch below V.
+ * ------------------------------------------------------------------------------------------- */
+#define AF_MAX_QUANT_TOKENS 65536
+af_status af_quantize_head(af_ctx* ctx, const void* W, int32_t V, int32_t d, int32_t group, void* codes, void* scale,
+                           void* values, void* stream);
+af_status af_quant_logits(af_ctx* ctx, const void* hidden, const void* codes, const void* scale, int64_t T, int32_t d,
+                          int32_t V, int32_t group, void* logits, int32_t logits_type, int64_t logits_pitch, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * af_draft_verify -- rejection sampling of drafted tokens: which of them the target's distribution lets pass, the token
+ * after them, and the log-probs of all that is emitted (a response's next tokens and their old_logp).
+ *
+ * Request r has n = cu_draft[r+1] - cu_draft[r] drafted tokens, rows cu_draft[r] .. of `draft`, u_accept and draft_logits,
+ * and n + 1 rows of target_logits, token and logp, from row cu_draft[r] + r on; row i of them is the target's distribution at
+ * the place of draft i, the last one that behind all drafts.  With tau = temperature > 0:
+ *   p_i = softmax(target_logits / tau);  q_i = softmax(draft_logits / tau), or all mass on the draft where draft_logits is NULL
+ *   draft i = x passes iff  u_accept * q_i(x) < p_i(x);  a = the first that does not pass, n if all do
+ *   the token after them, y: from p_a if a = n, else from max(p_a - q_a, 0) (which without draft_logits is p_a without x); where
+ *   that holds no more than 2^-30 of mass, from p_a itself.  With its weights w_v and C_v = sum_{v' <= v} w_v':
+ *   y = min { v : C_v > u_sample[r] * C_{V-1} }
+ *   token = x_0 .. x_{a-1}, y, then -1;  logp = log p_i(token_i), then 0;  n_emitted[r] = a + 1.
+ * temperature = 0 is greedy: x passes iff it is the target row's first maximum, y is that, logp is of softmax(target_logits), and
+ * draft_logits and the uniforms are not looked at.
+ * u_accept [D] and u_sample [R] are uniforms in [0, 1) fp32 (u_sample is brought into it).  Logits of -inf are masked entries.
+ * A draft outside [0, V) does not pass and raises AF_DEVERR_TARGET_RANGE.  A row that is looked at and is no distribution (a NaN, an
+ * infinity, nothing but -inf) ends its request: token -1, logp NaN, n_emitted = the drafts passed before it, and
+ * AF_DEVERR_DISTRIBUTION.  Rows behind the first draft that does not pass are not looked at (but may be read).
+ * A request whose part of cu_draft is not within [0, D], decreasing or longer than max_draft gets n_emitted = 0, its rows are left
+ * as they are, and AF_DEVERR_CU_SEQLENS is raised, as it is where cu_draft does not run from 0 to D.
+ *
+ * Comparisons and draws are made from sums in 64 bits where 32 could decide otherwise; log-probs of passed drafts are within
+ * 1e-6 of 64 bits, that of y is rounded once.
+ * target_logits [D + R, V], draft_logits [D, V]: fp32 or bf16 dev, row pitch in elements (>= V), aligned to their type.  draft [D],
+ * cu_draft [R+1], token [D + R], n_emitted [R] int32, logp (nullable) [D + R] fp32, dev.  0 <= R <= 2^20, 0 <= D <= 2^24,
+ * D <= R * max_draft, 0 <= max_draft <= AF_MAX_DRAFT, temperature 0 or from 1e-4 to 1e4.
+ * Workspace: 16 bytes per row, 75 KB at least; af_reserve_rollout sizes it ahead, for smaller batches too.
+ * ------------------------------------------------------------------------------------------- */
+#define AF_MAX_DRAFT 1023
+af_status af_draft_verify(af_ctx* ctx, const void* target_logits, int32_t target_type, int64_t target_pitch,
+                          const void* draft_logits, int32_t draft_type, int64_t draft_pitch, const int32_t* draft,
+                          const int32_t* cu_draft, const float* u_accept, const float* u_sample, int32_t R, int32_t D, int32_t V,
+                          int32_t max_draft, float temperature, int32_t* token, float* logp, int32_t* n_emitted, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * af_block_slots -- block tables and slot maps from request lengths: where the tokens of responses of unknown length go
+ * in a store of fixed blocks (columns whose rows are addressed through a table, where af_pack_microbatch's are one stretch
+ * per sample).
+ *
+ * A request keeps length[r] tokens and is to hold grow[r] more; held[r] is how many blocks of block_size rows its row of
+ * block_table has.  need = ceil((length + grow) / block_size).
+ *   need < held (drafts that did not pass, a response that has ended: length = grow = 0): the blocks behind the first `need` go
+ *   back to the free list;  need > held: need - held blocks are taken from it.
+ * free_blocks is a stack of *free_count block numbers.  First all blocks given back are put on it, in the order of the requests
+ * and within one of its table; then the blocks wanted are taken from its top one by one, in the same order.  A request
+ * that the blocks left do not serve in whole, counting what those before it want, is refused: it keeps its table and held
+ * blocks, its slots are -1, and AF_DEVERR_BLOCKS is raised; so are those behind it that want blocks.
+ *   held_out[r], granted[r] (1 or 0; nullable), *free_count_out; block_table[r][held .. need) and free_blocks[*free_count ..
+ *   *free_count_out) are written, everything else in both is left as it is.
+ *   cu_new [R+1]: running sums of grow;  for the i-th new token of request r, at cu_new[r] + i:  position = length[r] + i,
+ *   slot = block_table[r][position / block_size] * block_size + position % block_size (64 bits).  Rows of slot and
+ *   position (nullable) behind cu_new[R] are left as they are.
+ * held_out may be held and free_count_out free_count (an update in place).  Lengths stay the caller's: next step's length is what
+ * was kept of this one.
+ * Impossible numbers (a negative length, grow or held, more blocks than max_blocks, length + grow above 2^31 - 1) refuse the
+ * request; a free count outside [0, n_blocks], more blocks than n_blocks and more than token_capacity tokens are cut to what
+ * there is; each raises AF_DEVERR_REQUEST.  Block numbers are not checked: they are only handed on.
+ *
+ * length, grow, held, held_out, granted [R], free_count, free_count_out [1], cu_new [R+1], position [token_capacity] int32;
+ * block_table [R, max_blocks] int32 with table_pitch >= max_blocks elements from row to row; free_blocks [n_blocks] int32; slot
+ * [token_capacity] int64; all dev.  0 <= R <= 2^20, block_size >= 1.  Workspace: 32 bytes per request (af_reserve_rollout).
+ * Errors: AF_ERR_INVALID_ARG for null pointers and negative sizes, AF_ERR_SHAPE for R out of range or a pitch below max_blocks.
+ * ------------------------------------------------------------------------------------------- */
+af_status af_block_slots(af_ctx* ctx, const int32_t* length, const int32_t* grow, const int32_t* held, int32_t R,
+                         int32_t block_size, int32_t* block_table, int64_t table_pitch, int32_t max_blocks, int32_t* free_blocks,
+                         int32_t n_blocks, const int32_t* free_count, int32_t* held_out, int32_t* free_count_out, int32_t* granted,
+                         int32_t* cu_new, int64_t* slot, int32_t* position, int64_t token_capacity, void* stream);
+
+/* Pre-size the workspace of af_draft_verify and af_block_slots for up to max_R requests and max_D drafted tokens in all.
+ * Synchronous (allocates). */
+af_status af_reserve_rollout(af_ctx* ctx, int32_t max_R, int32_t max_D);
 
 /* ---------------------------------------------------------------------------------------------
  * af_controller_put / af_controller_get / af_controller_clear -- the status table of the

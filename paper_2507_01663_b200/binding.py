@@ -22,6 +22,7 @@ STATUS_NAMES = {0: "AF_OK", -1: "AF_ERR_INVALID_ARG", -2: "AF_ERR_SHAPE", -3: "A
                 -4: "AF_ERR_CAPACITY", -5: "AF_ERR_INDEX", -6: "AF_ERR_WORKSPACE", -7: "AF_ERR_CUDA",
                 -8: "AF_ERR_UNSUPPORTED_DEVICE", -9: "AF_ERR_DEVICE_FLAGGED"}
 DEVERR_TARGET_RANGE, DEVERR_WATCHDOG, DEVERR_CU_SEQLENS, DEVERR_SAMPLE_INDEX, DEVERR_GROUP_ID = 1, 2, 4, 8, 16
+DEVERR_DISTRIBUTION, DEVERR_BLOCKS, DEVERR_REQUEST = 32, 64, 128
 
 EXPORTS = ["af_create", "af_destroy", "af_status_string", "af_reserve", "af_workspace_bytes",
            "af_set_tuning", "af_check_device_errors", "af_pack_microbatch", "af_token_logprob",
@@ -30,9 +31,12 @@ EXPORTS = ["af_create", "af_destroy", "af_status_string", "af_reserve", "af_work
            "af_token_logprob_shard", "af_merge_logprob_shards", "af_policy_update", "af_unpack_microbatch", "af_policy_loss_backward_shard", "af_set_dw_ready_event", "af_die_split", "af_selftest_bounded_wait",
            "af_plan_token_logprob", "af_plan_units",
            "af_candidate_logprob", "af_candidate_logprob_backward", "af_reserve_candidates", "af_distill_loss",
-           "af_distill_update", "af_preference_loss", "af_reserve_preference"]
+           "af_distill_update", "af_preference_loss", "af_reserve_preference",
+           "af_quantize_head", "af_quant_logits", "af_draft_verify", "af_block_slots", "af_reserve_rollout"]
 MAX_WRITE_COLS = 4
 MAX_CANDIDATES = 256
+MAX_QUANT_TOKENS = 65536
+MAX_DRAFT = 1023
 F32, BF16 = 0, 1                                                     # af_dtype
 DIVERGENCE_FORWARD, DIVERGENCE_REVERSE = 0, 1                        # teacher to student, student to teacher
 SUPPORT_LISTED, SUPPORT_RENORMALISED, SUPPORT_TAIL = 0, 1, 2
@@ -162,6 +166,11 @@ def load_library() -> C.CDLL:
                                       vp, vp, vp, vp, vp, vp, vp, i32, i32, vp]
     lib.af_preference_loss.argtypes = [vp, vp, vp, vp, i32, i64, C.POINTER(PreferenceParams), vp, vp, vp, vp, vp]
     lib.af_reserve_preference.argtypes = [vp, i64, i32]
+    lib.af_quantize_head.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp]
+    lib.af_quant_logits.argtypes = [vp, vp, vp, vp, i64, i32, i32, i32, vp, i32, i64, vp]
+    lib.af_draft_verify.argtypes = [vp, vp, i32, i64, vp, i32, i64, vp, vp, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, vp]
+    lib.af_block_slots.argtypes = [vp, vp, vp, vp, i32, i32, vp, i64, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.af_reserve_rollout.argtypes = [vp, i32, i32]
     for name in EXPORTS:
         if name not in ("af_status_string", "af_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
@@ -495,6 +504,86 @@ class Context:
 
     def reserve_preference(self, max_T: int, max_B: int):
         _check(self.lib.af_reserve_preference(self.handle, max_T, max_B), "af_reserve_preference")
+
+    # -- rollout: a head in 4 bits, draft verification, block tables -------------------------------------
+    def _rows(self, t: Optional[torch.Tensor], rows: int, cols: int):
+        """(address, af_dtype, pitch) of a float32 or bfloat16 matrix whose rows may lie apart; (None, F32, cols) for None."""
+        if t is None:
+            return None, F32, cols
+        dtype, shape = t.dtype, t.shape
+        if (dtype is torch.float32 or dtype is torch.bfloat16) and len(shape) == 2 and shape[1] == cols and shape[0] >= rows \
+                and t.get_device() == self.device:
+            pitch, step = t.stride()
+            if shape[0] <= 1:
+                pitch = cols                                  # a single row lies in one piece, whatever its stride says
+            if (step == 1 or cols == 1) and pitch >= cols:
+                return t.data_ptr(), (F32 if dtype is torch.float32 else BF16), pitch
+        raise ValueError(f"expected float32 or bfloat16 [{rows}, {cols}] of whole rows on device {self.device}, "
+                         f"not {t.dtype} {list(shape)} with strides {t.stride()} on {t.device}")
+
+    def _quant_head(self, codes, scale, V: int, d: int, group: int):
+        if group not in (32, 64, 128):
+            raise ValueError("groups of 32, 64 or 128 weights")
+        return (self._matrix(codes, torch.int32, V, d // 8), self._matrix(scale, torch.bfloat16, V, (d + group - 1) // group))
+
+    def quantize_head(self, W, codes, scale, group: int = 128, values=None, stream=None):
+        """``W``: bfloat16 [V, d]; ``codes``: int32 [V, d / 8]; ``scale``: bfloat16 [V, ceil(d / group)]; ``values``: bfloat16
+        [V, d], the weights that the codes stand for, or None."""
+        V, d = W.shape
+        bf16 = torch.bfloat16
+        codes_at, scale_at = self._quant_head(codes, scale, V, d, group)
+        _check(self.lib.af_quantize_head(self.handle, self._matrix(W, bf16, V, d), V, d, group, codes_at, scale_at,
+                                         self._matrix(values, bf16, V, d), self._stream_of(stream)), "af_quantize_head")
+
+    def quant_logits(self, hidden, codes, scale, logits, group: int = 128, T=None, stream=None):
+        """``logits``: float32 or bfloat16 [T, V]; its rows may lie apart (a step's rows of a larger buffer)."""
+        T = hidden.shape[0] if T is None else T
+        V, d = codes.shape[0], codes.shape[1] * 8
+        codes_at, scale_at = self._quant_head(codes, scale, V, d, group)
+        logits_at, kind, pitch = self._rows(logits, T, V)
+        _check(self.lib.af_quant_logits(self.handle, self._matrix(hidden, torch.bfloat16, T, d), codes_at, scale_at, T, d, V, group,
+                                        logits_at, kind, pitch, self._stream_of(stream)), "af_quant_logits")
+
+    def draft_verify(self, target_logits, draft_logits, draft, cu_draft, u_accept, u_sample, token, n_emitted, logp=None,
+                     max_draft: Optional[int] = None, temperature: float = 1.0, R=None, D=None, stream=None):
+        """``target_logits`` [D + R, V] and ``draft_logits`` [D, V] (None: drafts without a distribution): float32 or bfloat16;
+        ``draft``: int32 [D]; ``cu_draft``: int32 [R + 1]; ``token``: int32 [D + R]; ``max_draft``: the longest request's
+        drafts (default: D)."""
+        R = self._sequences(cu_draft, R)
+        D = draft.shape[0] if D is None else D
+        V = target_logits.shape[1]
+        array, i32, f32 = self._array, torch.int32, torch.float32
+        target_at, target_type, target_pitch = self._rows(target_logits, D + R, V)
+        draft_at, draft_type, draft_pitch = self._rows(draft_logits, D, V)
+        _check(self.lib.af_draft_verify(self.handle, target_at, target_type, target_pitch, draft_at, draft_type, draft_pitch,
+                                        array(draft, i32, 4 * D), array(cu_draft, i32, 0), array(u_accept, f32, 4 * D),
+                                        array(u_sample, f32, 4 * R), R, D, V, D if max_draft is None else max_draft, temperature,
+                                        array(token, i32, 4 * (D + R)), array(logp, f32, 4 * (D + R)), array(n_emitted, i32, 4 * R),
+                                        self._stream_of(stream)), "af_draft_verify")
+
+    def block_slots(self, length, grow, held, block_table, free_blocks, free_count, held_out, free_count_out, cu_new, slot,
+                    block_size: int, position=None, granted=None, R=None, stream=None):
+        """int32 throughout but ``slot`` (int64 [token_capacity]); ``block_table`` [R, max_blocks], its rows may lie apart;
+        ``held_out`` may be ``held`` and ``free_count_out`` ``free_count``."""
+        R = length.shape[0] if R is None else R
+        array, i32 = self._array, torch.int32
+        if (block_table.dtype is not i32 or block_table.dim() != 2 or block_table.shape[0] < R or
+                block_table.get_device() != self.device or (block_table.shape[1] > 1 and block_table.stride(1) != 1)):
+            raise ValueError(f"block_table is int32 [{R}, max_blocks] of whole rows on device {self.device}")
+        max_blocks = block_table.shape[1]
+        pitch = block_table.stride(0) if block_table.shape[0] > 1 else max_blocks
+        if pitch < max_blocks:
+            raise ValueError("rows of block_table overlap")
+        capacity = slot.shape[0]
+        _check(self.lib.af_block_slots(self.handle, array(length, i32, 4 * R), array(grow, i32, 4 * R), array(held, i32, 4 * R), R,
+                                       block_size, block_table.data_ptr(), pitch, max_blocks, array(free_blocks, i32, 0),
+                                       free_blocks.shape[0], array(free_count, i32, 4), array(held_out, i32, 4 * R),
+                                       array(free_count_out, i32, 4), array(granted, i32, 4 * R), array(cu_new, i32, 4 * (R + 1)),
+                                       array(slot, torch.int64, 8 * capacity), array(position, i32, 4 * capacity), capacity,
+                                       self._stream_of(stream)), "af_block_slots")
+
+    def reserve_rollout(self, max_R: int, max_D: int):
+        _check(self.lib.af_reserve_rollout(self.handle, max_R, max_D), "af_reserve_rollout")
 
     # -- controller: status table of the streaming store ----------------------------------------
     @staticmethod

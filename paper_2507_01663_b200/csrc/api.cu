@@ -10,6 +10,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "common.cuh"
+#include "rollout.cuh"
 
 namespace af {
 
@@ -24,6 +25,7 @@ af_status ws_grow(Buf& b, size_t bytes) {
 
 namespace {
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned_to(const void* p, int32_t type) { return (reinterpret_cast<uintptr_t>(p) & (type == AF_F32 ? 3u : 1u)) == 0; }
 
 // A named range around every entry point that enqueues work, for timelines of a profiler that
 // understands NVTX (header-only: without such a tool attached the calls do nothing).
@@ -112,7 +114,7 @@ af_status af_destroy(af_ctx* c) {
   DeviceGuard guard(c->device);
   cudaDeviceSynchronize();
   Buf* bufs[] = {&c->partial, &c->loss_ws, &c->pack_meta, &c->dz, &c->ctrl_ws, &c->zlog, &c->adv_ws, &c->cand_keys,
-                 &c->dw_sums, &c->split_k, &c->distill_ws, &c->pref_ws};
+                 &c->dw_sums, &c->split_k, &c->distill_ws, &c->pref_ws, &c->verify_ws, &c->slots_ws};
   for (Buf* b : bufs) if (b->p) cudaFree(b->p);
   for (int i = 0; i < kPackRing; ++i) {
     if (c->pack_host[i]) cudaFreeHost(c->pack_host[i]);
@@ -126,7 +128,7 @@ af_status af_destroy(af_ctx* c) {
 int64_t af_workspace_bytes(const af_ctx* c) {
   if (!c) return 0;
   return (int64_t)(c->partial.cap + c->loss_ws.cap + c->pack_meta.cap + c->dz.cap + c->ctrl_ws.cap + c->zlog.cap + c->adv_ws.cap +
-                   c->cand_keys.cap + c->dw_sums.cap + c->split_k.cap + c->distill_ws.cap + c->pref_ws.cap);
+                   c->cand_keys.cap + c->dw_sums.cap + c->split_k.cap + c->distill_ws.cap + c->pref_ws.cap + c->verify_ws.cap + c->slots_ws.cap);
 }
 
 af_status af_selftest_bounded_wait(af_ctx* c, uint32_t* waited_us, void* stream) {
@@ -668,6 +670,97 @@ af_status af_reserve_preference(af_ctx* c, int64_t max_T, int32_t max_B) {
   if (st != AF_OK) return st;
   DeviceGuard guard(c->device);
   return ws_grow(c->pref_ws, preference_workspace_bytes(max_B));
+}
+
+// A head in 4 bits: rows of whole 16-byte pieces of codes, groups of 32, 64 or 128 weights.
+static af_status quant_head_sizes(int32_t V, int32_t d, int32_t group) {
+  if (V < 1 || d < 1) return AF_ERR_INVALID_ARG;
+  if (group != 32 && group != 64 && group != 128) return AF_ERR_INVALID_ARG;
+  return d % 32 != 0 ? AF_ERR_ALIGNMENT : AF_OK;
+}
+
+af_status af_quantize_head(af_ctx* c, const void* W, int32_t V, int32_t d, int32_t group, void* codes, void* scale, void* values,
+                           void* stream) {
+  NvtxRange range("af_quantize_head");
+  if (!c || !W || !codes || !scale) return AF_ERR_INVALID_ARG;
+  const af_status st = quant_head_sizes(V, d, group);
+  if (st != AF_OK) return st;
+  if (!aligned16(W) || !aligned16(codes) || !aligned16(scale) || !aligned16(values)) return AF_ERR_ALIGNMENT;
+  DeviceGuard guard(c->device);
+  return launch_quantize_head(W, V, d, group, codes, scale, values, c->sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? AF_OK : AF_ERR_CUDA;
+}
+
+af_status af_quant_logits(af_ctx* c, const void* hidden, const void* codes, const void* scale, int64_t T, int32_t d, int32_t V,
+                          int32_t group, void* logits, int32_t logits_type, int64_t logits_pitch, void* stream) {
+  NvtxRange range("af_quant_logits");
+  if (!c || T < 0 || (logits_type != AF_F32 && logits_type != AF_BF16)) return AF_ERR_INVALID_ARG;
+  const af_status st = quant_head_sizes(V, d, group);
+  if (st != AF_OK) return st;
+  if (T > AF_MAX_QUANT_TOKENS || logits_pitch < V) return AF_ERR_SHAPE;
+  if (T == 0) return AF_OK;
+  if (!hidden || !codes || !scale || !logits) return AF_ERR_INVALID_ARG;
+  if (!aligned16(hidden) || !aligned16(codes) || !aligned16(scale) || !aligned_to(logits, logits_type)) return AF_ERR_ALIGNMENT;
+  DeviceGuard guard(c->device);
+  const QuantHead head{static_cast<const uint32_t*>(codes), static_cast<const __nv_bfloat16*>(scale), V, d, group};
+  return launch_quant_logits(c, hidden, head, T, logits, logits_type, logits_pitch, static_cast<cudaStream_t>(stream));
+}
+
+static af_status verify_sizes(int32_t R, int32_t D, int32_t V, int32_t max_draft) {
+  if (R < 0 || D < 0 || V < 1 || max_draft < 0) return AF_ERR_INVALID_ARG;
+  if (max_draft > AF_MAX_DRAFT || R > (1 << 20) || (int64_t)D > (int64_t)R * max_draft || D > (1 << 24)) return AF_ERR_SHAPE;
+  return AF_OK;
+}
+
+af_status af_draft_verify(af_ctx* c, const void* target_logits, int32_t target_type, int64_t target_pitch,
+                          const void* draft_logits, int32_t draft_type, int64_t draft_pitch, const int32_t* draft,
+                          const int32_t* cu_draft, const float* u_accept, const float* u_sample, int32_t R, int32_t D, int32_t V,
+                          int32_t max_draft, float temperature, int32_t* token, float* logp, int32_t* n_emitted, void* stream) {
+  NvtxRange range("af_draft_verify");
+  if (!c) return AF_ERR_INVALID_ARG;
+  const af_status st = verify_sizes(R, D, V, max_draft);
+  if (st != AF_OK) return st;
+  if ((target_type != AF_F32 && target_type != AF_BF16) || (draft_type != AF_F32 && draft_type != AF_BF16)) return AF_ERR_INVALID_ARG;
+  if (!(temperature == 0.f || (temperature >= 1e-4f && temperature <= 1e4f))) return AF_ERR_INVALID_ARG;
+  if (R == 0) return AF_OK;
+  if (!target_logits || !cu_draft || !token || !n_emitted || (D > 0 && !draft)) return AF_ERR_INVALID_ARG;
+  if (temperature > 0.f && (!u_sample || (D > 0 && !u_accept))) return AF_ERR_INVALID_ARG;
+  if (target_pitch < V || (draft_logits && draft_pitch < V)) return AF_ERR_SHAPE;
+  if (!aligned_to(target_logits, target_type) || !aligned_to(draft_logits, draft_type)) return AF_ERR_ALIGNMENT;
+  DeviceGuard guard(c->device);
+  const bool dense = draft_logits && temperature > 0.f;
+  const VerifyCall call{{target_logits, target_type, target_pitch}, {dense ? draft_logits : nullptr, draft_type, draft_pitch}, draft, cu_draft,
+                        u_accept, u_sample, R, D, V, max_draft, temperature, token, logp, n_emitted};
+  return launch_draft_verify(c, call, static_cast<cudaStream_t>(stream));
+}
+
+static af_status slots_sizes(int32_t R) { return R < 0 ? AF_ERR_INVALID_ARG : R > (1 << 20) ? AF_ERR_SHAPE : AF_OK; }
+
+af_status af_block_slots(af_ctx* c, const int32_t* length, const int32_t* grow, const int32_t* held, int32_t R, int32_t block_size,
+                         int32_t* block_table, int64_t table_pitch, int32_t max_blocks, int32_t* free_blocks, int32_t n_blocks,
+                         const int32_t* free_count, int32_t* held_out, int32_t* free_count_out, int32_t* granted, int32_t* cu_new,
+                         int64_t* slot, int32_t* position, int64_t token_capacity, void* stream) {
+  NvtxRange range("af_block_slots");
+  if (!c || block_size < 1 || max_blocks < 0 || n_blocks < 0 || token_capacity < 0) return AF_ERR_INVALID_ARG;
+  const af_status st = slots_sizes(R);
+  if (st != AF_OK) return st;
+  if (!free_count || !free_count_out || !cu_new) return AF_ERR_INVALID_ARG;
+  if (R > 0 && (!length || !grow || !held || !held_out || (max_blocks > 0 && !block_table))) return AF_ERR_INVALID_ARG;
+  if ((n_blocks > 0 && !free_blocks) || (token_capacity > 0 && !slot)) return AF_ERR_INVALID_ARG;
+  if (table_pitch < max_blocks) return AF_ERR_SHAPE;
+  DeviceGuard guard(c->device);
+  const SlotsCall call{length, grow, held, R, block_size, block_table, table_pitch, max_blocks, free_blocks, n_blocks, free_count,
+                       held_out, free_count_out, granted, cu_new, slot, position, token_capacity};
+  return launch_block_slots(c, call, static_cast<cudaStream_t>(stream));
+}
+
+af_status af_reserve_rollout(af_ctx* c, int32_t max_R, int32_t max_D) {
+  NvtxRange range("af_reserve_rollout");
+  if (!c || max_R < 0 || max_D < 0) return AF_ERR_INVALID_ARG;
+  if (max_R > (1 << 20) || max_D > (1 << 24)) return AF_ERR_SHAPE;
+  DeviceGuard guard(c->device);
+  const af_status st = ws_grow(c->verify_ws, verify_workspace_bytes(max_R, max_D, c->sm_count));
+  return st == AF_OK ? ws_grow(c->slots_ws, slots_workspace_bytes(max_R)) : st;
 }
 
 af_status af_controller_put(af_ctx* c, const af_controller_view* table, const int32_t* idx, int64_t n,
