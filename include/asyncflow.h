@@ -533,10 +533,11 @@ af_status af_reserve_preference(af_ctx* ctx, int64_t max_T, int32_t max_B);
  *   i + 4; a digit holds q + 8.  scale [V, ceil(d / group)] bf16.  values [V,d] bf16, or NULL: the policy that tokens are really
  *   sampled from -- af_token_logprob on them gives its log-probs.
  *
- * af_quant_logits:  logits[t,v] = sum_k hidden[t,k] * scale[v, k / group] * (digit[v,k] - 8), sums in fp32, of type
+ * af_quant_logits:  logits[t,v] = sum_k hidden[t,k] * bf16(scale[v, k / group] * (digit[v,k] - 8)), sums in fp32, of type
  * logits_type (AF_F32 or AF_BF16), row t at logits + t * logits_pitch elements (logits_pitch >= V).  Any digits 0..15 and any
- * bf16 scales are taken, so heads quantised elsewhere in this layout are too.  A NaN in a scale or in a hidden row stays in
- * its vocabulary row or token.  0 <= T <= AF_MAX_QUANT_TOKENS; meant for few: it costs one pass over the codes per 64 tokens.
+ * bf16 scales are taken, so heads quantised elsewhere in this layout are too; a weight that is no bf16 is rounded to one (those of
+ * af_quantize_head are).  A NaN in a scale or in a hidden row stays in its vocabulary row or token.
+ * 0 <= T <= AF_MAX_QUANT_TOKENS; meant for few: it costs one pass over the codes per 64 tokens.
  *
  * W, hidden, values bf16 dev; d % 32 == 0; matrices contiguous (but for the logits' pitch) and 16-byte aligned, logits aligned
  * to their type.  No workspace.

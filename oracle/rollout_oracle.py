@@ -68,10 +68,17 @@ def unpack_digits(words):
     return q
 
 
+def to_bf16(x):
+    """float64 values that are exact in fp32, rounded to bf16 (halves to even)."""
+    bits = np.asarray(x, dtype=np.float32).view(np.uint32).astype(np.uint64)
+    bits = (bits + 0x7fff + ((bits >> 16) & 1)) & 0xffff0000
+    return np.where(np.isnan(x), x, bits.astype(np.uint32).view(np.float32).astype(np.float64))
+
+
 def quant_logits_ref(H, words, scale, group):
-    """(logits [T, V], sums of absolute terms) in 64 bits."""
+    """(logits [T, V], sums of absolute terms) in 64 bits; a weight is scale * digit as a bf16."""
     q = unpack_digits(words)
-    w = q * np.repeat(np.asarray(scale, dtype=np.float64), group, axis=1)[:, :q.shape[1]]
+    w = to_bf16(q * np.repeat(np.asarray(scale, dtype=np.float64), group, axis=1)[:, :q.shape[1]])
     return H @ w.T, np.abs(H) @ np.abs(w).T
 
 

@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libasyncflow.so")
 SOURCES = ["api.cu", "pack.cu", "advantage.cu", "advantage_ids.cu", "loss.cu", "logprob.cu", "backward.cu", "controller.cu", "update.cu", "candidate.cu", "candidate_stream.cu",
-           "distill.cu", "distill_renorm.cu", "distill_tail.cu", "distill_update.cu", "preference.cu", "head_quant.cu", "quant_logits.cu", "draft_verify.cu", "block_slots.cu", "diemap.cu", "selftest.cu"]
+           "distill.cu", "distill_renorm.cu", "distill_tail.cu", "distill_update.cu", "preference.cu", "head_quant.cu", "quant_logits.cu", "quant_umma.cu", "draft_verify.cu", "block_slots.cu", "diemap.cu", "selftest.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

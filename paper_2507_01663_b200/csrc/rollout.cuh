@@ -19,6 +19,9 @@ cudaError_t launch_quantize_head(const void* W, int32_t V, int32_t d, int32_t gr
                                  int sm_count, cudaStream_t s);
 af_status launch_quant_logits(af_ctx* ctx, const void* hidden, const QuantHead& head, int64_t T, void* logits, int32_t type,
                               int64_t pitch, cudaStream_t s);
+constexpr int kQuantTokens = 64;  // of one launch (quant_umma.cu)
+af_status launch_quant_umma(af_ctx* ctx, const void* hidden, const QuantHead& head, int T, void* logits, int32_t type, int64_t pitch,
+                            cudaStream_t s);
 
 // ---- draft verification -----------------------------------------------------------------------
 struct LogitRows {

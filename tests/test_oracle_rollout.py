@@ -60,6 +60,13 @@ def test_logits_by_hand():
     assert z.tolist() == [[-2.0], [-4.0]] and mag.tolist() == [[18.0], [4.0]]
 
 
+def test_weights_are_rounded_to_bf16():
+    import torch
+    x = np.random.default_rng(5).standard_normal(4000) * 10.0 ** np.random.default_rng(6).integers(-20, 20, 4000)
+    x = np.concatenate([x.astype(np.float32), np.float32([1 + 2.0 ** -8, 1 + 3 * 2.0 ** -8, -1 - 2.0 ** -8, 0.0])])
+    assert np.array_equal(O.to_bf16(x), torch.as_tensor(x).to(torch.bfloat16).double().numpy())
+
+
 def test_verification_has_the_targets_law():
     """Rejection sampling gives the target's distribution whatever the draft's is: exact, by integrating over the uniforms on a
     grid that their borders fall on."""
