@@ -12,10 +12,9 @@
 // So a pair costs a shift, a mask-and-or (both on the ALU pipe, at half rate, which is what this kernel is bound by next to
 // memory) and a multiply-add.
 //
-// Warps: 0 loads boxes of 256 weights by 128 rows and the tokens' 256 k into a ring, 1 issues the MMAs, the next four per
-// 128 rows read accumulators, the others dequantise in groups of four, 128 weights of 128 rows at a time, into four buffers
-// in tensor memory.  Sums are taken in parts of 512 of k, which the readers add in fp32, rounding to nearest (see umma.cuh on
-// truncation).
+// Warps: 0 loads stages of 256 of k into a ring (a box of 128 rows' codes and the tokens'), 1 issues the MMAs, 4 to 7 read
+// accumulators, the others dequantise, a stage per group of four and a buffer in tensor memory per group.  Sums are taken in
+// parts of 512 of k, which the readers add in fp32, rounding to nearest (see umma.cuh on truncation).
 #include "gemm_launch.cuh"
 #include "rollout.cuh"
 
@@ -26,15 +25,45 @@ using namespace umma;
 
 constexpr int kRowsM = 128;                        // rows of an MMA
 constexpr int kStageK = 256;                       // k of a stage: 128 bytes of codes
-constexpr int kHalfK = 128;                        // k that a group dequantises at a time
-constexpr int kBufs = 4;                           // of dequantised rows in tensor memory
-constexpr int kBufCols = kHalfK / 2;               // columns of one: two bf16 each
-constexpr int kBufCol0 = 256;
-constexpr int kMiscWarps = 4;                      // loads, MMAs, and two that make the readers start at a quarter of TMEM's lanes
+constexpr int kGroups = 3;                         // of four dequantising warps
+constexpr int kBufCols = kStageK / 2;              // columns of a buffer of dequantised rows: two bf16 each
+constexpr int kBufCol0 = 128;                      // behind two accumulators of up to 64 columns
+constexpr int kReaders = 4;                        // the first of the warps that read accumulators: a multiple of 4, as TMEM's lanes go
+constexpr int kThreads = 32 * (kReaders + 4 + 4 * kGroups);
 constexpr int kCodesBytes = kRowsM * 128;
 constexpr int kMaxRing = 10;
 constexpr int kSmemLimit = 225 * 1024;
 
+// A bounded wait in which the warp sleeps: the scheduler's issue slots belong to the warps that dequantise.
+__device__ __forceinline__ bool sleep_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  constexpr uint32_t kNapNs = 100000, kNaps = (uint32_t)(kWaitLimitNs / kNapNs);
+#pragma unroll 1
+  for (uint32_t i = 0; i < kNaps; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(kNapNs) : "memory");
+    if (ok) return true;
+    if (*abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+// The same for a warp that others wait for: it keeps asking for a while first.
+__device__ __forceinline__ bool ready_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+#pragma unroll 1
+  for (int i = 0; i < 64; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  return sleep_wait(bar, parity, abort_flag);
+}
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
+}
 __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -73,13 +102,14 @@ template <bool kQuick>
 __device__ __forceinline__ uint32_t weight_pair(uint32_t v, const Pair& p) {
   return kQuick ? bf2_fma(v, p.s, p.c) : bf2_fma(bf2_fma(v, kOne2, kMinus24), p.s, kZero2);
 }
-template <bool kQuick, int kPerHalf>
-__device__ __forceinline__ void dequantise(const uint8_t* row, uint32_t swizzle, const Pair (&p)[kPerHalf], uint32_t to) {
+template <bool kQuick, int kScales>
+__device__ __forceinline__ void dequantise(const uint8_t* row, uint32_t swizzle, const Pair (&p)[kScales], uint32_t to) {
+  constexpr int kPieces = kStageK / 32;
 #pragma unroll
-  for (int piece = 0; piece < kHalfK / 32; ++piece) {
+  for (int piece = 0; piece < kPieces; ++piece) {
     const uint4 w4 = *reinterpret_cast<const uint4*>(row + (((uint32_t)piece << 4) ^ swizzle));
     const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-    const Pair& s = p[piece * kPerHalf / 4];
+    const Pair& s = p[piece * kScales / kPieces];
     uint32_t r[16];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -94,7 +124,7 @@ __device__ __forceinline__ void dequantise(const uint8_t* row, uint32_t swizzle,
 
 struct UmmaShape {
   int T, V, d, groups;
-  int halves, stages;            // pieces of 128 and of 256 of k in a row
+  int stages;                    // pieces of 256 of k in a row
   int rows_box;                  // rows of a box, 128 at most
   int boxes;                     // boxes of the head
   int ring;                      // stages of the ring
@@ -105,19 +135,17 @@ __device__ __forceinline__ void put_logit(void* logits, int type, int64_t at, fl
   else static_cast<__nv_bfloat16*>(logits)[at] = __float2bfloat16_rn(v);
 }
 
-// kN: tokens, rounded up; kM: boxes that share a stage's tokens; kGroups: of four dequantising warps; kPerHalf: scales in 128 weights.
-template <int kM, int kGroups>
-constexpr int kUmmaThreads = 32 * (kMiscWarps + 4 * kM + 4 * kGroups);
-template <int kN, int kM>
-constexpr int kUmmaStageBytes = kM * kCodesBytes + 4 * kN * 128;
+template <int kN>
+constexpr int kUmmaStageBytes = kCodesBytes + 4 * kN * 128;
 
-template <int kN, int kM, int kGroups, int kPerHalf>
-__global__ void __launch_bounds__(kUmmaThreads<kM, kGroups>, 1) quant_umma_kernel(
+// kN: tokens, rounded up; kScales: scales in 256 weights.
+template <int kN, int kScales>
+__global__ void __launch_bounds__(kThreads, 1) quant_umma_kernel(
     const __grid_constant__ CUtensorMap codes, const __grid_constant__ CUtensorMap hidden, const __nv_bfloat16* __restrict__ scale,
     const UmmaShape sh, void* __restrict__ logits, int type, int64_t pitch, unsigned int* d_err) {
-  constexpr int kStage = kUmmaStageBytes<kN, kM>;
+  constexpr int kStage = kUmmaStageBytes<kN>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_bars[2 * kMaxRing + 2 * kBufs + 4];
+  __shared__ __align__(8) uint64_t s_bars[2 * kMaxRing + 2 * kGroups + 4];
   __shared__ uint32_t s_tmem;
   __shared__ int abort_flag;
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -125,15 +153,15 @@ __global__ void __launch_bounds__(kUmmaThreads<kM, kGroups>, 1) quant_umma_kerne
   auto full_bar = [&](int s) { return bars + 8u * s; };
   auto empty_bar = [&](int s) { return bars + 8u * (kMaxRing + s); };
   auto a_full = [&](int b) { return bars + 8u * (2 * kMaxRing + b); };
-  auto a_empty = [&](int b) { return bars + 8u * (2 * kMaxRing + kBufs + b); };
-  auto acc_full = [&](int a) { return bars + 8u * (2 * kMaxRing + 2 * kBufs + a); };
-  auto acc_empty = [&](int a) { return bars + 8u * (2 * kMaxRing + 2 * kBufs + 2 + a); };
+  auto a_empty = [&](int b) { return bars + 8u * (2 * kMaxRing + kGroups + b); };
+  auto acc_full = [&](int a) { return bars + 8u * (2 * kMaxRing + 2 * kGroups + a); };
+  auto acc_empty = [&](int a) { return bars + 8u * (2 * kMaxRing + 2 * kGroups + 2 + a); };
   const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int s = 0; s < sh.ring; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int b = 0; b < kBufs; ++b) { mbar_init(a_full(b), 4); mbar_init(a_empty(b), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 4 * kM); }
+    for (int b = 0; b < kGroups; ++b) { mbar_init(a_full(b), 4); mbar_init(a_empty(b), 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 4); }
     fence_mbar_init();
     tma_prefetch_desc(&codes);
     tma_prefetch_desc(&hidden);
@@ -148,160 +176,139 @@ __global__ void __launch_bounds__(kUmmaThreads<kM, kGroups>, 1) quant_umma_kerne
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  // boxes b, b + grid, ... are this CTA's; kM of them at a time are a tile
-  const int my_boxes = (sh.boxes - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
-  const int tiles = (my_boxes + kM - 1) / kM;
-  auto boxes_in = [&](int tile) { return kM == 1 ? 1 : min(kM, my_boxes - tile * kM); };
-  auto box_row = [&](int tile, int m) { return (int64_t)((int64_t)(tile * kM + m) * gridDim.x + blockIdx.x) * sh.rows_box; };
-  auto halves_in = [&](int s) { return min(2, sh.halves - 2 * s); };
+  // boxes b, b + grid, ... are this CTA's
+  const int boxes = (sh.boxes - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+  const int64_t row0 = (int64_t)blockIdx.x * sh.rows_box, row_step = (int64_t)gridDim.x * sh.rows_box;
 
   if (warp == 0) {
     if (lane == 0) {                               // ---- loads
       int slot = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int tile = 0; tile < tiles && ok; ++tile) {
-        const int boxes = boxes_in(tile);
+      for (int box = 0; box < boxes && ok; ++box)
         for (int s = 0; s < sh.stages; ++s) {
-          if (!mbar_wait(empty_bar(slot), phase ^ 1u, &abort_flag)) { ok = false; break; }
+          if (!sleep_wait(empty_bar(slot), phase ^ 1u, &abort_flag)) { ok = false; break; }
           const int blocks = min(4, (sh.d - s * kStageK + 63) / 64);
           const uint32_t at = ring_at + slot * kStage;
-          mbar_arrive_expect_tx(full_bar(slot), boxes * sh.rows_box * 128 + blocks * kN * 128);
-          for (int m = 0; m < boxes; ++m)
-            tma_load_2d(at + m * kCodesBytes, &codes, full_bar(slot), s * (kStageK / 4), (int)box_row(tile, m));
+          mbar_arrive_expect_tx(full_bar(slot), sh.rows_box * 128 + blocks * kN * 128);
+          tma_load_2d(at, &codes, full_bar(slot), s * (kStageK / 4), (int)(row0 + box * row_step));
           for (int b = 0; b < blocks; ++b)
-            tma_load_2d(at + kM * kCodesBytes + b * kN * 128, &hidden, full_bar(slot), s * kStageK + b * 64, 0);
+            tma_load_2d(at + kCodesBytes + b * kN * 128, &hidden, full_bar(slot), s * kStageK + b * 64, 0);
           if (++slot == sh.ring) { slot = 0; phase ^= 1u; }
         }
-      }
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0) {                               // ---- products
-      const uint32_t idesc = instr_desc_bf16_f32(kRowsM, kN);
-      int slot = 0, buf = 0, acc = 0;
-      uint32_t phase = 0, buf_phase = 0, acc_phase = 0;
-      bool ok = true;
-      for (int tile = 0; tile < tiles && ok; ++tile) {
-        const int boxes = boxes_in(tile);
-        for (int s = 0; s < sh.stages && ok; ++s) {
-          if (!mbar_wait(full_bar(slot), phase, &abort_flag)) { ok = false; break; }
-          if (s % 2 == 0 && !mbar_wait(acc_empty(acc), acc_phase ^ 1u, &abort_flag)) { ok = false; break; }
-          const uint32_t x_at = ring_at + slot * kStage + kM * kCodesBytes;
-          for (int h = 0; h < halves_in(s) && ok; ++h) {
-            const int steps = min(kHalfK, sh.d - s * kStageK - h * kHalfK) / 16;
-            for (int m = 0; m < boxes; ++m) {
-              if (!mbar_wait(a_full(buf), buf_phase, &abort_flag)) { ok = false; break; }
-              tc_fence_after();
-              const uint32_t a_at = tmem + kBufCol0 + buf * kBufCols, d_at = tmem + (acc * kM + m) * kN;
-              for (int k = 0; k < steps; ++k) {
-                const uint64_t b_desc = smem_desc_k_sw128(x_at + (h * 2 + k / 4) * (kN * 128)) + (uint64_t)(k % 4) * 2;
-                mma_bf16_ts(d_at, a_at + k * 8, b_desc, idesc, s % 2 == 0 && h == 0 && k == 0 ? 0u : 1u);
-              }
-              mma_commit(a_empty(buf));
-              if (++buf == kBufs) { buf = 0; buf_phase ^= 1u; }
-            }
+    // ---- products: the whole warp keeps step, one lane issues; so that addresses stay in uniform registers
+    const uint32_t idesc = instr_desc_bf16_f32(kRowsM, kN);
+    const uint64_t desc0 = smem_desc_k_sw128(ring_at + kCodesBytes);
+    int slot = 0, buf = 0, acc = 0;
+    uint32_t buf_phase = 0, acc_phase = 0;
+    bool ok = true;
+    for (int box = 0; box < boxes && ok; ++box)
+      for (int s = 0; s < sh.stages; ++s) {
+        // a group that hands rows over has seen their stage arrive, the tokens with it
+        if (s % 2 == 0) ok = __all_sync(0xffffffffu, ready_wait(acc_empty(acc), acc_phase ^ 1u, &abort_flag));
+        ok = ok && __all_sync(0xffffffffu, ready_wait(a_full(buf), buf_phase, &abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        const int steps = min(kStageK, sh.d - s * kStageK) / 16;
+        const uint32_t a_at = tmem + kBufCol0 + buf * kBufCols, d_at = tmem + acc * kN;
+        const uint64_t desc = desc0 + (uint64_t)(uint32_t)(slot * (kStage / 16));
+        const bool part_ends = s % 2 == 1 || s + 1 == sh.stages;
+        if (elect_one()) {
+          if (steps == kStageK / 16) {
+#pragma unroll
+            for (int k = 0; k < kStageK / 16; ++k)
+              mma_bf16_ts(d_at, a_at + k * 8, desc + (uint64_t)((k / 4) * (kN * 128 / 16) + (k % 4) * 2), idesc, k != 0 ? 1u : (uint32_t)(s % 2));
+          } else {
+            for (int k = 0; k < steps; ++k)
+              mma_bf16_ts(d_at, a_at + k * 8, desc + (uint64_t)((k / 4) * (kN * 128 / 16) + (k % 4) * 2), idesc, k != 0 ? 1u : (uint32_t)(s % 2));
           }
-          if (!ok) break;
+          mma_commit(a_empty(buf));
           mma_commit(empty_bar(slot));
-          if (++slot == sh.ring) { slot = 0; phase ^= 1u; }
-          if (s % 2 == 1 || s + 1 == sh.stages) {  // a part ends
-            mma_commit(acc_full(acc));
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
-          }
+          if (part_ends) mma_commit(acc_full(acc));
         }
+        __syncwarp();
+        if (part_ends && ++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        if (++buf == kGroups) { buf = 0; buf_phase ^= 1u; }
+        if (++slot == sh.ring) slot = 0;
       }
-    }
-    __syncwarp();
-  } else if (warp >= kMiscWarps && warp < kMiscWarps + 4 * kM) {
+  } else if (warp >= kReaders && warp < kReaders + 4) {
     // ---- sums of the parts, and out
-    const int m = (warp - kMiscWarps) / 4, quarter = warp & 3, r = quarter * 32 + lane;
+    const int quarter = warp & 3, r = quarter * 32 + lane;
     const int parts = (sh.stages + 1) / 2;
     int acc = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
-    for (int tile = 0; tile < tiles && ok; ++tile) {
+    for (int box = 0; box < boxes && ok; ++box) {
       float sum[kN];
 #pragma unroll
       for (int n = 0; n < kN; ++n) sum[n] = 0.f;
-      const bool here = m < boxes_in(tile);
       for (int part = 0; part < parts; ++part) {
-        ok = __all_sync(0xffffffffu, mbar_wait(acc_full(acc), acc_phase, &abort_flag));
+        ok = __all_sync(0xffffffffu, sleep_wait(acc_full(acc), acc_phase, &abort_flag));
         if (!ok) break;
         tc_fence_after();
-        if (here) {
 #pragma unroll
-          for (int n0 = 0; n0 < kN; n0 += 16) {
-            uint32_t v[16];
-            tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + (acc * kM + m) * kN + n0, v);
-            tmem_ld_wait();
+        for (int n0 = 0; n0 < kN; n0 += 16) {
+          uint32_t v[16];
+          tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + acc * kN + n0, v);
+          tmem_ld_wait();
 #pragma unroll
-            for (int n = 0; n < 16; ++n) sum[n0 + n] += __uint_as_float(v[n]);
-          }
+          for (int n = 0; n < 16; ++n) sum[n0 + n] += __uint_as_float(v[n]);
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(acc_empty(acc));
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
-      const int64_t v = box_row(tile, m) + r;
-      if (ok && here && r < sh.rows_box && v < sh.V) {
+      const int64_t v = row0 + box * row_step + r;
+      if (ok && r < sh.rows_box && v < sh.V) {
 #pragma unroll
         for (int n = 0; n < kN; ++n)
           if (n < sh.T) put_logit(logits, type, n * pitch + v, sum[n]);
       }
     }
-  } else if (warp >= kMiscWarps + 4 * kM) {
-    // ---- digits to weights
-    const int group = (warp - kMiscWarps - 4 * kM) / 4, quarter = warp & 3, r = quarter * 32 + lane;
-    const uint32_t swizzle_row = (uint32_t)(r & 7) << 4;
-    const bool row_in_box = r < sh.rows_box;
-    // units in the order of the products: tile, stage, half, box
-    int tile = 0, s = 0, h = 0, m = 0, slot = 0, buf = 0;
+  } else if (warp >= kReaders + 4) {
+    // ---- digits to weights: every kGroups-th stage
+    const int group = (warp - kReaders - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t swizzle = (uint32_t)(r & 7) << 4;
+    const uint32_t to = tmem + ((uint32_t)(quarter * 32) << 16) + kBufCol0 + group * kBufCols;
+    const uint8_t* const rows = smem + r * 128;
+    int box = 0, s = group, slot = group % sh.ring;
     uint32_t phase = 0, buf_phase = 0;
-    auto next = [&] {
-      if (++buf == kBufs) { buf = 0; buf_phase ^= 1u; }
-      if (++m < boxes_in(tile)) return;
-      m = 0;
-      if (++h < halves_in(s)) return;
-      h = 0;
-      if (++slot == sh.ring) { slot = 0; phase ^= 1u; }
-      if (++s < sh.stages) return;
-      s = 0;
-      ++tile;
-    };
-    uint32_t bits[kPerHalf];                       // the unit's scales, one unit ahead of its codes
+    while (s >= sh.stages) { s -= sh.stages; ++box; }
+    int64_t v = row0 + box * row_step + r;
+    // the stage's scales, one turn ahead of its codes
+    const uint16_t* const scales = reinterpret_cast<const uint16_t*>(scale);
+    uint32_t bits[kScales];
     auto fetch = [&] {
-      const int64_t v = tile < tiles ? box_row(tile, m) + r : sh.V;
-      const int g0 = (2 * s + h) * kPerHalf;
+      const bool in = box < boxes && r < sh.rows_box && v < sh.V;
 #pragma unroll
-      for (int k = 0; k < kPerHalf; ++k)
-        bits[k] = row_in_box && v < sh.V ? __ldg(reinterpret_cast<const uint16_t*>(scale) + v * sh.groups + min(g0 + k, sh.groups - 1)) : 0u;
+      for (int k = 0; k < kScales; ++k) bits[k] = in ? __ldg(scales + v * sh.groups + min(s * kScales + k, sh.groups - 1)) : 0u;
     };
-    for (int k = 0; k < group; ++k) next();
     fetch();
-    while (tile < tiles) {
-      if (!__all_sync(0xffffffffu, mbar_wait(full_bar(slot), phase, &abort_flag))) break;
-      const uint8_t* const row = smem + slot * kStage + m * kCodesBytes + r * 128;
-      const uint32_t swizzle = ((uint32_t)h << 6) ^ swizzle_row;
-      const int this_buf = buf;
-      const uint32_t this_phase = buf_phase;
-      Pair p[kPerHalf];
+    while (box < boxes) {
+      Pair p[kScales];
       bool quick = true;
 #pragma unroll
-      for (int k = 0; k < kPerHalf; ++k) { p[k] = scale_pair(bits[k]); quick = quick && p[k].quick; }
+      for (int k = 0; k < kScales; ++k) { p[k] = scale_pair(bits[k]); quick = quick && p[k].quick; }
       quick = __all_sync(0xffffffffu, quick);
-      for (int k = 0; k < kGroups; ++k) next();
+      const uint8_t* const row = rows + slot * kStage;
+      if (!__all_sync(0xffffffffu, sleep_wait(full_bar(slot), phase, &abort_flag) && sleep_wait(a_empty(group), buf_phase ^ 1u, &abort_flag))) break;
+      slot += kGroups;
+      if (slot >= sh.ring) { slot -= sh.ring; phase ^= 1u; }
+      s += kGroups;
+      while (s >= sh.stages) { s -= sh.stages; ++box; v += row_step; }
       fetch();
-      if (!__all_sync(0xffffffffu, mbar_wait(a_empty(this_buf), this_phase ^ 1u, &abort_flag))) break;
       tc_fence_after();
-      const uint32_t to = tmem + ((uint32_t)(quarter * 32) << 16) + kBufCol0 + this_buf * kBufCols;
-      if (quick) dequantise<true, kPerHalf>(row, swizzle, p, to);
-      else dequantise<false, kPerHalf>(row, swizzle, p, to);
+      if (quick) dequantise<true, kScales>(row, swizzle, p, to);
+      else dequantise<false, kScales>(row, swizzle, p, to);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(a_full(this_buf));
+      if (lane == 0) mbar_arrive(a_full(group));
+      buf_phase ^= 1u;
     }
   }
   __syncwarp();
@@ -315,18 +322,18 @@ __global__ void __launch_bounds__(kUmmaThreads<kM, kGroups>, 1) quant_umma_kerne
   if (warp == 1) tmem_dealloc(tmem, kTmemCols);
 }
 
-template <int kN, int kM, int kGroups, int kPerHalf>
+template <int kN, int kScales>
 af_status launch_umma(af_ctx* ctx, const void* hidden, const QuantHead& h, int T, void* logits, int type, int64_t pitch, cudaStream_t s) {
   UmmaShape sh;
   sh.T = T; sh.V = h.V; sh.d = h.d; sh.groups = h.groups();
-  sh.halves = (h.d + kHalfK - 1) / kHalfK;
   sh.stages = (h.d + kStageK - 1) / kStageK;
   // boxes of one size, as many to every CTA: 128 rows or a little less
   const int64_t per_cta = ((int64_t)h.V + (int64_t)ctx->sm_count * kRowsM - 1) / ((int64_t)ctx->sm_count * kRowsM);
   const int64_t want = per_cta * ctx->sm_count;
   sh.rows_box = (int)((h.V + want - 1) / want);
   sh.boxes = (h.V + sh.rows_box - 1) / sh.rows_box;
-  constexpr int stage = kUmmaStageBytes<kN, kM>, ring = (kSmemLimit - 1024) / stage < kMaxRing ? (kSmemLimit - 1024) / stage : kMaxRing;
+  constexpr int stage = kUmmaStageBytes<kN>, ring = (kSmemLimit - 1024) / stage < kMaxRing ? (kSmemLimit - 1024) / stage : kMaxRing;
+  static_assert(ring >= kGroups, "every group has a stage");
   sh.ring = ring;
   constexpr int smem = 1024 + ring * stage;
   CUtensorMap codes, x;                            // the codes as a matrix of d / 4 16-bit elements
@@ -335,25 +342,25 @@ af_status launch_umma(af_ctx* ctx, const void* hidden, const QuantHead& h, int T
   if (st == AF_OK) st = encode_operand(env, &x, Operand{hidden, (uint64_t)T, (uint64_t)h.d, (uint64_t)h.d * 2}, kN);
   if (st != AF_OK) return st;
   static SmemAttrOnce once;
-  if (set_smem_once(once, quant_umma_kernel<kN, kM, kGroups, kPerHalf>, smem) != cudaSuccess) return AF_ERR_CUDA;
+  if (set_smem_once(once, quant_umma_kernel<kN, kScales>, smem) != cudaSuccess) return AF_ERR_CUDA;
   const int blocks = sh.boxes < ctx->sm_count ? sh.boxes : ctx->sm_count;
-  return launch_overlapped(quant_umma_kernel<kN, kM, kGroups, kPerHalf>, blocks, kUmmaThreads<kM, kGroups>, smem, s, codes, x, h.scale, sh,
-                           logits, type, pitch, ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  return launch_overlapped(quant_umma_kernel<kN, kScales>, blocks, kThreads, smem, s, codes, x, h.scale, sh, logits, type, pitch,
+                           ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
-template <int kN, int kM, int kGroups>
+template <int kN>
 af_status launch_umma_group(af_ctx* ctx, const void* hidden, const QuantHead& h, int T, void* logits, int type, int64_t pitch, cudaStream_t s) {
-  if (h.group == 32) return launch_umma<kN, kM, kGroups, 4>(ctx, hidden, h, T, logits, type, pitch, s);
-  if (h.group == 64) return launch_umma<kN, kM, kGroups, 2>(ctx, hidden, h, T, logits, type, pitch, s);
-  return launch_umma<kN, kM, kGroups, 1>(ctx, hidden, h, T, logits, type, pitch, s);
+  if (h.group == 32) return launch_umma<kN, 8>(ctx, hidden, h, T, logits, type, pitch, s);
+  if (h.group == 64) return launch_umma<kN, 4>(ctx, hidden, h, T, logits, type, pitch, s);
+  return launch_umma<kN, 2>(ctx, hidden, h, T, logits, type, pitch, s);
 }
 
 }  // namespace
 
 af_status launch_quant_umma(af_ctx* ctx, const void* hidden, const QuantHead& h, int T, void* logits, int32_t type, int64_t pitch,
                             cudaStream_t s) {
-  if (T <= 16) return launch_umma_group<16, 1, 2>(ctx, hidden, h, T, logits, type, pitch, s);
-  if (T <= 32) return launch_umma_group<32, 1, 2>(ctx, hidden, h, T, logits, type, pitch, s);
-  return launch_umma_group<64, 1, 2>(ctx, hidden, h, T, logits, type, pitch, s);
+  if (T <= 16) return launch_umma_group<16>(ctx, hidden, h, T, logits, type, pitch, s);
+  if (T <= 32) return launch_umma_group<32>(ctx, hidden, h, T, logits, type, pitch, s);
+  return launch_umma_group<64>(ctx, hidden, h, T, logits, type, pitch, s);
 }
 
 }  // namespace af
