@@ -295,7 +295,9 @@ __global__ void __launch_bounds__(kThreads, 1) quant_umma_kernel(
       for (int k = 0; k < kScales; ++k) { p[k] = scale_pair(bits[k]); quick = quick && p[k].quick; }
       quick = __all_sync(0xffffffffu, quick);
       const uint8_t* const row = rows + slot * kStage;
-      if (!__all_sync(0xffffffffu, sleep_wait(full_bar(slot), phase, &abort_flag) && sleep_wait(a_empty(group), buf_phase ^ 1u, &abort_flag))) break;
+      // the buffer first: once the products of this group's last stage are done, so are all before it, and the slot's barrier
+      // is in the phase that is waited for or past it.  Asked before, a parity could be that of the phase before the last.
+      if (!__all_sync(0xffffffffu, sleep_wait(a_empty(group), buf_phase ^ 1u, &abort_flag) && sleep_wait(full_bar(slot), phase, &abort_flag))) break;
       slot += kGroups;
       if (slot >= sh.ring) { slot -= sh.ring; phase ^= 1u; }
       s += kGroups;
