@@ -12,9 +12,13 @@
 // So a pair costs a shift, a mask-and-or (both on the ALU pipe, at half rate, which is what this kernel is bound by next to
 // memory) and a multiply-add.
 //
-// Warps: 0 loads stages of 256 of k into a ring (a box of 128 rows' codes and the tokens'), 1 issues the MMAs, 4 to 7 read
-// accumulators, the others dequantise, a stage per group of four and a buffer in tensor memory per group.  Sums are taken in
-// parts of 512 of k, which the readers add in fp32, rounding to nearest (see umma.cuh on truncation).
+// Warps: 0 loads stages of 256 of k into a ring (the codes of a box of 128 rows, or of two, and the tokens'), 1 and 2 issue the
+// MMAs, each for an accumulator of its own, the next four (or eight) read accumulators, the others dequantise, in groups of four
+// warps with two buffers of 128 of k in tensor memory each, so that a group writes one while the other is multiplied.  Sums are
+// taken in parts of 512 of k, which the readers add in fp32, rounding to nearest (see umma.cuh on truncation).
+// Up to 32 tokens: one box a stage, three groups taking stages in turn, the accumulators taking parts in turn.  More: the
+// tokens' share of a stage, fetched from L2 by every CTA, outweighs the codes', so two boxes share it, each with its group,
+// accumulator and readers.
 #include "gemm_launch.cuh"
 #include "rollout.cuh"
 
@@ -25,14 +29,30 @@ using namespace umma;
 
 constexpr int kRowsM = 128;                        // rows of an MMA
 constexpr int kStageK = 256;                       // k of a stage: 128 bytes of codes
-constexpr int kGroups = 3;                         // of four dequantising warps
-constexpr int kBufCols = kStageK / 2;              // columns of a buffer of dequantised rows: two bf16 each
+constexpr int kHalfK = 128;                        // k of a buffer of dequantised rows
+constexpr int kBufCols = kHalfK / 2;               // its columns: two bf16 each
 constexpr int kBufCol0 = 128;                      // behind two accumulators of up to 64 columns
 constexpr int kReaders = 4;                        // the first of the warps that read accumulators: a multiple of 4, as TMEM's lanes go
-constexpr int kThreads = 32 * (kReaders + 4 + 4 * kGroups);
 constexpr int kCodesBytes = kRowsM * 128;
-constexpr int kMaxRing = 10;
+constexpr int kMaxRing = 9, kMaxBufs = 6;
 constexpr int kSmemLimit = 225 * 1024;
+// kM: boxes that share a stage.
+template <int kM>
+struct Roles {
+  static constexpr int kGroups = kM == 1 ? 3 : 2;  // of four dequantising warps
+  static constexpr int kFirstGroup = kReaders + 4 * kM;
+  static constexpr int kThreads = 32 * (kFirstGroup + 4 * kGroups);
+};
+template <int kN, int kM>
+struct Stage {
+  static constexpr int kTokensAt = kM * kCodesBytes;
+  static constexpr int kBytes = kTokensAt + 4 * kN * 128;
+  // with one box a slot belongs to one group, which so has seen each of its phases: a parity cannot be mistaken for that of the
+  // phase before the last
+  static constexpr int kFit = (kSmemLimit - 1024) / kBytes, kMost = kFit < kMaxRing ? kFit : kMaxRing;
+  static constexpr int kRing = kM == 1 ? kMost / Roles<1>::kGroups * Roles<1>::kGroups : kMost;
+  static_assert(kRing >= 3, "loads ahead of the products");
+};
 
 // A bounded wait in which the warp sleeps: the scheduler's issue slots belong to the warps that dequantise.
 __device__ __forceinline__ bool sleep_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -102,14 +122,14 @@ template <bool kQuick>
 __device__ __forceinline__ uint32_t weight_pair(uint32_t v, const Pair& p) {
   return kQuick ? bf2_fma(v, p.s, p.c) : bf2_fma(bf2_fma(v, kOne2, kMinus24), p.s, kZero2);
 }
-template <bool kQuick, int kScales>
+// 128 of k of a row, with scales p[first], ...; piece0: 16-byte piece of the line that they start at.
+template <bool kQuick, int kScales, int kPiece0>
 __device__ __forceinline__ void dequantise(const uint8_t* row, uint32_t swizzle, const Pair (&p)[kScales], uint32_t to) {
-  constexpr int kPieces = kStageK / 32;
 #pragma unroll
-  for (int piece = 0; piece < kPieces; ++piece) {
+  for (int piece = kPiece0; piece < kPiece0 + kHalfK / 32; ++piece) {
     const uint4 w4 = *reinterpret_cast<const uint4*>(row + (((uint32_t)piece << 4) ^ swizzle));
     const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-    const Pair& s = p[piece * kScales / kPieces];
+    const Pair& s = p[piece * kScales / (kStageK / 32)];
     uint32_t r[16];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -118,7 +138,7 @@ __device__ __forceinline__ void dequantise(const uint8_t* row, uint32_t swizzle,
       r[4 * j + 2] = weight_pair<kQuick>(digit_pair<2>(w[j]), s);
       r[4 * j + 3] = weight_pair<kQuick>(digit_pair<3>(w[j]), s);
     }
-    tmem_st16(to + piece * 16, r);
+    tmem_st16(to + (piece - kPiece0) * 16, r);
   }
 }
 
@@ -127,7 +147,6 @@ struct UmmaShape {
   int stages;                    // pieces of 256 of k in a row
   int rows_box;                  // rows of a box, 128 at most
   int boxes;                     // boxes of the head
-  int ring;                      // stages of the ring
 };
 
 __device__ __forceinline__ void put_logit(void* logits, int type, int64_t at, float v) {
@@ -135,32 +154,31 @@ __device__ __forceinline__ void put_logit(void* logits, int type, int64_t at, fl
   else static_cast<__nv_bfloat16*>(logits)[at] = __float2bfloat16_rn(v);
 }
 
-template <int kN>
-constexpr int kUmmaStageBytes = kCodesBytes + 4 * kN * 128;
-
-// kN: tokens, rounded up; kScales: scales in 256 weights.
-template <int kN, int kScales>
-__global__ void __launch_bounds__(kThreads, 1) quant_umma_kernel(
+// kN: tokens, rounded up; kM: boxes that share a stage; kScales: scales in 256 weights.
+template <int kN, int kM, int kScales>
+__global__ void __launch_bounds__(Roles<kM>::kThreads, 1) quant_umma_kernel(
     const __grid_constant__ CUtensorMap codes, const __grid_constant__ CUtensorMap hidden, const __nv_bfloat16* __restrict__ scale,
     const UmmaShape sh, void* __restrict__ logits, int type, int64_t pitch, unsigned int* d_err) {
-  constexpr int kStage = kUmmaStageBytes<kN>;
+  using St = Stage<kN, kM>;
+  constexpr int kStage = St::kBytes, kRing = St::kRing, kGroups = Roles<kM>::kGroups;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_bars[2 * kMaxRing + 2 * kGroups + 4];
+  __shared__ __align__(8) uint64_t s_bars[2 * kRing + 3 * kMaxBufs + 4];
   __shared__ uint32_t s_tmem;
   __shared__ int abort_flag;
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t ring_at = smem_u32(smem), bars = smem_u32(s_bars);
   auto full_bar = [&](int s) { return bars + 8u * s; };
-  auto empty_bar = [&](int s) { return bars + 8u * (kMaxRing + s); };
-  auto a_full = [&](int b) { return bars + 8u * (2 * kMaxRing + b); };
-  auto a_empty = [&](int b) { return bars + 8u * (2 * kMaxRing + kGroups + b); };
-  auto acc_full = [&](int a) { return bars + 8u * (2 * kMaxRing + 2 * kGroups + a); };
-  auto acc_empty = [&](int a) { return bars + 8u * (2 * kMaxRing + 2 * kGroups + 2 + a); };
+  auto empty_bar = [&](int s) { return bars + 8u * (kRing + s); };
+  // a buffer is full for one of the accumulators: each issuing warp follows its own barriers, phase by phase
+  auto a_full = [&](int a, int group, int half) { return bars + 8u * (2 * kRing + kMaxBufs * a + 2 * group + half); };
+  auto a_empty = [&](int group, int half) { return bars + 8u * (2 * kRing + 2 * kMaxBufs + 2 * group + half); };
+  auto acc_full = [&](int a) { return bars + 8u * (2 * kRing + 3 * kMaxBufs + a); };
+  auto acc_empty = [&](int a) { return bars + 8u * (2 * kRing + 3 * kMaxBufs + 2 + a); };
   const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   if (threadIdx.x == 0) {
     abort_flag = 0;
-    for (int s = 0; s < sh.ring; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int b = 0; b < kGroups; ++b) { mbar_init(a_full(b), 4); mbar_init(a_empty(b), 1); }
+    for (int s = 0; s < kRing; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), kM); }
+    for (int b = 0; b < 2 * kGroups; ++b) { mbar_init(a_full(0, 0, b), 4); mbar_init(a_full(1, 0, b), 4); mbar_init(a_empty(0, b), 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 4); }
     fence_mbar_init();
     tma_prefetch_desc(&codes);
@@ -176,91 +194,111 @@ __global__ void __launch_bounds__(kThreads, 1) quant_umma_kernel(
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  // boxes b, b + grid, ... are this CTA's
-  const int boxes = (sh.boxes - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+  // boxes b, b + grid, ... are this CTA's; kM of them at a time are a tile
+  const int boxes = (sh.boxes - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x, tiles = (boxes + kM - 1) / kM;
   const int64_t row0 = (int64_t)blockIdx.x * sh.rows_box, row_step = (int64_t)gridDim.x * sh.rows_box;
+  const int parts = (sh.stages + 1) / 2;
 
   if (warp == 0) {
     if (lane == 0) {                               // ---- loads
       int slot = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int box = 0; box < boxes && ok; ++box)
+      for (int tile = 0; tile < tiles && ok; ++tile) {
+        const int here = min(kM, boxes - tile * kM);
         for (int s = 0; s < sh.stages; ++s) {
           if (!sleep_wait(empty_bar(slot), phase ^ 1u, &abort_flag)) { ok = false; break; }
           const int blocks = min(4, (sh.d - s * kStageK + 63) / 64);
           const uint32_t at = ring_at + slot * kStage;
-          mbar_arrive_expect_tx(full_bar(slot), sh.rows_box * 128 + blocks * kN * 128);
-          tma_load_2d(at, &codes, full_bar(slot), s * (kStageK / 4), (int)(row0 + box * row_step));
+          mbar_arrive_expect_tx(full_bar(slot), here * sh.rows_box * 128 + blocks * kN * 128);
+          for (int m = 0; m < here; ++m)
+            tma_load_2d(at + m * kCodesBytes, &codes, full_bar(slot), s * (kStageK / 4), (int)(row0 + (tile * kM + m) * row_step));
           for (int b = 0; b < blocks; ++b)
-            tma_load_2d(at + kCodesBytes + b * kN * 128, &hidden, full_bar(slot), s * kStageK + b * 64, 0);
-          if (++slot == sh.ring) { slot = 0; phase ^= 1u; }
+            tma_load_2d(at + St::kTokensAt + b * kN * 128, &hidden, full_bar(slot), s * kStageK + b * 64, 0);
+          if (++slot == kRing) { slot = 0; phase ^= 1u; }
         }
+      }
     }
     __syncwarp();
-  } else if (warp == 1) {
+  } else if (warp <= 2) {
     // ---- products: the whole warp keeps step, one lane issues; so that addresses stay in uniform registers
-    const uint32_t idesc = instr_desc_bf16_f32(kRowsM, kN);
-    const uint64_t desc0 = smem_desc_k_sw128(ring_at + kCodesBytes);
-    int slot = 0, buf = 0, acc = 0;
-    uint32_t buf_phase = 0, acc_phase = 0;
+    const int a = warp - 1;                        // its accumulator
+    const uint32_t idesc = instr_desc_bf16_f32(kRowsM, kN), d_at = tmem + a * kN;
+    const uint64_t desc0 = smem_desc_k_sw128(ring_at + St::kTokensAt);
+    int slot = 0, group = kM == 1 ? 0 : a, part = 0;
+    uint32_t phase = 0, acc_phase = 0, seen = 0;   // seen: a bit per group, the parity of what it has handed this warp
     bool ok = true;
-    for (int box = 0; box < boxes && ok; ++box)
+    for (int tile = 0; tile < tiles && ok; ++tile) {
+      const bool absent = kM == 2 && tile * kM + a >= boxes;
       for (int s = 0; s < sh.stages; ++s) {
-        // a group that hands rows over has seen their stage arrive, the tokens with it
-        if (s % 2 == 0) ok = __all_sync(0xffffffffu, ready_wait(acc_empty(acc), acc_phase ^ 1u, &abort_flag));
-        ok = ok && __all_sync(0xffffffffu, ready_wait(a_full(buf), buf_phase, &abort_flag));
-        if (!ok) break;
-        tc_fence_after();
-        const int steps = min(kStageK, sh.d - s * kStageK) / 16;
-        const uint32_t a_at = tmem + kBufCol0 + buf * kBufCols, d_at = tmem + acc * kN;
-        const uint64_t desc = desc0 + (uint64_t)(uint32_t)(slot * (kStage / 16));
         const bool part_ends = s % 2 == 1 || s + 1 == sh.stages;
-        if (elect_one()) {
-          if (steps == kStageK / 16) {
+        if (absent) {                              // the last tile has one box: its stages are freed for the other accumulator
+          ok = __all_sync(0xffffffffu, ready_wait(full_bar(slot), phase, &abort_flag));
+          if (!ok) break;
+          if (elect_one()) mbar_arrive(empty_bar(slot));
+        } else if (kM == 2 || (part & 1) == a) {
+          if (s % 2 == 0) ok = __all_sync(0xffffffffu, ready_wait(acc_empty(a), acc_phase ^ 1u, &abort_flag));
+          const uint64_t desc = desc0 + (uint64_t)(uint32_t)(slot * (kStage / 16));
+          const uint32_t a_at = tmem + kBufCol0 + group * (2 * kBufCols);
 #pragma unroll
-            for (int k = 0; k < kStageK / 16; ++k)
-              mma_bf16_ts(d_at, a_at + k * 8, desc + (uint64_t)((k / 4) * (kN * 128 / 16) + (k % 4) * 2), idesc, k != 0 ? 1u : (uint32_t)(s % 2));
-          } else {
-            for (int k = 0; k < steps; ++k)
-              mma_bf16_ts(d_at, a_at + k * 8, desc + (uint64_t)((k / 4) * (kN * 128 / 16) + (k % 4) * 2), idesc, k != 0 ? 1u : (uint32_t)(s % 2));
+          for (int half = 0; half < 2; ++half) {
+            // a group that hands rows over has seen their stage arrive, the tokens with it
+            ok = ok && __all_sync(0xffffffffu, ready_wait(a_full(a, group, half), seen >> group & 1u, &abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            const int steps = min(kHalfK, sh.d - s * kStageK - half * kHalfK) / 16;       // none: a last half past the row
+            if (elect_one()) {
+              auto product = [&](int k) {
+                mma_bf16_ts(d_at, a_at + half * kBufCols + k * 8, desc + (uint64_t)((2 * half + k / 4) * (kN * 128 / 16) + (k % 4) * 2), idesc,
+                            half + k != 0 ? 1u : (uint32_t)(s % 2));
+              };
+              if (steps == kHalfK / 16) {
+#pragma unroll
+                for (int k = 0; k < kHalfK / 16; ++k) product(k);
+              } else {
+                for (int k = 0; k < steps; ++k) product(k);
+              }
+              mma_commit(a_empty(group, half));
+              if (half == 1) mma_commit(empty_bar(slot));
+              if (half == 1 && part_ends) mma_commit(acc_full(a));
+            }
+            __syncwarp();
           }
-          mma_commit(a_empty(buf));
-          mma_commit(empty_bar(slot));
-          if (part_ends) mma_commit(acc_full(acc));
+          if (!ok) break;
+          seen ^= 1u << group;
+          if (part_ends) acc_phase ^= 1u;
         }
-        __syncwarp();
-        if (part_ends && ++acc == 2) { acc = 0; acc_phase ^= 1u; }
-        if (++buf == kGroups) { buf = 0; buf_phase ^= 1u; }
-        if (++slot == sh.ring) slot = 0;
+        if (part_ends) ++part;
+        if (kM == 1 && ++group == kGroups) group = 0;
+        if (++slot == kRing) { slot = 0; phase ^= 1u; }
       }
-  } else if (warp >= kReaders && warp < kReaders + 4) {
+    }
+  } else if (warp >= kReaders && warp < Roles<kM>::kFirstGroup) {
     // ---- sums of the parts, and out
-    const int quarter = warp & 3, r = quarter * 32 + lane;
-    const int parts = (sh.stages + 1) / 2;
-    int acc = 0;
+    const int m = (warp - kReaders) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    int a = m;
     uint32_t acc_phase = 0;
     bool ok = true;
-    for (int box = 0; box < boxes && ok; ++box) {
+    for (int box = m; box < boxes && ok; box += kM) {
       float sum[kN];
 #pragma unroll
       for (int n = 0; n < kN; ++n) sum[n] = 0.f;
       for (int part = 0; part < parts; ++part) {
-        ok = __all_sync(0xffffffffu, sleep_wait(acc_full(acc), acc_phase, &abort_flag));
+        ok = __all_sync(0xffffffffu, sleep_wait(acc_full(a), acc_phase, &abort_flag));
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
         for (int n0 = 0; n0 < kN; n0 += 16) {
           uint32_t v[16];
-          tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + acc * kN + n0, v);
+          tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + a * kN + n0, v);
           tmem_ld_wait();
 #pragma unroll
           for (int n = 0; n < 16; ++n) sum[n0 + n] += __uint_as_float(v[n]);
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(acc_empty(acc));
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        if (lane == 0) mbar_arrive(acc_empty(a));
+        if (kM == 2 || (a ^= 1) == 0) acc_phase ^= 1u;
       }
       const int64_t v = row0 + box * row_step + r;
       if (ok && r < sh.rows_box && v < sh.V) {
@@ -269,15 +307,17 @@ __global__ void __launch_bounds__(kThreads, 1) quant_umma_kernel(
           if (n < sh.T) put_logit(logits, type, n * pitch + v, sum[n]);
       }
     }
-  } else if (warp >= kReaders + 4) {
-    // ---- digits to weights: every kGroups-th stage
-    const int group = (warp - kReaders - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+  } else if (warp >= Roles<kM>::kFirstGroup) {
+    // ---- digits to weights: one box a stage: every third stage; two: every stage of one of them
+    const int group = (warp - Roles<kM>::kFirstGroup) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    constexpr int kTurn = kM == 1 ? kGroups : 1;   // stages from turn to turn
     const uint32_t swizzle = (uint32_t)(r & 7) << 4;
-    const uint32_t to = tmem + ((uint32_t)(quarter * 32) << 16) + kBufCol0 + group * kBufCols;
-    const uint8_t* const rows = smem + r * 128;
-    int box = 0, s = group, slot = group % sh.ring;
+    const uint32_t to = tmem + ((uint32_t)(quarter * 32) << 16) + kBufCol0 + group * (2 * kBufCols);
+    const uint8_t* const rows = smem + (kM == 1 ? 0 : group * kCodesBytes) + r * 128;
+    int box = kM == 1 ? 0 : group, s = kM == 1 ? group : 0, slot = s;
+    auto owner = [&] { return kM == 1 ? (box * parts + (s >> 1)) & 1 : group; };   // accumulator of the stage's part
     uint32_t phase = 0, buf_phase = 0;
-    while (s >= sh.stages) { s -= sh.stages; ++box; }
+    while (s >= sh.stages) { s -= sh.stages; box += kM; }
     int64_t v = row0 + box * row_step + r;
     // the stage's scales, one turn ahead of its codes
     const uint16_t* const scales = reinterpret_cast<const uint16_t*>(scale);
@@ -295,21 +335,28 @@ __global__ void __launch_bounds__(kThreads, 1) quant_umma_kernel(
       for (int k = 0; k < kScales; ++k) { p[k] = scale_pair(bits[k]); quick = quick && p[k].quick; }
       quick = __all_sync(0xffffffffu, quick);
       const uint8_t* const row = rows + slot * kStage;
-      // the buffer first: once the products of this group's last stage are done, so are all before it, and the slot's barrier
-      // is in the phase that is waited for or past it.  Asked before, a parity could be that of the phase before the last.
-      if (!__all_sync(0xffffffffu, sleep_wait(a_empty(group), buf_phase ^ 1u, &abort_flag) && sleep_wait(full_bar(slot), phase, &abort_flag))) break;
-      slot += kGroups;
-      if (slot >= sh.ring) { slot -= sh.ring; phase ^= 1u; }
-      s += kGroups;
-      while (s >= sh.stages) { s -= sh.stages; ++box; v += row_step; }
+      const int a = owner();
+      if (!__all_sync(0xffffffffu, sleep_wait(full_bar(slot), phase, &abort_flag) && sleep_wait(a_empty(group, 0), buf_phase ^ 1u, &abort_flag))) break;
+      slot += kTurn;
+      if (slot >= kRing) { slot -= kRing; phase ^= 1u; }
+      s += kTurn;
+      while (s >= sh.stages) { s -= sh.stages; box += kM; v += kM * row_step; }
       fetch();
+      auto hand_over = [&](int half) {
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(a_full(a, group, half));
+      };
       tc_fence_after();
-      if (quick) dequantise<true, kScales>(row, swizzle, p, to);
-      else dequantise<false, kScales>(row, swizzle, p, to);
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(a_full(group));
+      if (quick) dequantise<true, kScales, 0>(row, swizzle, p, to);
+      else dequantise<false, kScales, 0>(row, swizzle, p, to);
+      hand_over(0);
+      if (!__all_sync(0xffffffffu, sleep_wait(a_empty(group, 1), buf_phase ^ 1u, &abort_flag))) break;
+      tc_fence_after();
+      if (quick) dequantise<true, kScales, 4>(row, swizzle, p, to + kBufCols);
+      else dequantise<false, kScales, 4>(row, swizzle, p, to + kBufCols);
+      hand_over(1);
       buf_phase ^= 1u;
     }
   }
@@ -324,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1) quant_umma_kernel(
   if (warp == 1) tmem_dealloc(tmem, kTmemCols);
 }
 
-template <int kN, int kScales>
+template <int kN, int kM, int kScales>
 af_status launch_umma(af_ctx* ctx, const void* hidden, const QuantHead& h, int T, void* logits, int type, int64_t pitch, cudaStream_t s) {
   UmmaShape sh;
   sh.T = T; sh.V = h.V; sh.d = h.d; sh.groups = h.groups();
@@ -334,35 +381,32 @@ af_status launch_umma(af_ctx* ctx, const void* hidden, const QuantHead& h, int T
   const int64_t want = per_cta * ctx->sm_count;
   sh.rows_box = (int)((h.V + want - 1) / want);
   sh.boxes = (h.V + sh.rows_box - 1) / sh.rows_box;
-  constexpr int stage = kUmmaStageBytes<kN>, ring = (kSmemLimit - 1024) / stage < kMaxRing ? (kSmemLimit - 1024) / stage : kMaxRing;
-  static_assert(ring >= kGroups, "every group has a stage");
-  sh.ring = ring;
-  constexpr int smem = 1024 + ring * stage;
+  constexpr int smem = 1024 + Stage<kN, kM>::kRing * Stage<kN, kM>::kBytes;
   CUtensorMap codes, x;                            // the codes as a matrix of d / 4 16-bit elements
   const GemmEnv env = gemm_env(ctx);
   af_status st = encode_operand(env, &codes, Operand{h.codes, (uint64_t)h.V, (uint64_t)h.d / 4, (uint64_t)h.d / 2}, (uint32_t)sh.rows_box);
   if (st == AF_OK) st = encode_operand(env, &x, Operand{hidden, (uint64_t)T, (uint64_t)h.d, (uint64_t)h.d * 2}, kN);
   if (st != AF_OK) return st;
   static SmemAttrOnce once;
-  if (set_smem_once(once, quant_umma_kernel<kN, kScales>, smem) != cudaSuccess) return AF_ERR_CUDA;
+  if (set_smem_once(once, quant_umma_kernel<kN, kM, kScales>, smem) != cudaSuccess) return AF_ERR_CUDA;
   const int blocks = sh.boxes < ctx->sm_count ? sh.boxes : ctx->sm_count;
-  return launch_overlapped(quant_umma_kernel<kN, kScales>, blocks, kThreads, smem, s, codes, x, h.scale, sh, logits, type, pitch,
+  return launch_overlapped(quant_umma_kernel<kN, kM, kScales>, blocks, Roles<kM>::kThreads, smem, s, codes, x, h.scale, sh, logits, type, pitch,
                            ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
-template <int kN>
+template <int kN, int kM>
 af_status launch_umma_group(af_ctx* ctx, const void* hidden, const QuantHead& h, int T, void* logits, int type, int64_t pitch, cudaStream_t s) {
-  if (h.group == 32) return launch_umma<kN, 8>(ctx, hidden, h, T, logits, type, pitch, s);
-  if (h.group == 64) return launch_umma<kN, 4>(ctx, hidden, h, T, logits, type, pitch, s);
-  return launch_umma<kN, 2>(ctx, hidden, h, T, logits, type, pitch, s);
+  if (h.group == 32) return launch_umma<kN, kM, 8>(ctx, hidden, h, T, logits, type, pitch, s);
+  if (h.group == 64) return launch_umma<kN, kM, 4>(ctx, hidden, h, T, logits, type, pitch, s);
+  return launch_umma<kN, kM, 2>(ctx, hidden, h, T, logits, type, pitch, s);
 }
 
 }  // namespace
 
 af_status launch_quant_umma(af_ctx* ctx, const void* hidden, const QuantHead& h, int T, void* logits, int32_t type, int64_t pitch,
                             cudaStream_t s) {
-  if (T <= 16) return launch_umma_group<16>(ctx, hidden, h, T, logits, type, pitch, s);
-  if (T <= 32) return launch_umma_group<32>(ctx, hidden, h, T, logits, type, pitch, s);
-  return launch_umma_group<64>(ctx, hidden, h, T, logits, type, pitch, s);
+  if (T <= 16) return launch_umma_group<16, 1>(ctx, hidden, h, T, logits, type, pitch, s);
+  if (T <= 32) return launch_umma_group<32, 1>(ctx, hidden, h, T, logits, type, pitch, s);
+  return launch_umma_group<64, 2>(ctx, hidden, h, T, logits, type, pitch, s);
 }
 
 }  // namespace af
