@@ -91,6 +91,11 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst_smem), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -147,6 +152,7 @@ struct UmmaShape {
   int stages;                    // pieces of 256 of k in a row
   int rows_box;                  // rows of a box, 128 at most
   int boxes;                     // boxes of the head
+  int whole_blocks;              // d is a multiple of 64: the tokens' map has a third dimension, the blocks of 64 of k
 };
 
 __device__ __forceinline__ void put_logit(void* logits, int type, int64_t at, float v) {
@@ -200,26 +206,33 @@ __global__ void __launch_bounds__(Roles<kM>::kThreads, 1) quant_umma_kernel(
   const int parts = (sh.stages + 1) / 2;
 
   if (warp == 0) {
-    if (lane == 0) {                               // ---- loads
-      int slot = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      for (int tile = 0; tile < tiles && ok; ++tile) {
-        const int here = min(kM, boxes - tile * kM);
-        for (int s = 0; s < sh.stages; ++s) {
-          if (!sleep_wait(empty_bar(slot), phase ^ 1u, &abort_flag)) { ok = false; break; }
-          const int blocks = min(4, (sh.d - s * kStageK + 63) / 64);
-          const uint32_t at = ring_at + slot * kStage;
-          mbar_arrive_expect_tx(full_bar(slot), here * sh.rows_box * 128 + blocks * kN * 128);
-          for (int m = 0; m < here; ++m)
-            tma_load_2d(at + m * kCodesBytes, &codes, full_bar(slot), s * (kStageK / 4), (int)(row0 + (tile * kM + m) * row_step));
-          for (int b = 0; b < blocks; ++b)
-            tma_load_2d(at + St::kTokensAt + b * kN * 128, &hidden, full_bar(slot), s * kStageK + b * 64, 0);
-          if (++slot == kRing) { slot = 0; phase ^= 1u; }
+    // ---- loads
+    int slot = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int tile = 0; tile < tiles && ok; ++tile) {
+      const int here = min(kM, boxes - tile * kM);
+      const int row = (int)(row0 + tile * kM * row_step);
+      for (int s = 0; s < sh.stages; ++s) {
+        ok = __all_sync(0xffffffffu, ready_wait(empty_bar(slot), phase ^ 1u, &abort_flag));
+        if (!ok) break;
+        const int blocks = min(4, (sh.d - s * kStageK + 63) / 64);
+        const uint32_t at = ring_at + slot * kStage;
+        if (elect_one()) {
+          mbar_arrive_expect_tx(full_bar(slot), here * sh.rows_box * 128 + (sh.whole_blocks ? 4 : blocks) * kN * 128);
+          tma_load_2d(at, &codes, full_bar(slot), s * (kStageK / 4), row);
+          if (kM == 2 && here == 2) tma_load_2d(at + kCodesBytes, &codes, full_bar(slot), s * (kStageK / 4), row + (int)row_step);
+          if (sh.whole_blocks) {                   // all blocks of 64 of k at once; those past the row arrive as zeros
+            tma_load_3d(at + St::kTokensAt, &hidden, full_bar(slot), 0, 0, s * 4);
+          } else {
+            for (int b = 0; b < blocks; ++b)
+              tma_load_2d(at + St::kTokensAt + b * kN * 128, &hidden, full_bar(slot), s * kStageK + b * 64, 0);
+          }
         }
+        __syncwarp();
+        if (++slot == kRing) { slot = 0; phase ^= 1u; }
       }
     }
-    __syncwarp();
   } else if (warp <= 2) {
     // ---- products: the whole warp keeps step, one lane issues; so that addresses stay in uniform registers
     const int a = warp - 1;                        // its accumulator
@@ -371,6 +384,15 @@ __global__ void __launch_bounds__(Roles<kM>::kThreads, 1) quant_umma_kernel(
   if (warp == 1) tmem_dealloc(tmem, kTmemCols);
 }
 
+// hidden [T, d] as [d / 64][T][64], boxes of four blocks of n tokens.
+af_status encode_tokens(af_ctx* ctx, CUtensorMap* map, const void* hidden, int T, int d, uint32_t n) {
+  const cuuint64_t dims[3] = {64, (cuuint64_t)T, (cuuint64_t)d / 64}, strides[2] = {(cuuint64_t)d * 2, 128};
+  const cuuint32_t box[3] = {64, n, 4}, step[3] = {1, 1, 1};
+  return ctx->encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(hidden), dims, strides, box, step,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? AF_OK : AF_ERR_CUDA;
+}
+
 template <int kN, int kM, int kScales>
 af_status launch_umma(af_ctx* ctx, const void* hidden, const QuantHead& h, int T, void* logits, int type, int64_t pitch, cudaStream_t s) {
   UmmaShape sh;
@@ -385,7 +407,9 @@ af_status launch_umma(af_ctx* ctx, const void* hidden, const QuantHead& h, int T
   CUtensorMap codes, x;                            // the codes as a matrix of d / 4 16-bit elements
   const GemmEnv env = gemm_env(ctx);
   af_status st = encode_operand(env, &codes, Operand{h.codes, (uint64_t)h.V, (uint64_t)h.d / 4, (uint64_t)h.d / 2}, (uint32_t)sh.rows_box);
-  if (st == AF_OK) st = encode_operand(env, &x, Operand{hidden, (uint64_t)T, (uint64_t)h.d, (uint64_t)h.d * 2}, kN);
+  sh.whole_blocks = h.d % 64 == 0;
+  if (st == AF_OK && !sh.whole_blocks) st = encode_operand(env, &x, Operand{hidden, (uint64_t)T, (uint64_t)h.d, (uint64_t)h.d * 2}, kN);
+  if (st == AF_OK && sh.whole_blocks) st = encode_tokens(ctx, &x, hidden, T, h.d, kN);
   if (st != AF_OK) return st;
   static SmemAttrOnce once;
   if (set_smem_once(once, quant_umma_kernel<kN, kM, kScales>, smem) != cudaSuccess) return AF_ERR_CUDA;
