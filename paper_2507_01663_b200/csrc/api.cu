@@ -114,7 +114,7 @@ af_status af_destroy(af_ctx* c) {
   DeviceGuard guard(c->device);
   cudaDeviceSynchronize();
   Buf* bufs[] = {&c->partial, &c->loss_ws, &c->pack_meta, &c->dz, &c->ctrl_ws, &c->zlog, &c->adv_ws, &c->cand_keys,
-                 &c->dw_sums, &c->split_k, &c->distill_ws, &c->pref_ws, &c->verify_ws, &c->slots_ws};
+                 &c->dw_sums, &c->split_k, &c->distill_ws, &c->pref_ws, &c->verify_ws, &c->verify_state, &c->slots_ws};
   for (Buf* b : bufs) if (b->p) cudaFree(b->p);
   for (int i = 0; i < kPackRing; ++i) {
     if (c->pack_host[i]) cudaFreeHost(c->pack_host[i]);
@@ -128,7 +128,7 @@ af_status af_destroy(af_ctx* c) {
 int64_t af_workspace_bytes(const af_ctx* c) {
   if (!c) return 0;
   return (int64_t)(c->partial.cap + c->loss_ws.cap + c->pack_meta.cap + c->dz.cap + c->ctrl_ws.cap + c->zlog.cap + c->adv_ws.cap +
-                   c->cand_keys.cap + c->dw_sums.cap + c->split_k.cap + c->distill_ws.cap + c->pref_ws.cap + c->verify_ws.cap + c->slots_ws.cap);
+                   c->cand_keys.cap + c->dw_sums.cap + c->split_k.cap + c->distill_ws.cap + c->pref_ws.cap + c->verify_ws.cap + c->verify_state.cap + c->slots_ws.cap);
 }
 
 af_status af_selftest_bounded_wait(af_ctx* c, uint32_t* waited_us, void* stream) {
@@ -759,7 +759,9 @@ af_status af_reserve_rollout(af_ctx* c, int32_t max_R, int32_t max_D) {
   if (!c || max_R < 0 || max_D < 0) return AF_ERR_INVALID_ARG;
   if (max_R > (1 << 20) || max_D > (1 << 24)) return AF_ERR_SHAPE;
   DeviceGuard guard(c->device);
-  const af_status st = ws_grow(c->verify_ws, verify_workspace_bytes(max_R, max_D, c->sm_count));
+  const af_status st = reserve_draft_verify(c, max_R, max_D, nullptr);
+  // the caller's stream may be one that does not wait for the default stream, on which the above was set
+  if (st == AF_OK && cudaStreamSynchronize(nullptr) != cudaSuccess) return AF_ERR_CUDA;
   return st == AF_OK ? ws_grow(c->slots_ws, slots_workspace_bytes(max_R)) : st;
 }
 

@@ -117,6 +117,7 @@ struct af_ctx {
   af::Buf distill_ws; // gradients [Tc, K] of one token block of af_distill_update when the caller wants none
   af::Buf pref_ws;    // partial sums of the sequences of af_preference_loss
   af::Buf verify_ws;  // maxima and sums of the slices of rows of af_draft_verify
+  af::Buf verify_state;  // its tickets and stops, at rest between calls
   af::Buf slots_ws;   // the requests' shares of af_block_slots
 
   // pinned staging ring for pack metadata

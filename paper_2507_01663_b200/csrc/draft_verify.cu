@@ -1,11 +1,14 @@
 // af_draft_verify: drafted tokens against the target's distribution, from given uniforms.
 //
-// Two launches.  The first reads rows of logits once, in slices, for the maximum and the sum of exponentials (fp32).  The
-// second decides request by request which drafts pass and draws the token after them.
+// Two launches.  The first reads rows of logits once, in slices, for their maxima and sums of exponentials (fp32: a stream at
+// the memory's rate, next to which the exponentials fit).  It goes through the batch by positions, first drafts first, and a
+// row of a request that has already been seen to stop is not read.  The second, a cluster per request, decides which drafts
+// pass and draws the token after them.
 //
 // What has to be exact is whole numbers: a comparison u q < p, and the place of u C among running sums C_v of up to
 // 10^5 terms, where fp32 would be off by as much as many terms are large.  So a comparison whose sides are within 1e-5 is
-// made again from sums in 64 bits, and a draw's sums are in 64 bits throughout.
+// made again from sums in 64 bits, and a draw's sums are in 64 bits throughout: per logit ten 64-bit operations, 2^x from a table
+// of 64 powers and a polynomial of degree 4 (2^-44 relative), which are what the second launch is bound by.
 #include <cooperative_groups.h>
 
 #include "device_util.cuh"
@@ -14,15 +17,23 @@
 namespace af {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kCluster = 8;                        // CTAs that draw for one request
+constexpr int kRowThreads = 1024;                  // one row, or slice, at a time on an SM: so that positions end in order
+constexpr int kDrawThreads = 512;
+constexpr int kDrawWarps = kDrawThreads / 32;
+constexpr int kMostCluster = 8;                    // CTAs that draw for one request
 constexpr float kNoMax = -INFINITY;
 constexpr double kResidualFloor = 0x1p-30;         // a residual with less mass than this is drawn from the target itself
+constexpr int kGoesOn = 0x7fffffff;
 
 struct RowPart {                                   // a slice of a row: max z, sum exp((z - m) / tau), place of the maximum
   float m, s;
   int32_t at, pad;
+};
+struct Workspace {
+  RowPart* target;                                 // [D + R][slices]
+  RowPart* draft;                                  // [D][slices]
+  unsigned int* ticket;                            // [positions * R] slices done, zero between calls
+  int* stop;                                       // [R] first draft that is known not to pass, kGoesOn between calls
 };
 struct Shape {
   int slices, positions;                           // slices of a row; max_draft + 1
@@ -42,6 +53,7 @@ __device__ __forceinline__ Span span_of(const VerifyCall& c, int r) {
   return {ok ? a : 0, ok ? b - a : 0, ok};
 }
 
+// ------------------------------------------------------------------------------------ rows, in fp32
 __device__ __forceinline__ RowPart join(const RowPart& a, const RowPart& b, float scale) {
   RowPart o;
   const bool first = a.m > b.m || (a.m == b.m && a.at < b.at);
@@ -49,53 +61,95 @@ __device__ __forceinline__ RowPart join(const RowPart& a, const RowPart& b, floa
   o.at = first ? a.at : b.at;
   // a part without mass adds nothing (its maximum may be -inf); a NaN stays
   o.s = (a.s == 0.f ? 0.f : a.s * ex2f((a.m - o.m) * scale)) + (b.s == 0.f ? 0.f : b.s * ex2f((b.m - o.m) * scale));
+  o.pad = 0;
   return o;
 }
 
-__device__ RowPart row_part(const LogitRows& x, int64_t row, int lo, int hi, float scale) {
-  RowPart a{kNoMax, 0.f, 0x7fffffff, 0};
-  for (int v = lo + threadIdx.x; v < hi; v += kThreads) {
-    const float z = load(x, row, v);
-    if (z > a.m) {
-      a.s = a.s == 0.f ? 0.f : a.s * ex2f((a.m - z) * scale);
-      a.m = z;
-      a.at = v;
-    }
-    if (z != kNoMax) a.s += ex2f((z - a.m) * scale);         // a NaN, and infinity less itself, make the sum NaN
-  }
-  __shared__ RowPart part[kWarps];
+template <int n>
+struct Values { float v[n]; };
+__device__ __forceinline__ Values<4> widen(const float*, uint4 x) {
+  return {{__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)}};
+}
+__device__ __forceinline__ Values<8> widen(const __nv_bfloat16*, uint4 x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  Values<8> o;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    RowPart b;
-    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-    b.at = __shfl_xor_sync(0xffffffffu, a.at, o);
-    a = join(a, b, scale);
+  for (int i = 0; i < 4; ++i) { o.v[2 * i] = __uint_as_float(w[i] << 16); o.v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  return o;
+}
+__device__ __forceinline__ Values<1> widen1(const float* p) { return {{__ldg(p)}}; }
+__device__ __forceinline__ Values<1> widen1(const __nv_bfloat16* p) { return {{__bfloat162float(*p)}}; }
+
+// Adds n neighbours, the first at place `at`, to a thread's part.
+template <bool kPlace, int n>
+__device__ __forceinline__ void add(RowPart& a, const Values<n>& x, int at, float scale) {
+  float top = x.v[0];
+#pragma unroll
+  for (int i = 1; i < n; ++i) top = fmaxf(top, x.v[i]);
+  if (top > a.m) {                                 // rare after the first few
+    a.s *= ex2f((a.m - top) * scale);              // 0 times 0 at first
+    a.m = top;
+    if constexpr (kPlace) {
+#pragma unroll
+      for (int i = n - 1; i >= 0; --i)
+        if (x.v[i] == top) a.at = at + i;
+    }
   }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = a;
-  __syncthreads();
-  a = part[0];
-  for (int w = 1; w < kWarps; ++w) a = join(a, part[w], scale);
+  if (a.m == kNoMax) {                             // nothing but -inf so far, or a NaN
+#pragma unroll
+    for (int i = 0; i < n; ++i)
+      if (x.v[i] != x.v[i]) a.s = x.v[i];
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < n; ++i) a.s += ex2f((x.v[i] - a.m) * scale);       // a NaN, and infinity less itself, make the sum NaN
+}
+
+template <bool kPlace, class T>
+__device__ RowPart row_part(const T* row, int lo, int hi, float scale) {
+  constexpr int kVec = 16 / sizeof(T), kLoads = 4;
+  RowPart a{kNoMax, 0.f, kGoesOn, 0};
+  // single elements up to a multiple of 16 bytes, and behind the last one
+  const int to_line = (int)((16u - ((uint32_t)reinterpret_cast<uintptr_t>(row + lo) & 15u)) & 15u) / (int)sizeof(T);
+  const int body = min(hi, lo + to_line), vecs = (hi - body) / kVec, tail = body + vecs * kVec;
+  if (lo + (int)threadIdx.x < body) add<kPlace>(a, widen1(row + lo + threadIdx.x), lo + threadIdx.x, scale);
+  const uint4* const at = reinterpret_cast<const uint4*>(row + body);
+  int i = threadIdx.x;
+  for (; i + (kLoads - 1) * kRowThreads < vecs; i += kLoads * kRowThreads) {
+    uint4 w[kLoads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) w[k] = __ldg(at + i + k * kRowThreads);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) add<kPlace>(a, widen(row, w[k]), body + (i + k * kRowThreads) * kVec, scale);
+  }
+  for (; i < vecs; i += kRowThreads) add<kPlace>(a, widen(row, __ldg(at + i)), body + i * kVec, scale);
+  if (tail + (int)threadIdx.x < hi) add<kPlace>(a, widen1(row + tail + threadIdx.x), tail + threadIdx.x, scale);
   return a;
 }
 
-__global__ void __launch_bounds__(kThreads) verify_rows_kernel(const VerifyCall c, const Shape shape, float scale, RowPart* target_parts,
-                                                               RowPart* draft_parts) {
-  wait_for_predecessor();
-  let_successor_start();
-  const int slice = (int)(blockIdx.x % shape.slices), unit = (int)(blockIdx.x / shape.slices);
-  const int r = unit % c.R, i = unit / c.R;
-  const Span sp = span_of(c, r);
-  if (!sp.ok || i > sp.n) return;
-  const int lo = (int)((int64_t)c.V * slice / shape.slices), hi = (int)((int64_t)c.V * (slice + 1) / shape.slices);
-  const int64_t row = sp.first + r + i;
-  const RowPart t = row_part(c.target, row, lo, hi, scale);
-  if (threadIdx.x == 0) target_parts[row * shape.slices + slice] = t;
-  if (c.draft.p && i < sp.n) {
-    const RowPart d = row_part(c.draft, sp.first + i, lo, hi, scale);
-    if (threadIdx.x == 0) draft_parts[(int64_t)(sp.first + i) * shape.slices + slice] = d;
+// The block's part of a row; the first warp has it.
+template <bool kPlace>
+__device__ RowPart block_part(const LogitRows& x, int64_t row, int lo, int hi, float scale, RowPart* warp_parts) {
+  RowPart a = x.type == AF_F32 ? row_part<kPlace>(static_cast<const float*>(x.p) + row * x.pitch, lo, hi, scale)
+                               : row_part<kPlace>(static_cast<const __nv_bfloat16*>(x.p) + row * x.pitch, lo, hi, scale);
+  auto over_warp = [&] {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      RowPart b;
+      b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+      b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
+      b.at = __shfl_xor_sync(0xffffffffu, a.at, o);
+      a = join(a, b, scale);
+    }
+  };
+  over_warp();
+  if ((threadIdx.x & 31) == 0) warp_parts[threadIdx.x >> 5] = a;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    a = warp_parts[threadIdx.x];
+    over_warp();
   }
+  return a;
 }
 
 // A row's distribution from its parts: maximum, its place, and the sum in 64 bits of the parts' sums.
@@ -104,7 +158,7 @@ __device__ __forceinline__ bool good(const Row& x) { return fabsf(x.m) < INFINIT
 // Called by a whole warp.
 __device__ Row warp_row(const RowPart* parts, int slices, double inv_tau) {
   const int lane = threadIdx.x & 31;
-  Row x{kNoMax, 0x7fffffff, 0.0};
+  Row x{kNoMax, kGoesOn, 0.0};
   for (int i = lane; i < slices; i += 32) {
     const float m = __ldcg(&parts[i].m);
     const int32_t at = __ldcg(&parts[i].at);
@@ -118,16 +172,107 @@ __device__ Row warp_row(const RowPart* parts, int slices, double inv_tau) {
   }
   for (int i = lane; i < slices; i += 32) {
     const float m = __ldcg(&parts[i].m), s = __ldcg(&parts[i].s);
-    if (s != 0.f) x.s += (double)s * exp(((double)m - (double)x.m) * inv_tau);
+    if (s != 0.f) x.s += m == x.m ? (double)s : (double)s * exp(((double)m - (double)x.m) * inv_tau);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) x.s += __shfl_xor_sync(0xffffffffu, x.s, o);
   return x;
 }
 
-__device__ __forceinline__ double weight(const LogitRows& x, int64_t row, int v, float m, double inv_tau) {
-  return exp(((double)load(x, row, v) - (double)m) * inv_tau);
+// u q(x) and p(x), both times both sums: x passes iff left < right.
+struct Sides { double left, right; };
+__device__ __forceinline__ Sides sides_of(const VerifyCall& c, const Row& t, const Row& q, int64_t row, int draft_row, int x, double inv_tau) {
+  const double u = (double)__ldg(c.u_accept + draft_row);
+  const double pw = exp(((double)load(c.target, row, x) - (double)t.m) * inv_tau);
+  const double qw = c.draft.p ? exp(((double)load(c.draft, draft_row, x) - (double)q.m) * inv_tau) : 1.0;
+  return {u * qw * t.s, pw * (c.draft.p ? q.s : 1.0)};
 }
+__device__ __forceinline__ bool too_near(const Sides& e) { return fabs(e.left - e.right) <= 1e-5 * fabs(e.right); }
+
+__global__ void __launch_bounds__(kRowThreads) verify_rows_kernel(const VerifyCall c, const Shape shape, float scale, const Workspace ws) {
+  __shared__ RowPart warp_parts[2][kRowThreads / 32];
+  __shared__ int s_skip;
+  wait_for_predecessor();
+  let_successor_start();
+  const int slice = (int)(blockIdx.x % shape.slices), unit = (int)(blockIdx.x / shape.slices);
+  const int r = unit % c.R, i = unit / c.R;        // first positions first
+  const Span sp = span_of(c, r);
+  if (!sp.ok || i > sp.n) return;
+  if (threadIdx.x == 0) s_skip = *reinterpret_cast<volatile int*>(ws.stop + r) < i;
+  __syncthreads();
+  // A skipped slice is counted too: the ticket has to come back to 0.  Whoever is last then finds the request stopped before i
+  // already, and what the skipped slice's part holds changes nothing.
+  const bool counted = i < sp.n && shape.slices > 1;
+  if (s_skip) {                                    // the request ends before this row, whatever is in it
+    if (counted && threadIdx.x == 0) atomicInc(ws.ticket + unit, shape.slices - 1);
+    return;
+  }
+  const int lo = (int)((int64_t)c.V * slice / shape.slices), hi = (int)((int64_t)c.V * (slice + 1) / shape.slices);
+  const int64_t row = sp.first + r + i;
+  const bool greedy = c.temperature == 0.f, dense = c.draft.p && i < sp.n;
+  const RowPart t = greedy ? block_part<true>(c.target, row, lo, hi, scale, warp_parts[0]) : block_part<false>(c.target, row, lo, hi, scale, warp_parts[0]);
+  RowPart d{};
+  if (dense) d = block_part<false>(c.draft, sp.first + i, lo, hi, scale, warp_parts[1]);
+  if (threadIdx.x >= 32) return;
+  RowPart* const t_at = ws.target + row * shape.slices;
+  RowPart* const d_at = ws.draft + (int64_t)(sp.first + i) * shape.slices;
+  if (threadIdx.x == 0) {
+    t_at[slice] = t;
+    if (dense) d_at[slice] = d;
+  }
+  if (i == sp.n) return;
+  // the last slice of the row: if the draft surely does not pass, later rows of the request need not be read
+  int last = 1;
+  if (threadIdx.x == 0) {
+    __threadfence();
+    if (counted) last = atomicInc(ws.ticket + unit, shape.slices - 1) == shape.slices - 1u;      // back to 0 with the last
+  }
+  last = __shfl_sync(0xffffffffu, last, 0);
+  if (!last) return;
+  __threadfence();
+  const double inv_tau = greedy ? 1.0 : 1.0 / (double)c.temperature;
+  const Row tr = warp_row(t_at, shape.slices, inv_tau);
+  Row dr{};
+  if (dense) dr = warp_row(d_at, shape.slices, inv_tau);
+  if (threadIdx.x != 0) return;
+  const int x = __ldg(c.draft_ids + sp.first + i);
+  bool ends;
+  if (!good(tr) || (dense && !good(dr)) || x < 0 || x >= c.V) ends = true;
+  else if (greedy) ends = x != tr.at;
+  else {
+    const Sides e = sides_of(c, tr, dr, row, sp.first + i, x, inv_tau);
+    ends = !(e.left < e.right) && !too_near(e);
+  }
+  if (ends) atomicMin(ws.stop + r, i);
+}
+
+// --------------------------------------------------------------------------------- draws, in 64 bits
+constexpr int kPowers = 64;
+// 2^((z - m) / tau log2 e), relative to within 2^-44; 0 from 2^-1021 down.
+struct Exp64 {
+  const double* power;                             // 2^(j / 64)
+  double c, b;                                     // log2 e / tau, -m times it
+  __device__ __forceinline__ double operator()(float z) const {
+    const double t = fma((double)z, c, b);
+    constexpr double kShift = 0x1.8p52 / kPowers;  // adding it rounds to a multiple of 1/64, a whole number in the low bits
+    const double shifted = t + kShift;
+    const int n = __double2loint(shifted);
+    const double r = t - (shifted - kShift);       // |r| <= 1/128
+    // 2^r - 1 = r (ln 2 + r (ln^2 2 / 2 + r (ln^3 2 / 6 + r ln^4 2 / 24))); the next term is below 2^-44
+    double p = fma(r, 9.6181291076284772e-3, 5.5504108664821580e-2);
+    p = fma(r, p, 2.4022650695910071e-1);
+    p = fma(r, p, 6.9314718055994531e-1);
+    const double y = power[n & (kPowers - 1)];
+    const double w = fma(y, r * p, y);
+    const double scaled = __hiloint2double(__double2hiint(w) + (n >> 6) * (1 << 20), __double2loint(w));
+    return t > -1021.0 ? scaled : 0.0;             // also for -inf
+  }
+};
+__device__ __forceinline__ Exp64 exp_about(const double* power, float m, double inv_tau) {
+  const double c = inv_tau * 1.4426950408889634074;
+  return {power, c, -(double)m * c};
+}
+
 // Sum over the block, in a fixed order; every thread gets it.
 __device__ double block_sum(double a, double* warp_sums) {
 #pragma unroll
@@ -136,28 +281,32 @@ __device__ double block_sum(double a, double* warp_sums) {
   if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5] = a;
   __syncthreads();
   double all = 0.0;
-  for (int w = 0; w < kWarps; ++w) all += warp_sums[w];
+#pragma unroll
+  for (int w = 0; w < kDrawWarps; ++w) all += warp_sums[w];
   return all;
 }
-__device__ double exact_sum(const LogitRows& x, int64_t row, int lo, int hi, float m, double inv_tau, double* warp_sums) {
+__device__ double exact_sum(const LogitRows& x, int64_t row, int lo, int hi, const Exp64& e, double* warp_sums) {
   double a = 0.0;
-  for (int v = lo + threadIdx.x; v < hi; v += kThreads) a += weight(x, row, v, m, inv_tau);
+#pragma unroll 4
+  for (int v = lo + threadIdx.x; v < hi; v += kDrawThreads) a += e(load(x, row, v));
   return block_sum(a, warp_sums);
 }
 
+constexpr int kBatch = 8;                          // positions looked at a time
+
 // A cluster per request.
-__global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyCall c, const Shape shape, float scale,
-                                                               const RowPart* target_parts, const RowPart* draft_parts,
-                                                               unsigned int* d_err) {
+__global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(const VerifyCall c, const Shape shape, const Workspace ws, unsigned int* d_err) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
-  __shared__ double s_warp[kWarps], s_sum[4];                 // s_sum: this CTA's shares, read by the cluster
-  __shared__ double s_thread[kThreads];
-  __shared__ Row s_target, s_draft;
+  const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  __shared__ double s_power[kPowers], s_warp[kDrawWarps], s_sum[4];       // s_sum: this CTA's shares, read by the cluster
+  __shared__ double s_segment[kDrawWarps];
+  __shared__ Row s_target[kBatch], s_draft[kBatch];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x < kPowers) s_power[threadIdx.x] = exp2((double)threadIdx.x / kPowers);
   wait_for_predecessor();
   let_successor_start();
-  const int r = (int)blockIdx.x / kCluster, rank = (int)blockIdx.x % kCluster;
-  const int warp = threadIdx.x >> 5;
+  const int r = (int)blockIdx.x / ctas;
   const Span sp = span_of(c, r);
   const bool leader = rank == 0 && threadIdx.x == 0;
   if (leader) {
@@ -166,31 +315,34 @@ __global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyCall 
     if (r == c.R - 1 && __ldg(c.cu + c.R) != c.D) bad |= AF_DEVERR_CU_SEQLENS;
     if (bad) atomicOr(d_err, bad);
     if (!sp.ok) c.n_emitted[r] = 0;
+    ws.stop[r] = kGoesOn;                                     // for the next call
   }
   if (!sp.ok) return;                                         // the whole cluster
   const bool greedy = c.temperature == 0.f;
   const double inv_tau = greedy ? 1.0 : 1.0 / (double)c.temperature;
   const int64_t base = sp.first + r;
-  const int lo = (int)((int64_t)c.V * rank / kCluster), hi = (int)((int64_t)c.V * (rank + 1) / kCluster);
+  const int lo = (int)((int64_t)c.V * rank / ctas), hi = (int)((int64_t)c.V * (rank + 1) / ctas);
 
   // ---- which drafts pass: every CTA of the cluster finds out by itself
   int i = 0;
   bool has_row = true;
   Row t{}, q{};
   for (;; ++i) {
-    __syncthreads();
-    if (warp == 0) {
-      const Row x = warp_row(target_parts + (base + i) * shape.slices, shape.slices, inv_tau);
-      if (threadIdx.x == 0) s_target = x;
-    } else if (warp == 1 && c.draft.p && i < sp.n) {
-      const Row x = warp_row(draft_parts + (int64_t)(sp.first + i) * shape.slices, shape.slices, inv_tau);
-      if (threadIdx.x == 32) s_draft = x;
+    if (i % kBatch == 0) {                                    // the next rows, a warp each
+      __syncthreads();
+      const int at = warp % kBatch, j = i + at;
+      if (j <= sp.n && warp < kBatch) {
+        const Row x = warp_row(ws.target + (base + j) * shape.slices, shape.slices, inv_tau);
+        if (lane == 0) s_target[at] = x;
+      } else if (j < sp.n && warp >= kBatch && c.draft.p) {
+        const Row x = warp_row(ws.draft + (int64_t)(sp.first + j) * shape.slices, shape.slices, inv_tau);
+        if (lane == 0) s_draft[at] = x;
+      }
+      __syncthreads();
     }
-    __syncthreads();
-    t = s_target;
+    t = s_target[i % kBatch];
     has_row = good(t);
-    if (!has_row) break;
-    if (i == sp.n) break;
+    if (!has_row || i == sp.n) break;
     const int x = __ldg(c.draft_ids + sp.first + i);
     const bool id_ok = x >= 0 && x < c.V;
     if (!id_ok && leader) atomicOr(d_err, AF_DEVERR_TARGET_RANGE);
@@ -199,22 +351,19 @@ __global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyCall 
       pass = x == t.at;
     } else {
       if (c.draft.p) {
-        q = s_draft;
+        q = s_draft[i % kBatch];
         has_row = good(q);
         if (!has_row) break;
       }
       pass = false;
       if (id_ok) {
-        const double u = (double)__ldg(c.u_accept + sp.first + i);
-        const double pw = weight(c.target, base + i, x, t.m, inv_tau), qw = c.draft.p ? weight(c.draft, sp.first + i, x, q.m, inv_tau) : 1.0;
-        double left = u * qw * t.s, right = pw * (c.draft.p ? q.s : 1.0);      // u q < p, times both sums
-        if (fabs(left - right) <= 1e-5 * fabs(right)) {
-          t.s = exact_sum(c.target, base + i, 0, c.V, t.m, inv_tau, s_warp);
-          if (c.draft.p) q.s = exact_sum(c.draft, sp.first + i, 0, c.V, q.m, inv_tau, s_warp);
-          left = u * qw * t.s;
-          right = pw * (c.draft.p ? q.s : 1.0);
+        Sides e = sides_of(c, t, q, base + i, sp.first + i, x, inv_tau);
+        if (too_near(e)) {                                    // the same in all threads of the cluster
+          t.s = exact_sum(c.target, base + i, 0, c.V, exp_about(s_power, t.m, inv_tau), s_warp);
+          if (c.draft.p) q.s = exact_sum(c.draft, sp.first + i, 0, c.V, exp_about(s_power, q.m, inv_tau), s_warp);
+          e = sides_of(c, t, q, base + i, sp.first + i, x, inv_tau);
         }
-        pass = left < right;
+        pass = e.left < e.right;
       }
     }
     if (!pass) break;
@@ -244,52 +393,67 @@ __global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyCall 
   // ---- the token after them, from row base + i
   const bool rejected = i < sp.n, dense = rejected && c.draft.p != nullptr;
   const int cut = rejected && !dense ? __ldg(c.draft_ids + sp.first + i) : -1;
+  const Exp64 pe = exp_about(s_power, t.m, inv_tau), qe = exp_about(s_power, q.m, inv_tau);
   double p_unit = 1.0, q_unit = 1.0;                          // dense: 1 / sums
   double row_sum = 0.0;                                       // of the target's weights
   if (dense) {
-    const double a = exact_sum(c.target, base + i, lo, hi, t.m, inv_tau, s_warp);
-    const double b = exact_sum(c.draft, sp.first + i, lo, hi, q.m, inv_tau, s_warp);
+    const double a = exact_sum(c.target, base + i, lo, hi, pe, s_warp);
+    const double b = exact_sum(c.draft, sp.first + i, lo, hi, qe, s_warp);
     if (threadIdx.x == 0) { s_sum[0] = a; s_sum[1] = b; }
     cluster.sync();
     double sum_q = 0.0;
-    for (int k = 0; k < kCluster; ++k) {
+    for (int k = 0; k < ctas; ++k) {
       row_sum += *cluster.map_shared_rank(&s_sum[0], k);
       sum_q += *cluster.map_shared_rank(&s_sum[1], k);
     }
     p_unit = 1.0 / row_sum;
     q_unit = 1.0 / sum_q;
   }
-  // a thread's stretch of the CTA's share
-  const int mine_lo = lo + (int)((int64_t)(hi - lo) * threadIdx.x / kThreads), mine_hi = lo + (int)((int64_t)(hi - lo) * (threadIdx.x + 1) / kThreads);
+  // a warp's segment of the CTA's share
+  const int seg_lo = lo + (int)((int64_t)(hi - lo) * warp / kDrawWarps), seg_hi = lo + (int)((int64_t)(hi - lo) * (warp + 1) / kDrawWarps);
   bool plain = !rejected;                                     // drawn from the target itself
   auto mass = [&](int v) {
-    double w = weight(c.target, base + i, v, t.m, inv_tau) * p_unit;
-    if (!plain && dense) w = fmax(w - weight(c.draft, sp.first + i, v, q.m, inv_tau) * q_unit, 0.0);
-    if (!plain && v == cut) w = 0.0;
+    double w = pe(load(c.target, base + i, v)) * p_unit;
+    if (!plain && dense) w = fmax(w - qe(load(c.draft, sp.first + i, v)) * q_unit, 0.0);
     return w;
   };
   double before, total;
   for (;;) {
     double a = 0.0, whole = 0.0;
-    for (int v = mine_lo; v < mine_hi; ++v) {
-      const double w = mass(v);
-      a += w;
-      if (!dense) whole += v == cut ? weight(c.target, base + i, v, t.m, inv_tau) : w;
+    if (dense || plain || cut < seg_lo || cut >= seg_hi) {
+#pragma unroll 4
+      for (int v = seg_lo + lane; v < seg_hi; v += 32) a += mass(v);
+      whole = a;
+    } else {                                                  // the segment that holds the draft that is cut out
+      for (int v = seg_lo + lane; v < seg_hi; v += 32) {
+        const double w = mass(v);
+        whole += w;
+        if (v != cut) a += w;
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      a += __shfl_xor_sync(0xffffffffu, a, o);
+      whole += __shfl_xor_sync(0xffffffffu, whole, o);
     }
     __syncthreads();
-    s_thread[threadIdx.x] = a;
+    if (lane == 0) { s_segment[warp] = a; s_warp[warp] = whole; }
     __syncthreads();
     if (threadIdx.x == 0) {
-      double run = 0.0;
-      for (int k = 0; k < kThreads; ++k) { const double x = s_thread[k]; s_thread[k] = run; run += x; }
+      double run = 0.0, all = 0.0;
+      for (int k = 0; k < kDrawWarps; ++k) {
+        const double x = s_segment[k];
+        s_segment[k] = run;
+        run += x;
+        all += s_warp[k];
+      }
       s_sum[2] = run;
+      s_sum[3] = all;
     }
-    whole = block_sum(whole, s_warp);
-    if (threadIdx.x == 0) s_sum[3] = whole;
     cluster.sync();
     before = total = 0.0;
     double all = 0.0;
-    for (int k = 0; k < kCluster; ++k) {
+    for (int k = 0; k < ctas; ++k) {
       if (k == rank) before = total;
       total += *cluster.map_shared_rank(&s_sum[2], k);
       all += *cluster.map_shared_rank(&s_sum[3], k);
@@ -299,64 +463,101 @@ __global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyCall 
     if (plain || (dense ? total : total / row_sum) > kResidualFloor) break;
     plain = true;                                             // next to nothing is left: the target itself
   }
-  // the thread whose stretch holds the first v with C_v > u C
+  // the warp whose segment holds the first v with C_v > u C
   const double u = (double)fminf(fmaxf(__ldg(c.u_sample + r), 0.f), 1.f - 0x1p-24f), goal = u * total;
-  const double start = before + s_thread[threadIdx.x];
-  const double end = before + (threadIdx.x + 1 < kThreads ? s_thread[threadIdx.x + 1] : s_sum[2]);
-  if (start <= goal && goal < end) {
-    double at = start;
-    int y = mine_lo;
-    for (int v = mine_lo; v < mine_hi; ++v) {
-      const double w = mass(v);
-      if (w > 0.0) y = v;                                     // the last with mass, if rounding leaves the goal beyond the stretch
-      at += w;
-      if (at > goal) break;
+  const double start = before + s_segment[warp];
+  const double end = before + (warp + 1 < kDrawWarps ? s_segment[warp + 1] : s_sum[2]);
+  if (!(start <= goal && goal < end)) return;
+  double run = start;
+  int y = seg_lo;                                             // the last with mass, if rounding leaves the goal beyond the segment
+  for (int v0 = seg_lo; v0 < seg_hi; v0 += 32) {
+    const int v = v0 + lane;
+    const double w = v < seg_hi && (plain || v != cut) ? mass(v) : 0.0;
+    double upto = w;                                          // sum over the lanes up to this one
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
     }
+    const unsigned some = __ballot_sync(0xffffffffu, w > 0.0), beyond = __ballot_sync(0xffffffffu, w > 0.0 && run + upto > goal);
+    if (beyond) { y = v0 + __ffs(beyond) - 1; break; }
+    if (some) y = v0 + 31 - __clz(some);
+    run += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  if (lane == 0) {
     c.token[base + i] = y;
     if (c.logp) c.logp[base + i] = (float)(((double)load(c.target, base + i, y) - (double)t.m) * inv_tau - log(row_sum));
   }
 }
 
-// Slices of a row: enough CTAs for every SM's warps, of 2048 logits at least.
+// Slices of a row.  A batch of rows that fills the device several times over goes row by row, so that positions end in order;
+// fewer are cut until every SM has about four slices, of 2048 logits at least.
 Shape shape_of(int32_t R, int32_t V, int32_t max_draft, int sm_count) {
-  const int64_t units = (int64_t)R * (max_draft + 1), want = ((int64_t)sm_count * 8 + units - 1) / units, most = V / 2048;
+  const int64_t units = (int64_t)R * (max_draft + 1), want = ((int64_t)sm_count * 4 + units - 1) / units, most = V / 2048;
   const int64_t slices = want < most ? want : most;
   return {(int)(slices < 1 ? 1 : slices), max_draft + 1};
+}
+// CTAs to a request: as many as a full device has room for.
+int cluster_of(int32_t R, int32_t V, int sm_count) {
+  int ctas = kMostCluster;
+  while (ctas > 1 && ((int64_t)R * ctas > (int64_t)sm_count * 4 || V / ctas < 512)) ctas /= 2;
+  return ctas;
+}
+
+size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
+struct Sizes { size_t parts, tickets, stops; };
+// Rows in several slices are few: fewer than 8 parts per SM in all, and as many of the drafts; and tickets are used only there.
+// So smaller calls of any kind fit in what a larger one needs.
+Sizes sizes_of(int32_t R, int32_t D, int sm_count) {
+  const size_t whole_rows = (size_t)R + 2 * (size_t)D, sliced = (size_t)sm_count * 16;
+  return {(whole_rows > sliced ? whole_rows : sliced) * sizeof(RowPart), (size_t)sm_count * 4 * sizeof(unsigned int), (size_t)R * sizeof(int)};
 }
 
 }  // namespace
 
-// Rows in several slices are few: fewer than 16 parts per SM in all, and as many of the drafts.  So smaller calls of any
-// kind fit in what a larger one needs.
-size_t verify_workspace_bytes(int32_t R, int32_t D, int sm_count) {
-  const size_t whole_rows = (size_t)R + 2 * (size_t)D, sliced = (size_t)sm_count * 32;
-  return (whole_rows > sliced ? whole_rows : sliced) * sizeof(RowPart);
+// Sizes the workspace; what a call leaves as it found it, the tickets and the stops, is set where the memory is new.
+af_status reserve_draft_verify(af_ctx* ctx, int32_t R, int32_t D, cudaStream_t s) {
+  const Sizes z = sizes_of(R, D, ctx->sm_count);
+  af_status st = ws_grow(ctx->verify_ws, z.parts);
+  if (st != AF_OK) return st;
+  const size_t had = ctx->verify_state.cap;
+  st = ws_grow(ctx->verify_state, round16(z.tickets) + z.stops);
+  if (st != AF_OK) return st;
+  if (ctx->verify_state.cap != had) {
+    char* const p = static_cast<char*>(ctx->verify_state.p);
+    const size_t stops = ctx->verify_state.cap - round16(z.tickets);
+    if (cudaMemsetAsync(p, 0, round16(z.tickets), s) != cudaSuccess || cudaMemsetAsync(p + round16(z.tickets), 0x7f, stops, s) != cudaSuccess)
+      return AF_ERR_CUDA;
+  }
+  return AF_OK;
 }
 
 af_status launch_draft_verify(af_ctx* ctx, const VerifyCall& c, cudaStream_t s) {
-  const af_status st = ws_grow(ctx->verify_ws, verify_workspace_bytes(c.R, c.D, ctx->sm_count));
+  const af_status st = reserve_draft_verify(ctx, c.R, c.D, s);
   if (st != AF_OK) return st;
   const Shape shape = shape_of(c.R, c.V, c.max_draft, ctx->sm_count);
-  RowPart* const target_parts = static_cast<RowPart*>(ctx->verify_ws.p);
-  RowPart* const draft_parts = target_parts + ((size_t)c.R + c.D) * shape.slices;
+  Workspace ws;
+  ws.target = static_cast<RowPart*>(ctx->verify_ws.p);
+  ws.draft = ws.target + ((size_t)c.R + c.D) * shape.slices;
+  ws.ticket = static_cast<unsigned int*>(ctx->verify_state.p);
+  ws.stop = reinterpret_cast<int*>(static_cast<char*>(ctx->verify_state.p) + round16(sizes_of(c.R, c.D, ctx->sm_count).tickets));
   const float scale = c.temperature == 0.f ? kLog2e : kLog2e / c.temperature;
   const int64_t blocks = (int64_t)c.R * shape.positions * shape.slices;
-  if (launch_overlapped(verify_rows_kernel, (unsigned)blocks, kThreads, 0, s, c, shape, scale, target_parts, draft_parts) != cudaSuccess)
-    return AF_ERR_CUDA;
+  if (launch_overlapped(verify_rows_kernel, (unsigned)blocks, kRowThreads, 0, s, c, shape, scale, ws) != cudaSuccess) return AF_ERR_CUDA;
+  const int ctas = c.temperature == 0.f ? 1 : cluster_of(c.R, c.V, ctx->sm_count);
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = (unsigned)c.R * kCluster;
-  cfg.blockDim = kThreads;
+  cfg.gridDim = (unsigned)c.R * ctas;
+  cfg.blockDim = kDrawThreads;
   cfg.stream = s;
   cudaLaunchAttribute attr[2]{};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = kCluster;
+  attr[1].val.clusterDim.x = ctas;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, verify_draw_kernel, c, shape, scale, (const RowPart*)target_parts, (const RowPart*)draft_parts,
-                            ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, verify_draw_kernel, c, shape, ws, ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
 }  // namespace af
