@@ -17,7 +17,8 @@
 namespace af {
 namespace {
 
-constexpr int kRowThreads = 1024;                  // one row, or slice, at a time on an SM: so that positions end in order
+constexpr int kRowThreads = 512;
+constexpr int kRowBlocks = 3;                      // rows, or slices, on an SM at a time: few, so that positions end in order
 constexpr int kDrawThreads = 512;
 constexpr int kDrawWarps = kDrawThreads / 32;
 constexpr int kMostCluster = 8;                    // CTAs that draw for one request
@@ -146,7 +147,7 @@ __device__ RowPart block_part(const LogitRows& x, int64_t row, int lo, int hi, f
   if ((threadIdx.x & 31) == 0) warp_parts[threadIdx.x >> 5] = a;
   __syncthreads();
   if (threadIdx.x < 32) {
-    a = warp_parts[threadIdx.x];
+    a = threadIdx.x < kRowThreads / 32 ? warp_parts[threadIdx.x] : RowPart{kNoMax, 0.f, kGoesOn, 0};
     over_warp();
   }
   return a;
@@ -189,7 +190,7 @@ __device__ __forceinline__ Sides sides_of(const VerifyCall& c, const Row& t, con
 }
 __device__ __forceinline__ bool too_near(const Sides& e) { return fabs(e.left - e.right) <= 1e-5 * fabs(e.right); }
 
-__global__ void __launch_bounds__(kRowThreads) verify_rows_kernel(const VerifyCall c, const Shape shape, float scale, const Workspace ws) {
+__global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(const VerifyCall c, const Shape shape, float scale, const Workspace ws) {
   __shared__ RowPart warp_parts[2][kRowThreads / 32];
   __shared__ int s_skip;
   wait_for_predecessor();
@@ -285,17 +286,54 @@ __device__ double block_sum(double a, double* warp_sums) {
   for (int w = 0; w < kDrawWarps; ++w) all += warp_sums[w];
   return all;
 }
-__device__ double exact_sum(const LogitRows& x, int64_t row, int lo, int hi, const Exp64& e, double* warp_sums) {
-  double a = 0.0;
-#pragma unroll 4
-  for (int v = lo + threadIdx.x; v < hi; v += kDrawThreads) a += e(load(x, row, v));
-  return block_sum(a, warp_sums);
+__device__ __forceinline__ float value(const float* p) { return __ldg(p); }
+__device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+template <class T>
+__device__ __forceinline__ const T* row_of(const LogitRows& x, int64_t row) { return static_cast<const T*>(x.p) + row * x.pitch; }
+
+constexpr int kAhead = 8;                          // loads under way per thread
+// Calls use(v, row[v]) for v = first, first + step, ... below hi.
+template <class T, class Use>
+__device__ __forceinline__ void each(const T* row, int first, int hi, int step, Use use) {
+  int v = first;
+  for (; v + (kAhead - 1) * step < hi; v += kAhead * step) {
+    float z[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) z[k] = value(row + v + k * step);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) use(v + k * step, z[k]);
+  }
+  for (; v < hi; v += step) use(v, value(row + v));
+}
+// The same for two rows at a time.
+template <class T, class Q, class Use>
+__device__ __forceinline__ void each_pair(const T* row, const Q* other, int first, int hi, int step, Use use) {
+  int v = first;
+  for (; v + (kAhead / 2 - 1) * step < hi; v += kAhead / 2 * step) {
+    float z[kAhead / 2], q[kAhead / 2];
+#pragma unroll
+    for (int k = 0; k < kAhead / 2; ++k) { z[k] = value(row + v + k * step); q[k] = value(other + v + k * step); }
+#pragma unroll
+    for (int k = 0; k < kAhead / 2; ++k) use(v + k * step, z[k], q[k]);
+  }
+  for (; v < hi; v += step) use(v, value(row + v), value(other + v));
+}
+template <class T>
+__device__ double exact_sum(const T* row, int lo, int hi, const Exp64& e, double* warp_sums) {
+  double a = 0.0, b = 0.0;
+  each(row, lo + (int)threadIdx.x, hi, kDrawThreads, [&](int, float z) {
+    const double w = a;                            // two chains
+    a = b;
+    b = w + e(z);
+  });
+  return block_sum(a + b, warp_sums);
 }
 
 constexpr int kBatch = 8;                          // positions looked at a time
 
-// A cluster per request.
-__global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(const VerifyCall c, const Shape shape, const Workspace ws, unsigned int* d_err) {
+// A cluster per request.  T, Q: types of the target's and the drafts' logits.
+template <class T, class Q>
+__global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const VerifyCall c, const Shape shape, const Workspace ws, unsigned int* d_err) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -359,8 +397,8 @@ __global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(const VerifyC
       if (id_ok) {
         Sides e = sides_of(c, t, q, base + i, sp.first + i, x, inv_tau);
         if (too_near(e)) {                                    // the same in all threads of the cluster
-          t.s = exact_sum(c.target, base + i, 0, c.V, exp_about(s_power, t.m, inv_tau), s_warp);
-          if (c.draft.p) q.s = exact_sum(c.draft, sp.first + i, 0, c.V, exp_about(s_power, q.m, inv_tau), s_warp);
+          t.s = exact_sum(row_of<T>(c.target, base + i), 0, c.V, exp_about(s_power, t.m, inv_tau), s_warp);
+          if (c.draft.p) q.s = exact_sum(row_of<Q>(c.draft, sp.first + i), 0, c.V, exp_about(s_power, q.m, inv_tau), s_warp);
           e = sides_of(c, t, q, base + i, sp.first + i, x, inv_tau);
         }
         pass = e.left < e.right;
@@ -393,12 +431,13 @@ __global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(const VerifyC
   // ---- the token after them, from row base + i
   const bool rejected = i < sp.n, dense = rejected && c.draft.p != nullptr;
   const int cut = rejected && !dense ? __ldg(c.draft_ids + sp.first + i) : -1;
+  const T* const p_row = row_of<T>(c.target, base + i);
+  const Q* const q_row = dense ? row_of<Q>(c.draft, sp.first + i) : nullptr;
   const Exp64 pe = exp_about(s_power, t.m, inv_tau), qe = exp_about(s_power, q.m, inv_tau);
   double p_unit = 1.0, q_unit = 1.0;                          // dense: 1 / sums
   double row_sum = 0.0;                                       // of the target's weights
   if (dense) {
-    const double a = exact_sum(c.target, base + i, lo, hi, pe, s_warp);
-    const double b = exact_sum(c.draft, sp.first + i, lo, hi, qe, s_warp);
+    const double a = exact_sum(p_row, lo, hi, pe, s_warp), b = exact_sum(q_row, lo, hi, qe, s_warp);
     if (threadIdx.x == 0) { s_sum[0] = a; s_sum[1] = b; }
     cluster.sync();
     double sum_q = 0.0;
@@ -412,25 +451,17 @@ __global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(const VerifyC
   // a warp's segment of the CTA's share
   const int seg_lo = lo + (int)((int64_t)(hi - lo) * warp / kDrawWarps), seg_hi = lo + (int)((int64_t)(hi - lo) * (warp + 1) / kDrawWarps);
   bool plain = !rejected;                                     // drawn from the target itself
-  auto mass = [&](int v) {
-    double w = pe(load(c.target, base + i, v)) * p_unit;
-    if (!plain && dense) w = fmax(w - qe(load(c.draft, sp.first + i, v)) * q_unit, 0.0);
-    return w;
-  };
+  auto left = [&](float z, float zq) { return fmax(pe(z) * p_unit - qe(zq) * q_unit, 0.0); };      // of p less q
   double before, total;
   for (;;) {
     double a = 0.0, whole = 0.0;
-    if (dense || plain || cut < seg_lo || cut >= seg_hi) {
-#pragma unroll 4
-      for (int v = seg_lo + lane; v < seg_hi; v += 32) a += mass(v);
-      whole = a;
-    } else {                                                  // the segment that holds the draft that is cut out
-      for (int v = seg_lo + lane; v < seg_hi; v += 32) {
-        const double w = mass(v);
-        whole += w;
-        if (v != cut) a += w;
-      }
-    }
+    if (dense && !plain) each_pair(p_row, q_row, seg_lo + lane, seg_hi, 32, [&](int, float z, float zq) { a += left(z, zq); });
+    else each(p_row, seg_lo + lane, seg_hi, 32, [&](int v, float z) {
+      const double w = pe(z);
+      whole += w;
+      a += !plain && v == cut ? 0.0 : w;
+    });
+    if (dense && plain) a *= p_unit;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       a += __shfl_xor_sync(0xffffffffu, a, o);
@@ -472,7 +503,11 @@ __global__ void __launch_bounds__(kDrawThreads) verify_draw_kernel(const VerifyC
   int y = seg_lo;                                             // the last with mass, if rounding leaves the goal beyond the segment
   for (int v0 = seg_lo; v0 < seg_hi; v0 += 32) {
     const int v = v0 + lane;
-    const double w = v < seg_hi && (plain || v != cut) ? mass(v) : 0.0;
+    double w = 0.0;
+    if (v < seg_hi && (plain || v != cut)) {
+      if (dense) w = plain ? pe(value(p_row + v)) * p_unit : left(value(p_row + v), value(q_row + v));
+      else w = pe(value(p_row + v));
+    }
     double upto = w;                                          // sum over the lanes up to this one
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -557,7 +592,11 @@ af_status launch_draft_verify(af_ctx* ctx, const VerifyCall& c, cudaStream_t s) 
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, verify_draw_kernel, c, shape, ws, ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+  auto go = [&](auto kernel) { return cudaLaunchKernelEx(&cfg, kernel, c, shape, ws, ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA; };
+  using bf16 = __nv_bfloat16;
+  const bool wide_draft = !c.draft.p || c.draft.type == AF_F32;
+  if (c.target.type == AF_F32) return wide_draft ? go(verify_draw_kernel<float, float>) : go(verify_draw_kernel<float, bf16>);
+  return wide_draft ? go(verify_draw_kernel<bf16, float>) : go(verify_draw_kernel<bf16, bf16>);
 }
 
 }  // namespace af
