@@ -570,14 +570,16 @@ af_status af_quant_logits(af_ctx* ctx, const void* hidden, const void* codes, co
  * infinity, nothing but -inf) ends its request: token -1, logp NaN, n_emitted = the drafts passed before it, and
  * AF_DEVERR_DISTRIBUTION.  Rows behind the first draft that does not pass are not looked at (but may be read).
  * A request whose part of cu_draft is not within [0, D], decreasing or longer than max_draft gets n_emitted = 0, its rows are left
- * as they are, and AF_DEVERR_CU_SEQLENS is raised, as it is where cu_draft does not run from 0 to D.
+ * as they are, and AF_DEVERR_CU_SEQLENS is raised, as it is where cu_draft does not run from 0 to D.  (Rows that two requests of
+ * such a cu_draft share hold one's or the other's results.)
  *
  * Comparisons and draws are made from sums in 64 bits where 32 could decide otherwise; log-probs of passed drafts are within
  * 1e-6 of 64 bits, that of y is rounded once.
  * target_logits [D + R, V], draft_logits [D, V]: fp32 or bf16 dev, row pitch in elements (>= V), aligned to their type.  draft [D],
- * cu_draft [R+1], token [D + R], n_emitted [R] int32, logp (nullable) [D + R] fp32, dev.  0 <= R <= 2^20, 0 <= D <= 2^24,
- * D <= R * max_draft, 0 <= max_draft <= AF_MAX_DRAFT, temperature 0 or from 1e-4 to 1e4.
- * Workspace: 16 bytes per row, 75 KB at least; af_reserve_rollout sizes it ahead, for smaller batches too.
+ * cu_draft [R+1], token [D + R], n_emitted [R] int32, logp (nullable) [D + R] fp32, dev.  0 <= max_draft <= AF_MAX_DRAFT,
+ * 0 <= R, R * (max_draft + 1) <= 2^24, 0 <= D <= R * max_draft, temperature 0 or from 1e-4 to 1e4.
+ * Workspace: 36 bytes per request and position (max_draft + 1 of them) and 4 per request, 40 KB beside; af_reserve_rollout sizes
+ * it ahead, for smaller batches too.
  * ------------------------------------------------------------------------------------------- */
 #define AF_MAX_DRAFT 1023
 af_status af_draft_verify(af_ctx* ctx, const void* target_logits, int32_t target_type, int64_t target_pitch,
@@ -619,9 +621,9 @@ af_status af_block_slots(af_ctx* ctx, const int32_t* length, const int32_t* grow
                          int32_t n_blocks, const int32_t* free_count, int32_t* held_out, int32_t* free_count_out, int32_t* granted,
                          int32_t* cu_new, int64_t* slot, int32_t* position, int64_t token_capacity, void* stream);
 
-/* Pre-size the workspace of af_draft_verify and af_block_slots for up to max_R requests and max_D drafted tokens in all.
+/* Pre-size the workspace of af_draft_verify and af_block_slots for up to max_R requests of up to max_draft drafted tokens.
  * Synchronous (allocates). */
-af_status af_reserve_rollout(af_ctx* ctx, int32_t max_R, int32_t max_D);
+af_status af_reserve_rollout(af_ctx* ctx, int32_t max_R, int32_t max_draft);
 
 /* ---------------------------------------------------------------------------------------------
  * af_controller_put / af_controller_get / af_controller_clear -- the status table of the

@@ -582,8 +582,9 @@ class Context:
                                        array(slot, torch.int64, 8 * capacity), array(position, i32, 4 * capacity), capacity,
                                        self._stream_of(stream)), "af_block_slots")
 
-    def reserve_rollout(self, max_R: int, max_D: int):
-        _check(self.lib.af_reserve_rollout(self.handle, max_R, max_D), "af_reserve_rollout")
+    def reserve_rollout(self, max_R: int, max_draft: int):
+        """Workspace of draft_verify and block_slots for up to max_R requests of up to max_draft drafted tokens."""
+        _check(self.lib.af_reserve_rollout(self.handle, max_R, max_draft), "af_reserve_rollout")
 
     # -- controller: status table of the streaming store ----------------------------------------
     @staticmethod

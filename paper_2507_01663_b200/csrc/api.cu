@@ -708,7 +708,7 @@ af_status af_quant_logits(af_ctx* c, const void* hidden, const void* codes, cons
 
 static af_status verify_sizes(int32_t R, int32_t D, int32_t V, int32_t max_draft) {
   if (R < 0 || D < 0 || V < 1 || max_draft < 0) return AF_ERR_INVALID_ARG;
-  if (max_draft > AF_MAX_DRAFT || R > (1 << 20) || (int64_t)D > (int64_t)R * max_draft || D > (1 << 24)) return AF_ERR_SHAPE;
+  if (max_draft > AF_MAX_DRAFT || (int64_t)R * (max_draft + 1) > (1 << 24) || (int64_t)D > (int64_t)R * max_draft) return AF_ERR_SHAPE;
   return AF_OK;
 }
 
@@ -754,12 +754,13 @@ af_status af_block_slots(af_ctx* c, const int32_t* length, const int32_t* grow, 
   return launch_block_slots(c, call, static_cast<cudaStream_t>(stream));
 }
 
-af_status af_reserve_rollout(af_ctx* c, int32_t max_R, int32_t max_D) {
+af_status af_reserve_rollout(af_ctx* c, int32_t max_R, int32_t max_draft) {
   NvtxRange range("af_reserve_rollout");
-  if (!c || max_R < 0 || max_D < 0) return AF_ERR_INVALID_ARG;
-  if (max_R > (1 << 20) || max_D > (1 << 24)) return AF_ERR_SHAPE;
+  if (!c) return AF_ERR_INVALID_ARG;
+  const af_status sizes = verify_sizes(max_R, 0, 1, max_draft);
+  if (sizes != AF_OK) return sizes;
   DeviceGuard guard(c->device);
-  const af_status st = reserve_draft_verify(c, max_R, max_D, nullptr);
+  const af_status st = reserve_draft_verify(c, max_R, max_draft, nullptr);
   // the caller's stream may be one that does not wait for the default stream, on which the above was set
   if (st == AF_OK && cudaStreamSynchronize(nullptr) != cudaSuccess) return AF_ERR_CUDA;
   return st == AF_OK ? ws_grow(c->slots_ws, slots_workspace_bytes(max_R)) : st;

@@ -2,8 +2,8 @@
 //
 // Two launches.  The first reads rows of logits once, in slices, for their maxima and sums of exponentials (fp32: a stream at
 // the memory's rate, next to which the exponentials fit).  It goes through the batch by positions, first drafts first, and a
-// row of a request that has already been seen to stop is not read.  The second, a cluster per request, decides which drafts
-// pass and draws the token after them.
+// row of a request that has already been seen to stop is not read.  Whoever finishes a row decides whether its draft passes.
+// The second, a cluster per request, finds the first that does not and draws the token after those before it.
 //
 // What has to be exact is whole numbers: a comparison u q < p, and the place of u C among running sums C_v of up to
 // 10^5 terms, where fp32 would be off by as much as many terms are large.  So a comparison whose sides are within 1e-5 is
@@ -30,10 +30,20 @@ struct RowPart {                                   // a slice of a row: max z, s
   float m, s;
   int32_t at, pad;
 };
+struct Row {                                       // of a whole row: maximum, its place, sum about the maximum in 64 bits
+  float m;
+  int32_t at;
+  double s;
+};
+enum Verdict : int32_t { kPasses, kFails, kTooNear, kNoRow };       // too near to tell in 32 bits; target or draft is no distribution
+// Places are by unit, position * R + request: each request has its own, whatever cu_draft says.
 struct Workspace {
-  RowPart* target;                                 // [D + R][slices]
-  RowPart* draft;                                  // [D][slices]
-  unsigned int* ticket;                            // [positions * R] slices done, zero between calls
+  RowPart* target;                                 // [units][slices]
+  RowPart* draft;                                  // [units][slices]
+  Row* target_row;                                 // [units]
+  Row* draft_row;                                  // [units]
+  int32_t* verdict;                                // [units]
+  unsigned int* ticket;                            // [units] slices done, zero between calls
   int* stop;                                       // [R] first draft that is known not to pass, kGoesOn between calls
 };
 struct Shape {
@@ -102,8 +112,19 @@ __device__ __forceinline__ void add(RowPart& a, const Values<n>& x, int at, floa
       if (x.v[i] != x.v[i]) a.s = x.v[i];
     return;
   }
+  // a NaN, and infinity less itself, make the sum NaN
+  if constexpr (n == 1) {
+    a.s += ex2f((x.v[0] - a.m) * scale);
+  } else {
+    const float2 less = make_float2(-a.m, -a.m), by = make_float2(scale, scale);
+    float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < n; ++i) a.s += ex2f((x.v[i] - a.m) * scale);       // a NaN, and infinity less itself, make the sum NaN
+    for (int i = 0; i < n; i += 2) {
+      const float2 e = __fmul2_rn(__fadd2_rn(make_float2(x.v[i], x.v[i + 1]), less), by);
+      sum = __fadd2_rn(sum, make_float2(ex2f(e.x), ex2f(e.y)));
+    }
+    a.s += sum.x + sum.y;
+  }
 }
 
 template <bool kPlace, class T>
@@ -128,33 +149,22 @@ __device__ RowPart row_part(const T* row, int lo, int hi, float scale) {
   return a;
 }
 
-// The block's part of a row; the first warp has it.
 template <bool kPlace>
-__device__ RowPart block_part(const LogitRows& x, int64_t row, int lo, int hi, float scale, RowPart* warp_parts) {
-  RowPart a = x.type == AF_F32 ? row_part<kPlace>(static_cast<const float*>(x.p) + row * x.pitch, lo, hi, scale)
-                               : row_part<kPlace>(static_cast<const __nv_bfloat16*>(x.p) + row * x.pitch, lo, hi, scale);
-  auto over_warp = [&] {
+__device__ RowPart thread_part(const LogitRows& x, int64_t row, int lo, int hi, float scale) {
+  return x.type == AF_F32 ? row_part<kPlace>(static_cast<const float*>(x.p) + row * x.pitch, lo, hi, scale)
+                          : row_part<kPlace>(static_cast<const __nv_bfloat16*>(x.p) + row * x.pitch, lo, hi, scale);
+}
+__device__ __forceinline__ void join_warp(RowPart& a, float scale) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      RowPart b;
-      b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-      b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-      b.at = __shfl_xor_sync(0xffffffffu, a.at, o);
-      a = join(a, b, scale);
-    }
-  };
-  over_warp();
-  if ((threadIdx.x & 31) == 0) warp_parts[threadIdx.x >> 5] = a;
-  __syncthreads();
-  if (threadIdx.x < 32) {
-    a = threadIdx.x < kRowThreads / 32 ? warp_parts[threadIdx.x] : RowPart{kNoMax, 0.f, kGoesOn, 0};
-    over_warp();
+  for (int o = 16; o > 0; o >>= 1) {
+    RowPart b;
+    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
+    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
+    b.at = __shfl_xor_sync(0xffffffffu, a.at, o);
+    a = join(a, b, scale);
   }
-  return a;
 }
 
-// A row's distribution from its parts: maximum, its place, and the sum in 64 bits of the parts' sums.
-struct Row { float m; int32_t at; double s; };
 __device__ __forceinline__ bool good(const Row& x) { return fabsf(x.m) < INFINITY && x.s > 0.0 && x.s < 1e300; }
 // Called by a whole warp.
 __device__ Row warp_row(const RowPart* parts, int slices, double inv_tau) {
@@ -201,50 +211,65 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
   if (!sp.ok || i > sp.n) return;
   if (threadIdx.x == 0) s_skip = *reinterpret_cast<volatile int*>(ws.stop + r) < i;
   __syncthreads();
-  // A skipped slice is counted too: the ticket has to come back to 0.  Whoever is last then finds the request stopped before i
-  // already, and what the skipped slice's part holds changes nothing.
-  const bool counted = i < sp.n && shape.slices > 1;
   if (s_skip) {                                    // the request ends before this row, whatever is in it
-    if (counted && threadIdx.x == 0) atomicInc(ws.ticket + unit, shape.slices - 1);
+    // A skipped slice is counted too: the ticket has to come back to 0.  Whoever is last then finds the request stopped before
+    // i already, and what the skipped slice's part holds changes nothing.
+    if (shape.slices > 1 && threadIdx.x == 0) atomicInc(ws.ticket + unit, shape.slices - 1);
     return;
   }
   const int lo = (int)((int64_t)c.V * slice / shape.slices), hi = (int)((int64_t)c.V * (slice + 1) / shape.slices);
   const int64_t row = sp.first + r + i;
+  const int k = sp.first + i;                      // the draft's row
   const bool greedy = c.temperature == 0.f, dense = c.draft.p && i < sp.n;
-  const RowPart t = greedy ? block_part<true>(c.target, row, lo, hi, scale, warp_parts[0]) : block_part<false>(c.target, row, lo, hi, scale, warp_parts[0]);
-  RowPart d{};
-  if (dense) d = block_part<false>(c.draft, sp.first + i, lo, hi, scale, warp_parts[1]);
+  RowPart t = greedy ? thread_part<true>(c.target, row, lo, hi, scale) : thread_part<false>(c.target, row, lo, hi, scale);
+  RowPart d{kNoMax, 0.f, kGoesOn, 0};
+  if (dense) d = thread_part<false>(c.draft, k, lo, hi, scale);
+  join_warp(t, scale);
+  if (dense) join_warp(d, scale);
+  if ((threadIdx.x & 31) == 0) { warp_parts[0][threadIdx.x >> 5] = t; warp_parts[1][threadIdx.x >> 5] = d; }
+  __syncthreads();
   if (threadIdx.x >= 32) return;
-  RowPart* const t_at = ws.target + row * shape.slices;
-  RowPart* const d_at = ws.draft + (int64_t)(sp.first + i) * shape.slices;
-  if (threadIdx.x == 0) {
-    t_at[slice] = t;
-    if (dense) d_at[slice] = d;
-  }
-  if (i == sp.n) return;
-  // the last slice of the row: if the draft surely does not pass, later rows of the request need not be read
-  int last = 1;
-  if (threadIdx.x == 0) {
-    __threadfence();
-    if (counted) last = atomicInc(ws.ticket + unit, shape.slices - 1) == shape.slices - 1u;      // back to 0 with the last
-  }
-  last = __shfl_sync(0xffffffffu, last, 0);
-  if (!last) return;
-  __threadfence();
+  const bool in = threadIdx.x < kRowThreads / 32;
+  t = in ? warp_parts[0][threadIdx.x] : RowPart{kNoMax, 0.f, kGoesOn, 0};
+  d = in ? warp_parts[1][threadIdx.x] : t;
+  join_warp(t, scale);
+  if (dense) join_warp(d, scale);
+  // whoever has the last slice puts the row together
   const double inv_tau = greedy ? 1.0 : 1.0 / (double)c.temperature;
-  const Row tr = warp_row(t_at, shape.slices, inv_tau);
-  Row dr{};
-  if (dense) dr = warp_row(d_at, shape.slices, inv_tau);
-  if (threadIdx.x != 0) return;
-  const int x = __ldg(c.draft_ids + sp.first + i);
-  bool ends;
-  if (!good(tr) || (dense && !good(dr)) || x < 0 || x >= c.V) ends = true;
-  else if (greedy) ends = x != tr.at;
-  else {
-    const Sides e = sides_of(c, tr, dr, row, sp.first + i, x, inv_tau);
-    ends = !(e.left < e.right) && !too_near(e);
+  Row tr{t.m, t.at, (double)t.s}, dr{d.m, d.at, (double)d.s};
+  if (shape.slices > 1) {
+    RowPart* const t_at = ws.target + (int64_t)unit * shape.slices;
+    RowPart* const d_at = ws.draft + (int64_t)unit * shape.slices;
+    int last = 0;
+    if (threadIdx.x == 0) {
+      t_at[slice] = t;
+      if (dense) d_at[slice] = d;
+      __threadfence();
+      last = atomicInc(ws.ticket + unit, shape.slices - 1) == shape.slices - 1u;       // back to 0 with the last
+    }
+    last = __shfl_sync(0xffffffffu, last, 0);
+    if (!last) return;
+    __threadfence();
+    tr = warp_row(t_at, shape.slices, inv_tau);
+    if (dense) dr = warp_row(d_at, shape.slices, inv_tau);
   }
-  if (ends) atomicMin(ws.stop + r, i);
+  if (threadIdx.x != 0) return;
+  ws.target_row[unit] = tr;
+  if (i == sp.n) return;
+  if (dense) ws.draft_row[unit] = dr;
+  // if the draft surely does not pass, later rows of the request need not be read
+  const int x = __ldg(c.draft_ids + k);
+  Verdict v = kFails;                              // an id outside the vocabulary does
+  if (!good(tr) || (dense && !good(dr))) v = kNoRow;
+  else if (x >= 0 && x < c.V) {
+    if (greedy) v = x == tr.at ? kPasses : kFails;
+    else {
+      const Sides e = sides_of(c, tr, dr, row, k, x, inv_tau);
+      v = too_near(e) ? kTooNear : e.left < e.right ? kPasses : kFails;
+    }
+  }
+  ws.verdict[unit] = v;
+  if (v == kFails || v == kNoRow) atomicMin(ws.stop + r, i);
 }
 
 // --------------------------------------------------------------------------------- draws, in 64 bits
@@ -329,7 +354,7 @@ __device__ double exact_sum(const T* row, int lo, int hi, const Exp64& e, double
   return block_sum(a + b, warp_sums);
 }
 
-constexpr int kBatch = 8;                          // positions looked at a time
+__device__ __forceinline__ Row dense_of(const Workspace& ws, const VerifyCall& c, int unit) { return c.draft.p ? ws.draft_row[unit] : Row{}; }
 
 // A cluster per request.  T, Q: types of the target's and the drafts' logits.
 template <class T, class Q>
@@ -339,7 +364,7 @@ __global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const Veri
   const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   __shared__ double s_power[kPowers], s_warp[kDrawWarps], s_sum[4];       // s_sum: this CTA's shares, read by the cluster
   __shared__ double s_segment[kDrawWarps];
-  __shared__ Row s_target[kBatch], s_draft[kBatch];
+  __shared__ int s_first;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x < kPowers) s_power[threadIdx.x] = exp2((double)threadIdx.x / kPowers);
   wait_for_predecessor();
@@ -361,69 +386,54 @@ __global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const Veri
   const int64_t base = sp.first + r;
   const int lo = (int)((int64_t)c.V * rank / ctas), hi = (int)((int64_t)c.V * (rank + 1) / ctas);
 
-  // ---- which drafts pass: every CTA of the cluster finds out by itself
+  // ---- the first draft that does not pass: every CTA of the cluster finds it by itself
+  auto unit = [&](int j) { return j * c.R + r; };
+  auto log_prob = [&](const Row& x, int64_t row, int v) {
+    return (float)(((double)load(c.target, row, v) - (double)x.m) * inv_tau - log(x.s));
+  };
   int i = 0;
-  bool has_row = true;
-  Row t{}, q{};
-  for (;; ++i) {
-    if (i % kBatch == 0) {                                    // the next rows, a warp each
-      __syncthreads();
-      const int at = warp % kBatch, j = i + at;
-      if (j <= sp.n && warp < kBatch) {
-        const Row x = warp_row(ws.target + (base + j) * shape.slices, shape.slices, inv_tau);
-        if (lane == 0) s_target[at] = x;
-      } else if (j < sp.n && warp >= kBatch && c.draft.p) {
-        const Row x = warp_row(ws.draft + (int64_t)(sp.first + j) * shape.slices, shape.slices, inv_tau);
-        if (lane == 0) s_draft[at] = x;
+  for (;;) {
+    if (warp == 0) {                                          // the next one that does not pass in 32 bits
+      int j = i;
+      for (; j < sp.n; j += 32) {
+        const bool stops = j + lane < sp.n && __ldcg(ws.verdict + unit(j + lane)) != kPasses;
+        const unsigned any = __ballot_sync(0xffffffffu, stops);
+        if (any) { j += __ffs(any) - 1; break; }
       }
-      __syncthreads();
+      if (lane == 0) s_first = min(j, sp.n);
     }
-    t = s_target[i % kBatch];
-    has_row = good(t);
-    if (!has_row || i == sp.n) break;
-    const int x = __ldg(c.draft_ids + sp.first + i);
-    const bool id_ok = x >= 0 && x < c.V;
-    if (!id_ok && leader) atomicOr(d_err, AF_DEVERR_TARGET_RANGE);
-    bool pass;
-    if (greedy) {
-      pass = x == t.at;
-    } else {
-      if (c.draft.p) {
-        q = s_draft[i % kBatch];
-        has_row = good(q);
-        if (!has_row) break;
-      }
-      pass = false;
-      if (id_ok) {
-        Sides e = sides_of(c, t, q, base + i, sp.first + i, x, inv_tau);
-        if (too_near(e)) {                                    // the same in all threads of the cluster
-          t.s = exact_sum(row_of<T>(c.target, base + i), 0, c.V, exp_about(s_power, t.m, inv_tau), s_warp);
-          if (c.draft.p) q.s = exact_sum(row_of<Q>(c.draft, sp.first + i), 0, c.V, exp_about(s_power, q.m, inv_tau), s_warp);
-          e = sides_of(c, t, q, base + i, sp.first + i, x, inv_tau);
-        }
-        pass = e.left < e.right;
-      }
-    }
-    if (!pass) break;
-    if (leader) {
-      c.token[base + i] = x;
-      if (c.logp) c.logp[base + i] = (float)(((double)load(c.target, base + i, x) - (double)t.m) * inv_tau - log(t.s));
-    }
+    __syncthreads();
+    i = s_first;
+    if (i == sp.n || __ldcg(ws.verdict + unit(i)) != kTooNear) break;
+    Row t = ws.target_row[unit(i)], q = dense_of(ws, c, unit(i));        // the same in all threads of the cluster
+    t.s = exact_sum(row_of<T>(c.target, base + i), 0, c.V, exp_about(s_power, t.m, inv_tau), s_warp);
+    if (c.draft.p) q.s = exact_sum(row_of<Q>(c.draft, sp.first + i), 0, c.V, exp_about(s_power, q.m, inv_tau), s_warp);
+    const Sides e = sides_of(c, t, q, base + i, sp.first + i, __ldg(c.draft_ids + sp.first + i), inv_tau);
+    if (!(e.left < e.right)) break;
+    ++i;                                                      // it passes; go on behind it
+    __syncthreads();                                          // s_first has been read
   }
-  if (leader) {
-    for (int j = i + 1; j <= sp.n; ++j) {
-      c.token[base + j] = -1;
-      if (c.logp) c.logp[base + j] = 0.f;
+  const Row t = ws.target_row[unit(i)];
+  const Row q = i < sp.n ? dense_of(ws, c, unit(i)) : Row{};
+  const bool has_row = good(t) && (i == sp.n || !c.draft.p || good(q));
+  if (rank == 0 && warp == 0) {
+    for (int j = lane; j <= sp.n; j += 32) {
+      const int x = j < i ? __ldg(c.draft_ids + sp.first + j) : j > i ? -1 : greedy && has_row ? t.at : -1;
+      if (j != i || greedy || !has_row) c.token[base + j] = x;        // the others draw it
+      if (!c.logp) continue;
+      if (j < i) c.logp[base + j] = log_prob(ws.target_row[unit(j)], base + j, x);
+      else if (j > i) c.logp[base + j] = 0.f;
+      else if (!has_row) c.logp[base + j] = __int_as_float(0x7fc00000);
+      else if (greedy) c.logp[base + j] = (float)-log(t.s);
     }
-    c.n_emitted[r] = has_row ? i + 1 : i;
-    if (!has_row) {
-      atomicOr(d_err, AF_DEVERR_DISTRIBUTION);
-      c.token[base + i] = -1;
-      if (c.logp) c.logp[base + i] = __int_as_float(0x7fc00000);
-    }
-    if (has_row && greedy) {
-      c.token[base + i] = t.at;
-      if (c.logp) c.logp[base + i] = (float)-log(t.s);
+    if (lane == 0) {
+      c.n_emitted[r] = has_row ? i + 1 : i;
+      unsigned int bad = has_row ? 0 : AF_DEVERR_DISTRIBUTION;
+      if (good(t) && i < sp.n) {
+        const int x = __ldg(c.draft_ids + sp.first + i);
+        if (x < 0 || x >= c.V) bad |= AF_DEVERR_TARGET_RANGE;
+      }
+      if (bad) atomicOr(d_err, bad);
     }
   }
   if (!has_row || greedy) return;                             // the whole cluster
@@ -437,7 +447,10 @@ __global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const Veri
   double p_unit = 1.0, q_unit = 1.0;                          // dense: 1 / sums
   double row_sum = 0.0;                                       // of the target's weights
   if (dense) {
-    const double a = exact_sum(p_row, lo, hi, pe, s_warp), b = exact_sum(q_row, lo, hi, qe, s_warp);
+    double a = 0.0, b = 0.0;
+    each_pair(p_row, q_row, lo + (int)threadIdx.x, hi, kDrawThreads, [&](int, float z, float zq) { a += pe(z); b += qe(zq); });
+    a = block_sum(a, s_warp);
+    b = block_sum(b, s_warp);
     if (threadIdx.x == 0) { s_sum[0] = a; s_sum[1] = b; }
     cluster.sync();
     double sum_q = 0.0;
@@ -540,42 +553,48 @@ int cluster_of(int32_t R, int32_t V, int sm_count) {
 }
 
 size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
-struct Sizes { size_t parts, tickets, stops; };
-// Rows in several slices are few: fewer than 8 parts per SM in all, and as many of the drafts; and tickets are used only there.
-// So smaller calls of any kind fit in what a larger one needs.
-Sizes sizes_of(int32_t R, int32_t D, int sm_count) {
-  const size_t whole_rows = (size_t)R + 2 * (size_t)D, sliced = (size_t)sm_count * 16;
-  return {(whole_rows > sliced ? whole_rows : sliced) * sizeof(RowPart), (size_t)sm_count * 4 * sizeof(unsigned int), (size_t)R * sizeof(int)};
+struct Sizes { size_t parts, rows, verdicts, tickets, stops; };
+// Rows in several slices are few: fewer than 8 parts per SM in all, and as many of the drafts; and parts and tickets are used
+// only there.  So smaller calls of any kind fit in what a larger one needs.
+Sizes sizes_of(int32_t R, int32_t max_draft, int sm_count) {
+  const size_t units = (size_t)R * ((size_t)max_draft + 1);
+  return {(size_t)sm_count * 16 * sizeof(RowPart), units * 2 * sizeof(Row), units * sizeof(int32_t),
+          round16((size_t)sm_count * 4 * sizeof(unsigned int)), (size_t)R * sizeof(int)};
 }
 
 }  // namespace
 
 // Sizes the workspace; what a call leaves as it found it, the tickets and the stops, is set where the memory is new.
-af_status reserve_draft_verify(af_ctx* ctx, int32_t R, int32_t D, cudaStream_t s) {
-  const Sizes z = sizes_of(R, D, ctx->sm_count);
-  af_status st = ws_grow(ctx->verify_ws, z.parts);
+af_status reserve_draft_verify(af_ctx* ctx, int32_t R, int32_t max_draft, cudaStream_t s) {
+  const Sizes z = sizes_of(R, max_draft, ctx->sm_count);
+  af_status st = ws_grow(ctx->verify_ws, z.parts + z.rows + z.verdicts);
   if (st != AF_OK) return st;
   const size_t had = ctx->verify_state.cap;
-  st = ws_grow(ctx->verify_state, round16(z.tickets) + z.stops);
+  st = ws_grow(ctx->verify_state, z.tickets + z.stops);
   if (st != AF_OK) return st;
   if (ctx->verify_state.cap != had) {
     char* const p = static_cast<char*>(ctx->verify_state.p);
-    const size_t stops = ctx->verify_state.cap - round16(z.tickets);
-    if (cudaMemsetAsync(p, 0, round16(z.tickets), s) != cudaSuccess || cudaMemsetAsync(p + round16(z.tickets), 0x7f, stops, s) != cudaSuccess)
+    const size_t stops = ctx->verify_state.cap - z.tickets;
+    if (cudaMemsetAsync(p, 0, z.tickets, s) != cudaSuccess || cudaMemsetAsync(p + z.tickets, 0x7f, stops, s) != cudaSuccess)
       return AF_ERR_CUDA;
   }
   return AF_OK;
 }
 
 af_status launch_draft_verify(af_ctx* ctx, const VerifyCall& c, cudaStream_t s) {
-  const af_status st = reserve_draft_verify(ctx, c.R, c.D, s);
+  const af_status st = reserve_draft_verify(ctx, c.R, c.max_draft, s);
   if (st != AF_OK) return st;
   const Shape shape = shape_of(c.R, c.V, c.max_draft, ctx->sm_count);
   Workspace ws;
-  ws.target = static_cast<RowPart*>(ctx->verify_ws.p);
-  ws.draft = ws.target + ((size_t)c.R + c.D) * shape.slices;
+  const Sizes z = sizes_of(c.R, c.max_draft, ctx->sm_count);
+  char* const at = static_cast<char*>(ctx->verify_ws.p);
+  ws.target = reinterpret_cast<RowPart*>(at);
+  ws.draft = ws.target + (size_t)c.R * shape.positions * shape.slices;
+  ws.target_row = reinterpret_cast<Row*>(at + z.parts);
+  ws.draft_row = ws.target_row + (size_t)c.R * shape.positions;
+  ws.verdict = reinterpret_cast<int32_t*>(at + z.parts + z.rows);
   ws.ticket = static_cast<unsigned int*>(ctx->verify_state.p);
-  ws.stop = reinterpret_cast<int*>(static_cast<char*>(ctx->verify_state.p) + round16(sizes_of(c.R, c.D, ctx->sm_count).tickets));
+  ws.stop = reinterpret_cast<int*>(static_cast<char*>(ctx->verify_state.p) + z.tickets);
   const float scale = c.temperature == 0.f ? kLog2e : kLog2e / c.temperature;
   const int64_t blocks = (int64_t)c.R * shape.positions * shape.slices;
   if (launch_overlapped(verify_rows_kernel, (unsigned)blocks, kRowThreads, 0, s, c, shape, scale, ws) != cudaSuccess) return AF_ERR_CUDA;

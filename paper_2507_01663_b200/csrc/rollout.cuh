@@ -41,7 +41,7 @@ struct VerifyCall {
   float* logp;
   int32_t* n_emitted;
 };
-af_status reserve_draft_verify(af_ctx* ctx, int32_t R, int32_t D, cudaStream_t s);
+af_status reserve_draft_verify(af_ctx* ctx, int32_t R, int32_t max_draft, cudaStream_t s);
 af_status launch_draft_verify(af_ctx* ctx, const VerifyCall& c, cudaStream_t s);
 
 // ---- block tables -----------------------------------------------------------------------------

@@ -300,7 +300,7 @@ def test_refusals(ctx):
     assert call(tt=2) == -1 and call(qt=-1) == -1
     for tau in (-1.0, 5e-5, 2e4, math.inf, math.nan):
         assert call(tau=tau) == -1
-    assert call(tp=63) == -2 and call(qp=63) == -2 and call(most=1024) == -2 and call(D=7) == -2 and call(R=(1 << 20) + 1) == -2
+    assert call(tp=63) == -2 and call(qp=63) == -2 and call(most=1024) == -2 and call(D=7) == -2 and call(R=(1 << 24) // 3 + 1) == -2
     assert call(t=p(t) + 2) == -3 and call(q=p(q) + 1, qt=1) == -3
     torch.cuda.synchronize()
     with pytest.raises(ValueError):
