@@ -17,11 +17,11 @@
 namespace af {
 namespace {
 
-constexpr int kRowThreads = 512;
-constexpr int kRowBlocks = 3;                      // rows, or slices, on an SM at a time: few, so that positions end in order
+constexpr int kRowThreads = 256;
+constexpr int kRowBlocks = 4;                      // rows, or slices, on an SM at a time: few, so that positions end in order
 constexpr int kDrawThreads = 512;
 constexpr int kDrawWarps = kDrawThreads / 32;
-constexpr int kMostCluster = 8;                    // CTAs that draw for one request
+constexpr int kMostCluster = 16;                   // CTAs that draw for one request
 constexpr float kNoMax = -INFINITY;
 constexpr double kResidualFloor = 0x1p-30;         // a residual with less mass than this is drawn from the target itself
 constexpr int kGoesOn = 0x7fffffff;
@@ -136,13 +136,22 @@ __device__ RowPart row_part(const T* row, int lo, int hi, float scale) {
   const int body = min(hi, lo + to_line), vecs = (hi - body) / kVec, tail = body + vecs * kVec;
   if (lo + (int)threadIdx.x < body) add<kPlace>(a, widen1(row + lo + threadIdx.x), lo + threadIdx.x, scale);
   const uint4* const at = reinterpret_cast<const uint4*>(row + body);
-  int i = threadIdx.x;
-  for (; i + (kLoads - 1) * kRowThreads < vecs; i += kLoads * kRowThreads) {
-    uint4 w[kLoads];
+  // the next loads are under way while the last ones' exponentials are taken
+  constexpr int kStep = kLoads * kRowThreads;
+  uint4 w[kLoads], ahead[kLoads];
+  auto fetch = [&](uint4 (&to)[kLoads], int i) {
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) w[k] = __ldg(at + i + k * kRowThreads);
+    for (int k = 0; k < kLoads; ++k) to[k] = __ldg(at + i + k * kRowThreads);
+  };
+  int i = threadIdx.x;
+  const int whole = vecs / kStep * kStep;          // the same number of whole steps for every thread
+  if (whole > 0) fetch(w, i);
+  for (; i < whole; i += kStep) {
+    if (i + kStep < whole) fetch(ahead, i + kStep);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) add<kPlace>(a, widen(row, w[k]), body + (i + k * kRowThreads) * kVec, scale);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) w[k] = ahead[k];
   }
   for (; i < vecs; i += kRowThreads) add<kPlace>(a, widen(row, __ldg(at + i)), body + i * kVec, scale);
   if (tail + (int)threadIdx.x < hi) add<kPlace>(a, widen1(row + tail + threadIdx.x), tail + threadIdx.x, scale);
@@ -274,12 +283,15 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
 
 // --------------------------------------------------------------------------------- draws, in 64 bits
 constexpr int kPowers = 64;
-// 2^((z - m) / tau log2 e), relative to within 2^-44; 0 from 2^-1021 down.
+// 2^((z - m) / tau log2 e), relative to within 2^-44, and 2^-1000 from there down: what is no more than kNothing is no mass.
+constexpr double kNothing = 0x1p-900;
 struct Exp64 {
   const double* power;                             // 2^(j / 64)
   double c, b;                                     // log2 e / tau, -m times it
   __device__ __forceinline__ double operator()(float z) const {
-    const double t = fma((double)z, c, b);
+    const double far = fma((double)z, c, b);
+    // no less than -1000 or so, -inf too: among high words as unsigned numbers, -1000's is below those of all lesser numbers
+    const double t = __hiloint2double((int)min((uint32_t)__double2hiint(far), 0xc08f4000u), __double2loint(far));
     constexpr double kShift = 0x1.8p52 / kPowers;  // adding it rounds to a multiple of 1/64, a whole number in the low bits
     const double shifted = t + kShift;
     const int n = __double2loint(shifted);
@@ -290,8 +302,7 @@ struct Exp64 {
     p = fma(r, p, 6.9314718055994531e-1);
     const double y = power[n & (kPowers - 1)];
     const double w = fma(y, r * p, y);
-    const double scaled = __hiloint2double(__double2hiint(w) + (n >> 6) * (1 << 20), __double2loint(w));
-    return t > -1021.0 ? scaled : 0.0;             // also for -inf
+    return __hiloint2double(__double2hiint(w) + ((n & -kPowers) << (20 - 6)), __double2loint(w));       // times 2^(n / 64)
   }
 };
 __device__ __forceinline__ Exp64 exp_about(const double* power, float m, double inv_tau) {
@@ -469,11 +480,13 @@ __global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const Veri
   for (;;) {
     double a = 0.0, whole = 0.0;
     if (dense && !plain) each_pair(p_row, q_row, seg_lo + lane, seg_hi, 32, [&](int, float z, float zq) { a += left(z, zq); });
-    else each(p_row, seg_lo + lane, seg_hi, 32, [&](int v, float z) {
-      const double w = pe(z);
-      whole += w;
-      a += !plain && v == cut ? 0.0 : w;
-    });
+    else {
+      const auto take = [&](int, float z) { a += pe(z); };
+      const bool cuts = !plain && cut >= seg_lo && cut < seg_hi;
+      each(p_row, seg_lo + lane, cuts ? cut : seg_hi, 32, take);
+      if (cuts) each(p_row, cut + 1 + lane, seg_hi, 32, take);
+      whole = a + (cuts && lane == 0 ? pe(value(p_row + cut)) : 0.0);
+    }
     if (dense && plain) a *= p_unit;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -507,27 +520,47 @@ __global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const Veri
     if (plain || (dense ? total : total / row_sum) > kResidualFloor) break;
     plain = true;                                             // next to nothing is left: the target itself
   }
-  // the warp whose segment holds the first v with C_v > u C
+  // the CTA whose share holds the first v with C_v > u C, and the segment of it that does
   const double u = (double)fminf(fmaxf(__ldg(c.u_sample + r), 0.f), 1.f - 0x1p-24f), goal = u * total;
-  const double start = before + s_segment[warp];
-  const double end = before + (warp + 1 < kDrawWarps ? s_segment[warp + 1] : s_sum[2]);
-  if (!(start <= goal && goal < end)) return;
-  double run = start;
-  int y = seg_lo;                                             // the last with mass, if rounding leaves the goal beyond the segment
-  for (int v0 = seg_lo; v0 < seg_hi; v0 += 32) {
+  if (!(before <= goal && goal < before + s_sum[2])) return;  // the whole CTA
+  int found = 0;
+  for (int k = 1; k < kDrawWarps; ++k)
+    if (before + s_segment[k] <= goal) found = k;
+  const double at_segment = before + s_segment[found];
+  const int f_lo = lo + (int)((int64_t)(hi - lo) * found / kDrawWarps), f_hi = lo + (int)((int64_t)(hi - lo) * (found + 1) / kDrawWarps);
+  auto mass = [&](int v) {
+    if (!plain && v == cut) return 0.0;
+    if (!dense) return pe(value(p_row + v));
+    return plain ? pe(value(p_row + v)) * p_unit : left(value(p_row + v), value(q_row + v));
+  };
+  // all warps share that segment out once more
+  const int part_lo = f_lo + (int)((int64_t)(f_hi - f_lo) * warp / kDrawWarps), part_hi = f_lo + (int)((int64_t)(f_hi - f_lo) * (warp + 1) / kDrawWarps);
+  double a = 0.0;
+#pragma unroll 4
+  for (int v = part_lo + lane; v < part_hi; v += 32) a += mass(v);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+  if (lane == 0) s_warp[warp] = a;
+  __syncthreads();
+  double run = at_segment, start = at_segment;
+  int mine = 0;                                               // the last part with mass that starts at or before the goal
+  for (int k = 0; k < kDrawWarps; ++k) {
+    if (run <= goal && s_warp[k] > kNothing) { mine = k; start = run; }
+    run += s_warp[k];
+  }
+  if (warp != mine) return;
+  run = start;
+  int y = part_lo;                                            // the last with mass, if rounding leaves the goal beyond the part
+  for (int v0 = part_lo; v0 < part_hi; v0 += 32) {
     const int v = v0 + lane;
-    double w = 0.0;
-    if (v < seg_hi && (plain || v != cut)) {
-      if (dense) w = plain ? pe(value(p_row + v)) * p_unit : left(value(p_row + v), value(q_row + v));
-      else w = pe(value(p_row + v));
-    }
+    const double w = v < part_hi ? mass(v) : 0.0;
     double upto = w;                                          // sum over the lanes up to this one
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const double x = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += x;
     }
-    const unsigned some = __ballot_sync(0xffffffffu, w > 0.0), beyond = __ballot_sync(0xffffffffu, w > 0.0 && run + upto > goal);
+    const unsigned some = __ballot_sync(0xffffffffu, w > kNothing), beyond = __ballot_sync(0xffffffffu, w > kNothing && run + upto > goal);
     if (beyond) { y = v0 + __ffs(beyond) - 1; break; }
     if (some) y = v0 + 31 - __clz(some);
     run += __shfl_sync(0xffffffffu, upto, 31);
@@ -548,8 +581,21 @@ Shape shape_of(int32_t R, int32_t V, int32_t max_draft, int sm_count) {
 // CTAs to a request: as many as a full device has room for.
 int cluster_of(int32_t R, int32_t V, int sm_count) {
   int ctas = kMostCluster;
-  while (ctas > 1 && ((int64_t)R * ctas > (int64_t)sm_count * 4 || V / ctas < 512)) ctas /= 2;
+  while (ctas > 1 && ((int64_t)R * ctas > (int64_t)sm_count * (ctas == kMostCluster ? 1 : 8) || V / ctas < 512)) ctas /= 2;
   return ctas;
+}
+
+template <class T, class Q>
+af_status launch_draws(const cudaLaunchConfig_t& cfg, const VerifyCall& c, const Shape& shape, const Workspace& ws, unsigned int* d_err) {
+  static SmemAttrOnce once;                                   // per device: clusters of more CTAs than every part has to take
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return AF_ERR_CUDA;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+  if (!bit || !(once.done.load(std::memory_order_acquire) & bit)) {
+    if (cudaFuncSetAttribute(verify_draw_kernel<T, Q>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return AF_ERR_CUDA;
+    once.done.fetch_or(bit, std::memory_order_release);
+  }
+  return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, Q>, c, shape, ws, d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
 size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
@@ -611,11 +657,11 @@ af_status launch_draft_verify(af_ctx* ctx, const VerifyCall& c, cudaStream_t s) 
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  auto go = [&](auto kernel) { return cudaLaunchKernelEx(&cfg, kernel, c, shape, ws, ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA; };
-  using bf16 = __nv_bfloat16;
   const bool wide_draft = !c.draft.p || c.draft.type == AF_F32;
-  if (c.target.type == AF_F32) return wide_draft ? go(verify_draw_kernel<float, float>) : go(verify_draw_kernel<float, bf16>);
-  return wide_draft ? go(verify_draw_kernel<bf16, float>) : go(verify_draw_kernel<bf16, bf16>);
+  using bf16 = __nv_bfloat16;
+  if (c.target.type == AF_F32)
+    return wide_draft ? launch_draws<float, float>(cfg, c, shape, ws, ctx->d_err) : launch_draws<float, bf16>(cfg, c, shape, ws, ctx->d_err);
+  return wide_draft ? launch_draws<bf16, float>(cfg, c, shape, ws, ctx->d_err) : launch_draws<bf16, bf16>(cfg, c, shape, ws, ctx->d_err);
 }
 
 }  // namespace af
