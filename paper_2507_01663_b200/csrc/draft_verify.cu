@@ -1,16 +1,17 @@
 // af_draft_verify: drafted tokens against the target's distribution, from given uniforms.
 //
-// Two launches.  The first reads rows of logits once, in slices, for their maxima and sums of exponentials (fp32: a stream at
-// the memory's rate, next to which the exponentials fit).  It goes through the batch by positions, first drafts first, and a
+// The first launch reads rows of logits once, in slices, for their maxima and sums of exponentials (fp32: a stream at the
+// memory's rate, next to which the exponentials fit).  It goes through the batch by positions, first drafts first, and a
 // row of a request that has already been seen to stop is not read.  Whoever finishes a row decides whether its draft passes.
-// The second, a cluster per request, finds the first that does not and draws the token after those before it.
+// Then, per request: the first draft that does not pass and, for a draw from what the draft leaves of the target, both rows' exact
+// sums; the mass of a few hundred segments; the segment, and in it the token, that the uniform points at.  Three launches of
+// slices that know nothing of one another: a cluster per request, with the sums in its shared memory, spent most of
+// its time waiting for its slowest CTA (64 requests: 75 us for 15 us of 64-bit operations).
 //
 // What has to be exact is whole numbers: a comparison u q < p, and the place of u C among running sums C_v of up to
 // 10^5 terms, where fp32 would be off by as much as many terms are large.  So a comparison whose sides are within 1e-5 is
 // made again from sums in 64 bits, and a draw's sums are in 64 bits throughout: per logit ten 64-bit operations, 2^x from a table
-// of 64 powers and a polynomial of degree 4 (2^-44 relative), which are what the second launch is bound by.
-#include <cooperative_groups.h>
-
+// of 64 powers and a polynomial of degree 4 (2^-44 relative).
 #include "device_util.cuh"
 #include "rollout.cuh"
 
@@ -19,9 +20,11 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kRowBlocks = 4;                      // rows, or slices, on an SM at a time: few, so that positions end in order
-constexpr int kDrawThreads = 512;
-constexpr int kDrawWarps = kDrawThreads / 32;
-constexpr int kMostCluster = 16;                   // CTAs that draw for one request
+constexpr int kDrawThreads = 256;                  // a slice of a request's vocabulary
+constexpr int kDrawWarps = kDrawThreads / 32;      // each with a segment of the slice
+constexpr int kMostSlices = 64;
+constexpr int kFindThreads = kMostSlices * kDrawWarps;       // one per segment
+constexpr int kFindWarps = kFindThreads / 32;
 constexpr float kNoMax = -INFINITY;
 constexpr double kResidualFloor = 0x1p-30;         // a residual with less mass than this is drawn from the target itself
 constexpr int kGoesOn = 0x7fffffff;
@@ -37,6 +40,7 @@ struct Row {                                       // of a whole row: maximum, i
 };
 enum Verdict : int32_t { kPasses, kFails, kTooNear, kNoRow };       // too near to tell in 32 bits; target or draft is no distribution
 // Places are by unit, position * R + request: each request has its own, whatever cu_draft says.
+struct Draw;
 struct Workspace {
   RowPart* target;                                 // [units][slices]
   RowPart* draft;                                  // [units][slices]
@@ -45,9 +49,19 @@ struct Workspace {
   int32_t* verdict;                                // [units]
   unsigned int* ticket;                            // [units] slices done, zero between calls
   int* stop;                                       // [R] first draft that is known not to pass, kGoesOn between calls
+  Draw* draw;                               // [R]
+  double2* sums;                                   // [R][draw slices] exact sums of the target's and the draft's row
+  double2* mass;                                   // [R][segments] mass, and the target's whole weight
+};
+enum Kind : int32_t { kNoDraw, kPlain, kCut, kDense };       // from the target; without the draft; from max(target - draft, 0)
+struct Draw {                                      // how a request's last token is drawn
+  int64_t row;                                     // the target's row
+  int32_t kind, draft_row, cut;                    // cut: the draft that is left out
+  float m, m_draft;                                // the rows' maxima
 };
 struct Shape {
   int slices, positions;                           // slices of a row; max_draft + 1
+  int draw_slices;                                 // slices of a vocabulary in a draw
 };
 
 __device__ __forceinline__ float load(const LogitRows& x, int64_t row, int v) {
@@ -310,7 +324,8 @@ __device__ __forceinline__ Exp64 exp_about(const double* power, float m, double 
   return {power, c, -(double)m * c};
 }
 
-// Sum over the block, in a fixed order; every thread gets it.
+// Sum over the block of kWarps warps, in a fixed order; every thread gets it.
+template <int kWarps>
 __device__ double block_sum(double a, double* warp_sums) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
@@ -319,7 +334,7 @@ __device__ double block_sum(double a, double* warp_sums) {
   __syncthreads();
   double all = 0.0;
 #pragma unroll
-  for (int w = 0; w < kDrawWarps; ++w) all += warp_sums[w];
+  for (int w = 0; w < kWarps; ++w) all += warp_sums[w];
   return all;
 }
 __device__ __forceinline__ float value(const float* p) { return __ldg(p); }
@@ -362,49 +377,49 @@ __device__ double exact_sum(const T* row, int lo, int hi, const Exp64& e, double
     a = b;
     b = w + e(z);
   });
-  return block_sum(a + b, warp_sums);
+  return block_sum<kDrawWarps>(a + b, warp_sums);
 }
 
 __device__ __forceinline__ Row dense_of(const Workspace& ws, const VerifyCall& c, int unit) { return c.draft.p ? ws.draft_row[unit] : Row{}; }
 
-// A cluster per request.  T, Q: types of the target's and the drafts' logits.
+// Segment k of a vocabulary cut into n.
+__device__ __forceinline__ int segment_at(int V, int k, int n) { return (int)((int64_t)V * k / n); }
+__device__ __forceinline__ double inverse_temperature(const VerifyCall& c) { return c.temperature == 0.f ? 1.0 : 1.0 / (double)c.temperature; }
+__device__ __forceinline__ void set_powers(double* power) {
+  if (threadIdx.x < kPowers) power[threadIdx.x] = exp2((double)threadIdx.x / kPowers);
+}
+
+// What passes, and how the token after it is drawn.  Every CTA of a request finds out by itself; the first writes it down.
+// T, Q: types of the target's and the drafts' logits.
 template <class T, class Q>
-__global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const VerifyCall c, const Shape shape, const Workspace ws, unsigned int* d_err) {
-  namespace cg = cooperative_groups;
-  cg::cluster_group cluster = cg::this_cluster();
-  const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  __shared__ double s_power[kPowers], s_warp[kDrawWarps], s_sum[4];       // s_sum: this CTA's shares, read by the cluster
-  __shared__ double s_segment[kDrawWarps];
+__global__ void __launch_bounds__(kDrawThreads) verify_sums_kernel(const VerifyCall c, const Shape shape, const Workspace ws, unsigned int* d_err) {
+  __shared__ double s_power[kPowers], s_warp[kDrawWarps];
   __shared__ int s_first;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (threadIdx.x < kPowers) s_power[threadIdx.x] = exp2((double)threadIdx.x / kPowers);
+  set_powers(s_power);
   wait_for_predecessor();
   let_successor_start();
-  const int r = (int)blockIdx.x / ctas;
+  const int r = (int)blockIdx.x / shape.draw_slices, slice = (int)blockIdx.x % shape.draw_slices;
   const Span sp = span_of(c, r);
-  const bool leader = rank == 0 && threadIdx.x == 0;
-  if (leader) {
+  if (slice == 0 && threadIdx.x == 0) {
     unsigned int bad = sp.ok ? 0 : AF_DEVERR_CU_SEQLENS;
     if (r == 0 && __ldg(c.cu) != 0) bad |= AF_DEVERR_CU_SEQLENS;
     if (r == c.R - 1 && __ldg(c.cu + c.R) != c.D) bad |= AF_DEVERR_CU_SEQLENS;
     if (bad) atomicOr(d_err, bad);
-    if (!sp.ok) c.n_emitted[r] = 0;
     ws.stop[r] = kGoesOn;                                     // for the next call
+    if (!sp.ok) {
+      c.n_emitted[r] = 0;
+      ws.draw[r] = Draw{0, kNoDraw, 0, 0, 0.f, 0.f};
+    }
   }
-  if (!sp.ok) return;                                         // the whole cluster
+  if (!sp.ok) return;
   const bool greedy = c.temperature == 0.f;
-  const double inv_tau = greedy ? 1.0 : 1.0 / (double)c.temperature;
+  const double inv_tau = inverse_temperature(c);
   const int64_t base = sp.first + r;
-  const int lo = (int)((int64_t)c.V * rank / ctas), hi = (int)((int64_t)c.V * (rank + 1) / ctas);
-
-  // ---- the first draft that does not pass: every CTA of the cluster finds it by itself
   auto unit = [&](int j) { return j * c.R + r; };
-  auto log_prob = [&](const Row& x, int64_t row, int v) {
-    return (float)(((double)load(c.target, row, v) - (double)x.m) * inv_tau - log(x.s));
-  };
   int i = 0;
   for (;;) {
-    if (warp == 0) {                                          // the next one that does not pass in 32 bits
+    if (warp == 0) {                                          // the next draft that does not pass in 32 bits
       int j = i;
       for (; j < sp.n; j += 32) {
         const bool stops = j + lane < sp.n && __ldcg(ws.verdict + unit(j + lane)) != kPasses;
@@ -416,7 +431,7 @@ __global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const Veri
     __syncthreads();
     i = s_first;
     if (i == sp.n || __ldcg(ws.verdict + unit(i)) != kTooNear) break;
-    Row t = ws.target_row[unit(i)], q = dense_of(ws, c, unit(i));        // the same in all threads of the cluster
+    Row t = ws.target_row[unit(i)], q = dense_of(ws, c, unit(i));        // the same in all threads of the request
     t.s = exact_sum(row_of<T>(c.target, base + i), 0, c.V, exp_about(s_power, t.m, inv_tau), s_warp);
     if (c.draft.p) q.s = exact_sum(row_of<Q>(c.draft, sp.first + i), 0, c.V, exp_about(s_power, q.m, inv_tau), s_warp);
     const Sides e = sides_of(c, t, q, base + i, sp.first + i, __ldg(c.draft_ids + sp.first + i), inv_tau);
@@ -427,147 +442,205 @@ __global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const Veri
   const Row t = ws.target_row[unit(i)];
   const Row q = i < sp.n ? dense_of(ws, c, unit(i)) : Row{};
   const bool has_row = good(t) && (i == sp.n || !c.draft.p || good(q));
-  if (rank == 0 && warp == 0) {
+  const int kind = !has_row || greedy ? kNoDraw : i == sp.n ? kPlain : c.draft.p ? kDense : kCut;
+  if (slice == 0 && warp == 0) {
     for (int j = lane; j <= sp.n; j += 32) {
       const int x = j < i ? __ldg(c.draft_ids + sp.first + j) : j > i ? -1 : greedy && has_row ? t.at : -1;
-      if (j != i || greedy || !has_row) c.token[base + j] = x;        // the others draw it
+      if (j != i || kind == kNoDraw) c.token[base + j] = x;   // else it is drawn
       if (!c.logp) continue;
-      if (j < i) c.logp[base + j] = log_prob(ws.target_row[unit(j)], base + j, x);
-      else if (j > i) c.logp[base + j] = 0.f;
+      if (j < i) {
+        const Row p = ws.target_row[unit(j)];
+        c.logp[base + j] = (float)(((double)load(c.target, base + j, x) - (double)p.m) * inv_tau - log(p.s));
+      } else if (j > i) c.logp[base + j] = 0.f;
       else if (!has_row) c.logp[base + j] = __int_as_float(0x7fc00000);
       else if (greedy) c.logp[base + j] = (float)-log(t.s);
     }
     if (lane == 0) {
+      const int x = i < sp.n ? __ldg(c.draft_ids + sp.first + i) : 0;
       c.n_emitted[r] = has_row ? i + 1 : i;
       unsigned int bad = has_row ? 0 : AF_DEVERR_DISTRIBUTION;
-      if (good(t) && i < sp.n) {
-        const int x = __ldg(c.draft_ids + sp.first + i);
-        if (x < 0 || x >= c.V) bad |= AF_DEVERR_TARGET_RANGE;
-      }
+      if (good(t) && (x < 0 || x >= c.V)) bad |= AF_DEVERR_TARGET_RANGE;
       if (bad) atomicOr(d_err, bad);
+      ws.draw[r] = Draw{base + i, kind, sp.first + i, x, t.m, q.m};
     }
   }
-  if (!has_row || greedy) return;                             // the whole cluster
-
-  // ---- the token after them, from row base + i
-  const bool rejected = i < sp.n, dense = rejected && c.draft.p != nullptr;
-  const int cut = rejected && !dense ? __ldg(c.draft_ids + sp.first + i) : -1;
-  const T* const p_row = row_of<T>(c.target, base + i);
-  const Q* const q_row = dense ? row_of<Q>(c.draft, sp.first + i) : nullptr;
+  if (kind != kDense) return;
+  const int segments = shape.draw_slices * kDrawWarps;
+  const int lo = segment_at(c.V, slice * kDrawWarps, segments), hi = segment_at(c.V, (slice + 1) * kDrawWarps, segments);
   const Exp64 pe = exp_about(s_power, t.m, inv_tau), qe = exp_about(s_power, q.m, inv_tau);
-  double p_unit = 1.0, q_unit = 1.0;                          // dense: 1 / sums
-  double row_sum = 0.0;                                       // of the target's weights
-  if (dense) {
-    double a = 0.0, b = 0.0;
-    each_pair(p_row, q_row, lo + (int)threadIdx.x, hi, kDrawThreads, [&](int, float z, float zq) { a += pe(z); b += qe(zq); });
-    a = block_sum(a, s_warp);
-    b = block_sum(b, s_warp);
-    if (threadIdx.x == 0) { s_sum[0] = a; s_sum[1] = b; }
-    cluster.sync();
-    double sum_q = 0.0;
-    for (int k = 0; k < ctas; ++k) {
-      row_sum += *cluster.map_shared_rank(&s_sum[0], k);
-      sum_q += *cluster.map_shared_rank(&s_sum[1], k);
-    }
-    p_unit = 1.0 / row_sum;
-    q_unit = 1.0 / sum_q;
+  double a = 0.0, b = 0.0;
+  each_pair(row_of<T>(c.target, base + i), row_of<Q>(c.draft, sp.first + i), lo + (int)threadIdx.x, hi, kDrawThreads,
+            [&](int, float z, float zq) { a += pe(z); b += qe(zq); });
+  a = block_sum<kDrawWarps>(a, s_warp);
+  b = block_sum<kDrawWarps>(b, s_warp);
+  if (threadIdx.x == 0) ws.sums[(int64_t)r * shape.draw_slices + slice] = make_double2(a, b);
+}
+
+// Sums of a request's slices, by a warp, in a fixed order.
+__device__ double2 slices_sum(const Workspace& ws, const Shape& shape, int r) {
+  double2 a = make_double2(0.0, 0.0);
+  for (int k = threadIdx.x & 31; k < shape.draw_slices; k += 32) {
+    const double2 x = ws.sums[(int64_t)r * shape.draw_slices + k];
+    a.x += x.x;
+    a.y += x.y;
   }
-  // a warp's segment of the CTA's share
-  const int seg_lo = lo + (int)((int64_t)(hi - lo) * warp / kDrawWarps), seg_hi = lo + (int)((int64_t)(hi - lo) * (warp + 1) / kDrawWarps);
-  bool plain = !rejected;                                     // drawn from the target itself
-  auto left = [&](float z, float zq) { return fmax(pe(z) * p_unit - qe(zq) * q_unit, 0.0); };      // of p less q
-  double before, total;
-  for (;;) {
-    double a = 0.0, whole = 0.0;
-    if (dense && !plain) each_pair(p_row, q_row, seg_lo + lane, seg_hi, 32, [&](int, float z, float zq) { a += left(z, zq); });
-    else {
-      const auto take = [&](int, float z) { a += pe(z); };
-      const bool cuts = !plain && cut >= seg_lo && cut < seg_hi;
-      each(p_row, seg_lo + lane, cuts ? cut : seg_hi, 32, take);
-      if (cuts) each(p_row, cut + 1 + lane, seg_hi, 32, take);
-      whole = a + (cuts && lane == 0 ? pe(value(p_row + cut)) : 0.0);
-    }
-    if (dense && plain) a *= p_unit;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      a += __shfl_xor_sync(0xffffffffu, a, o);
-      whole += __shfl_xor_sync(0xffffffffu, whole, o);
-    }
-    __syncthreads();
-    if (lane == 0) { s_segment[warp] = a; s_warp[warp] = whole; }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      double run = 0.0, all = 0.0;
-      for (int k = 0; k < kDrawWarps; ++k) {
-        const double x = s_segment[k];
-        s_segment[k] = run;
-        run += x;
-        all += s_warp[k];
-      }
-      s_sum[2] = run;
-      s_sum[3] = all;
-    }
-    cluster.sync();
-    before = total = 0.0;
-    double all = 0.0;
-    for (int k = 0; k < ctas; ++k) {
-      if (k == rank) before = total;
-      total += *cluster.map_shared_rank(&s_sum[2], k);
-      all += *cluster.map_shared_rank(&s_sum[3], k);
-    }
-    cluster.sync();                                           // s_sum is read by all before it is written again, or its CTA ends
-    if (!dense) row_sum = all;
-    if (plain || (dense ? total : total / row_sum) > kResidualFloor) break;
-    plain = true;                                             // next to nothing is left: the target itself
+  for (int o = 16; o > 0; o >>= 1) {
+    a.x += __shfl_xor_sync(0xffffffffu, a.x, o);
+    a.y += __shfl_xor_sync(0xffffffffu, a.y, o);
   }
-  // the CTA whose share holds the first v with C_v > u C, and the segment of it that does
-  const double u = (double)fminf(fmaxf(__ldg(c.u_sample + r), 0.f), 1.f - 0x1p-24f), goal = u * total;
-  if (!(before <= goal && goal < before + s_sum[2])) return;  // the whole CTA
-  int found = 0;
-  for (int k = 1; k < kDrawWarps; ++k)
-    if (before + s_segment[k] <= goal) found = k;
-  const double at_segment = before + s_segment[found];
-  const int f_lo = lo + (int)((int64_t)(hi - lo) * found / kDrawWarps), f_hi = lo + (int)((int64_t)(hi - lo) * (found + 1) / kDrawWarps);
-  auto mass = [&](int v) {
-    if (!plain && v == cut) return 0.0;
-    if (!dense) return pe(value(p_row + v));
-    return plain ? pe(value(p_row + v)) * p_unit : left(value(p_row + v), value(q_row + v));
-  };
-  // all warps share that segment out once more
-  const int part_lo = f_lo + (int)((int64_t)(f_hi - f_lo) * warp / kDrawWarps), part_hi = f_lo + (int)((int64_t)(f_hi - f_lo) * (warp + 1) / kDrawWarps);
-  double a = 0.0;
-#pragma unroll 4
-  for (int v = part_lo + lane; v < part_hi; v += 32) a += mass(v);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-  if (lane == 0) s_warp[warp] = a;
+  return a;
+}
+// The mass of a token in a draw.
+template <class T, class Q>
+struct Mass {
+  const T* p;
+  const Q* q;
+  Exp64 pe, qe;
+  double p_unit, q_unit;                                      // kDense: 1 / sums
+  __device__ __forceinline__ Mass(const VerifyCall& c, const Draw& d, const double2& sums, const double* power, double inv_tau)
+      : p(row_of<T>(c.target, d.row)), q(d.kind == kDense ? row_of<Q>(c.draft, d.draft_row) : nullptr), pe(exp_about(power, d.m, inv_tau)),
+        qe(exp_about(power, d.m_draft, inv_tau)), p_unit(1.0 / sums.x), q_unit(1.0 / sums.y) {}
+  __device__ __forceinline__ double left(float z, float zq) const { return fmax(pe(z) * p_unit - qe(zq) * q_unit, 0.0); }
+};
+
+// A warp per segment: its mass, and what the target has there.
+template <class T, class Q>
+__global__ void __launch_bounds__(kDrawThreads) verify_mass_kernel(const VerifyCall c, const Shape shape, const Workspace ws) {
+  __shared__ double s_power[kPowers];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  set_powers(s_power);
   __syncthreads();
-  double run = at_segment, start = at_segment;
-  int mine = 0;                                               // the last part with mass that starts at or before the goal
-  for (int k = 0; k < kDrawWarps; ++k) {
-    if (run <= goal && s_warp[k] > kNothing) { mine = k; start = run; }
-    run += s_warp[k];
+  wait_for_predecessor();
+  let_successor_start();
+  const int r = (int)blockIdx.x / shape.draw_slices, k = (int)blockIdx.x % shape.draw_slices * kDrawWarps + warp;
+  const Draw d = ws.draw[r];
+  if (d.kind == kNoDraw) return;
+  const Mass<T, Q> mass(c, d, d.kind == kDense ? slices_sum(ws, shape, r) : make_double2(1.0, 1.0), s_power, inverse_temperature(c));
+  const int segments = shape.draw_slices * kDrawWarps, lo = segment_at(c.V, k, segments), hi = segment_at(c.V, k + 1, segments);
+  double a = 0.0, whole = 0.0;
+  if (d.kind == kDense) {
+    each_pair(mass.p, mass.q, lo + lane, hi, 32, [&](int, float z, float zq) { a += mass.left(z, zq); });
+  } else {
+    const auto take = [&](int, float z) { a += mass.pe(z); };
+    const bool cuts = d.kind == kCut && d.cut >= lo && d.cut < hi;
+    each(mass.p, lo + lane, cuts ? d.cut : hi, 32, take);
+    if (cuts) each(mass.p, d.cut + 1 + lane, hi, 32, take);
+    whole = a + (cuts && lane == 0 ? mass.pe(value(mass.p + d.cut)) : 0.0);
   }
-  if (warp != mine) return;
-  run = start;
-  int y = part_lo;                                            // the last with mass, if rounding leaves the goal beyond the part
-  for (int v0 = part_lo; v0 < part_hi; v0 += 32) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    a += __shfl_xor_sync(0xffffffffu, a, o);
+    whole += __shfl_xor_sync(0xffffffffu, whole, o);
+  }
+  if (lane == 0) ws.mass[(int64_t)r * segments + k] = make_double2(a, whole);
+}
+
+// The token: the segment that holds the first v with C_v > u C, a part of it, and the place in that.
+template <class T, class Q>
+__global__ void __launch_bounds__(kFindThreads) verify_find_kernel(const VerifyCall c, const Shape shape, const Workspace ws) {
+  __shared__ double s_power[kPowers], s_warp[kFindWarps], s_upto[kFindThreads];
+  __shared__ double2 s_sums;
+  __shared__ int s_found;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  set_powers(s_power);
+  if (threadIdx.x == 0) s_found = 0;
+  wait_for_predecessor();
+  let_successor_start();
+  const int r = (int)blockIdx.x;
+  const Draw d = ws.draw[r];
+  if (d.kind == kNoDraw) return;
+  if (warp == 0) {
+    const double2 x = d.kind == kDense ? slices_sum(ws, shape, r) : make_double2(1.0, 1.0);
+    if (lane == 0) s_sums = x;
+  }
+  // running sums over the segments
+  const int segments = shape.draw_slices * kDrawWarps, k = threadIdx.x;
+  const double2 mine = k < segments ? ws.mass[(int64_t)r * segments + k] : make_double2(0.0, 0.0);
+  double upto = mine.x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const double x = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 31) s_warp[warp] = upto;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) upto += s_warp[w];
+  s_upto[k] = upto;
+  const double whole = block_sum<kFindWarps>(mine.y, s_warp);           // meets all threads
+  double total = s_upto[kFindThreads - 1];
+  const double row_sum = d.kind == kDense ? s_sums.x : whole;
+  const Mass<T, Q> m(c, d, s_sums, s_power, inverse_temperature(c));
+  // next to nothing is left of a residual: the target itself
+  const bool plain = d.kind == kPlain || !((d.kind == kDense ? total : total / row_sum) > kResidualFloor);
+  auto mass = [&](int v) {
+    if (plain) return m.pe(value(m.p + v));
+    if (d.kind == kDense) return m.left(value(m.p + v), value(m.q + v));
+    return v == d.cut ? 0.0 : m.pe(value(m.p + v));
+  };
+  const double u = (double)fminf(fmaxf(__ldg(c.u_sample + r), 0.f), 1.f - 0x1p-24f);
+  int lo = 0, hi = c.V;
+  double start = 0.0, goal = 0.0;
+  const bool afresh = plain && d.kind != kPlain;              // the segments' mass is of the residual
+  if (!afresh) {
+    goal = u * total;
+    // the last segment with mass that starts at or before the goal
+    if (mine.x > kNothing && (k == 0 ? 0.0 : s_upto[k - 1]) <= goal) atomicMax(&s_found, k);
+    __syncthreads();
+    const int f = s_found;
+    start = f == 0 ? 0.0 : s_upto[f - 1];
+    lo = segment_at(c.V, f, segments);
+    hi = segment_at(c.V, f + 1, segments);
+  }
+  // all warps share the stretch out, and one's part is the next stretch
+  for (bool first = true;; first = false) {
+    const int n = hi - lo;
+    auto part = [&](int w) { return lo + (int)((int64_t)n * w / kFindWarps); };
+    double a = 0.0;
+    const int end = part(warp + 1);
+#pragma unroll 4
+    for (int v = part(warp) + lane; v < end; v += 32) a += mass(v);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+    __syncthreads();
+    if (lane == 0) s_warp[warp] = a;
+    __syncthreads();
+    if (afresh && first) {
+      double all = 0.0;
+      for (int w = 0; w < kFindWarps; ++w) all += s_warp[w];
+      goal = u * all;
+    }
+    double run = start;
+    int found = 0;                                            // the last part with mass that starts at or before the goal
+    for (int w = 0; w < kFindWarps; ++w) {
+      if (run <= goal && s_warp[w] > kNothing) { found = w; start = run; }
+      run += s_warp[w];
+    }
+    const int next_lo = part(found);
+    hi = part(found + 1);
+    lo = next_lo;
+    if (hi - lo <= 128) break;
+  }
+  if (warp != 0) return;
+  int y = lo;                                                 // the last with mass, if rounding leaves the goal beyond the part
+  for (int v0 = lo; v0 < hi; v0 += 32) {
     const int v = v0 + lane;
-    const double w = v < part_hi ? mass(v) : 0.0;
-    double upto = w;                                          // sum over the lanes up to this one
+    const double w = v < hi ? mass(v) : 0.0;
+    double upto_lane = w;                                     // sum over the lanes up to this one
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const double x = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += x;
+      const double x = __shfl_up_sync(0xffffffffu, upto_lane, o);
+      if (lane >= o) upto_lane += x;
     }
-    const unsigned some = __ballot_sync(0xffffffffu, w > kNothing), beyond = __ballot_sync(0xffffffffu, w > kNothing && run + upto > goal);
+    const unsigned some = __ballot_sync(0xffffffffu, w > kNothing), beyond = __ballot_sync(0xffffffffu, w > kNothing && start + upto_lane > goal);
     if (beyond) { y = v0 + __ffs(beyond) - 1; break; }
     if (some) y = v0 + 31 - __clz(some);
-    run += __shfl_sync(0xffffffffu, upto, 31);
+    start += __shfl_sync(0xffffffffu, upto_lane, 31);
   }
   if (lane == 0) {
-    c.token[base + i] = y;
-    if (c.logp) c.logp[base + i] = (float)(((double)load(c.target, base + i, y) - (double)t.m) * inv_tau - log(row_sum));
+    // in the tokens' row of the request's: rows of the target and of the tokens are the same
+    c.token[d.row] = y;
+    if (c.logp) c.logp[d.row] = (float)(((double)value(m.p + y) - (double)d.m) * inverse_temperature(c) - log(row_sum));
   }
 }
 
@@ -576,44 +649,42 @@ __global__ void __launch_bounds__(kDrawThreads, 2) verify_draw_kernel(const Veri
 Shape shape_of(int32_t R, int32_t V, int32_t max_draft, int sm_count) {
   const int64_t units = (int64_t)R * (max_draft + 1), want = ((int64_t)sm_count * 4 + units - 1) / units, most = V / 2048;
   const int64_t slices = want < most ? want : most;
-  return {(int)(slices < 1 ? 1 : slices), max_draft + 1};
+  // a draw's slices: a few to an SM, of 1024 logits at least
+  int64_t draw = ((int64_t)sm_count * 8 + R - 1) / R;
+  if (draw > V / 1024) draw = V / 1024;
+  if (draw > kMostSlices) draw = kMostSlices;
+  return {(int)(slices < 1 ? 1 : slices), max_draft + 1, (int)(draw < 1 ? 1 : draw)};
 }
-// CTAs to a request: as many as a full device has room for.
-int cluster_of(int32_t R, int32_t V, int sm_count) {
-  int ctas = kMostCluster;
-  while (ctas > 1 && ((int64_t)R * ctas > (int64_t)sm_count * (ctas == kMostCluster ? 1 : 8) || V / ctas < 512)) ctas /= 2;
-  return ctas;
-}
-
 template <class T, class Q>
-af_status launch_draws(const cudaLaunchConfig_t& cfg, const VerifyCall& c, const Shape& shape, const Workspace& ws, unsigned int* d_err) {
-  static SmemAttrOnce once;                                   // per device: clusters of more CTAs than every part has to take
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return AF_ERR_CUDA;
-  const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
-  if (!bit || !(once.done.load(std::memory_order_acquire) & bit)) {
-    if (cudaFuncSetAttribute(verify_draw_kernel<T, Q>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return AF_ERR_CUDA;
-    once.done.fetch_or(bit, std::memory_order_release);
-  }
-  return cudaLaunchKernelEx(&cfg, verify_draw_kernel<T, Q>, c, shape, ws, d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
+af_status launch_draws(const VerifyCall& c, Shape shape, const Workspace& ws, unsigned int* d_err, cudaStream_t s) {
+  const bool greedy = c.temperature == 0.f;
+  if (greedy) shape.draw_slices = 1;
+  const unsigned slices = (unsigned)c.R * shape.draw_slices;
+  if (launch_overlapped(verify_sums_kernel<T, Q>, slices, kDrawThreads, 0, s, c, shape, ws, d_err) != cudaSuccess) return AF_ERR_CUDA;
+  if (greedy) return AF_OK;
+  if (launch_overlapped(verify_mass_kernel<T, Q>, slices, kDrawThreads, 0, s, c, shape, ws) != cudaSuccess) return AF_ERR_CUDA;
+  return launch_overlapped(verify_find_kernel<T, Q>, (unsigned)c.R, kFindThreads, 0, s, c, shape, ws) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
 }
 
 size_t round16(size_t n) { return (n + 15) & ~(size_t)15; }
-struct Sizes { size_t parts, rows, verdicts, tickets, stops; };
+struct Sizes { size_t parts, rows, draws, sums, mass, verdicts, tickets, stops; };
 // Rows in several slices are few: fewer than 8 parts per SM in all, and as many of the drafts; and parts and tickets are used
-// only there.  So smaller calls of any kind fit in what a larger one needs.
+// only there.  A draw's slices are 8 per SM and one per request at most.  So smaller calls of any kind fit in what a larger one
+// needs.
 Sizes sizes_of(int32_t R, int32_t max_draft, int sm_count) {
-  const size_t units = (size_t)R * ((size_t)max_draft + 1);
-  return {(size_t)sm_count * 16 * sizeof(RowPart), units * 2 * sizeof(Row), units * sizeof(int32_t),
-          round16((size_t)sm_count * 4 * sizeof(unsigned int)), (size_t)R * sizeof(int)};
+  const size_t units = (size_t)R * ((size_t)max_draft + 1), slices = (size_t)sm_count * 8 + R;
+  return {(size_t)sm_count * 16 * sizeof(RowPart), units * 2 * sizeof(Row), (size_t)R * sizeof(Draw), slices * sizeof(double2),
+          slices * kDrawWarps * sizeof(double2), units * sizeof(int32_t), round16((size_t)sm_count * 4 * sizeof(unsigned int)),
+          (size_t)R * sizeof(int)};
 }
+static_assert(sizeof(Draw) % 16 == 0 && sizeof(Row) % 16 == 0, "what lies behind them is aligned");
 
 }  // namespace
 
 // Sizes the workspace; what a call leaves as it found it, the tickets and the stops, is set where the memory is new.
 af_status reserve_draft_verify(af_ctx* ctx, int32_t R, int32_t max_draft, cudaStream_t s) {
   const Sizes z = sizes_of(R, max_draft, ctx->sm_count);
-  af_status st = ws_grow(ctx->verify_ws, z.parts + z.rows + z.verdicts);
+  af_status st = ws_grow(ctx->verify_ws, z.parts + z.rows + z.draws + z.sums + z.mass + z.verdicts);
   if (st != AF_OK) return st;
   const size_t had = ctx->verify_state.cap;
   st = ws_grow(ctx->verify_state, z.tickets + z.stops);
@@ -633,35 +704,26 @@ af_status launch_draft_verify(af_ctx* ctx, const VerifyCall& c, cudaStream_t s) 
   const Shape shape = shape_of(c.R, c.V, c.max_draft, ctx->sm_count);
   Workspace ws;
   const Sizes z = sizes_of(c.R, c.max_draft, ctx->sm_count);
-  char* const at = static_cast<char*>(ctx->verify_ws.p);
-  ws.target = reinterpret_cast<RowPart*>(at);
+  char* at = static_cast<char*>(ctx->verify_ws.p);
+  auto take = [&](size_t bytes) { char* const p = at; at += bytes; return p; };
+  ws.target = reinterpret_cast<RowPart*>(take(z.parts));
   ws.draft = ws.target + (size_t)c.R * shape.positions * shape.slices;
-  ws.target_row = reinterpret_cast<Row*>(at + z.parts);
+  ws.target_row = reinterpret_cast<Row*>(take(z.rows));
   ws.draft_row = ws.target_row + (size_t)c.R * shape.positions;
-  ws.verdict = reinterpret_cast<int32_t*>(at + z.parts + z.rows);
+  ws.draw = reinterpret_cast<Draw*>(take(z.draws));
+  ws.sums = reinterpret_cast<double2*>(take(z.sums));
+  ws.mass = reinterpret_cast<double2*>(take(z.mass));
+  ws.verdict = reinterpret_cast<int32_t*>(take(z.verdicts));
   ws.ticket = static_cast<unsigned int*>(ctx->verify_state.p);
   ws.stop = reinterpret_cast<int*>(static_cast<char*>(ctx->verify_state.p) + z.tickets);
   const float scale = c.temperature == 0.f ? kLog2e : kLog2e / c.temperature;
   const int64_t blocks = (int64_t)c.R * shape.positions * shape.slices;
   if (launch_overlapped(verify_rows_kernel, (unsigned)blocks, kRowThreads, 0, s, c, shape, scale, ws) != cudaSuccess) return AF_ERR_CUDA;
-  const int ctas = c.temperature == 0.f ? 1 : cluster_of(c.R, c.V, ctx->sm_count);
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = (unsigned)c.R * ctas;
-  cfg.blockDim = kDrawThreads;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2]{};
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = ctas;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
   const bool wide_draft = !c.draft.p || c.draft.type == AF_F32;
   using bf16 = __nv_bfloat16;
   if (c.target.type == AF_F32)
-    return wide_draft ? launch_draws<float, float>(cfg, c, shape, ws, ctx->d_err) : launch_draws<float, bf16>(cfg, c, shape, ws, ctx->d_err);
-  return wide_draft ? launch_draws<bf16, float>(cfg, c, shape, ws, ctx->d_err) : launch_draws<bf16, bf16>(cfg, c, shape, ws, ctx->d_err);
+    return wide_draft ? launch_draws<float, float>(c, shape, ws, ctx->d_err, s) : launch_draws<float, bf16>(c, shape, ws, ctx->d_err, s);
+  return wide_draft ? launch_draws<bf16, float>(c, shape, ws, ctx->d_err, s) : launch_draws<bf16, bf16>(c, shape, ws, ctx->d_err, s);
 }
 
 }  // namespace af
