@@ -190,36 +190,28 @@ __device__ __forceinline__ void join_warp(RowPart& a, float scale) {
 
 __device__ __forceinline__ bool good(const Row& x) { return fabsf(x.m) < INFINITY && x.s > 0.0 && x.s < 1e300; }
 // Called by a whole warp.
-__device__ Row warp_row(const RowPart* parts, int slices, double inv_tau) {
+__device__ __forceinline__ RowPart warp_part(const RowPart* parts, int slices) {
+  RowPart a{kNoMax, 0.f, kGoesOn, 0};
   const int lane = threadIdx.x & 31;
-  Row x{kNoMax, kGoesOn, 0.0};
-  for (int i = lane; i < slices; i += 32) {
-    const float m = __ldcg(&parts[i].m);
-    const int32_t at = __ldcg(&parts[i].at);
-    if (m > x.m || (m == x.m && at < x.at)) { x.m = m; x.at = at; }
+  if (lane < slices) {
+    const uint4 x = __ldcg(reinterpret_cast<const uint4*>(parts) + lane);
+    a = RowPart{__uint_as_float(x.x), __uint_as_float(x.y), (int32_t)x.z, 0};
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float m = __shfl_xor_sync(0xffffffffu, x.m, o);
-    const int32_t at = __shfl_xor_sync(0xffffffffu, x.at, o);
-    if (m > x.m || (m == x.m && at < x.at)) { x.m = m; x.at = at; }
+  return a;
+}
+__device__ __forceinline__ void join_slices(RowPart& a, const RowPart* parts, int slices, float scale) {
+  for (int i = (threadIdx.x & 31) + 32; i < slices; i += 32) {
+    const uint4 x = __ldcg(reinterpret_cast<const uint4*>(parts) + i);
+    a = join(a, RowPart{__uint_as_float(x.x), __uint_as_float(x.y), (int32_t)x.z, 0}, scale);
   }
-  for (int i = lane; i < slices; i += 32) {
-    const float m = __ldcg(&parts[i].m), s = __ldcg(&parts[i].s);
-    if (s != 0.f) x.s += m == x.m ? (double)s : (double)s * exp(((double)m - (double)x.m) * inv_tau);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x.s += __shfl_xor_sync(0xffffffffu, x.s, o);
-  return x;
+  join_warp(a, scale);
 }
 
 // u q(x) and p(x), both times both sums: x passes iff left < right.
 struct Sides { double left, right; };
-__device__ __forceinline__ Sides sides_of(const VerifyCall& c, const Row& t, const Row& q, int64_t row, int draft_row, int x, double inv_tau) {
-  const double u = (double)__ldg(c.u_accept + draft_row);
-  const double pw = exp(((double)load(c.target, row, x) - (double)t.m) * inv_tau);
-  const double qw = c.draft.p ? exp(((double)load(c.draft, draft_row, x) - (double)q.m) * inv_tau) : 1.0;
-  return {u * qw * t.s, pw * (c.draft.p ? q.s : 1.0)};
+__device__ __forceinline__ Sides sides_of(const Row& t, const Row& q, float u, float z, float zq, bool dense, double inv_tau) {
+  const double pw = exp(((double)z - (double)t.m) * inv_tau), qw = dense ? exp(((double)zq - (double)q.m) * inv_tau) : 1.0;
+  return {(double)u * qw * t.s, pw * (dense ? q.s : 1.0)};
 }
 __device__ __forceinline__ bool too_near(const Sides& e) { return fabs(e.left - e.right) <= 1e-5 * fabs(e.right); }
 
@@ -244,9 +236,20 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
   const int64_t row = sp.first + r + i;
   const int k = sp.first + i;                      // the draft's row
   const bool greedy = c.temperature == 0.f, dense = c.draft.p && i < sp.n;
+  // what the verdict will need, asked for early
+  int x = 0;
+  float u_x = 0.f, z_x = 0.f, zq_x = 0.f;
+  if (threadIdx.x == 0 && i < sp.n) {
+    x = __ldg(c.draft_ids + k);
+    if (!greedy) u_x = __ldg(c.u_accept + k);
+  }
   RowPart t = greedy ? thread_part<true>(c.target, row, lo, hi, scale) : thread_part<false>(c.target, row, lo, hi, scale);
   RowPart d{kNoMax, 0.f, kGoesOn, 0};
   if (dense) d = thread_part<false>(c.draft, k, lo, hi, scale);
+  if (threadIdx.x == 0 && i < sp.n && x >= 0 && x < c.V) {
+    z_x = load(c.target, row, x);
+    if (dense) zq_x = load(c.draft, k, x);
+  }
   join_warp(t, scale);
   if (dense) join_warp(d, scale);
   if ((threadIdx.x & 31) == 0) { warp_parts[0][threadIdx.x >> 5] = t; warp_parts[1][threadIdx.x >> 5] = d; }
@@ -259,7 +262,6 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
   if (dense) join_warp(d, scale);
   // whoever has the last slice puts the row together
   const double inv_tau = greedy ? 1.0 : 1.0 / (double)c.temperature;
-  Row tr{t.m, t.at, (double)t.s}, dr{d.m, d.at, (double)d.s};
   if (shape.slices > 1) {
     RowPart* const t_at = ws.target + (int64_t)unit * shape.slices;
     RowPart* const d_at = ws.draft + (int64_t)unit * shape.slices;
@@ -273,21 +275,23 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
     last = __shfl_sync(0xffffffffu, last, 0);
     if (!last) return;
     __threadfence();
-    tr = warp_row(t_at, shape.slices, inv_tau);
-    if (dense) dr = warp_row(d_at, shape.slices, inv_tau);
+    t = warp_part(t_at, shape.slices);
+    if (dense) d = warp_part(d_at, shape.slices);
+    join_slices(t, t_at, shape.slices, scale);
+    if (dense) join_slices(d, d_at, shape.slices, scale);
   }
+  const Row tr{t.m, t.at, (double)t.s}, dr{d.m, d.at, (double)d.s};
   if (threadIdx.x != 0) return;
   ws.target_row[unit] = tr;
   if (i == sp.n) return;
   if (dense) ws.draft_row[unit] = dr;
   // if the draft surely does not pass, later rows of the request need not be read
-  const int x = __ldg(c.draft_ids + k);
   Verdict v = kFails;                              // an id outside the vocabulary does
   if (!good(tr) || (dense && !good(dr))) v = kNoRow;
   else if (x >= 0 && x < c.V) {
     if (greedy) v = x == tr.at ? kPasses : kFails;
     else {
-      const Sides e = sides_of(c, tr, dr, row, k, x, inv_tau);
+      const Sides e = sides_of(tr, dr, u_x, z_x, zq_x, dense, inv_tau);
       v = too_near(e) ? kTooNear : e.left < e.right ? kPasses : kFails;
     }
   }
@@ -297,6 +301,23 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
 
 // --------------------------------------------------------------------------------- draws, in 64 bits
 constexpr int kPowers = 64;
+__constant__ double kPower[kPowers] = {          // 2^(j / 64), rounded to nearest
+    0x1.0000000000000p+0, 0x1.02c9a3e778061p+0, 0x1.059b0d3158574p+0, 0x1.0874518759bc8p+0,
+    0x1.0b5586cf9890fp+0, 0x1.0e3ec32d3d1a2p+0, 0x1.11301d0125b51p+0, 0x1.1429aaea92de0p+0,
+    0x1.172b83c7d517bp+0, 0x1.1a35beb6fcb75p+0, 0x1.1d4873168b9aap+0, 0x1.2063b88628cd6p+0,
+    0x1.2387a6e756238p+0, 0x1.26b4565e27cddp+0, 0x1.29e9df51fdee1p+0, 0x1.2d285a6e4030bp+0,
+    0x1.306fe0a31b715p+0, 0x1.33c08b26416ffp+0, 0x1.371a7373aa9cbp+0, 0x1.3a7db34e59ff7p+0,
+    0x1.3dea64c123422p+0, 0x1.4160a21f72e2ap+0, 0x1.44e086061892dp+0, 0x1.486a2b5c13cd0p+0,
+    0x1.4bfdad5362a27p+0, 0x1.4f9b2769d2ca7p+0, 0x1.5342b569d4f82p+0, 0x1.56f4736b527dap+0,
+    0x1.5ab07dd485429p+0, 0x1.5e76f15ad2148p+0, 0x1.6247eb03a5585p+0, 0x1.6623882552225p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.6dfb23c651a2fp+0, 0x1.71f75e8ec5f74p+0, 0x1.75feb564267c9p+0,
+    0x1.7a11473eb0187p+0, 0x1.7e2f336cf4e62p+0, 0x1.82589994cce13p+0, 0x1.868d99b4492edp+0,
+    0x1.8ace5422aa0dbp+0, 0x1.8f1ae99157736p+0, 0x1.93737b0cdc5e5p+0, 0x1.97d829fde4e50p+0,
+    0x1.9c49182a3f090p+0, 0x1.a0c667b5de565p+0, 0x1.a5503b23e255dp+0, 0x1.a9e6b5579fdbfp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b33a2b84f15fbp+0, 0x1.b7f76f2fb5e47p+0, 0x1.bcc1e904bc1d2p+0,
+    0x1.c199bdd85529cp+0, 0x1.c67f12e57d14bp+0, 0x1.cb720dcef9069p+0, 0x1.d072d4a07897cp+0,
+    0x1.d5818dcfba487p+0, 0x1.da9e603db3285p+0, 0x1.dfc97337b9b5fp+0, 0x1.e502ee78b3ff6p+0,
+    0x1.ea4afa2a490dap+0, 0x1.efa1bee615a27p+0, 0x1.f50765b6e4540p+0, 0x1.fa7c1819e90d8p+0};
 // 2^((z - m) / tau log2 e), relative to within 2^-44, and 2^-1000 from there down: what is no more than kNothing is no mass.
 constexpr double kNothing = 0x1p-900;
 struct Exp64 {
@@ -386,7 +407,7 @@ __device__ __forceinline__ Row dense_of(const Workspace& ws, const VerifyCall& c
 __device__ __forceinline__ int segment_at(int V, int k, int n) { return (int)((int64_t)V * k / n); }
 __device__ __forceinline__ double inverse_temperature(const VerifyCall& c) { return c.temperature == 0.f ? 1.0 : 1.0 / (double)c.temperature; }
 __device__ __forceinline__ void set_powers(double* power) {
-  if (threadIdx.x < kPowers) power[threadIdx.x] = exp2((double)threadIdx.x / kPowers);
+  if (threadIdx.x < kPowers) power[threadIdx.x] = kPower[threadIdx.x];
 }
 
 // What passes, and how the token after it is drawn.  Every CTA of a request finds out by itself; the first writes it down.
@@ -434,7 +455,9 @@ __global__ void __launch_bounds__(kDrawThreads) verify_sums_kernel(const VerifyC
     Row t = ws.target_row[unit(i)], q = dense_of(ws, c, unit(i));        // the same in all threads of the request
     t.s = exact_sum(row_of<T>(c.target, base + i), 0, c.V, exp_about(s_power, t.m, inv_tau), s_warp);
     if (c.draft.p) q.s = exact_sum(row_of<Q>(c.draft, sp.first + i), 0, c.V, exp_about(s_power, q.m, inv_tau), s_warp);
-    const Sides e = sides_of(c, t, q, base + i, sp.first + i, __ldg(c.draft_ids + sp.first + i), inv_tau);
+    const int x = __ldg(c.draft_ids + sp.first + i);
+    const Sides e = sides_of(t, q, __ldg(c.u_accept + sp.first + i), load(c.target, base + i, x),
+                             c.draft.p ? load(c.draft, sp.first + i, x) : 0.f, c.draft.p != nullptr, inv_tau);
     if (!(e.left < e.right)) break;
     ++i;                                                      // it passes; go on behind it
     __syncthreads();                                          // s_first has been read
