@@ -236,20 +236,9 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
   const int64_t row = sp.first + r + i;
   const int k = sp.first + i;                      // the draft's row
   const bool greedy = c.temperature == 0.f, dense = c.draft.p && i < sp.n;
-  // what the verdict will need, asked for early
-  int x = 0;
-  float u_x = 0.f, z_x = 0.f, zq_x = 0.f;
-  if (threadIdx.x == 0 && i < sp.n) {
-    x = __ldg(c.draft_ids + k);
-    if (!greedy) u_x = __ldg(c.u_accept + k);
-  }
   RowPart t = greedy ? thread_part<true>(c.target, row, lo, hi, scale) : thread_part<false>(c.target, row, lo, hi, scale);
   RowPart d{kNoMax, 0.f, kGoesOn, 0};
   if (dense) d = thread_part<false>(c.draft, k, lo, hi, scale);
-  if (threadIdx.x == 0 && i < sp.n && x >= 0 && x < c.V) {
-    z_x = load(c.target, row, x);
-    if (dense) zq_x = load(c.draft, k, x);
-  }
   join_warp(t, scale);
   if (dense) join_warp(d, scale);
   if ((threadIdx.x & 31) == 0) { warp_parts[0][threadIdx.x >> 5] = t; warp_parts[1][threadIdx.x >> 5] = d; }
@@ -286,12 +275,13 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
   if (i == sp.n) return;
   if (dense) ws.draft_row[unit] = dr;
   // if the draft surely does not pass, later rows of the request need not be read
+  const int x = __ldg(c.draft_ids + k);
   Verdict v = kFails;                              // an id outside the vocabulary does
   if (!good(tr) || (dense && !good(dr))) v = kNoRow;
   else if (x >= 0 && x < c.V) {
     if (greedy) v = x == tr.at ? kPasses : kFails;
     else {
-      const Sides e = sides_of(tr, dr, u_x, z_x, zq_x, dense, inv_tau);
+      const Sides e = sides_of(tr, dr, __ldg(c.u_accept + k), load(c.target, row, x), dense ? load(c.draft, k, x) : 0.f, dense, inv_tau);
       v = too_near(e) ? kTooNear : e.left < e.right ? kPasses : kFails;
     }
   }
@@ -407,7 +397,7 @@ __device__ __forceinline__ Row dense_of(const Workspace& ws, const VerifyCall& c
 __device__ __forceinline__ int segment_at(int V, int k, int n) { return (int)((int64_t)V * k / n); }
 __device__ __forceinline__ double inverse_temperature(const VerifyCall& c) { return c.temperature == 0.f ? 1.0 : 1.0 / (double)c.temperature; }
 __device__ __forceinline__ void set_powers(double* power) {
-  if (threadIdx.x < kPowers) power[threadIdx.x] = kPower[threadIdx.x];
+  if (threadIdx.x < kPowers) power[threadIdx.x] = exp2((double)threadIdx.x / kPowers);
 }
 
 // What passes, and how the token after it is drawn.  Every CTA of a request finds out by itself; the first writes it down.
