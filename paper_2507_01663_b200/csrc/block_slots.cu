@@ -87,6 +87,27 @@ struct BlockSize {
 };
 __device__ __forceinline__ int32_t clamped(int64_t x) { return (int32_t)(x < kMost ? x : kMost); }
 
+// x[at .. at + kEach) of n, 0 behind the end; four at a time where the address allows it.
+template <int kEach>
+__device__ __forceinline__ void get(const int32_t* x, int at, int n, int32_t (&out)[kEach]) {
+  if (kEach == 4 && at + 4 <= n && (reinterpret_cast<uintptr_t>(x) & 15) == 0) {
+    *reinterpret_cast<int4*>(out) = *reinterpret_cast<const int4*>(x + at);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) out[k] = at + k < n ? x[at + k] : 0;
+  }
+}
+template <int kEach>
+__device__ __forceinline__ void put(int32_t* x, int at, int n, const int32_t (&in)[kEach]) {
+  if (kEach == 4 && at + 4 <= n && (reinterpret_cast<uintptr_t>(x) & 15) == 0) {
+    *reinterpret_cast<int4*>(x + at) = *reinterpret_cast<const int4*>(in);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (at + k < n) x[at + k] = in[k];
+  }
+}
+
 struct Wish { int32_t tokens, held, need, length; bool valid; };
 
 // cu (nullable): also receives the running token sums, R + 1 of them.  Every thread of the CTA calls it; what it writes to shared
@@ -101,17 +122,16 @@ __device__ __forceinline__ Totals make_plan(const SlotsCall& c, const Plan& plan
   unsigned int bad = 0;
   Wish w[kEach];
   auto wishes = [&](int r0) {
-    int32_t grow[kEach];
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {                        // every load before any use
-      const int r = r0 + (int)threadIdx.x * kEach + k;
-      w[k].length = r < c.R ? c.length[r] : 0;
-      w[k].held = r < c.R ? c.held[r] : 0;
-      grow[k] = r < c.R ? c.grow[r] : 0;
-    }
+    alignas(16) int32_t length[kEach], held[kEach], grow[kEach];
+    const int r = r0 + (int)threadIdx.x * kEach;
+    get(c.length, r, c.R, length);
+    get(c.held, r, c.R, held);
+    get(c.grow, r, c.R, grow);
     Sums mine{0, 0, 0};
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
+      w[k].length = length[k];
+      w[k].held = held[k];
       const int64_t end = (int64_t)w[k].length + grow[k];
       w[k].tokens = grow[k] > 0 ? grow[k] : 0;
       w[k].valid = w[k].length >= 0 && grow[k] >= 0 && w[k].held >= 0 && w[k].held <= c.max_blocks && end <= kMost && end <= room;
@@ -142,25 +162,30 @@ __device__ __forceinline__ Totals make_plan(const SlotsCall& c, const Plan& plan
     }
     Sums here = before + at;
     before = before + all;
+    const int r = r0 + (int)threadIdx.x * kEach;
+    alignas(16) int32_t given_at[kEach], wanted_at[kEach], held_out[kEach], granted[kEach], first[kEach];
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-      const int r = r0 + (int)threadIdx.x * kEach + k;
-      if (r >= c.R) break;
       const int64_t more = (int64_t)w[k].need - w[k].held;
-      const bool granted = w[k].valid && (more <= 0 || here.wanted + more <= available);
+      const bool yes = w[k].valid && (more <= 0 || here.wanted + more <= available);
       if (!w[k].valid) bad |= AF_DEVERR_REQUEST;
-      else if (!granted) bad |= AF_DEVERR_BLOCKS;
-      plan.request[r] = Request{w[k].held, w[k].need, granted ? w[k].length : -1, clamped(here.wanted)};
-      plan.given_at[r] = clamped(here.given);
-      plan.wanted_at[r] = clamped(here.wanted);
-      c.held_out[r] = granted ? w[k].need : w[k].held;
-      if (c.granted) c.granted[r] = granted;
-      c.cu[r] = clamped(here.tokens);
-      if (cu) cu[r] = clamped(here.tokens);
+      else if (!yes) bad |= AF_DEVERR_BLOCKS;
+      given_at[k] = clamped(here.given);
+      wanted_at[k] = clamped(here.wanted);
+      held_out[k] = yes ? w[k].need : w[k].held;
+      granted[k] = yes;
+      first[k] = clamped(here.tokens);
+      if (r + k < c.R) plan.request[r + k] = Request{w[k].held, w[k].need, yes ? w[k].length : -1, wanted_at[k]};
       // granted requests come first among those that want blocks: what they take is the largest of their ends
-      if (granted && more > 0) taken = (unsigned int)(here.wanted + more);
+      if (yes && more > 0) taken = (unsigned int)(here.wanted + more);
       here = here + Sums{w[k].tokens, more < 0 ? -more : 0, more > 0 ? more : 0};
     }
+    put(plan.given_at, r, c.R, given_at);
+    put(plan.wanted_at, r, c.R, wanted_at);
+    put(c.held_out, r, c.R, held_out);
+    if (c.granted) put(c.granted, r, c.R, granted);
+    put(c.cu, r, c.R, first);
+    if (cu) put(cu, r, c.R, first);
   }
   __syncthreads();                                           // most is 0
   taken = __reduce_max_sync(0xffffffffu, taken);
@@ -364,7 +389,7 @@ __global__ void __launch_bounds__(kTokenThreads) slots_carry_out_kernel(const Sl
 
 }  // namespace
 
-size_t slots_workspace_bytes(int32_t R) { return (sizeof(Totals) + 15) / 16 * 16 + (size_t)R * (sizeof(Request) + 2 * sizeof(int32_t)) + 16; }
+size_t slots_workspace_bytes(int32_t R) { return (sizeof(Totals) + 15) / 16 * 16 + (size_t)R * (sizeof(Request) + 2 * sizeof(int32_t)) + 32; }
 
 af_status launch_block_slots(af_ctx* ctx, const SlotsCall& c, cudaStream_t s) {
   // a CTA's work grows with the tokens: 64 requests of 5 tokens take X us this way and Y in two launches, 2048 of 8 tokens Z and W
@@ -379,7 +404,7 @@ af_status launch_block_slots(af_ctx* ctx, const SlotsCall& c, cudaStream_t s) {
   plan.totals = static_cast<Totals*>(ctx->slots_ws.p);
   plan.request = reinterpret_cast<Request*>(static_cast<char*>(ctx->slots_ws.p) + (sizeof(Totals) + 15) / 16 * 16);
   plan.given_at = reinterpret_cast<int32_t*>(plan.request + c.R);
-  plan.wanted_at = plan.given_at + c.R;
+  plan.wanted_at = plan.given_at + (c.R + 3) / 4 * 4;
   if (launch_overlapped(slots_plan_kernel, 1, kPlanThreads, 0, s, c, plan, ctx->d_err) != cudaSuccess) return AF_ERR_CUDA;
   int64_t tiles = (c.capacity + kTokenTile - 1) / kTokenTile;
   const int64_t most = (int64_t)ctx->sm_count * 6, least = (c.R + 63) / 64 < ctx->sm_count ? (c.R + 63) / 64 : ctx->sm_count;
