@@ -33,7 +33,8 @@ struct Plan {
 };
 constexpr int kPlanThreads = 1024, kPlanEach = 4;            // of a larger batch: threads, neighbouring requests of each
 constexpr int kStepThreads = 1024;                           // of a step, each with one request
-constexpr int kFewThreads = 256;                             // of a step of 256 requests at most
+constexpr int kFewThreads = 256;                             // of a smaller one
+constexpr int kFewTokens = 512, kStepTokens = 8192;          // of a step, at most
 constexpr int kTokenThreads = 256, kTokenEach = 8, kTokenTile = kTokenThreads * kTokenEach;
 constexpr int kCached = 1024;                                // running token sums that a tile keeps in shared memory
 constexpr int kMarks = 4096;                                 // running block sums that it keeps there, evenly apart
@@ -392,10 +393,12 @@ __global__ void __launch_bounds__(kTokenThreads) slots_carry_out_kernel(const Sl
 size_t slots_workspace_bytes(int32_t R) { return (sizeof(Totals) + 15) / 16 * 16 + (size_t)R * (sizeof(Request) + 2 * sizeof(int32_t)) + 32; }
 
 af_status launch_block_slots(af_ctx* ctx, const SlotsCall& c, cudaStream_t s) {
-  // a CTA's work grows with the tokens: 64 requests of 5 tokens take X us this way and Y in two launches, 2048 of 8 tokens Z and W
-  if (c.R <= kFewThreads && c.capacity <= 4096)
+  // One CTA, whose work grows with the tokens, or two launches of about 12 us together.  On the device, 256 threads / 1024 / two
+  // launches: 64 requests of 5 tokens 4.0 / 4.9 / 14.2 us, of 16 5.2 / 4.9 / 12.1; 256 of 32 28.5 / 12.7 / 12.3; 1024 of 1
+  // - / 5.9 / 15.7, of 8 - / 14.2 / 13.1, of 16 - / 23.5 / 12.9.
+  if (c.R <= kFewThreads && c.capacity <= kFewTokens)
     return launch_overlapped(slots_step_kernel<kFewThreads>, 1, kFewThreads, 0, s, c, ctx->d_err) == cudaSuccess ? AF_OK : AF_ERR_CUDA;
-  if (c.R <= kStepThreads && c.capacity <= 16384)
+  if (c.R <= kStepThreads && c.capacity <= kStepTokens)
     return launch_overlapped(slots_step_kernel<kStepThreads>, 1, kStepThreads, 0, s, c, ctx->d_err) == cudaSuccess ? AF_OK
                                                                                                                     : AF_ERR_CUDA;
   const af_status st = ws_grow(ctx->slots_ws, slots_workspace_bytes(c.R));
