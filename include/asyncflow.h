@@ -539,10 +539,10 @@ af_status af_reserve_preference(af_ctx* ctx, int64_t max_T, int32_t max_B);
  * af_quantize_head are).  A NaN in a scale or in a hidden row stays in its vocabulary row or token.
  * 0 <= T <= AF_MAX_QUANT_TOKENS; meant for few: it costs one pass over the codes per 64 tokens.
  *
- * W, hidden, values bf16 dev; d % 32 == 0; matrices contiguous (but for the logits' pitch) and 16-byte aligned, logits aligned
+ * W, hidden, values bf16 dev; V <= 2^30, d % 32 == 0; matrices contiguous (but for the logits' pitch) and 16-byte aligned, logits aligned
  * to their type.  No workspace.
  * Errors: AF_ERR_INVALID_ARG for null pointers, sizes below 1, another group size or type; AF_ERR_ALIGNMENT; AF_ERR_SHAPE for
- * T out of range or a pitch below V.
+ * T or V out of range or a pitch below V.
  * ------------------------------------------------------------------------------------------- */
 #define AF_MAX_QUANT_TOKENS 65536
 af_status af_quantize_head(af_ctx* ctx, const void* W, int32_t V, int32_t d, int32_t group, void* codes, void* scale,
@@ -574,11 +574,12 @@ af_status af_quant_logits(af_ctx* ctx, const void* hidden, const void* codes, co
  * such a cu_draft share hold one's or the other's results.)
  *
  * Comparisons and draws are made from sums in 64 bits where 32 could decide otherwise; log-probs of passed drafts are within
- * 1e-6 of 64 bits, that of y is rounded once.
+ * 1e-6 of 64 bits, that of y is rounded once.  In a draw weights below 2^-900 of the row's largest are nothing.
  * target_logits [D + R, V], draft_logits [D, V]: fp32 or bf16 dev, row pitch in elements (>= V), aligned to their type.  draft [D],
  * cu_draft [R+1], token [D + R], n_emitted [R] int32, logp (nullable) [D + R] fp32, dev.  0 <= max_draft <= AF_MAX_DRAFT,
  * 0 <= R, R * (max_draft + 1) <= 2^24, 0 <= D <= R * max_draft, temperature 0 or from 1e-4 to 1e4.
- * Workspace: 36 bytes per request and position (max_draft + 1 of them) and 4 per request, 40 KB beside; af_reserve_rollout sizes
+ * 1 <= V <= 2^30.
+ * Workspace: 36 bytes per request and position (max_draft + 1 of them), 180 per request, 210 KB beside; af_reserve_rollout sizes
  * it ahead, for smaller batches too.
  * ------------------------------------------------------------------------------------------- */
 #define AF_MAX_DRAFT 1023
@@ -613,7 +614,7 @@ af_status af_draft_verify(af_ctx* ctx, const void* target_logits, int32_t target
  *
  * length, grow, held, held_out, granted [R], free_count, free_count_out [1], cu_new [R+1], position [token_capacity] int32;
  * block_table [R, max_blocks] int32 with table_pitch >= max_blocks elements from row to row; free_blocks [n_blocks] int32; slot
- * [token_capacity] int64; all dev.  0 <= R <= 2^20, block_size >= 1.  Workspace: 32 bytes per request (af_reserve_rollout).
+ * [token_capacity] int64; all dev.  0 <= R <= 2^20, block_size >= 1.  Workspace: 24 bytes per request (af_reserve_rollout).
  * Errors: AF_ERR_INVALID_ARG for null pointers and negative sizes, AF_ERR_SHAPE for R out of range or a pitch below max_blocks.
  * ------------------------------------------------------------------------------------------- */
 af_status af_block_slots(af_ctx* ctx, const int32_t* length, const int32_t* grow, const int32_t* held, int32_t R,

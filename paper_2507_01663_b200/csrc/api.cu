@@ -676,6 +676,7 @@ af_status af_reserve_preference(af_ctx* c, int64_t max_T, int32_t max_B) {
 static af_status quant_head_sizes(int32_t V, int32_t d, int32_t group) {
   if (V < 1 || d < 1) return AF_ERR_INVALID_ARG;
   if (group != 32 && group != 64 && group != 128) return AF_ERR_INVALID_ARG;
+  if (V > (1 << 30)) return AF_ERR_SHAPE;                   // rows, and tiles past the last one, are 32-bit numbers
   return d % 32 != 0 ? AF_ERR_ALIGNMENT : AF_OK;
 }
 
@@ -708,6 +709,7 @@ af_status af_quant_logits(af_ctx* c, const void* hidden, const void* codes, cons
 
 static af_status verify_sizes(int32_t R, int32_t D, int32_t V, int32_t max_draft) {
   if (R < 0 || D < 0 || V < 1 || max_draft < 0) return AF_ERR_INVALID_ARG;
+  if (V > (1 << 30)) return AF_ERR_SHAPE;                   // places of logits, and steps past them, are 32-bit numbers
   if (max_draft > AF_MAX_DRAFT || (int64_t)R * (max_draft + 1) > (1 << 24) || (int64_t)D > (int64_t)R * max_draft) return AF_ERR_SHAPE;
   return AF_OK;
 }

@@ -247,3 +247,13 @@ def test_after_a_reservation_any_smaller_batch(ctx):
         check_verify(ctx, verify_case(90 + turn, R, most, V, "dense" if turn & 1 else "lookup"), max_draft=most)
         check_blocks(ctx, blocks_case(turn, R, 16, 4, 3 * R))
         assert ctx.workspace_bytes() == reserved
+
+
+def test_vocabularies_past_2_30_are_refused(ctx):
+    """Before anything is read: the pointers are of one small buffer."""
+    from paper_2507_01663_b200 import binding as B
+    p, V = torch.zeros(64, device=device()).data_ptr(), (1 << 30) + 1
+    shape = next(k for k, name in B.STATUS_NAMES.items() if name == "AF_ERR_SHAPE")
+    assert ctx.lib.af_quantize_head(ctx.handle, p, V, 32, 32, p, p, None, None) == shape
+    assert ctx.lib.af_quant_logits(ctx.handle, p, p, p, 1, 32, V, 32, p, B.F32, V, None) == shape
+    assert ctx.lib.af_draft_verify(ctx.handle, p, B.F32, V, None, B.F32, 0, p, p, p, p, 1, 1, V, 1, 1.0, p, p, p, None) == shape
