@@ -10,8 +10,8 @@
 //
 // What has to be exact is whole numbers: a comparison u q < p, and the place of u C among running sums C_v of up to
 // 10^5 terms, where fp32 would be off by as much as many terms are large.  So a comparison whose sides are within 1e-5 is
-// made again from sums in 64 bits, and a draw's sums are in 64 bits throughout: per logit ten 64-bit operations, 2^x from a table
-// of 64 powers and a polynomial of degree 4 (2^-44 relative).
+// made again from sums in 64 bits, and a draw's sums are in 64 bits throughout: per logit eight 64-bit operations, 2^x from a table
+// of 256 powers and a polynomial of degree 3 (2^-42 relative).
 #include "device_util.cuh"
 #include "rollout.cuh"
 
@@ -290,27 +290,27 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
 }
 
 // --------------------------------------------------------------------------------- draws, in 64 bits
-constexpr int kPowers = 64;
-// 2^((z - m) / tau log2 e), relative to within 2^-44, and 2^-1000 from there down: what is no more than kNothing is no mass.
+constexpr int kPowers = 256;
+// 2^((z - m) / tau log2 e), relative to within 2^-42, and 2^-1000 from there down: what is no more than kNothing is no mass.
 constexpr double kNothing = 0x1p-900;
 struct Exp64 {
-  const double* power;                             // 2^(j / 64)
+  const double* power;                             // 2^(j / 256)
   double c, b;                                     // log2 e / tau, -m times it
   __device__ __forceinline__ double operator()(float z) const {
     const double far = fma((double)z, c, b);
     // no less than -1000 or so, -inf too: among high words as unsigned numbers, -1000's is below those of all lesser numbers
     const double t = __hiloint2double((int)min((uint32_t)__double2hiint(far), 0xc08f4000u), __double2loint(far));
-    constexpr double kShift = 0x1.8p52 / kPowers;  // adding it rounds to a multiple of 1/64, a whole number in the low bits
+    constexpr double kShift = 0x1.8p52 / kPowers;  // adding it rounds to a multiple of 1/256, a whole number in the low bits
     const double shifted = t + kShift;
     const int n = __double2loint(shifted);
-    const double r = t - (shifted - kShift);       // |r| <= 1/128
-    // 2^r - 1 = r (ln 2 + r (ln^2 2 / 2 + r (ln^3 2 / 6 + r ln^4 2 / 24))); the next term is below 2^-44
-    double p = fma(r, 9.6181291076284772e-3, 5.5504108664821580e-2);
-    p = fma(r, p, 2.4022650695910071e-1);
+    const double r = t - (shifted - kShift);       // |r| <= 1/512
+    // 2^r = 1 + r (ln 2 + r (ln^2 2 / 2 + r ln^3 2 / 6)); the next term is below 2^-42
+    double p = fma(r, 5.5504108664821580e-2, 2.4022650695910071e-1);
     p = fma(r, p, 6.9314718055994531e-1);
+    p = fma(r, p, 1.0);
     const double y = power[n & (kPowers - 1)];
-    const double w = fma(y, r * p, y);
-    return __hiloint2double(__double2hiint(w) + ((n & -kPowers) << (20 - 6)), __double2loint(w));       // times 2^(n / 64)
+    // times 2^(n / 256); where it is added to a sum, so is the product
+    return __hiloint2double(__double2hiint(y) + ((n & -kPowers) << (20 - 8)), __double2loint(y)) * p;
   }
 };
 __device__ __forceinline__ Exp64 exp_about(const double* power, float m, double inv_tau) {
