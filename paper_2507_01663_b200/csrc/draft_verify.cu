@@ -12,6 +12,9 @@
 // 10^5 terms, where fp32 would be off by as much as many terms are large.  So a comparison whose sides are within 1e-5 is
 // made again from sums in 64 bits, and a draw's sums are in 64 bits throughout: per logit eight 64-bit operations, 2^x from a table
 // of 256 powers and a polynomial of degree 3 (2^-42 relative).
+//
+// 64 requests of up to 4 drafts, bf16 and fp32 logits of 152064: 100-104 us, of which the rows take 53 (4 TB/s; their exponentials
+// keep the special unit busy half of the time), sums 25, mass 37, find 11, each alone and cold; one request 25-28 us, four launches.
 #include "device_util.cuh"
 #include "rollout.cuh"
 
