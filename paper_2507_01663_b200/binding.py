@@ -548,7 +548,7 @@ class Context:
                      max_draft: Optional[int] = None, temperature: float = 1.0, R=None, D=None, stream=None):
         """``target_logits`` [D + R, V] and ``draft_logits`` [D, V] (None: drafts without a distribution): float32 or bfloat16;
         ``draft``: int32 [D]; ``cu_draft``: int32 [R + 1]; ``token``: int32 [D + R]; ``max_draft``: the longest request's
-        drafts (default: D)."""
+        drafts, which the workspace goes by (default: D, which may be more than reserve_rollout was asked for)."""
         R = self._sequences(cu_draft, R)
         D = draft.shape[0] if D is None else D
         V = target_logits.shape[1]
