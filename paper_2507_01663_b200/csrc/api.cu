@@ -688,7 +688,7 @@ af_status af_quantize_head(af_ctx* c, const void* W, int32_t V, int32_t d, int32
   if (st != AF_OK) return st;
   if (!aligned16(W) || !aligned16(codes) || !aligned16(scale) || !aligned16(values)) return AF_ERR_ALIGNMENT;
   DeviceGuard guard(c->device);
-  return launch_quantize_head(W, V, d, group, codes, scale, values, c->sm_count, static_cast<cudaStream_t>(stream)) == cudaSuccess
+  return launch_quantize_head(W, V, d, group, codes, scale, values, static_cast<cudaStream_t>(stream)) == cudaSuccess
              ? AF_OK : AF_ERR_CUDA;
 }
 

@@ -8,7 +8,7 @@
 // by 1/255 of itself at least; w times 1/s (1 + 2^-20), exact within the fused multiply-add that also rounds it to a
 // whole number, lies on the far side of every half and on the right side of everything else.
 //
-// A stream: 2 bytes read per weight, 1/2 (and 2 for the value) written.  152064 x 3584 in groups of 128 with the values: 459 us,
+// A stream: 2 bytes read per weight, 1/2 (and 2 for the value) written.  152064 x 3584 in groups of 128 with the values: 412 us,
 // 5.4 TB/s, five ninths of it writes (a plain fill of this memory reaches 3.9); 4096 x 256: 2.7 us on the device.
 #include "device_util.cuh"
 #include "rollout.cuh"
@@ -16,7 +16,7 @@
 namespace af {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kUnroll = 4;                         // loads of 16 bytes in flight per thread
 constexpr float kWhole = 12582920.f;               // 1.5 * 2^23 + 8: adding it rounds to a whole number, digit in the low bits
 constexpr uint32_t kLargest = 0x7b80, kSmallest = 0x0d80;   // 2^120 and 2^-100 as bf16
@@ -44,58 +44,58 @@ __global__ void __launch_bounds__(kThreads) quantize_head_kernel(const uint4* __
                                                                  uint32_t* __restrict__ codes,
                                                                  __nv_bfloat16* __restrict__ scale, uint4* __restrict__ values) {
   const int lane = threadIdx.x & 31, lanes = 1 << lane_shift;      // a group's lanes: 8 weights each
-  const int64_t warp = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), warps = (int64_t)gridDim.x * (kThreads / 32);
+  const int64_t first = ((int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kUnroll;
   const int row_steps = (row_chunks + 31) / 32;
-  for (int64_t first = warp * kUnroll; first < steps; first += warps * kUnroll) {
-    uint4 w[kUnroll];
-    int64_t at[kUnroll], group_at[kUnroll];
-    bool in[kUnroll];
+  if (first >= steps) return;
+  uint4 w[kUnroll];
+  int64_t at[kUnroll], group_at[kUnroll];
+  bool in[kUnroll];
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
-      const int64_t step = first + j;
-      if constexpr (kOneRow) {
-        at[j] = step * 32 + lane;
-        group_at[j] = at[j] >> lane_shift;
-        in[j] = at[j] < chunks;
-      } else {
-        const int64_t row = step / row_steps;
-        const int chunk = (int)(step - row * row_steps) * 32 + lane;
-        at[j] = row * row_chunks + chunk;
-        group_at[j] = row * groups + (chunk >> lane_shift);
-        in[j] = step < steps && chunk < row_chunks;
-      }
-      w[j] = in[j] ? __ldcs(W + at[j]) : make_uint4(0, 0, 0, 0);
+  for (int j = 0; j < kUnroll; ++j) {
+    const int64_t step = first + j;
+    if constexpr (kOneRow) {
+      at[j] = step * 32 + lane;
+      group_at[j] = at[j] >> lane_shift;
+      in[j] = at[j] < chunks;
+    } else {
+      const int64_t row = step / row_steps;
+      const int chunk = (int)(step - row * row_steps) * 32 + lane;
+      at[j] = row * row_chunks + chunk;
+      group_at[j] = row * groups + (chunk >> lane_shift);
+      in[j] = step < steps && chunk < row_chunks;
     }
+    w[j] = in[j] ? __ldcs(W + at[j]) : make_uint4(0, 0, 0, 0);
+  }
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
-      const Scale g = group_scale(group_max(w[j], lanes));
-      const uint32_t half[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
-      uint32_t word = 0, v[4];
+  for (int j = 0; j < kUnroll; ++j) {
+    const Scale g = group_scale(group_max(w[j], lanes));
+    const uint32_t half[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+    uint32_t word = 0, v[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float a = fmaf(__uint_as_float(half[i] << 16), g.inv, kWhole), b = fmaf(__uint_as_float(half[i] & 0xffff0000u), g.inv, kWhole);
-        word |= __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410) << (4 * i);
-        if constexpr (kValues) v[i] = pack_bf16x2((a - kWhole) * g.s, (b - kWhole) * g.s);
-      }
-      if (g.s != g.s) word = 0x88888888u;
-      if (in[j]) {
-        codes[at[j]] = word;
-        if ((lane & (lanes - 1)) == 0) scale[group_at[j]] = __float2bfloat16_rn(g.s);
-        if constexpr (kValues) __stcs(values + at[j], make_uint4(v[0], v[1], v[2], v[3]));
-      }
+    for (int i = 0; i < 4; ++i) {
+      const float a = fmaf(__uint_as_float(half[i] << 16), g.inv, kWhole), b = fmaf(__uint_as_float(half[i] & 0xffff0000u), g.inv, kWhole);
+      word |= __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410) << (4 * i);
+      if constexpr (kValues) v[i] = pack_bf16x2((a - kWhole) * g.s, (b - kWhole) * g.s);
+    }
+    if (g.s != g.s) word = 0x88888888u;
+    if (in[j]) {
+      codes[at[j]] = word;
+      if ((lane & (lanes - 1)) == 0) scale[group_at[j]] = __float2bfloat16_rn(g.s);
+      if constexpr (kValues) values[at[j]] = make_uint4(v[0], v[1], v[2], v[3]);
     }
   }
 }
 
 template <bool kOneRow, bool kValues>
-cudaError_t quantize(const void* W, int32_t V, int32_t d, int32_t group, void* codes, void* scale, void* values, int sm_count,
-                     cudaStream_t s) {
+cudaError_t quantize(const void* W, int32_t V, int32_t d, int32_t group, void* codes, void* scale, void* values, cudaStream_t s) {
   const int row_chunks = d / 8;
   const int64_t chunks = (int64_t)V * row_chunks;
   const int64_t steps = kOneRow ? (chunks + 31) / 32 : (int64_t)V * ((row_chunks + 31) / 32);
-  const int64_t per_block = kUnroll * (kThreads / 32), want = (steps + per_block - 1) / per_block;
-  const int blocks = (int)(want < (int64_t)sm_count * 8 ? want : (int64_t)sm_count * 8);
-  quantize_head_kernel<kOneRow, kValues><<<blocks, kThreads, 0, s>>>(
+  // Every warp has one batch: CTAs that come and go overlap one's loads with another's stores better than those that stay and loop
+  // (412 us against 459 for 152064 x 3584; 256 threads 420, two batches' loads at a time 452, half a batch's 454).
+  const int64_t per_block = kUnroll * (kThreads / 32), blocks = (steps + per_block - 1) / per_block;
+  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;       // a head of more than 10^12 weights
+  quantize_head_kernel<kOneRow, kValues><<<(unsigned)blocks, kThreads, 0, s>>>(
       static_cast<const uint4*>(W), steps, chunks, row_chunks, group == 32 ? 2 : group == 64 ? 3 : 4, (d + group - 1) / group,
       static_cast<uint32_t*>(codes), static_cast<__nv_bfloat16*>(scale), static_cast<uint4*>(values));
   return cudaGetLastError();
@@ -104,12 +104,12 @@ cudaError_t quantize(const void* W, int32_t V, int32_t d, int32_t group, void* c
 }  // namespace
 
 cudaError_t launch_quantize_head(const void* W, int32_t V, int32_t d, int32_t group, void* codes, void* scale, void* values,
-                                 int sm_count, cudaStream_t s) {
+                                 cudaStream_t s) {
   if (d % group == 0)
-    return values ? quantize<true, true>(W, V, d, group, codes, scale, values, sm_count, s)
-                  : quantize<true, false>(W, V, d, group, codes, scale, values, sm_count, s);
-  return values ? quantize<false, true>(W, V, d, group, codes, scale, values, sm_count, s)
-                : quantize<false, false>(W, V, d, group, codes, scale, values, sm_count, s);
+    return values ? quantize<true, true>(W, V, d, group, codes, scale, values, s)
+                  : quantize<true, false>(W, V, d, group, codes, scale, values, s);
+  return values ? quantize<false, true>(W, V, d, group, codes, scale, values, s)
+                : quantize<false, false>(W, V, d, group, codes, scale, values, s);
 }
 
 }  // namespace af

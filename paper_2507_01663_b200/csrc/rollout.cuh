@@ -16,7 +16,7 @@ struct QuantHead {
   int32_t groups() const { return (d + group - 1) / group; }
 };
 cudaError_t launch_quantize_head(const void* W, int32_t V, int32_t d, int32_t group, void* codes, void* scale, void* values,
-                                 int sm_count, cudaStream_t s);
+                                 cudaStream_t s);
 af_status launch_quant_logits(af_ctx* ctx, const void* hidden, const QuantHead& head, int64_t T, void* logits, int32_t type,
                               int64_t pitch, cudaStream_t s);
 constexpr int kQuantTokens = 64;  // of one launch (quant_umma.cu)
