@@ -8,8 +8,8 @@
 // by 1/255 of itself at least; w times 1/s (1 + 2^-20), exact within the fused multiply-add that also rounds it to a
 // whole number, lies on the far side of every half and on the right side of everything else.
 //
-// A stream: 2 bytes read per weight, 1/2 (and 2 for the value) written.  152064 x 3584 in groups of 128 with the values: 412 us,
-// 5.4 TB/s, five ninths of it writes (a plain fill of this memory reaches 3.9); 4096 x 256: 2.7 us on the device.
+// A stream: 2 bytes read per weight, 1/2 (and 2 for the value) written.  152064 x 3584 in groups of 128 with the values: 371-386 us,
+// 6.4-6.6 TB/s, the rate of a copy; 4096 x 256: 2.6 us on the device.
 #include "device_util.cuh"
 #include "rollout.cuh"
 
@@ -92,7 +92,7 @@ cudaError_t quantize(const void* W, int32_t V, int32_t d, int32_t group, void* c
   const int64_t chunks = (int64_t)V * row_chunks;
   const int64_t steps = kOneRow ? (chunks + 31) / 32 : (int64_t)V * ((row_chunks + 31) / 32);
   // Every warp has one batch: CTAs that come and go overlap one's loads with another's stores better than those that stay and loop
-  // (412 us against 459 for 152064 x 3584; 256 threads 420, two batches' loads at a time 452, half a batch's 454).
+  // (386 us against 459 for 152064 x 3584; with a loop that runs once 412, so with 256 threads 420, 8 loads at a time 452, 2 454).
   const int64_t per_block = kUnroll * (kThreads / 32), blocks = (steps + per_block - 1) / per_block;
   if (blocks > 0x7fffffff) return cudaErrorInvalidValue;       // a head of more than 10^12 weights
   quantize_head_kernel<kOneRow, kValues><<<(unsigned)blocks, kThreads, 0, s>>>(
