@@ -10,7 +10,7 @@
 //
 // What has to be exact is whole numbers: a comparison u q < p, and the place of u C among running sums C_v of up to
 // 10^5 terms, where fp32 would be off by as much as many terms are large.  So a comparison whose sides are within 1e-5 is
-// made again from sums in 64 bits, and a draw's sums are in 64 bits throughout: per logit eight 64-bit operations, 2^x from a table
+// made again from sums in 64 bits, and a draw's sums are in 64 bits throughout: per logit nine 64-bit operations, 2^x from a table
 // of 256 powers and a polynomial of degree 3 (2^-42 relative).
 //
 // 64 requests of up to 4 drafts, bf16 and fp32 logits of 152064: 100-104 us, of which the rows take 53 (4 TB/s; their exponentials
@@ -298,9 +298,11 @@ constexpr int kPowers = 256;
 constexpr double kNothing = 0x1p-900;
 struct Exp64 {
   const double* power;                             // 2^(j / 256)
-  double c, b;                                     // log2 e / tau, -m times it
+  double c, m;                                     // log2 e / tau, and what is subtracted before it multiplies:
+  // z c - m c in one operation would be off by the rounding of m c, which for the lowest logits of a type is far beyond the range of
+  // any exponential, at z = m too
   __device__ __forceinline__ double operator()(float z) const {
-    const double far = fma((double)z, c, b);
+    const double far = ((double)z - m) * c;
     // no less than -1000 or so, -inf too: among high words as unsigned numbers, -1000's is below those of all lesser numbers
     const double t = __hiloint2double((int)min((uint32_t)__double2hiint(far), 0xc08f4000u), __double2loint(far));
     constexpr double kShift = 0x1.8p52 / kPowers;  // adding it rounds to a multiple of 1/256, a whole number in the low bits
@@ -317,8 +319,7 @@ struct Exp64 {
   }
 };
 __device__ __forceinline__ Exp64 exp_about(const double* power, float m, double inv_tau) {
-  const double c = inv_tau * 1.4426950408889634074;
-  return {power, c, -(double)m * c};
+  return {power, inv_tau * 1.4426950408889634074, (double)m};
 }
 
 // Sum over the block of kWarps warps, in a fixed order; every thread gets it.
