@@ -294,8 +294,10 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
 
 // --------------------------------------------------------------------------------- draws, in 64 bits
 constexpr int kPowers = 256;
-// 2^((z - m) / tau log2 e), relative to within 2^-42, and 2^-1000 from there down: what is no more than kNothing is no mass.
+// 2^((z - m) / tau log2 e), relative to within 2^-42, and 2^-1000 from there down: what is no more than kNothing is no mass,
+// and sums of it count as 0 (a uniform of 0 takes the first token with mass, which a sum above 0 before it would hide).
 constexpr double kNothing = 0x1p-900;
+__device__ __forceinline__ double some_mass(double sum) { return sum > kNothing ? sum : 0.0; }
 struct Exp64 {
   const double* power;                             // 2^(j / 256)
   double c, m;                                     // log2 e / tau, and what is subtracted before it multiplies:
@@ -533,7 +535,7 @@ __global__ void __launch_bounds__(kDrawThreads) verify_mass_kernel(const VerifyC
     a += __shfl_xor_sync(0xffffffffu, a, o);
     whole += __shfl_xor_sync(0xffffffffu, whole, o);
   }
-  if (lane == 0) ws.mass[(int64_t)r * segments + k] = make_double2(a, whole);
+  if (lane == 0) ws.mass[(int64_t)r * segments + k] = make_double2(some_mass(a), whole);
 }
 
 // The token: the segment that holds the first v with C_v > u C, a part of it, and the place in that.
@@ -585,7 +587,7 @@ __global__ void __launch_bounds__(kFindThreads) verify_find_kernel(const VerifyC
   if (!afresh) {
     goal = u * total;
     // the last segment with mass that starts at or before the goal
-    if (mine.x > kNothing && (k == 0 ? 0.0 : s_upto[k - 1]) <= goal) atomicMax(&s_found, k);
+    if (mine.x > 0.0 && (k == 0 ? 0.0 : s_upto[k - 1]) <= goal) atomicMax(&s_found, k);
     __syncthreads();
     const int f = s_found;
     start = f == 0 ? 0.0 : s_upto[f - 1];
@@ -603,7 +605,7 @@ __global__ void __launch_bounds__(kFindThreads) verify_find_kernel(const VerifyC
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
     __syncthreads();
-    if (lane == 0) s_warp[warp] = a;
+    if (lane == 0) s_warp[warp] = some_mass(a);
     __syncthreads();
     if (afresh && first) {
       double all = 0.0;
@@ -613,7 +615,7 @@ __global__ void __launch_bounds__(kFindThreads) verify_find_kernel(const VerifyC
     double run = start;
     int found = 0;                                            // the last part with mass that starts at or before the goal
     for (int w = 0; w < kFindWarps; ++w) {
-      if (run <= goal && s_warp[w] > kNothing) { found = w; start = run; }
+      if (run <= goal && s_warp[w] > 0.0) { found = w; start = run; }
       run += s_warp[w];
     }
     const int next_lo = part(found);
