@@ -573,8 +573,8 @@ af_status af_quant_logits(af_ctx* ctx, const void* hidden, const void* codes, co
  * as they are, and AF_DEVERR_CU_SEQLENS is raised, as it is where cu_draft does not run from 0 to D.  (Rows that two requests of
  * such a cu_draft share hold one's or the other's results.)
  *
- * Comparisons and draws are made from sums in 64 bits where 32 could decide otherwise; log-probs of passed drafts are within
- * 1e-6 of 64 bits, that of y is rounded once.  In a draw weights below 2^-900 of the row's largest are nothing.
+ * Comparisons and draws are made from sums in 64 bits where 32 could decide otherwise; log-probs of passed drafts and of greedy
+ * tokens are within 8e-6 of 64 bits whatever the row holds (ordinary rows: 2e-7), that of a drawn y is rounded once.  In a draw weights below 2^-900 of the row's largest are nothing.
  * target_logits [D + R, V], draft_logits [D, V]: fp32 or bf16 dev, row pitch in elements (>= V), aligned to their type.  draft [D],
  * cu_draft [R+1], token [D + R], n_emitted [R] int32, logp (nullable) [D + R] fp32, dev.  0 <= max_draft <= AF_MAX_DRAFT,
  * 0 <= R, R * (max_draft + 1) <= 2^24, 0 <= D <= R * max_draft, temperature 0 or from 1e-4 to 1e4.

@@ -9,7 +9,7 @@
 // its time waiting for its slowest CTA (64 requests: 75 us for 15 us of 64-bit operations).
 //
 // What has to be exact is whole numbers: a comparison u q < p, and the place of u C among running sums C_v of up to
-// 10^5 terms, where fp32 would be off by as much as many terms are large.  So a comparison whose sides are within 1e-5 is
+// 10^5 terms, where fp32 would be off by as much as many terms are large.  So a comparison whose sides are within 2e-5 is
 // made again from sums in 64 bits, and a draw's sums are in 64 bits throughout: per logit nine 64-bit operations, 2^x from a table
 // of 256 powers and a polynomial of degree 3 (2^-42 relative).
 //
@@ -93,6 +93,19 @@ __device__ __forceinline__ RowPart join(const RowPart& a, const RowPart& b, floa
   return o;
 }
 
+// A thread's part on the way.  `sum` takes eight additions at most before it is folded into `whole`, whose roundings `rest` keeps: in a
+// long row of equal terms those of one plain sum would all go the same way (4 million flat logits: 1.5e-5 off).
+struct RowSum {
+  float m, sum, whole, rest;
+  int32_t at;
+  __device__ __forceinline__ void fold() {
+    const float t = __fadd_rn(whole, sum), b = __fsub_rn(t, whole);
+    rest += __fadd_rn(__fsub_rn(whole, __fsub_rn(t, b)), __fsub_rn(sum, b));         // what t lacks, exactly
+    whole = t;
+    sum = 0.f;
+  }
+};
+
 template <int n>
 struct Values { float v[n]; };
 __device__ __forceinline__ Values<4> widen(const float*, uint4 x) {
@@ -110,12 +123,15 @@ __device__ __forceinline__ Values<1> widen1(const __nv_bfloat16* p) { return {{_
 
 // Adds n neighbours, the first at place `at`, to a thread's part.
 template <bool kPlace, int n>
-__device__ __forceinline__ void add(RowPart& a, const Values<n>& x, int at, float scale) {
+__device__ __forceinline__ void add(RowSum& a, const Values<n>& x, int at, float scale) {
   float top = x.v[0];
 #pragma unroll
   for (int i = 1; i < n; ++i) top = fmaxf(top, x.v[i]);
   if (top > a.m) {                                 // rare after the first few
-    a.s *= ex2f((a.m - top) * scale);              // 0 times 0 at first
+    const float less = ex2f((a.m - top) * scale);  // 0 times 0 at first
+    a.sum *= less;
+    a.whole *= less;
+    a.rest *= less;
     a.m = top;
     if constexpr (kPlace) {
 #pragma unroll
@@ -126,12 +142,12 @@ __device__ __forceinline__ void add(RowPart& a, const Values<n>& x, int at, floa
   if (a.m == kNoMax) {                             // nothing but -inf so far, or a NaN
 #pragma unroll
     for (int i = 0; i < n; ++i)
-      if (x.v[i] != x.v[i]) a.s = x.v[i];
+      if (x.v[i] != x.v[i]) a.sum = x.v[i];
     return;
   }
   // a NaN, and infinity less itself, make the sum NaN
   if constexpr (n == 1) {
-    a.s += ex2f((x.v[0] - a.m) * scale);
+    a.sum += ex2f((x.v[0] - a.m) * scale);
   } else {
     const float2 less = make_float2(-a.m, -a.m), by = make_float2(scale, scale);
     float2 sum = make_float2(0.f, 0.f);
@@ -140,14 +156,14 @@ __device__ __forceinline__ void add(RowPart& a, const Values<n>& x, int at, floa
       const float2 e = __fmul2_rn(__fadd2_rn(make_float2(x.v[i], x.v[i + 1]), less), by);
       sum = __fadd2_rn(sum, make_float2(ex2f(e.x), ex2f(e.y)));
     }
-    a.s += sum.x + sum.y;
+    a.sum += sum.x + sum.y;
   }
 }
 
 template <bool kPlace, class T>
 __device__ RowPart row_part(const T* row, int lo, int hi, float scale) {
   constexpr int kVec = 16 / sizeof(T), kLoads = 4;
-  RowPart a{kNoMax, 0.f, kGoesOn, 0};
+  RowSum a{kNoMax, 0.f, 0.f, 0.f, kGoesOn};
   // single elements up to a multiple of 16 bytes, and behind the last one
   const int to_line = (int)((16u - ((uint32_t)reinterpret_cast<uintptr_t>(row + lo) & 15u)) & 15u) / (int)sizeof(T);
   const int body = min(hi, lo + to_line), vecs = (hi - body) / kVec, tail = body + vecs * kVec;
@@ -167,12 +183,14 @@ __device__ RowPart row_part(const T* row, int lo, int hi, float scale) {
     if (i + kStep < whole) fetch(ahead, i + kStep);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) add<kPlace>(a, widen(row, w[k]), body + (i + k * kRowThreads) * kVec, scale);
+    a.fold();
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) w[k] = ahead[k];
   }
   for (; i < vecs; i += kRowThreads) add<kPlace>(a, widen(row, __ldg(at + i)), body + i * kVec, scale);
   if (tail + (int)threadIdx.x < hi) add<kPlace>(a, widen1(row + tail + threadIdx.x), tail + threadIdx.x, scale);
-  return a;
+  a.fold();
+  return {a.m, a.whole + a.rest, a.at, 0};
 }
 
 template <bool kPlace>
@@ -216,7 +234,11 @@ __device__ __forceinline__ Sides sides_of(const Row& t, const Row& q, float u, f
   const double pw = exp(((double)z - (double)t.m) * inv_tau), qw = dense ? exp(((double)zq - (double)q.m) * inv_tau) : 1.0;
   return {(double)u * qw * t.s, pw * (dense ? q.s : 1.0)};
 }
-__device__ __forceinline__ bool too_near(const Sides& e) { return fabs(e.left - e.right) <= 1e-5 * fabs(e.right); }
+// A row's sum is off by 8e-6 at most: an argument of e halvings is rounded three times (difference, 1 / tau, product), 3 u e ln 2 with
+// u = 2^-24, and e is log2 V on the weighted average of the terms at most;  ex2.approx is good to 4 u, for the term and for each
+// joining;  40 additions, eight of a thread's and those that join parts.  Both sides together stay within this:
+constexpr double kNear = 2e-5;
+__device__ __forceinline__ bool too_near(const Sides& e) { return fabs(e.left - e.right) <= kNear * fabs(e.right); }
 
 __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(const VerifyCall c, const Shape shape, float scale, const Workspace ws) {
   __shared__ RowPart warp_parts[2][kRowThreads / 32];
