@@ -32,11 +32,13 @@ constexpr float kNoMax = -INFINITY;
 constexpr double kResidualFloor = 0x1p-30;         // a residual with less mass than this is drawn from the target itself
 constexpr int kGoesOn = 0x7fffffff;
 
-struct RowPart {                                   // a slice of a row: max z, sum exp((z - m) / tau), place of the maximum
+// A row's sum exp((z - m) / tau) is about its maximum, or about a logit up to four halvings of the exponential less (greedy: the
+// maximum, and its place).
+struct RowPart {                                   // of a slice
   float m, s;
   int32_t at, pad;
 };
-struct Row {                                       // of a whole row: maximum, its place, sum about the maximum in 64 bits
+struct Row {                                       // of the whole, in 64 bits
   float m;
   int32_t at;
   double s;
@@ -60,7 +62,7 @@ enum Kind : int32_t { kNoDraw, kPlain, kCut, kDense };       // from the target;
 struct Draw {                                      // how a request's last token is drawn
   int64_t row;                                     // the target's row
   int32_t kind, draft_row, cut;                    // cut: the draft that is left out
-  float m, m_draft;                                // the rows' maxima
+  float m, m_draft;                                // what the rows' sums are about
 };
 struct Shape {
   int slices, positions;                           // slices of a row; max_draft + 1
@@ -82,25 +84,16 @@ __device__ __forceinline__ Span span_of(const VerifyCall& c, int r) {
 }
 
 // ------------------------------------------------------------------------------------ rows, in fp32
-__device__ __forceinline__ RowPart join(const RowPart& a, const RowPart& b, float scale) {
-  RowPart o;
-  const bool first = a.m > b.m || (a.m == b.m && a.at < b.at);
-  o.m = first ? a.m : b.m;
-  o.at = first ? a.at : b.at;
-  // a part without mass adds nothing (its maximum may be -inf); a NaN stays
-  o.s = (a.s == 0.f ? 0.f : a.s * ex2f((a.m - o.m) * scale)) + (b.s == 0.f ? 0.f : b.s * ex2f((b.m - o.m) * scale));
-  o.pad = 0;
-  return o;
-}
-
 // A thread's part on the way.  `sum` takes eight additions at most before it is folded into `whole`, whose roundings `rest` keeps: in a
-// long row of equal terms those of one plain sum would all go the same way (4 million flat logits: 1.5e-5 off).
+// long row of equal terms those of one plain sum would all go the same way (4 million flat logits: 1.5e-5 off).  m moves only to a
+// logit of two halvings more, so that the sums are scaled once or twice, not with every step of a rising row.
 struct RowSum {
   float m, sum, whole, rest;
+  float limit;                                     // above it m moves; kPlace: the maximum, and its place
   int32_t at;
   __device__ __forceinline__ void fold() {
-    const float t = __fadd_rn(whole, sum), b = __fsub_rn(t, whole);
-    rest += __fadd_rn(__fsub_rn(whole, __fsub_rn(t, b)), __fsub_rn(sum, b));         // what t lacks, exactly
+    const float t = __fadd_rn(whole, sum);
+    rest += __fsub_rn(sum, __fsub_rn(t, whole));             // what t lacks, exactly but where m has just moved and `whole` is the less
     whole = t;
     sum = 0.f;
   }
@@ -123,20 +116,24 @@ __device__ __forceinline__ Values<1> widen1(const __nv_bfloat16* p) { return {{_
 
 // Adds n neighbours, the first at place `at`, to a thread's part.
 template <bool kPlace, int n>
-__device__ __forceinline__ void add(RowSum& a, const Values<n>& x, int at, float scale) {
+__device__ __forceinline__ void add(RowSum& a, const Values<n>& x, int at, float scale, float slack) {
   float top = x.v[0];
 #pragma unroll
   for (int i = 1; i < n; ++i) top = fmaxf(top, x.v[i]);
-  if (top > a.m) {                                 // rare after the first few
-    const float less = ex2f((a.m - top) * scale);  // 0 times 0 at first
-    a.sum *= less;
-    a.whole *= less;
-    a.rest *= less;
-    a.m = top;
+  if (top > a.limit) {                             // rare after the first few
     if constexpr (kPlace) {
+      a.limit = top;
 #pragma unroll
       for (int i = n - 1; i >= 0; --i)
         if (x.v[i] == top) a.at = at + i;
+    }
+    if (!kPlace || top > a.m + slack) {
+      const float less = ex2f((a.m - top) * scale);          // 0 times 0 at first
+      a.sum *= less;
+      a.whole *= less;
+      a.rest *= less;
+      a.m = top;
+      if (!kPlace) a.limit = top + slack;
     }
   }
   if (a.m == kNoMax) {                             // nothing but -inf so far, or a NaN
@@ -161,13 +158,13 @@ __device__ __forceinline__ void add(RowSum& a, const Values<n>& x, int at, float
 }
 
 template <bool kPlace, class T>
-__device__ RowPart row_part(const T* row, int lo, int hi, float scale) {
+__device__ RowPart row_part(const T* row, int lo, int hi, float scale, float slack) {
   constexpr int kVec = 16 / sizeof(T), kLoads = 4;
-  RowSum a{kNoMax, 0.f, 0.f, 0.f, kGoesOn};
+  RowSum a{kNoMax, 0.f, 0.f, 0.f, kNoMax, kGoesOn};
   // single elements up to a multiple of 16 bytes, and behind the last one
   const int to_line = (int)((16u - ((uint32_t)reinterpret_cast<uintptr_t>(row + lo) & 15u)) & 15u) / (int)sizeof(T);
   const int body = min(hi, lo + to_line), vecs = (hi - body) / kVec, tail = body + vecs * kVec;
-  if (lo + (int)threadIdx.x < body) add<kPlace>(a, widen1(row + lo + threadIdx.x), lo + threadIdx.x, scale);
+  if (lo + (int)threadIdx.x < body) add<kPlace>(a, widen1(row + lo + threadIdx.x), lo + threadIdx.x, scale, slack);
   const uint4* const at = reinterpret_cast<const uint4*>(row + body);
   // the next loads are under way while the last ones' exponentials are taken
   constexpr int kStep = kLoads * kRowThreads;
@@ -182,50 +179,64 @@ __device__ RowPart row_part(const T* row, int lo, int hi, float scale) {
   for (; i < whole; i += kStep) {
     if (i + kStep < whole) fetch(ahead, i + kStep);
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) add<kPlace>(a, widen(row, w[k]), body + (i + k * kRowThreads) * kVec, scale);
+    for (int k = 0; k < kLoads; ++k) add<kPlace>(a, widen(row, w[k]), body + (i + k * kRowThreads) * kVec, scale, slack);
     a.fold();
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) w[k] = ahead[k];
   }
-  for (; i < vecs; i += kRowThreads) add<kPlace>(a, widen(row, __ldg(at + i)), body + i * kVec, scale);
-  if (tail + (int)threadIdx.x < hi) add<kPlace>(a, widen1(row + tail + threadIdx.x), tail + threadIdx.x, scale);
+  for (; i < vecs; i += kRowThreads) add<kPlace>(a, widen(row, __ldg(at + i)), body + i * kVec, scale, slack);
+  if (tail + (int)threadIdx.x < hi) add<kPlace>(a, widen1(row + tail + threadIdx.x), tail + threadIdx.x, scale, slack);
   a.fold();
-  return {a.m, a.whole + a.rest, a.at, 0};
+  const float s = a.whole + a.rest;
+  if (kPlace && a.limit > a.m) return {a.limit, s * ex2f((a.m - a.limit) * scale), a.at, 0};
+  return {a.m, s, a.at, 0};
 }
 
 template <bool kPlace>
-__device__ RowPart thread_part(const LogitRows& x, int64_t row, int lo, int hi, float scale) {
-  return x.type == AF_F32 ? row_part<kPlace>(static_cast<const float*>(x.p) + row * x.pitch, lo, hi, scale)
-                          : row_part<kPlace>(static_cast<const __nv_bfloat16*>(x.p) + row * x.pitch, lo, hi, scale);
+__device__ RowPart thread_part(const LogitRows& x, int64_t row, int lo, int hi, float scale, float slack) {
+  return x.type == AF_F32 ? row_part<kPlace>(static_cast<const float*>(x.p) + row * x.pitch, lo, hi, scale, slack)
+                          : row_part<kPlace>(static_cast<const __nv_bfloat16*>(x.p) + row * x.pitch, lo, hi, scale, slack);
+}
+__device__ __forceinline__ RowPart no_part() { return {kNoMax, 0.f, kGoesOn, 0}; }
+// Parts are joined about the largest m of all, each scaled once.  Floats that are no NaN order as whole numbers do once the bits below the
+// sign of negative ones are turned over.
+__device__ __forceinline__ int32_t ordered(int32_t bits) { return bits ^ ((bits >> 31) & 0x7fffffff); }
+__device__ __forceinline__ float warp_max(float m) {
+  return __int_as_float(ordered(__reduce_max_sync(0xffffffffu, ordered(__float_as_int(m)))));
+}
+// A part without mass adds nothing (its m may be -inf); a NaN stays.
+__device__ __forceinline__ float sum_about(const RowPart& a, float m, float scale) { return a.s == 0.f ? 0.f : a.s * ex2f((a.m - m) * scale); }
+// s, at: of a lane, about the warp's m.
+__device__ __forceinline__ RowPart join_lanes(float m, float s, int at) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return {m, s, __reduce_min_sync(0xffffffffu, at), 0};
 }
 __device__ __forceinline__ void join_warp(RowPart& a, float scale) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    RowPart b;
-    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-    b.at = __shfl_xor_sync(0xffffffffu, a.at, o);
-    a = join(a, b, scale);
-  }
+  const float m = warp_max(a.m);
+  a = join_lanes(m, sum_about(a, m, scale), a.m == m ? a.at : kGoesOn);
 }
 
 __device__ __forceinline__ bool good(const Row& x) { return fabsf(x.m) < INFINITY && x.s > 0.0 && x.s < 1e300; }
-// Called by a whole warp.
-__device__ __forceinline__ RowPart warp_part(const RowPart* parts, int slices) {
-  RowPart a{kNoMax, 0.f, kGoesOn, 0};
-  const int lane = threadIdx.x & 31;
-  if (lane < slices) {
-    const uint4 x = __ldcg(reinterpret_cast<const uint4*>(parts) + lane);
-    a = RowPart{__uint_as_float(x.x), __uint_as_float(x.y), (int32_t)x.z, 0};
-  }
-  return a;
+__device__ __forceinline__ RowPart fetch_part(const RowPart* p) {
+  const uint4 x = __ldcg(reinterpret_cast<const uint4*>(p));
+  return {__uint_as_float(x.x), __uint_as_float(x.y), (int32_t)x.z, 0};
 }
-__device__ __forceinline__ void join_slices(RowPart& a, const RowPart* parts, int slices, float scale) {
-  for (int i = (threadIdx.x & 31) + 32; i < slices; i += 32) {
-    const uint4 x = __ldcg(reinterpret_cast<const uint4*>(parts) + i);
-    a = join(a, RowPart{__uint_as_float(x.x), __uint_as_float(x.y), (int32_t)x.z, 0}, scale);
+// A row's slices, by a whole warp.
+__device__ __forceinline__ RowPart join_slices(const RowPart* parts, int slices, float scale) {
+  const int lane = threadIdx.x & 31;
+  const RowPart first = lane < slices ? fetch_part(parts + lane) : no_part();
+  float m = first.m;
+  for (int i = lane + 32; i < slices; i += 32) m = fmaxf(m, fetch_part(parts + i).m);
+  m = warp_max(m);
+  float s = sum_about(first, m, scale);
+  int at = first.m == m ? first.at : kGoesOn;
+  for (int i = lane + 32; i < slices; i += 32) {
+    const RowPart a = fetch_part(parts + i);
+    s += sum_about(a, m, scale);
+    if (a.m == m) at = min(at, a.at);
   }
-  join_warp(a, scale);
+  return join_lanes(m, s, at);
 }
 
 // u q(x) and p(x), both times both sums: x passes iff left < right.
@@ -235,12 +246,12 @@ __device__ __forceinline__ Sides sides_of(const Row& t, const Row& q, float u, f
   return {(double)u * qw * t.s, pw * (dense ? q.s : 1.0)};
 }
 // A row's sum is off by 8e-6 at most: an argument of e halvings is rounded three times (difference, 1 / tau, product), 3 u e ln 2 with
-// u = 2^-24, and e is log2 V on the weighted average of the terms at most;  ex2.approx is good to 4 u, for the term and for each
-// joining;  40 additions, eight of a thread's and those that join parts.  Both sides together stay within this:
+// u = 2^-24, and e is log2 V on the weighted average of the terms at most, 4 more for what m is short of;  ex2.approx is good to 4 u,
+// for the term, at most twice where m moves, and three times where parts are joined;  40 additions, eight of a thread's and those that join parts.  Both sides together stay within this:
 constexpr double kNear = 2e-5;
 __device__ __forceinline__ bool too_near(const Sides& e) { return fabs(e.left - e.right) <= kNear * fabs(e.right); }
 
-__global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(const VerifyCall c, const Shape shape, float scale, const Workspace ws) {
+__global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(const VerifyCall c, const Shape shape, float scale, float slack, const Workspace ws) {
   __shared__ RowPart warp_parts[2][kRowThreads / 32];
   __shared__ int s_skip;
   wait_for_predecessor();
@@ -261,16 +272,16 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
   const int64_t row = sp.first + r + i;
   const int k = sp.first + i;                      // the draft's row
   const bool greedy = c.temperature == 0.f, dense = c.draft.p && i < sp.n;
-  RowPart t = greedy ? thread_part<true>(c.target, row, lo, hi, scale) : thread_part<false>(c.target, row, lo, hi, scale);
-  RowPart d{kNoMax, 0.f, kGoesOn, 0};
-  if (dense) d = thread_part<false>(c.draft, k, lo, hi, scale);
+  RowPart t = greedy ? thread_part<true>(c.target, row, lo, hi, scale, slack) : thread_part<false>(c.target, row, lo, hi, scale, slack);
+  RowPart d = no_part();
+  if (dense) d = thread_part<false>(c.draft, k, lo, hi, scale, slack);
   join_warp(t, scale);
   if (dense) join_warp(d, scale);
   if ((threadIdx.x & 31) == 0) { warp_parts[0][threadIdx.x >> 5] = t; warp_parts[1][threadIdx.x >> 5] = d; }
   __syncthreads();
   if (threadIdx.x >= 32) return;
   const bool in = threadIdx.x < kRowThreads / 32;
-  t = in ? warp_parts[0][threadIdx.x] : RowPart{kNoMax, 0.f, kGoesOn, 0};
+  t = in ? warp_parts[0][threadIdx.x] : no_part();
   d = in ? warp_parts[1][threadIdx.x] : t;
   join_warp(t, scale);
   if (dense) join_warp(d, scale);
@@ -289,10 +300,8 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) verify_rows_kernel(co
     last = __shfl_sync(0xffffffffu, last, 0);
     if (!last) return;
     __threadfence();
-    t = warp_part(t_at, shape.slices);
-    if (dense) d = warp_part(d_at, shape.slices);
-    join_slices(t, t_at, shape.slices, scale);
-    if (dense) join_slices(d, d_at, shape.slices, scale);
+    t = join_slices(t_at, shape.slices, scale);
+    if (dense) d = join_slices(d_at, shape.slices, scale);
   }
   const Row tr{t.m, t.at, (double)t.s}, dr{d.m, d.at, (double)d.s};
   if (threadIdx.x != 0) return;
@@ -742,7 +751,7 @@ af_status launch_draft_verify(af_ctx* ctx, const VerifyCall& c, cudaStream_t s) 
   ws.stop = reinterpret_cast<int*>(static_cast<char*>(ctx->verify_state.p) + z.tickets);
   const float scale = c.temperature == 0.f ? kLog2e : kLog2e / c.temperature;
   const int64_t blocks = (int64_t)c.R * shape.positions * shape.slices;
-  if (launch_overlapped(verify_rows_kernel, (unsigned)blocks, kRowThreads, 0, s, c, shape, scale, ws) != cudaSuccess) return AF_ERR_CUDA;
+  if (launch_overlapped(verify_rows_kernel, (unsigned)blocks, kRowThreads, 0, s, c, shape, scale, 2.f / scale, ws) != cudaSuccess) return AF_ERR_CUDA;
   const bool wide_draft = !c.draft.p || c.draft.type == AF_F32;
   using bf16 = __nv_bfloat16;
   if (c.target.type == AF_F32)

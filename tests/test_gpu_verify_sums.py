@@ -69,3 +69,35 @@ def test_comparisons_on_flat_rows(ctx, V, dtype):  # noqa: F811
             for off in (-1e-4, -3e-5, -1e-5, -2e-6, 2e-6, 1e-5, 3e-5, 1e-4):
                 u = np.float32(p * (1 + off))
                 assert (passed(ctx, row, 0, tau, u) is not None) == (float(u) < p), (tail, tau, off)
+
+
+def ramp(V, width, order):
+    """Logits that rise by `width` from the first looked at to the last: over the row, the other way, or from one group of eight to the
+    next of the same thread (256 threads of eight neighbours) and back down within the groups."""
+    x = torch.arange(V, device=device(), dtype=torch.float64)
+    if order == "down":
+        x = x.flip(0)
+    elif order == "threads":
+        x = (x // 2048) * 2048 + (x % 2048).flip(0)
+    return (x * (width / V)).float()
+
+
+@pytest.mark.parametrize("order", ["up", "down", "threads"])
+@pytest.mark.parametrize("V", [152064, 1 << 20, 1 << 22])
+@pytest.mark.parametrize("greedy", [False, True])
+def test_log_probs_of_rising_rows(ctx, V, order, greedy):  # noqa: F811
+    """Every new maximum scales what was added up before."""
+    for width in (1e-3, 0.03, 0.3, 1.0, 3.0, 20.0):
+        row = ramp(V, width, order)
+        z = row.double()
+        x = int(row.argmax()) if greedy else V // 2 + 5
+        for max_draft in (1, ONE_SLICE):
+            two = torch.stack([row, row])
+            c = {"target": two, "draft": None, "ids": np.array([x], np.int32), "cu": np.array([0, 1], np.int32),
+                 "ua": np.zeros(1, np.float32), "us": np.array([0.5], np.float32)}
+            token, lp, n = run(ctx, c, 0.0 if greedy else 1.0, max_draft=max_draft)
+            want = float(z[x] - z.max() - (z - z.max()).exp().sum().log())
+            assert ctx.check_device_errors() == 0 and n[0] == 2 and token[0] == x
+            assert abs(lp[0] - want) <= sum_bound(V) + 20 * U + 2 * U * abs(want), (width, max_draft)      # 20 more additions join slices
+            if greedy:
+                assert token[1] == x and lp[1] == lp[0]
