@@ -37,6 +37,7 @@ MAX_WRITE_COLS = 4
 MAX_CANDIDATES = 256
 MAX_QUANT_TOKENS = 65536
 MAX_DRAFT = 1023
+MAX_DRAFT_ROWS = 1 << 24                                             # most requests * (max_draft + 1) of one call
 F32, BF16 = 0, 1                                                     # af_dtype
 DIVERGENCE_FORWARD, DIVERGENCE_REVERSE = 0, 1                        # teacher to student, student to teacher
 SUPPORT_LISTED, SUPPORT_RENORMALISED, SUPPORT_TAIL = 0, 1, 2
@@ -548,16 +549,20 @@ class Context:
                      max_draft: Optional[int] = None, temperature: float = 1.0, R=None, D=None, stream=None):
         """``target_logits`` [D + R, V] and ``draft_logits`` [D, V] (None: drafts without a distribution): float32 or bfloat16;
         ``draft``: int32 [D]; ``cu_draft``: int32 [R + 1]; ``token``: int32 [D + R]; ``max_draft``: the longest request's
-        drafts, which the workspace goes by (default: D, which may be more than reserve_rollout was asked for)."""
+        drafts.  Give it where it is known: workspace and launch go by R * (max_draft + 1) rows, and without it by the most that
+        a request of this batch could have (D, within MAX_DRAFT and MAX_DRAFT_ROWS), which may be far more rows than there are
+        and more workspace than reserve_rollout was asked for."""
         R = self._sequences(cu_draft, R)
         D = draft.shape[0] if D is None else D
         V = target_logits.shape[1]
+        if max_draft is None:
+            max_draft = max(0, min(D, MAX_DRAFT, MAX_DRAFT_ROWS // max(R, 1) - 1))
         array, i32, f32 = self._array, torch.int32, torch.float32
         target_at, target_type, target_pitch = self._rows(target_logits, D + R, V)
         draft_at, draft_type, draft_pitch = self._rows(draft_logits, D, V)
         _check(self.lib.af_draft_verify(self.handle, target_at, target_type, target_pitch, draft_at, draft_type, draft_pitch,
                                         array(draft, i32, 4 * D), array(cu_draft, i32, 0), array(u_accept, f32, 4 * D),
-                                        array(u_sample, f32, 4 * R), R, D, V, D if max_draft is None else max_draft, temperature,
+                                        array(u_sample, f32, 4 * R), R, D, V, max_draft, temperature,
                                         array(token, i32, 4 * (D + R)), array(logp, f32, 4 * (D + R)), array(n_emitted, i32, 4 * R),
                                         self._stream_of(stream)), "af_draft_verify")
 
