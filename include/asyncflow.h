@@ -105,9 +105,9 @@ af_status af_set_tuning(af_ctx* ctx, int32_t v_splits, int32_t bwd_token_block, 
 
 /* Self-test of the bounded waits (the paper has no counterpart; failure handling of this library).
  * Every wait inside the kernels gives up after a time limit, sets AF_DEVERR_WATCHDOG and lets the
- * kernel return; nothing traps or spins without bound.  This call runs that same wait for one warp
- * on a barrier nobody arrives at, with a limit of one millisecond, synchronises `stream` and returns
- * how long the warp waited (microseconds, nullable).  Afterwards af_check_device_errors reports (and
+ * kernel return; nothing traps or spins without bound.  This call runs both forms of that wait, asking and
+ * sleeping, for one warp on a barrier nobody arrives at, with a limit of one millisecond each, synchronises
+ * `stream` and returns how long the shorter one took (microseconds, nullable).  Afterwards af_check_device_errors reports (and
  * clears) AF_DEVERR_WATCHDOG, and the context is as usable as before. */
 af_status af_selftest_bounded_wait(af_ctx* ctx, uint32_t* waited_us, void* stream);
 

@@ -244,8 +244,8 @@ class Context:
         return int(a.value), int(b.value)
 
     def selftest_bounded_wait(self, stream=None) -> int:
-        """Run the library's bounded wait on a barrier nobody arrives at (limit: 1 ms); returns the
-        microseconds the warp waited.  Leaves DEVERR_WATCHDOG set for check_device_errors."""
+        """Run the library's bounded waits, asking and sleeping, on a barrier nobody arrives at (limit: 1 ms each); returns
+        the microseconds that the shorter one took.  Leaves DEVERR_WATCHDOG set for check_device_errors."""
         us = C.c_uint32(0)
         _check(self.lib.af_selftest_bounded_wait(self.handle, C.byref(us), _stream(stream)), "af_selftest_bounded_wait")
         return int(us.value)

@@ -57,29 +57,13 @@ struct Stage {
   static_assert(kRing >= 3, "loads ahead of the products");
 };
 
-// A bounded wait in which the warp sleeps: the scheduler's issue slots belong to the warps that dequantise.
-__device__ __forceinline__ bool sleep_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  constexpr uint32_t kNapNs = 100000, kNaps = (uint32_t)(kWaitLimitNs / kNapNs);
-#pragma unroll 1
-  for (uint32_t i = 0; i < kNaps; ++i) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity), "r"(kNapNs) : "memory");
-    if (ok) return true;
-    if (*abort_flag) return false;
-  }
-  *abort_flag = 1;
-  return false;
-}
-// The same for a warp that others wait for: it keeps asking for a while first.
+// The dequantising warps sleep while they wait (mbar_sleep_wait): the scheduler's issue slots belong to those that have work.  A warp
+// that others wait for keeps asking for a while first.
 __device__ __forceinline__ bool ready_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
 #pragma unroll 1
   for (int i = 0; i < 64; ++i)
     if (mbar_try_wait(bar, parity)) return true;
-  return sleep_wait(bar, parity, abort_flag);
+  return mbar_sleep_wait(bar, parity, abort_flag);
 }
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
@@ -300,7 +284,7 @@ __global__ void __launch_bounds__(Roles<kM>::kThreads, 1) quant_umma_kernel(
 #pragma unroll
       for (int n = 0; n < kN; ++n) sum[n] = 0.f;
       for (int part = 0; part < parts; ++part) {
-        ok = __all_sync(0xffffffffu, sleep_wait(acc_full(a), acc_phase, &abort_flag));
+        ok = __all_sync(0xffffffffu, mbar_sleep_wait(acc_full(a), acc_phase, &abort_flag));
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
@@ -352,7 +336,7 @@ __global__ void __launch_bounds__(Roles<kM>::kThreads, 1) quant_umma_kernel(
       quick = __all_sync(0xffffffffu, quick);
       const uint8_t* const row = rows + slot * kStage;
       const int a = owner();
-      if (!__all_sync(0xffffffffu, sleep_wait(full_bar(slot), phase, &abort_flag) && sleep_wait(a_empty(group, 0), buf_phase ^ 1u, &abort_flag))) break;
+      if (!__all_sync(0xffffffffu, mbar_sleep_wait(full_bar(slot), phase, &abort_flag) && mbar_sleep_wait(a_empty(group, 0), buf_phase ^ 1u, &abort_flag))) break;
       slot += kTurn;
       if (slot >= kRing) { slot -= kRing; phase ^= 1u; }
       s += kTurn;
@@ -368,7 +352,7 @@ __global__ void __launch_bounds__(Roles<kM>::kThreads, 1) quant_umma_kernel(
       if (quick) dequantise<true, kScales, 0>(row, swizzle, p, to);
       else dequantise<false, kScales, 0>(row, swizzle, p, to);
       hand_over(0);
-      if (!__all_sync(0xffffffffu, sleep_wait(a_empty(group, 1), buf_phase ^ 1u, &abort_flag))) break;
+      if (!__all_sync(0xffffffffu, mbar_sleep_wait(a_empty(group, 1), buf_phase ^ 1u, &abort_flag))) break;
       tc_fence_after();
       if (quick) dequantise<true, kScales, 4>(row, swizzle, p, to + kBufCols);
       else dequantise<false, kScales, 4>(row, swizzle, p, to + kBufCols);

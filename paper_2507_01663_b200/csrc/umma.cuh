@@ -94,6 +94,29 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return true;
 }
 
+// The same for a warp that sleeps meanwhile.  How long one try sleeps is the hardware's choice (4 us, with a hint of 100), so the limit
+// goes by the clock here too.
+__device__ __forceinline__ bool mbar_try_sleep(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity), "r"(100000u) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool mbar_sleep_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                                unsigned long long limit_ns = kWaitLimitNs) {
+  if (mbar_try_sleep(bar, parity)) return true;
+  const unsigned long long t0 = globaltimer_ns();
+#pragma unroll 1
+  while (!mbar_try_sleep(bar, parity)) {
+    if (*abort_flag) return false;
+    if (globaltimer_ns() - t0 > limit_ns) { *abort_flag = 1; return false; }
+  }
+  return true;
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t dst_smem, const CUtensorMap* map, uint32_t bar,
                                             int x, int y) {
   asm volatile(
