@@ -539,10 +539,10 @@ af_status af_reserve_preference(af_ctx* ctx, int64_t max_T, int32_t max_B);
  * af_quantize_head are).  A NaN in a scale or in a hidden row stays in its vocabulary row or token.
  * 0 <= T <= AF_MAX_QUANT_TOKENS; meant for few: it costs one pass over the codes per 64 tokens.
  *
- * W, hidden, values bf16 dev; V <= 2^30, d % 32 == 0; matrices contiguous (but for the logits' pitch) and 16-byte aligned, logits aligned
+ * W, hidden, values bf16 dev; V <= 2^30, d <= 2^30, d % 32 == 0; matrices contiguous (but for the logits' pitch) and 16-byte aligned, logits aligned
  * to their type.  No workspace.
  * Errors: AF_ERR_INVALID_ARG for null pointers, sizes below 1, another group size or type; AF_ERR_ALIGNMENT; AF_ERR_SHAPE for
- * T or V out of range or a pitch below V.
+ * T, V or d out of range or a pitch below V.
  * ------------------------------------------------------------------------------------------- */
 #define AF_MAX_QUANT_TOKENS 65536
 af_status af_quantize_head(af_ctx* ctx, const void* W, int32_t V, int32_t d, int32_t group, void* codes, void* scale,

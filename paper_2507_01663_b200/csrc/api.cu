@@ -676,7 +676,7 @@ af_status af_reserve_preference(af_ctx* c, int64_t max_T, int32_t max_B) {
 static af_status quant_head_sizes(int32_t V, int32_t d, int32_t group) {
   if (V < 1 || d < 1) return AF_ERR_INVALID_ARG;
   if (group != 32 && group != 64 && group != 128) return AF_ERR_INVALID_ARG;
-  if (V > (1 << 30)) return AF_ERR_SHAPE;                   // rows, and tiles past the last one, are 32-bit numbers
+  if (V > (1 << 30) || d > (1 << 30)) return AF_ERR_SHAPE;  // rows and columns, and tiles past the last ones, are 32-bit numbers
   return d % 32 != 0 ? AF_ERR_ALIGNMENT : AF_OK;
 }
 
