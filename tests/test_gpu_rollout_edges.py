@@ -88,3 +88,28 @@ def test_ctas_with_two_and_three_boxes(ctx, V, T, group):  # noqa: F811
     got = run_logits(ctx, H, words, scale, group)
     want, mag = O.quant_logits_ref(f64(H), words.numpy(), f64(scale), group)
     assert (np.abs(got - want) <= logits_tol(192, mag, want, False)).all()
+
+
+@pytest.mark.parametrize("T", [1000, 65536])
+def test_as_many_tokens_as_the_call_takes(ctx, T):  # noqa: F811
+    H, words, scale = head(3, T, 64, 40, 32, any_scale=True)
+    got = run_logits(ctx, H, words, scale, 32)
+    want, mag = O.quant_logits_ref(f64(H), words.numpy(), f64(scale), 32)
+    assert (np.abs(got - want) <= logits_tol(64, mag, want, False)).all()
+
+
+@pytest.mark.parametrize("mode", ["dense", "lookup", "greedy"])
+@pytest.mark.parametrize("passes", [False, True])
+def test_requests_of_a_thousand_drafts(ctx, mode, passes):  # noqa: F811
+    """Up to 1023 of one request; nearly equal distributions, so that many pass, or uniforms of 0 and first maxima, so that all do."""
+    c = verify_case(31, 4, 1023, 60, mode, masked=False, noise=0.02)
+    if passes:
+        c["ua"][:] = 0.0
+        if mode == "greedy":
+            z = f64(c["target"])
+            for r in range(4):
+                for i in range(c["cu"][r + 1] - c["cu"][r]):
+                    c["ids"][c["cu"][r] + i] = z[c["cu"][r] + r + i].argmax()
+    want = check_verify(ctx, c, 0.0 if mode == "greedy" else 1.0, max_draft=1023)
+    if passes:
+        assert np.array_equal(want["n_emitted"], np.diff(c["cu"]) + 1) and want["n_emitted"].max() > 500
