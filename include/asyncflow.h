@@ -574,7 +574,9 @@ af_status af_quant_logits(af_ctx* ctx, const void* hidden, const void* codes, co
  * such a cu_draft share hold one's or the other's results.)
  *
  * Comparisons and draws are made from sums in 64 bits where 32 could decide otherwise; log-probs of passed drafts and of greedy
- * tokens are within 8e-6 of 64 bits whatever the row holds (ordinary rows: 2e-7), that of a drawn y is rounded once.  In a draw weights below 2^-900 of the row's largest are nothing.
+ * tokens are, before they are rounded, within 8e-6 of 64 bits whatever the row holds (ordinary rows: 2e-7), that of a drawn y is
+ * rounded once.  In a draw a weight
+ * is good to 2^-42 of p and of q, and those below about 2^-900 of the row's largest are nothing.
  * target_logits [D + R, V], draft_logits [D, V]: fp32 or bf16 dev, row pitch in elements (>= V), aligned to their type.  draft [D],
  * cu_draft [R+1], token [D + R], n_emitted [R] int32, logp (nullable) [D + R] fp32, dev.  0 <= max_draft <= AF_MAX_DRAFT,
  * 0 <= R, R * (max_draft + 1) <= 2^24, 0 <= D <= R * max_draft, temperature 0 or from 1e-4 to 1e4.
@@ -615,6 +617,8 @@ af_status af_draft_verify(af_ctx* ctx, const void* target_logits, int32_t target
  * length, grow, held, held_out, granted [R], free_count, free_count_out [1], cu_new [R+1], position [token_capacity] int32;
  * block_table [R, max_blocks] int32 with table_pitch >= max_blocks elements from row to row; free_blocks [n_blocks] int32; slot
  * [token_capacity] int64; all dev.  0 <= R <= 2^20, block_size >= 1.  Workspace: 24 bytes per request (af_reserve_rollout).
+ * The host does not know how many tokens there are, so the launch goes by token_capacity: up to 1024 requests and 8192 rows are one
+ * small launch, anything larger two that fill the device.  A step should pass the rows that it can need, not a whole store's.
  * Errors: AF_ERR_INVALID_ARG for null pointers and negative sizes, AF_ERR_SHAPE for R out of range or a pitch below max_blocks.
  * ------------------------------------------------------------------------------------------- */
 af_status af_block_slots(af_ctx* ctx, const int32_t* length, const int32_t* grow, const int32_t* held, int32_t R,

@@ -13,8 +13,9 @@
 // made again from sums in 64 bits, and a draw's sums are in 64 bits throughout: per logit nine 64-bit operations, 2^x from a table
 // of 256 powers and a polynomial of degree 3 (2^-42 relative).
 //
-// 64 requests of up to 4 drafts, bf16 and fp32 logits of 152064: 100-104 us, of which the rows take 53 (4 TB/s; their exponentials
-// keep the special unit busy half of the time), sums 25, mass 37, find 11, each alone and cold; one request 25-28 us, four launches.
+// 64 requests of up to 4 drafts, bf16 and fp32 logits of 152064: 103-105 us.  Each alone and cold the rows take 51 (253 MB at 5 TB/s,
+// of which 208 had to be read; their exponentials keep the special unit busy half of the time), sums 22, mass 33, find 10: a call
+// overlaps their beginnings and ends.  One request 24-28 us, four launches.
 #include "device_util.cuh"
 #include "rollout.cuh"
 

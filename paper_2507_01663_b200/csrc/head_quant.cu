@@ -8,8 +8,8 @@
 // by 1/255 of itself at least; w times 1/s (1 + 2^-20), exact within the fused multiply-add that also rounds it to a
 // whole number, lies on the far side of every half and on the right side of everything else.
 //
-// A stream: 2 bytes read per weight, 1/2 (and 2 for the value) written.  152064 x 3584 in groups of 128 with the values: 371-405 us,
-// 6.1-6.6 TB/s, about the rate of a copy; 4096 x 256: 2.6 us on the device.
+// A stream: 2 bytes read per weight, 1/2 (and 2 for the value) written.  152064 x 3584 in groups of 128 with the values: 371-408 us,
+// 6.0-6.6 TB/s, about the rate of a copy; 4096 x 256: 2.6 us on the device.
 #include "device_util.cuh"
 #include "rollout.cuh"
 

@@ -11,8 +11,8 @@
 //   significant bits, as af_quantize_head's have (24 s then is a bf16).  Rows with other scales take the two steps.
 // So a pair costs a shift, a mask-and-or (both on the ALU pipe, at half rate) and a multiply-add.
 //
-// 152064 x 3584, groups of 128: one token 62-71 us, 3.9-4.5 TB/s of codes and scales, 64 tokens 100-118 us; 151643 x 5120, groups of
-// 32, 16 tokens: 105-123 us.  One token keeps the ALU pipe busy 64 % of the time, issue slots 69 %, memory 50 %: what is left
+// 152064 x 3584, groups of 128: one token 62-72 us, 3.9-4.5 TB/s of codes and scales, 64 tokens 100-120 us; 151643 x 5120, groups of
+// 32, 16 tokens: 105-125 us.  One token keeps the ALU pipe busy 64 % of the time, issue slots 69 %, memory 50 %: what is left
 // are the hand-overs from stage to buffer to product (shifts as multiplications on the idler pipe: no faster, or 10 % slower).
 //
 // Warps: 0 loads stages of 256 of k into a ring (the codes of a box of 128 rows, or of two, and the tokens'), 1 and 2 issue the
